@@ -316,6 +316,129 @@ sdnn_status sdnn_net_read_profile(sdnn_net net, sdnn_kernel_time *out, int32_t m
 /* Free the net's host handle (synchronises its stream); the arena is the caller's to release afterwards. */
 sdnn_status sdnn_net_free(sdnn_net net);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------------
+ * A layer of experts on 8-bit operands.
+ *
+ * In a layer of experts each token's row passes through k of E small networks that a router picks for it: a layer
+ * whose W is block sparse with a pattern the input chooses.  The calls below are its parts for serving (forward only,
+ * prompts and single tokens); each also stands alone.  They belong to no net: a call works on the HIP device that is
+ * current on the calling thread, on `stream` (a hipStream_t, NULL = the default stream), with memory of that device;
+ * it is asynchronous, allocates nothing, keeps nothing, never synchronises and may be recorded into a HIP graph.
+ * Results do not depend on timing: there is no atomic in any of them.
+ *
+ * Dense tensors are row-major with a row stride in elements (ld*, at least the row's length) and element type
+ * SDNN_TYPE_*; any element-aligned address is accepted, 16-byte aligned rows are read and written faster.
+ *
+ * A blocked 8-bit matrix of `rows` x k is a pair of device arrays:
+ *   codes   uint8, rows x sdnn_blocks_pitch(k) (k rounded up to a multiple of 128), e4m3 values (1 sign, 4 exponent,
+ *           3 mantissa bits, bias 7, largest 448, 0x7f / 0xff NaN, no infinities); zeros from column k on;
+ *   scales  uint8, one row of sdnn_blocks_scale_pitch(k) codes (the number of 128-column blocks rounded up to a
+ *           multiple of 4) for every `block_rows` rows, code c (1 to 254) standing for 2^(c - 127).
+ * Element (r, i) is codes[r][i] * 2^(scales[r / block_rows][i / 128] - 127).  Activations have block_rows 1, weights
+ * 128 (a last row of blocks may be cut short).  Codes are 16-byte aligned, scales 4-byte aligned.  The zeros from
+ * column k on are read as operands: the quantizing calls write them, and a caller who fills the arrays otherwise has
+ * to as well.
+ */
+enum {
+    SDNN_TYPE_F32 = 0, /* IEEE single precision */
+    SDNN_TYPE_BF16 = 1 /* bfloat16 */
+};
+
+/* Bytes of one row of codes, and of one row of scales, of a blocked matrix of k columns (0 if k is out of range). */
+int64_t sdnn_blocks_pitch(int64_t k);
+int64_t sdnn_blocks_scale_pitch(int64_t k);
+
+/*
+ * Round a stack of `count` matrices of rows x k (matrix i starts at row i * rows of x) to blocked 8-bit matrices.  A
+ * block's scale is the least power of two, 2^-126 at least, that brings its largest finite magnitude to 448 or less;
+ * codes are rounded to nearest even; infinities and NaN become NaN.  block_rows 1 (activations) or 128 (weights);
+ * with 128, every matrix of the stack has blocks of its own (ceil(rows / 128) rows of scales).
+ * Errors: NULL_POINTER, INVALID_VALUE, DEVICE.
+ */
+sdnn_status sdnn_quantize_blocks(int64_t count, int64_t rows, int64_t k, int32_t block_rows, int32_t type,
+                                 const void *x, int64_t ldx, uint8_t *codes, uint8_t *scales, void *stream);
+
+/*
+ * s = x + residual (s = x where residual is NULL), z = s / sqrt(mean(s^2) + eps) * gamma over each row of k columns,
+ * and z as a blocked 8-bit matrix with block_rows 1.  sum (NULL, or s rounded to the type; it may be x or residual
+ * itself) and normed (NULL, or z rounded to the type; it may be x itself, or residual where sum is not) are written
+ * too.  s, the mean and z are carried in fp64 and rounded once to each output.  Rows of up to 32768 columns.
+ * Errors: NULL_POINTER, INVALID_VALUE (sum without residual, eps negative or not finite), UNSUPPORTED, DEVICE.
+ */
+sdnn_status sdnn_norm_quantize(int64_t rows, int64_t k, int32_t type, const void *x, int64_t ldx,
+                               const void *residual, int64_t ldr, const float *gamma, float eps, void *sum,
+                               int64_t lds, void *normed, int64_t ldn, uint8_t *codes, uint8_t *scales,
+                               void *stream);
+
+/*
+ * Y = h(A W^T + bias) for blocked 8-bit A (m x k, block_rows 1) and W (n x k, block_rows 128: row j holds output j's
+ * weights): Y (m x n, of the type) in fp32 sums, rounded once.  bias: n fp32 values or NULL.  activate 0: h is the
+ * identity; 1: h(z) = min(max(z, 0), ymax), ymax > 0 (+INFINITY for plain ReLU; NaN stays NaN).
+ * With SDNN_TYPE_F32 every product is exact and sums are fp32.  With SDNN_TYPE_BF16 the 8-bit matrix instructions are
+ * used, which align the products of an instruction to their largest and drop what is below about 2^-14 of it: a
+ * relative error near 1.5e-5 for normally distributed values, well under the output's rounding of 2^-9.
+ * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED (more tiles than a launch holds), DEVICE.
+ */
+sdnn_status sdnn_product_blocks(int64_t m, int64_t n, int64_t k, const uint8_t *a, const uint8_t *a_scale,
+                                const uint8_t *w, const uint8_t *w_scale, const float *bias, int32_t activate,
+                                float ymax, int32_t type, void *y, int64_t ldy, void *stream);
+
+/* How sdnn_route turns a token's logits into scores. */
+enum {
+    SDNN_SCORE_SOFTMAX = 0, /* exp(l_e) / sum of exp(l) */
+    SDNN_SCORE_SIGMOID = 1  /* 1 / (1 + exp(-l_e)) */
+};
+
+/* Bytes of device workspace sdnn_route needs.  Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED. */
+sdnn_status sdnn_route_workspace_size(int64_t tokens, int32_t experts, int32_t chosen, int64_t *bytes);
+
+/*
+ * Route tokens to experts.  For each token: score(e) from its logits (tokens x experts, of the type); choice(e) =
+ * score(e) + bias(e) (bias: `experts` fp32 values for balance, or NULL); with groups > 1 the experts form that many
+ * equal runs, a run's worth is the sum of its group_best (1 or 2) largest choices, and only the groups_kept
+ * worthiest runs stay; of the experts that stay the `chosen` with the largest choice are taken, largest first.
+ * Scores and choices are held in fp64, and ties go to the lower index.  A weight is the expert's score, divided by the
+ * sum of the chosen scores if normalize is 1, times factor.  An expert whose logit is -inf or NaN, or whose choice is
+ * -inf or NaN, is never taken; +inf logits share a softmax among themselves.  Places without an expert have id -1 and
+ * weight 0, so a row that is masked whole has no expert.
+ * Outputs: ids and weight (tokens x chosen); the plan of the experts' products: a slot is t * chosen + j, offsets
+ * (experts + 1) counts the slots of the experts before e, order (tokens * chosen) lists the slots by expert, ascending
+ * within each, then -1 to its end.
+ * experts <= 1024, chosen <= 64, groups <= 64.
+ * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED, WORKSPACE_TOO_SMALL, DEVICE.
+ */
+sdnn_status sdnn_route(int64_t tokens, int32_t experts, int32_t chosen, int32_t score, int32_t type,
+                       const void *logits, int64_t ldl, const float *bias, int32_t groups, int32_t groups_kept,
+                       int32_t group_best, int32_t normalize, float factor, int32_t *ids, float *weight,
+                       int32_t *offsets, int32_t *order, void *ws, int64_t ws_bytes, void *stream);
+
+/* Bytes of device workspace sdnn_experts_forward needs.  Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED. */
+sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t inner, int32_t experts,
+                                        int32_t chosen, int32_t type, int64_t *bytes);
+
+/*
+ * The chosen experts' gated feed-forward networks and their weighted sum.  With a_t row t of A (tokens x width,
+ * blocked, block_rows 1), for each slot (t, j) with expert e = ids(t, j) >= 0:
+ *   g = W_gate(e) a_t,  u = W_up(e) a_t,  p = g / (1 + exp(-g)) * u   (inner values)
+ *   o = W_out(e) q(p)   (width values; q rounds p to 8 bits by the rule of sdnn_quantize_blocks, block_rows 1)
+ *   out_t = residual_t + sum_j weight(t, j) o(t, j)
+ * Weights are stacks of blocked matrices with block_rows 128: w_in holds, for each expert, the gate's and then the
+ * up-projection's inner x width matrix (2 * experts matrices), w_out each expert's width x inner matrix.
+ * ids, weight, offsets and order as sdnn_route writes them; residual (tokens x width, of the type) may be NULL and may
+ * be out itself.  With SDNN_TYPE_F32 and SDNN_TYPE_BF16 the two products have the arithmetic that sdnn_product_blocks
+ * has with that type.  The sum over j is fp32 in the order of j.
+ * Entries of offsets and order outside their ranges are brought into them, so no access leaves the arrays, but the
+ * result is then undefined.
+ * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED, WORKSPACE_TOO_SMALL, DEVICE.
+ */
+sdnn_status sdnn_experts_forward(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen,
+                                 const uint8_t *a, const uint8_t *a_scale, const int32_t *ids, const float *weight,
+                                 const int32_t *offsets, const int32_t *order, const uint8_t *w_in,
+                                 const uint8_t *w_in_scale, const uint8_t *w_out, const uint8_t *w_out_scale,
+                                 int32_t type, const void *residual, int64_t ldr, void *out, int64_t ldo, void *ws,
+                                 int64_t ws_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *sdnn_status_string(sdnn_status status);
 

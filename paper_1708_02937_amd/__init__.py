@@ -33,6 +33,10 @@ SDNN_SEMIRING_MAX_PLUS = 1
 SDNN_SEMIRING_MAX_MIN = 2
 SDNN_SEMIRING_MIN_MAX = 3
 SDNN_SEMIRING_XOR_AND = 4
+SDNN_TYPE_F32 = 0
+SDNN_TYPE_BF16 = 1
+SDNN_SCORE_SOFTMAX = 0
+SDNN_SCORE_SIGMOID = 1
 
 # kernel ids of the profiling log (SDNN_KERNEL_*) and the kernels they stand for
 KERNEL_NAMES = {
@@ -80,6 +84,15 @@ _sig = {
     "sdnn_mxm_csr": [_P, _I32, _I32, _I64, _P, _P, _P, _P, _P, _I64],
     "sdnn_net_free": [_P],
     "sdnn_net_set_profiling": [_P, _I32],
+    "sdnn_quantize_blocks": [_I64, _I64, _I64, _I32, _I32, _P, _I64, _P, _P, _P],
+    "sdnn_norm_quantize": [_I64, _I64, _I32, _P, _I64, _P, _I64, _P, _c.c_float, _P, _I64, _P, _I64, _P, _P, _P],
+    "sdnn_product_blocks": [_I64, _I64, _I64, _P, _P, _P, _P, _P, _I32, _c.c_float, _I32, _P, _I64, _P],
+    "sdnn_route_workspace_size": [_I64, _I32, _I32, _c.POINTER(_I64)],
+    "sdnn_route": [_I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _I32, _I32, _I32, _I32, _c.c_float, _P, _P, _P, _P,
+                   _P, _I64, _P],
+    "sdnn_experts_workspace_size": [_I64, _I64, _I64, _I32, _I32, _I32, _c.POINTER(_I64)],
+    "sdnn_experts_forward": [_I64, _I64, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I32, _P, _I64,
+                             _P, _I64, _P, _I64, _P],
 }
 
 
@@ -95,6 +108,9 @@ lib.sdnn_net_read_profile.argtypes = lib_read_profile_args
 lib.sdnn_net_read_profile.restype = _c.c_int
 lib.sdnn_noalloc_scratch_bytes.argtypes = []
 lib.sdnn_noalloc_scratch_bytes.restype = _I64
+for _name in ("sdnn_blocks_pitch", "sdnn_blocks_scale_pitch"):
+    getattr(lib, _name).argtypes = [_I64]
+    getattr(lib, _name).restype = _I64
 lib.sdnn_status_string.argtypes = [_c.c_int]
 lib.sdnn_status_string.restype = _c.c_char_p
 lib.sdnn_last_error.argtypes = []
@@ -208,6 +224,61 @@ def sdnn_net_read_profile(net, max_records: int = 1 << 16):
     count = _I32()
     _check(lib.sdnn_net_read_profile(net, buf, max_records, _c.byref(count)))
     return [(r.layer, r.kernel, r.ms) for r in buf[:min(count.value, max_records)]]
+
+
+def sdnn_blocks_pitch(k: int) -> int:
+    return lib.sdnn_blocks_pitch(k)
+
+
+def sdnn_blocks_scale_pitch(k: int) -> int:
+    return lib.sdnn_blocks_scale_pitch(k)
+
+
+def sdnn_quantize_blocks(count: int, rows: int, k: int, block_rows: int, type: int, x, ldx: int, codes, scales,
+                         stream=None):
+    _check(lib.sdnn_quantize_blocks(count, rows, k, block_rows, type, _ptr(x), ldx, _ptr(codes), _ptr(scales),
+                                    _ptr(stream)))
+
+
+def sdnn_norm_quantize(rows: int, k: int, type: int, x, ldx: int, residual, ldr: int, gamma, eps: float, sum,
+                       lds: int, normed, ldn: int, codes, scales, stream=None):
+    _check(lib.sdnn_norm_quantize(rows, k, type, _ptr(x), ldx, _ptr(residual), ldr, _ptr(gamma), eps, _ptr(sum), lds,
+                                  _ptr(normed), ldn, _ptr(codes), _ptr(scales), _ptr(stream)))
+
+
+def sdnn_product_blocks(m: int, n: int, k: int, a, a_scale, w, w_scale, bias, activate: int, ymax: float, type: int,
+                        y, ldy: int, stream=None):
+    _check(lib.sdnn_product_blocks(m, n, k, _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), activate,
+                                   ymax, type, _ptr(y), ldy, _ptr(stream)))
+
+
+def sdnn_route_workspace_size(tokens: int, experts: int, chosen: int) -> int:
+    out = _I64()
+    _check(lib.sdnn_route_workspace_size(tokens, experts, chosen, _c.byref(out)))
+    return out.value
+
+
+def sdnn_route(tokens: int, experts: int, chosen: int, score: int, type: int, logits, ldl: int, bias, groups: int,
+               groups_kept: int, group_best: int, normalize: int, factor: float, ids, weight, offsets, order, ws,
+               ws_bytes: int, stream=None):
+    _check(lib.sdnn_route(tokens, experts, chosen, score, type, _ptr(logits), ldl, _ptr(bias), groups, groups_kept,
+                          group_best, normalize, factor, _ptr(ids), _ptr(weight), _ptr(offsets), _ptr(order),
+                          _ptr(ws), ws_bytes, _ptr(stream)))
+
+
+def sdnn_experts_workspace_size(tokens: int, width: int, inner: int, experts: int, chosen: int, type: int) -> int:
+    out = _I64()
+    _check(lib.sdnn_experts_workspace_size(tokens, width, inner, experts, chosen, type, _c.byref(out)))
+    return out.value
+
+
+def sdnn_experts_forward(tokens: int, width: int, inner: int, experts: int, chosen: int, a, a_scale, ids, weight,
+                         offsets, order, w_in, w_in_scale, w_out, w_out_scale, type: int, residual, ldr: int, out,
+                         ldo: int, ws, ws_bytes: int, stream=None):
+    _check(lib.sdnn_experts_forward(tokens, width, inner, experts, chosen, _ptr(a), _ptr(a_scale), _ptr(ids),
+                                    _ptr(weight), _ptr(offsets), _ptr(order), _ptr(w_in), _ptr(w_in_scale),
+                                    _ptr(w_out), _ptr(w_out_scale), type, _ptr(residual), ldr, _ptr(out), ldo,
+                                    _ptr(ws), ws_bytes, _ptr(stream)))
 
 
 class Net:
@@ -381,3 +452,6 @@ def net_from_problem(problem, device: str = "cuda:0", dense=0, bias_mode: int = 
     if dense:
         net.build_dense()
     return net
+
+
+from .experts import Routes, experts_forward, norm_quantize, product_blocks, quantize_blocks, route  # noqa: E402

@@ -13,6 +13,7 @@
 
 #include "common.h"
 #include "sdnn.h"
+#include "status.h"
 
 using sdnn::Edge;
 
@@ -482,6 +483,18 @@ void prof_clear(sdnn_net net) {
 }
 
 }  // namespace
+
+namespace sdnn {
+
+sdnn_status set_error(sdnn_status s, const char *msg) noexcept {
+    try {
+        g_last_error = msg;
+    } catch (...) {  // no memory for the text: the status alone is returned
+    }
+    return s;
+}
+
+}  // namespace sdnn
 
 static_assert(SDNN_KERNEL_TRANSPOSE == sdnn::kKernTranspose && SDNN_KERNEL_GATHER == sdnn::kKernGather &&
                   SDNN_KERNEL_NARROW == sdnn::kKernNarrow && SDNN_KERNEL_SLOTS == sdnn::kKernSlots &&

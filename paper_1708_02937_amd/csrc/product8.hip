@@ -1,0 +1,267 @@
+// Products of blocked 8-bit matrices, one weight matrix for all rows or one per expert.
+//
+//   Y(m, n) = sum_b 2^(Ea(m, b) + Ew(n / 128, b)) sum_{i in block b} qa(m, i) qw(n, i)
+//
+// The weights are the matrix instruction's first operand and the activations its second, so a lane ends with four
+// consecutive outputs of one row.  e4m3 codes are widened to bfloat16, which is exact, for the 16-bit matrix
+// instructions, whose products and sums are fp32; each block's sum is scaled as it joins the total.
+#include "blocks8.h"
+
+namespace sdnn {
+namespace {
+
+constexpr int kOne = 127;  // the scale code of 1
+
+__device__ __forceinline__ v8bf widen8(int lo, int hi) {
+    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false),
+               b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false),
+               d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// acc += scaled product of 16 weight rows and 16 activation rows over one block of 128 columns, every product exact.
+// Lane l holds columns 32 (l / 16) .. + 31 of weight row and activation row l % 16; acc[i] is output 4 (l / 16) + i of
+// row l % 16, so the activation's scale code is the lane's own and the weight rows share one.
+__device__ __forceinline__ v4f block16(const v8i &w, const v8i &x, v4f acc, int w_code, int x_code) {
+    v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * i], w[2 * i + 1]), widen8(x[2 * i], x[2 * i + 1]), z,
+                                                    0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; i++) acc[i] += ldexpf(z[i], w_code + x_code - 2 * kOne);
+    return acc;
+}
+
+__device__ __forceinline__ v8i load32(const uint8_t *p) {
+    const v4i a = *(const v4i *)p, b = *(const v4i *)(p + 16);
+    return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// Which expert's 16-row tile number `pair` is: tiles are numbered expert by expert.  Returns the expert (-1 past the
+// last tile) and the tile's first row and row count among the sorted slots.
+__device__ __forceinline__ int find_tile(const int32_t *offsets, int experts, int64_t slots, int tile, int rows_per_tile,
+                                         int64_t &row0, int &rows) {
+    const int lane = threadIdx.x % 64;
+    int before = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int e = e0 + lane;
+        int64_t lo = 0, hi = 0;
+        if (e < experts) {
+            lo = min(max((int64_t)offsets[e], (int64_t)0), slots);
+            hi = min(max((int64_t)offsets[e + 1], lo), slots);
+        }
+        const int tiles = (int)((hi - lo + rows_per_tile - 1) / rows_per_tile);
+        int upto = tiles;
+        for (int m = 1; m < 64; m <<= 1) {
+            const int o = __shfl_up(upto, m);
+            if (lane >= m) upto += o;
+        }
+        const uint64_t hit = __ballot(before + upto > tile);
+        if (hit) {
+            const int src = __ffsll((unsigned long long)hit) - 1;
+            const int first = before + __shfl(upto - tiles, src);
+            row0 = __shfl(lo, src) + (int64_t)(tile - first) * rows_per_tile;
+            const int64_t left = __shfl(hi, src) - row0;
+            rows = (int)(left < rows_per_tile ? left : rows_per_tile);
+            return e0 + src;
+        }
+        before += __shfl(upto, 63);
+    }
+    return -1;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_out(T *p, float v) {
+    *p = (T)v;
+}
+
+__device__ __forceinline__ float relu_clamp(float z, float ymax) {
+    if (z < 0.0f) z = 0.0f;
+    if (z > ymax) z = ymax;
+    return z;
+}
+
+// ------------------------------------------------------------------------------------------------ few rows
+// 16 outputs x 16 rows per workgroup, whose waves share the blocks of the inner dimension and join their sums in LDS.
+constexpr int kSplit = 4;
+
+__device__ __forceinline__ v4f stream_tile(const uint8_t *w, const uint8_t *ws, const uint8_t *x, const uint8_t *xs,
+                                           int64_t kb, int wave) {
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int part = (threadIdx.x % 64) / 16 * 32;
+    for (int64_t b = wave; b < kb; b += kSplit)
+        acc = block16(load32(w + b * kBlock + part), load32(x + b * kBlock + part), acc, ws[b], xs[b]);
+    return acc;
+}
+
+__device__ __forceinline__ v4f join(v4f acc, v4f (*part)[64]) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    part[wave][lane] = acc;
+    __syncthreads();
+    v4f s = part[0][lane];
+    for (int i = 1; i < kSplit; i++) s += part[i][lane];
+    return s;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(64 * kSplit) product_stream_kernel(ProductArgs a) {
+    __shared__ v4f part[kSplit][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t n_tiles = (a.n + 15) / 16;
+    const int64_t n0 = blockIdx.x % n_tiles * 16, m0 = blockIdx.x / n_tiles * 16;
+    const int64_t n = min(n0 + lane % 16, a.n - 1), m = min(m0 + lane % 16, a.m - 1);
+    const int64_t pitch = code_pitch(a.k), spitch = scale_pitch(a.k);
+    v4f acc = stream_tile(a.w + n * pitch, a.w_scale + n0 / kBlock * spitch, a.a + m * pitch,
+                                  a.a_scale + m * spitch, blocks_of(a.k), wave);
+    acc = join(acc, part);
+    if (wave != 0 || m0 + lane % 16 >= a.m) return;
+    T *y = (T *)a.y + m * a.ldy;
+    for (int i = 0; i < 4; i++) {
+        const int64_t col = n0 + lane / 16 * 4 + i;
+        if (col >= a.n) break;
+        float z = acc[i];
+        if (a.bias) z += a.bias[col];
+        if (a.activate) z = relu_clamp(z, a.ymax);
+        store_out(y + col, z);
+    }
+}
+
+// p(slot, f) = silu(gate) * up in fp32, one row of `pitch` values per sorted slot.
+__global__ void __launch_bounds__(64 * kSplit) experts_in_stream_kernel(ExpertsArgs a, float *p) {
+    __shared__ v4f part[2][kSplit][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t f_tiles = (a.inner + 15) / 16, slots = a.tokens * a.chosen;
+    const int64_t f0 = blockIdx.x % f_tiles * 16;
+    int64_t row0;
+    int rows;
+    const int e = find_tile(a.offsets, a.experts, slots, (int)(blockIdx.x / f_tiles), 16, row0, rows);
+    if (e < 0) return;
+    const int64_t at = row0 + min(lane % 16, rows - 1);
+    const int64_t slot = min(max((int64_t)a.order[at], (int64_t)0), slots - 1), token = slot / a.chosen;
+    const int64_t f = min(f0 + lane % 16, a.inner - 1);
+    const int64_t pitch = code_pitch(a.width), spitch = scale_pitch(a.width), fb = blocks_of(a.inner);
+    const uint8_t *x = a.a + token * pitch, *xs = a.a_scale + token * spitch;
+    const uint8_t *gate = a.w_in + ((int64_t)e * 2 * a.inner + f) * pitch, *up = gate + a.inner * pitch;
+    const uint8_t *gate_s = a.w_in_scale + ((int64_t)e * 2 * fb + f0 / kBlock) * spitch, *up_s = gate_s + fb * spitch;
+    const v4f g = join(stream_tile(gate, gate_s, x, xs, blocks_of(a.width), wave), part[0]);
+    const v4f u = join(stream_tile(up, up_s, x, xs, blocks_of(a.width), wave), part[1]);
+    if (wave != 0 || lane % 16 >= rows) return;
+    for (int i = 0; i < 4; i++) {
+        const int64_t col = f0 + lane / 16 * 4 + i;
+        if (col < a.inner) p[at * code_pitch(a.inner) + col] = g[i] / (1.0f + expf(-g[i])) * u[i];
+    }
+}
+
+// One block of 128 columns of p (fp32) rounded to 8 bits in registers: the same codes as if it had been stored so.
+__device__ __forceinline__ v8i quantize_row(const float *p, int64_t col, int64_t k, int &code) {
+    float v[32], amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; i++) {
+        v[i] = col + i < k ? p[col + i] : 0.0f;
+        amax = fmaxf(amax, finite_abs(v[i]));
+    }
+    amax = fmaxf(amax, __shfl_xor(amax, 16));
+    amax = fmaxf(amax, __shfl_xor(amax, 32));
+    code = scale_code(amax);
+    const float inv = inverse_scale(code);
+    v8i q;
+#pragma unroll
+    for (int i = 0; i < 8; i++) q[i] = pack_e4m3(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+    return q;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(64 * kSplit) experts_out_stream_kernel(ExpertsArgs a, const float *p, T *o) {
+    __shared__ v4f part[kSplit][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t n_tiles = (a.width + 15) / 16, slots = a.tokens * a.chosen;
+    const int64_t n0 = blockIdx.x % n_tiles * 16;
+    int64_t row0;
+    int rows;
+    const int e = find_tile(a.offsets, a.experts, slots, (int)(blockIdx.x / n_tiles), 16, row0, rows);
+    if (e < 0) return;
+    const int64_t at = row0 + min(lane % 16, rows - 1);
+    const int64_t n = min(n0 + lane % 16, a.width - 1);
+    const int64_t pitch = code_pitch(a.inner), spitch = scale_pitch(a.inner), kb = blocks_of(a.inner);
+    const uint8_t *w = a.w_out + ((int64_t)e * a.width + n) * pitch;
+    const uint8_t *ws = a.w_out_scale + ((int64_t)e * blocks_of(a.width) + n0 / kBlock) * spitch;
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t b = wave; b < kb; b += kSplit) {
+        const int64_t col = b * kBlock + lane / 16 * 32;
+        int code;
+        const v8i x = quantize_row(p + at * pitch, col, a.inner, code);
+        acc = block16(load32(w + col), x, acc, ws[b], code);
+    }
+    acc = join(acc, part);
+    if (wave != 0 || lane % 16 >= rows) return;
+    const int64_t slot = min(max((int64_t)a.order[at], (int64_t)0), slots - 1);
+    for (int i = 0; i < 4; i++) {
+        const int64_t col = n0 + lane / 16 * 4 + i;
+        if (col < a.width) store_out(o + slot * a.width + col, acc[i]);
+    }
+}
+
+// out(t) = residual(t) + sum_j weight(t, j) o(t k + j), in fp32, in the order of j.
+template <typename T>
+__global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, const T *o) {
+    const int64_t cells = a.tokens * a.width;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < cells; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / a.width, c = i % a.width;
+        float s = a.residual ? load_f32((const T *)a.residual + t * a.ldr + c) : 0.0f;
+        for (int j = 0; j < a.chosen; j++) {
+            const int64_t slot = t * a.chosen + j;
+            if (a.ids[slot] >= 0) s += a.weight[slot] * load_f32(o + slot * a.width + c);
+        }
+        store_out((T *)a.out + t * a.ldo + c, s);
+    }
+}
+
+struct ExpertsPlan {
+    size_t p, o, bytes;
+};
+
+ExpertsPlan experts_plan(int64_t tokens, int64_t width, int64_t inner, int32_t chosen, bool bf16) {
+    const size_t slots = (size_t)tokens * chosen;
+    ExpertsPlan e;
+    e.p = 0;
+    e.o = (slots * code_pitch(inner) * 4 + 255) / 256 * 256;
+    e.bytes = e.o + slots * width * (bf16 ? 2 : 4);
+    return e;
+}
+
+template <typename T>
+hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
+    const ExpertsPlan plan = experts_plan(a.tokens, a.width, a.inner, a.chosen, sizeof(T) == 2);
+    float *p = (float *)((char *)a.ws + plan.p);
+    T *o = (T *)((char *)a.ws + plan.o);
+    const int64_t slots = a.tokens * a.chosen;
+    const int64_t tiles = (slots < a.experts ? slots : a.experts) + slots / 16;
+    experts_in_stream_kernel<<<(unsigned)(tiles * ((a.inner + 15) / 16)), 64 * kSplit, 0, s>>>(a, p);
+    experts_out_stream_kernel<T><<<(unsigned)(tiles * ((a.width + 15) / 16)), 64 * kSplit, 0, s>>>(a, p, o);
+    const int64_t groups = (a.tokens * a.width + 255) / 256;
+    experts_combine_kernel<T><<<(unsigned)(groups < (1 << 16) ? groups : (1 << 16)), 256, 0, s>>>(a, o);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t experts_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t chosen, bool bf16) {
+    return experts_plan(tokens, width, inner, chosen, bf16).bytes;
+}
+
+hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
+    if (a.m == 0 || a.n == 0) return hipSuccess;
+    const unsigned grid = (unsigned)((a.n + 15) / 16 * ((a.m + 15) / 16));
+    if (bf16) product_stream_kernel<__bf16><<<grid, 64 * kSplit, 0, stream>>>(a);
+    else product_stream_kernel<float><<<grid, 64 * kSplit, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_experts(const ExpertsArgs &a, bool bf16, hipStream_t stream) {
+    if (a.tokens == 0 || a.width == 0) return hipSuccess;
+    return bf16 ? experts_go<__bf16>(a, stream) : experts_go<float>(a, stream);
+}
+
+}  // namespace sdnn
