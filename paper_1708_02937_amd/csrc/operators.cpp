@@ -174,7 +174,7 @@ sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t i
     sdnn::set_error(SDNN_OK, "");
     if (!bytes) return fail(SDNN_ERR_NULL_POINTER, "bytes is NULL");
     SDNN_CHECK(check_experts(tokens, width, inner, experts, chosen, type));
-    *bytes = (int64_t)sdnn::experts_workspace(tokens, width, inner, chosen, type == SDNN_TYPE_BF16);
+    *bytes = (int64_t)sdnn::experts_workspace(tokens, width, inner, experts, chosen, type == SDNN_TYPE_BF16);
     return SDNN_OK;
 }
 
@@ -196,7 +196,7 @@ sdnn_status sdnn_experts_forward(int64_t tokens, int64_t width, int64_t inner, i
         return fail(SDNN_ERR_INVALID_VALUE, "a route tensor is misaligned");
     if (bad_dense(out, type, ldo, width) || (residual && bad_dense(residual, type, ldr, width)))
         return fail(SDNN_ERR_INVALID_VALUE, "out or residual is misaligned or its row stride below width");
-    const size_t need = sdnn::experts_workspace(tokens, width, inner, chosen, type == SDNN_TYPE_BF16);
+    const size_t need = sdnn::experts_workspace(tokens, width, inner, experts, chosen, type == SDNN_TYPE_BF16);
     if (!ws) return fail(SDNN_ERR_NULL_POINTER, "ws is NULL");
     if (ws_bytes < 0 || (size_t)ws_bytes < need)
         return fail(SDNN_ERR_WORKSPACE_TOO_SMALL, "ws_bytes below sdnn_experts_workspace_size");

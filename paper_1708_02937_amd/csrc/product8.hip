@@ -5,20 +5,10 @@
 // The weights are the matrix instruction's first operand and the activations its second, so a lane ends with four
 // consecutive outputs of one row.  e4m3 codes are widened to bfloat16, which is exact, for the 16-bit matrix
 // instructions, whose products and sums are fp32; each block's sum is scaled as it joins the total.
-#include "blocks8.h"
+#include "product8.h"
 
 namespace sdnn {
 namespace {
-
-constexpr int kOne = 127;  // the scale code of 1
-
-__device__ __forceinline__ v8bf widen8(int lo, int hi) {
-    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false),
-               b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
-               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false),
-               d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
-    return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 
 // acc += scaled product of 16 weight rows and 16 activation rows over one block of 128 columns, every product exact.
 // Lane l holds columns 32 (l / 16) .. + 31 of weight row and activation row l % 16; acc[i] is output 4 (l / 16) + i of
@@ -37,50 +27,6 @@ __device__ __forceinline__ v4f block16(const v8i &w, const v8i &x, v4f acc, int 
 __device__ __forceinline__ v8i load32(const uint8_t *p) {
     const v4i a = *(const v4i *)p, b = *(const v4i *)(p + 16);
     return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-
-// Which expert's 16-row tile number `pair` is: tiles are numbered expert by expert.  Returns the expert (-1 past the
-// last tile) and the tile's first row and row count among the sorted slots.
-__device__ __forceinline__ int find_tile(const int32_t *offsets, int experts, int64_t slots, int tile, int rows_per_tile,
-                                         int64_t &row0, int &rows) {
-    const int lane = threadIdx.x % 64;
-    int before = 0;
-    for (int e0 = 0; e0 < experts; e0 += 64) {
-        const int e = e0 + lane;
-        int64_t lo = 0, hi = 0;
-        if (e < experts) {
-            lo = min(max((int64_t)offsets[e], (int64_t)0), slots);
-            hi = min(max((int64_t)offsets[e + 1], lo), slots);
-        }
-        const int tiles = (int)((hi - lo + rows_per_tile - 1) / rows_per_tile);
-        int upto = tiles;
-        for (int m = 1; m < 64; m <<= 1) {
-            const int o = __shfl_up(upto, m);
-            if (lane >= m) upto += o;
-        }
-        const uint64_t hit = __ballot(before + upto > tile);
-        if (hit) {
-            const int src = __ffsll((unsigned long long)hit) - 1;
-            const int first = before + __shfl(upto - tiles, src);
-            row0 = __shfl(lo, src) + (int64_t)(tile - first) * rows_per_tile;
-            const int64_t left = __shfl(hi, src) - row0;
-            rows = (int)(left < rows_per_tile ? left : rows_per_tile);
-            return e0 + src;
-        }
-        before += __shfl(upto, 63);
-    }
-    return -1;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_out(T *p, float v) {
-    *p = (T)v;
-}
-
-__device__ __forceinline__ float relu_clamp(float z, float ymax) {
-    if (z < 0.0f) z = 0.0f;
-    if (z > ymax) z = ymax;
-    return z;
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
@@ -150,7 +96,7 @@ __global__ void __launch_bounds__(64 * kSplit) experts_in_stream_kernel(ExpertsA
     if (wave != 0 || lane % 16 >= rows) return;
     for (int i = 0; i < 4; i++) {
         const int64_t col = f0 + lane / 16 * 4 + i;
-        if (col < a.inner) p[at * code_pitch(a.inner) + col] = g[i] / (1.0f + expf(-g[i])) * u[i];
+        if (col < a.inner) p[at * code_pitch(a.inner) + col] = silu_times(g[i], u[i]);
     }
 }
 
@@ -218,28 +164,44 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, con
     }
 }
 
+// Few rows, or many: an average of fewer than 16 slots to a busy expert.
+bool few_slots(int64_t slots, int32_t experts) { return slots < 16 * (slots < experts ? slots : (int64_t)experts); }
+
 struct ExpertsPlan {
-    size_t p, o, bytes;
+    size_t p, scales, o, bytes;
 };
 
-ExpertsPlan experts_plan(int64_t tokens, int64_t width, int64_t inner, int32_t chosen, bool bf16) {
+ExpertsPlan experts_plan(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen, bool bf16) {
     const size_t slots = (size_t)tokens * chosen;
     ExpertsPlan e;
     e.p = 0;
-    e.o = (slots * code_pitch(inner) * 4 + 255) / 256 * 256;
+    e.scales = slots * code_pitch(inner);
+    e.o = few_slots((int64_t)slots, experts) ? slots * code_pitch(inner) * 4
+                                             : e.scales + slots * scale_pitch(inner);
+    e.o = align_up(e.o);
     e.bytes = e.o + slots * width * (bf16 ? 2 : 4);
     return e;
 }
 
 template <typename T>
 hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
-    const ExpertsPlan plan = experts_plan(a.tokens, a.width, a.inner, a.chosen, sizeof(T) == 2);
-    float *p = (float *)((char *)a.ws + plan.p);
+    const ExpertsPlan plan = experts_plan(a.tokens, a.width, a.inner, a.experts, a.chosen, sizeof(T) == 2);
     T *o = (T *)((char *)a.ws + plan.o);
     const int64_t slots = a.tokens * a.chosen;
-    const int64_t tiles = (slots < a.experts ? slots : a.experts) + slots / 16;
-    experts_in_stream_kernel<<<(unsigned)(tiles * ((a.inner + 15) / 16)), 64 * kSplit, 0, s>>>(a, p);
-    experts_out_stream_kernel<T><<<(unsigned)(tiles * ((a.width + 15) / 16)), 64 * kSplit, 0, s>>>(a, p, o);
+    if (few_slots(slots, a.experts)) {
+        float *p = (float *)((char *)a.ws + plan.p);
+        const int64_t tiles = (slots < a.experts ? slots : a.experts) + slots / 16;
+        experts_in_stream_kernel<<<(unsigned)(tiles * ((a.inner + 15) / 16)), 64 * kSplit, 0, s>>>(a, p);
+        experts_out_stream_kernel<T><<<(unsigned)(tiles * ((a.width + 15) / 16)), 64 * kSplit, 0, s>>>(a, p, o);
+    } else {
+        TileWork work{};
+        work.wide = a.width % (16 / (int)sizeof(T)) == 0;
+        work.p_codes = work.p_codes_out = (uint8_t *)a.ws + plan.p;
+        work.p_scales = work.p_scales_out = (uint8_t *)a.ws + plan.scales;
+        work.o = o;
+        const hipError_t e = launch_experts_tile(a, work, sizeof(T) == 2, s);
+        if (e != hipSuccess) return e;
+    }
     const int64_t groups = (a.tokens * a.width + 255) / 256;
     experts_combine_kernel<T><<<(unsigned)(groups < (1 << 16) ? groups : (1 << 16)), 256, 0, s>>>(a, o);
     return hipGetLastError();
@@ -247,12 +209,18 @@ hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
 
 }  // namespace
 
-size_t experts_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t chosen, bool bf16) {
-    return experts_plan(tokens, width, inner, chosen, bf16).bytes;
+size_t experts_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen, bool bf16) {
+    return experts_plan(tokens, width, inner, experts, chosen, bf16).bytes;
 }
 
 hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
     if (a.m == 0 || a.n == 0) return hipSuccess;
+    if (a.m > 32) {
+        TileWork work{};
+        const int size = bf16 ? 2 : 4;
+        work.wide = a.n % 4 == 0 && ((uintptr_t)a.y & 15) == 0 && a.ldy * size % 16 == 0;
+        return launch_product_tile(a, work, bf16, stream);
+    }
     const unsigned grid = (unsigned)((a.n + 15) / 16 * ((a.m + 15) / 16));
     if (bf16) product_stream_kernel<__bf16><<<grid, 64 * kSplit, 0, stream>>>(a);
     else product_stream_kernel<float><<<grid, 64 * kSplit, 0, stream>>>(a);

@@ -303,7 +303,7 @@ def test_product(torch, sd, m, n, k, dtype):
 def test_product_of_integers_is_exact(torch, sd):
     """Small integers: every product and sum is exact in both arithmetics, whatever the tile a row falls into."""
     rng = np.random.default_rng(1)
-    for m, n, k in ((5, 40, 300), (70, 300, 1000), (300, 520, 700)):
+    for m, n, k in ((5, 40, 300), (70, 300, 1000), (300, 520, 700), (4100, 4097, 200)):
         a, sa, av = _blocked(torch, sd, rng.integers(-4, 5, (m, k)).astype(float), 1)
         w, sw, wv = _blocked(torch, sd, rng.integers(-4, 5, (n, k)).astype(float), 128)
         for dt in (torch.float32, torch.bfloat16):
