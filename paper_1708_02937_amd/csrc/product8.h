@@ -65,22 +65,11 @@ __device__ __forceinline__ float relu_clamp(float z, float ymax) {
 // silu(gate) * up
 __device__ __forceinline__ float silu_times(float gate, float up) { return gate / (1.0f + expf(-gate)) * up; }
 
-// Four consecutive outputs n .. n + 3 of a row of `cols`; wide: rows start at multiples of 16 bytes and hold a
-// multiple of four outputs.
-template <typename T>
-__device__ __forceinline__ void store4(T *y, int64_t n, int64_t cols, const float (&z)[4], bool wide) {
-    if (wide) {
-        if (n >= cols) return;
-        if constexpr (sizeof(T) == 4) {
-            *(v4f *)(y + n) = v4f{z[0], z[1], z[2], z[3]};
-        } else {
-            typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
-            *(v4bf *)(y + n) = v4bf{(__bf16)z[0], (__bf16)z[1], (__bf16)z[2], (__bf16)z[3]};
-        }
-    } else {
-        for (int v = 0; v < 4; v++)
-            if (n + v < cols) y[n + v] = (T)z[v];
-    }
+// Four values as T at an address that is a multiple of their size.
+__device__ __forceinline__ void put4(float *p, const v4f &z) { *(v4f *)p = z; }
+__device__ __forceinline__ void put4(__bf16 *p, const v4f &z) {
+    typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+    *(v4bf *)p = v4bf{(__bf16)z[0], (__bf16)z[1], (__bf16)z[2], (__bf16)z[3]};
 }
 
 // Workgroup `id` of `count` goes to chiplet id % 8: the tile that gives every chiplet a run of neighbours.
@@ -91,7 +80,7 @@ __device__ __forceinline__ int64_t chiplet_order(int64_t id, int64_t count) {
 
 struct TileWork {
     int64_t n_tiles;  // tiles along the outputs
-    bool wide;        // output rows start at multiples of 16 bytes and hold a multiple of four values
+    bool wide;        // output rows start at multiples of 16 bytes
     const uint8_t *p_codes, *p_scales;  // the experts' inner rows, one per sorted slot
     uint8_t *p_codes_out, *p_scales_out;
     void *o;  // the experts' output rows, one per slot

@@ -149,19 +149,44 @@ __global__ void __launch_bounds__(64 * kSplit) experts_out_stream_kernel(Experts
     }
 }
 
-// out(t) = residual(t) + sum_j weight(t, j) o(t k + j), in fp32, in the order of j.
-template <typename T>
-__global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, const T *o) {
-    const int64_t cells = a.tokens * a.width;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < cells; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = i / a.width, c = i % a.width;
-        float s = a.residual ? load_f32((const T *)a.residual + t * a.ldr + c) : 0.0f;
+// out(t) = residual(t) + sum_j weight(t, j) o(t k + j), in fp32, in the order of j.  A thread takes 8 columns of one
+// token; VEC: every row starts at a multiple of 16 bytes.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, const T *o, int parts) {
+    const int64_t cells = a.tokens * parts;
+    for (int64_t g = blockIdx.x; g < cells; g += gridDim.x) {
+        const int64_t t = g / parts, c = (g % parts * 256 + threadIdx.x) * 8;
+        if (c >= a.width) continue;
+        float s[8];
+        if (a.residual)
+            load8<T, VEC>((const T *)a.residual + t * a.ldr, c, a.width, s);
+        else
+            for (int i = 0; i < 8; i++) s[i] = 0.0f;
+#pragma unroll 4
         for (int j = 0; j < a.chosen; j++) {
             const int64_t slot = t * a.chosen + j;
-            if (a.ids[slot] >= 0) s += a.weight[slot] * load_f32(o + slot * a.width + c);
+            if (a.ids[slot] < 0) continue;
+            const float w = a.weight[slot];
+            float v[8];
+            load8<T, VEC>(o + slot * a.width, c, a.width, v);
+            for (int i = 0; i < 8; i++) s[i] = fmaf(w, v[i], s[i]);
         }
-        store_out((T *)a.out + t * a.ldo + c, s);
+        store8<T, VEC>((T *)a.out + t * a.ldo, c, a.width, s);
     }
+}
+
+template <typename T>
+void combine_go(const ExpertsArgs &a, const T *o, hipStream_t s) {
+    const int parts = (int)((a.width + 2047) / 2048);
+    const int64_t cells = a.tokens * parts;
+    const unsigned grid = (unsigned)(cells < (1 << 20) ? cells : (1 << 20));
+    const int size = sizeof(T);
+    const bool vec = a.width * size % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.ldo * size % 16 == 0 &&
+                     (!a.residual || (((uintptr_t)a.residual & 15) == 0 && a.ldr * size % 16 == 0));
+    if (vec)
+        experts_combine_kernel<T, true><<<grid, 256, 0, s>>>(a, o, parts);
+    else
+        experts_combine_kernel<T, false><<<grid, 256, 0, s>>>(a, o, parts);
 }
 
 // Few rows, or many: an average of fewer than 16 slots to a busy expert.
@@ -202,8 +227,7 @@ hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
         const hipError_t e = launch_experts_tile(a, work, sizeof(T) == 2, s);
         if (e != hipSuccess) return e;
     }
-    const int64_t groups = (a.tokens * a.width + 255) / 256;
-    experts_combine_kernel<T><<<(unsigned)(groups < (1 << 16) ? groups : (1 << 16)), 256, 0, s>>>(a, o);
+    combine_go<T>(a, o, s);
     return hipGetLastError();
 }
 
@@ -218,7 +242,7 @@ hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
     if (a.m > 32) {
         TileWork work{};
         const int size = bf16 ? 2 : 4;
-        work.wide = a.n % 4 == 0 && ((uintptr_t)a.y & 15) == 0 && a.ldy * size % 16 == 0;
+        work.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy * size % 16 == 0;
         return launch_product_tile(a, work, bf16, stream);
     }
     const unsigned grid = (unsigned)((a.n + 15) / 16 * ((a.m + 15) / 16));

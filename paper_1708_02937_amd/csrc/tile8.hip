@@ -278,33 +278,48 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
             *(v4i *)(work.p_codes_out + (row0 + c / 8) * p_pitch + n0 + c % 8 * 16) =
                 *(const v4i *)(lds + c / 8 * kPitch + c % 8 * 16);
     } else {
+        // Through LDS, 32 rows of every wave at a time, so that whole lines leave for memory.
+        constexpr int kCells = 16 / sizeof(T), kPitch = BN + kCells, kSlice = WM * 32;
+        static_assert(kSlice * kPitch * sizeof(T) + BN * 4 <= S::kLds, "a slice of the outputs fits the stages");
+        T *out = (T *)lds;
+        float *bias = (float *)(lds + kSlice * kPitch * sizeof(T));
+        stage_barrier();  // the last stage has been read
+        if constexpr (MODE == kTileProduct)
+            for (int c = threadIdx.x; c < BN; c += S::kThreads)
+                bias[c] = a.bias && n0 + c < n_rows ? a.bias[n0 + c] : 0.0f;
 #pragma unroll
         for (int j = 0; j < MJ; j++) {
-            const int r = (wm * MJ + j) * 32 + lane % 32;
-            if (r >= rows) continue;
-            T *y;
-            if constexpr (MODE == kTileProduct) {
-                y = (T *)a.y + (row0 + r) * a.ldy;
-            } else {
-                const int64_t slots = x.tokens * x.chosen;
-                y = (T *)work.o + min(max((int64_t)x.order[row0 + r], (int64_t)0), slots - 1) * n_rows;
-            }
+            __syncthreads();
 #pragma unroll
             for (int i = 0; i < NI; i++)
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
-                    const int64_t n = n0 + sub_row(i) + 8 * q + 4 * (lane / 32);
-                    float z[4];
-#pragma unroll
-                    for (int v = 0; v < 4; v++) {
-                        z[v] = acc[i][j][4 * q + v];
-                        if constexpr (MODE == kTileProduct) {
-                            if (a.bias && n + v < n_rows) z[v] += a.bias[n + v];
-                            if (a.activate) z[v] = relu_clamp(z[v], a.ymax);
-                        }
+                    const int c = sub_row(i) + 8 * q + 4 * (lane / 32);
+                    v4f z = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    if constexpr (MODE == kTileProduct) {
+                        z += *(const v4f *)(bias + c);
+                        if (a.activate)
+                            for (int v = 0; v < 4; v++) z[v] = relu_clamp(z[v], a.ymax);
                     }
-                    store4(y, n, n_rows, z, work.wide);
+                    put4(out + (wm * 32 + lane % 32) * kPitch + c, z);
                 }
+            __syncthreads();
+            constexpr int kPieces = BN / kCells;
+#pragma unroll
+            for (int c = threadIdx.x; c < kSlice * kPieces; c += S::kThreads) {
+                const int lr = c / kPieces, r = (lr / 32 * MJ + j) * 32 + lr % 32, col = c % kPieces * kCells;
+                if (r >= rows || n0 + col >= n_rows) continue;
+                T *y;
+                if constexpr (MODE == kTileProduct)
+                    y = (T *)a.y + (row0 + r) * a.ldy;
+                else
+                    y = (T *)work.o + min(max((int64_t)x.order[row0 + r], (int64_t)0), x.tokens * x.chosen - 1) * n_rows;
+                const T *from = out + lr * kPitch + col;
+                if (work.wide && n0 + col + kCells <= n_rows)
+                    *(v4i *)(y + n0 + col) = *(const v4i *)from;
+                else
+                    for (int v = 0; v < kCells && n0 + col + v < n_rows; v++) y[n0 + col + v] = from[v];
+            }
         }
     }
 }
