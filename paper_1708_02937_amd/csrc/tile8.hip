@@ -13,7 +13,7 @@
 namespace sdnn {
 namespace {
 
-constexpr int kRowBytes = kBlock;  // a row of a stage: one block
+constexpr int kRowBytes = kBlock / 2;  // a row of a stage: half a block
 
 enum TileMode { kTileProduct, kTileExpertsIn, kTileExpertsOut };
 
@@ -23,36 +23,39 @@ __device__ __forceinline__ void stage16(const uint8_t *from, uint8_t *lds) {
                                      (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
 }
 
-// This wave's loads into LDS have landed, and every wave is here.
+// All but this wave's last LEFT loads have landed, its reads of LDS are over, and every wave is here.
+template <int LEFT>
 __device__ __forceinline__ void stage_barrier() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-template <int MODE, typename T, int BN, int BM, int WN, int WM>
+template <int MODE, typename T, int BN, int BM, int WN, int WM, int STAGES>
 struct Tile {
     static constexpr int kThreads = 64 * WN * WM, kWaves = WN * WM;
     static constexpr int NI = BN / WN / 32, MJ = BM / WM / 32;
-    static constexpr int kRows = BN + BM, kLoads = kRows / 8 / kWaves;
-    static constexpr int kStage = kRows * kRowBytes, kLds = 2 * kStage;
-    static constexpr bool kExact = sizeof(T) == 4;
-    static_assert(kRows % (8 * kWaves) == 0, "every wave stages the same number of rows");
+    static constexpr int kRows = BN + BM, kLoads = kRows / 16 / kWaves;
+    static constexpr int kStage = kRows * kRowBytes, kLds = STAGES * kStage + 2 * (BM + 64) * 4;
+    static constexpr bool kExact = sizeof(T) == 4, kTurns = kWaves == 8 && !kExact;
+    static_assert(kRows % (16 * kWaves) == 0, "every wave stages the same number of rows");
 };
 
 // Which weight row LDS row r of a tile stands for, relative to the tile's first.  In the experts' first product the
 // lower half of the tile is gate rows and the upper half the up rows of the same outputs.
-template <int MODE, typename T, int BN, int BM, int WN, int WM>
-__global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs a, ExpertsArgs x, TileWork work) {
-    using S = Tile<MODE, T, BN, BM, WN, WM>;
-    constexpr int NI = S::NI, MJ = S::MJ;
+template <int MODE, typename T, int BN, int BM, int WN, int WM, int STAGES>
+__global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductArgs a, ExpertsArgs x, TileWork work) {
+    using S = Tile<MODE, T, BN, BM, WN, WM, STAGES>;
+    constexpr int NI = S::NI, MJ = S::MJ, kStages = STAGES;
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wn = wave % WN, wm = wave / WN;
 
-    // The chiplets take workgroups in turn; each is given a run of neighbouring tiles, which share operand rows in
-    // its L2.
-    const int64_t tile = chiplet_order(blockIdx.x, gridDim.x);
-    const int64_t nt = tile % work.n_tiles;
-    int64_t mt = tile / work.n_tiles;
+    // The chiplets take workgroups in turn; each is given a run of neighbouring tiles, four tiles of rows wide, so that
+    // the 32 tiles in flight on a chiplet share 12 panels of operand rows in its L2.
+    constexpr int kGroup = MODE == kTileProduct ? 4 : 1;
+    const int64_t tile = chiplet_order(blockIdx.x, gridDim.x), m_tiles = gridDim.x / work.n_tiles;
+    const int64_t first = tile / (kGroup * work.n_tiles) * kGroup, wide = min(m_tiles - first, (int64_t)kGroup);
+    const int64_t in_group = tile - first * work.n_tiles;
+    const int64_t nt = in_group / wide, mt = first + in_group % wide;
 
     const uint8_t *act, *act_scale, *wt, *wt_scale;
     int64_t n_rows, k, row0 = 0;  // n_rows: outputs of this matrix; row0: the tile's first activation row
@@ -92,13 +95,14 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
         }
     };
 
-    // Staging: instruction i of a wave fills 8 rows of 128 bytes; the 16-byte piece c of row r lies at c ^ (r & 7), so
-    // that the lanes of a read, which hold different rows, spread over the banks.  The swap is made on the global side.
+    // Staging: instruction i of a wave fills 16 rows of 64 bytes; the 16-byte piece c of row r lies at c ^ (r / 4 & 3),
+    // so that the 16 lanes of a read that go together, which hold different rows, cover all banks.  The swap is made on
+    // the global side.
     const uint8_t *from[S::kLoads];
 #pragma unroll
     for (int i = 0; i < S::kLoads; i++) {
-        const int r = (i * S::kWaves + wave) * 8 + lane / 8;
-        const int piece = ((lane % 8) ^ (r & 7)) * 16;
+        const int r = (i * S::kWaves + wave) * 16 + lane / 4;
+        const int piece = ((lane % 4) ^ (r >> 2 & 3)) * 16;
         if (r < BN) {
             int64_t n;
             if constexpr (MODE == kTileExpertsIn)
@@ -110,11 +114,11 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
             from[i] = act + act_row(r - BN) * pitch + piece;
         }
     }
-    auto stage = [&](int buf) {
+    auto stage = [&](int t) {
 #pragma unroll
         for (int i = 0; i < S::kLoads; i++) {
-            stage16(from[i], lds + buf * S::kStage + (i * S::kWaves + wave) * 1024);
-            from[i] += kBlock;
+            stage16(from[i], lds + t % kStages * S::kStage + (i * S::kWaves + wave) * 1024);
+            from[i] += kRowBytes;
         }
     };
 
@@ -126,22 +130,26 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
             return wn * NI * 32 + i * 32;
     };
 
-    // Scale codes, four blocks to a word: the lane's activation rows, and the weights' block rows of the wave (a
-    // subtile of 32 weight rows lies in one).
-    const uint8_t *asc[MJ];
-#pragma unroll
-    for (int j = 0; j < MJ; j++) asc[j] = act_scale + act_row((wm * MJ + j) * 32 + lane % 32) * spitch;
-    const uint8_t *wsc[NI];
-#pragma unroll
-    for (int i = 0; i < NI; i++) {
-        int64_t n = n0 + sub_row(i);
-        if constexpr (MODE == kTileExpertsIn)
-            n = n0 + sub_row(i) % (BN / 2);
+    // Scale codes, four blocks to a word, go through LDS too: the words of the tile's activation rows, then of its block
+    // rows of weights (in the experts' first product the gate's and the up rows').
+    constexpr int kWords = BM + 64;
+    uint8_t *const scales = lds + kStages * S::kStage;
+    const uint8_t *scale_from = nullptr;
+    if (wave < BM / 64) {
+        scale_from = act_scale + act_row(wave * 64 + lane) * spitch;
+    } else if (wave == BM / 64) {
         const int64_t last = (n_rows - 1) / kBlock;
-        int64_t block = min(n / kBlock, last);
-        if constexpr (MODE == kTileExpertsIn) block += i < NI / 2 ? 0 : last + 1;
-        wsc[i] = wt_scale + block * spitch;
+        if constexpr (MODE == kTileExpertsIn)
+            scale_from = wt_scale + (min(n0 / kBlock, last) + (lane % 2) * (last + 1)) * spitch;
+        else
+            scale_from = wt_scale + min(n0 / kBlock + lane % (BN / kBlock), last) * spitch;
     }
+    auto stage_scales = [&](int group) {
+        if (wave <= BM / 64)
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void *)(scale_from + group * 4),
+                (__attribute__((address_space(3))) void *)(scales + (group & 1) * kWords * 4 + wave * 256), 4, 0, 0);
+    };
 
     v16f acc[NI][MJ];
 #pragma unroll
@@ -151,79 +159,135 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
 #pragma unroll
             for (int r = 0; r < 16; r++) acc[i][j][r] = 0.0f;
 
-    stage(0);
-    uint32_t as[MJ], ws[NI], as_next[MJ], ws_next[NI];
+    uint32_t xs[MJ], ws[NI];
+    auto read_scales = [&](int group) {
+        const uint32_t *w = (const uint32_t *)(scales + (group & 1) * kWords * 4);
 #pragma unroll
-    for (int j = 0; j < MJ; j++) as_next[j] = *(const uint32_t *)asc[j];
+        for (int j = 0; j < MJ; j++) xs[j] = w[(wm * MJ + j) * 32 + lane % 32];
 #pragma unroll
-    for (int i = 0; i < NI; i++) ws_next[i] = *(const uint32_t *)wsc[i];
-
-    for (int b = 0; b < kb; b++) {
-        if (b % 4 == 0) {
-            const int next = min(b + 4, (int)spitch - 4);
-#pragma unroll
-            for (int j = 0; j < MJ; j++) as[j] = as_next[j], as_next[j] = *(const uint32_t *)(asc[j] + next);
-#pragma unroll
-            for (int i = 0; i < NI; i++) ws[i] = ws_next[i], ws_next[i] = *(const uint32_t *)(wsc[i] + next);
+        for (int i = 0; i < NI; i++) ws[i] = w[BM + sub_row(i) / kBlock];
+    };
+    // Several stages are on their way while one is multiplied: a load takes longer than a stage's products.
+    constexpr int kLeft = S::kLoads * (kStages - 2);
+    const int stages = 2 * kb;
+    stage_scales(0);
+    for (int t = 0; t < kStages - 1; t++)
+        if (t < stages) stage(t);
+    // The scales of stage t, read anew every four blocks, and the next ones sent for.
+    auto scales_at = [&](int t) {
+        if (t % 8 == 0) {
+            read_scales(t / 8);
+            if (t + 8 < stages) stage_scales(t / 8 + 1);
         }
-        stage_barrier();
-        if (b + 1 < kb) stage((b + 1) & 1);
-        const uint8_t *buf = lds + (b & 1) * S::kStage;
-        // lane's 32 bytes of LDS row r in half h of the block
-        auto fetch = [&](int r, int h) -> v8i {
-            const int c = h * 4 + lane / 32 * 2, sw = r & 7;
-            const v4i lo = *(const v4i *)(buf + r * kRowBytes + ((c ^ sw) * 16));
-            const v4i hi = *(const v4i *)(buf + r * kRowBytes + (((c + 1) ^ sw) * 16));
-            return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    // The lane's 32 bytes of LDS row r of stage t.
+    auto fetch = [&](int t, int r) -> v8i {
+        const uint8_t *row = lds + t % kStages * S::kStage + r * kRowBytes;
+        const int c = lane / 32 * 2, sw = r >> 2 & 3;
+        const v4i lo = *(const v4i *)(row + ((c ^ sw) * 16)), hi = *(const v4i *)(row + (((c + 1) ^ sw) * 16));
+        return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    auto fetch_x = [&](int t, int j) { return fetch(t, BN + (wm * MJ + j) * 32 + lane % 32); };
+    auto fetch_w = [&](int t, int i) { return fetch(t, sub_row(i) + lane % 32); };
+    uint32_t xc[MJ], wc[NI];  // the codes of a stage's block, in the low byte
+    auto codes_at = [&](int t) {
+        const int shift = t / 2 % 4 * 8;
+#pragma unroll
+        for (int j = 0; j < MJ; j++) xc[j] = xs[j] >> shift;
+#pragma unroll
+        for (int i = 0; i < NI; i++) wc[i] = ws[i] >> shift;
+    };
+    if constexpr (S::kTurns) {
+        // The two waves of a SIMD take turns: while one reads a stage's operands the other keeps the matrix cores busy.
+        // Turns change at a barrier, and the second half of the waves is one turn late.  Wave and turn 2 t: reads of
+        // stage t, sends for stage t + 3, whose buffer was last read (by the late waves) in turn 2 t - 1; turn 2 t + 1:
+        // products.  Stage t + 1 has landed for every wave at the end of turn 2 t + 1, when it is first needed.
+        const bool late = wave >= 4;
+        auto turn = [&]() {
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
         };
-        if constexpr (!S::kExact) {
+        auto landed = [&](int t) {  // this wave's part of stage t + 1
+            if (t + kStages - 1 < stages)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLeft) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        };
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        turn();
+        if (late) turn();
+        for (int t = 0; t < stages; t++) {
+            scales_at(t);
+            v8i xf[MJ], wf[NI];
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                v8i wf[NI], af[MJ];
+            for (int j = 0; j < MJ; j++) xf[j] = fetch_x(t, j);
 #pragma unroll
-                for (int j = 0; j < MJ; j++) af[j] = fetch(BN + (wm * MJ + j) * 32 + lane % 32, h);
+            for (int i = 0; i < NI; i++) wf[i] = fetch_w(t, i);
+            __builtin_amdgcn_sched_barrier(0);
+            if (t + kStages - 1 < stages) stage(t + kStages - 1);
+            codes_at(t);
+            if (late) landed(t);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            turn();
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int i = 0; i < NI; i++) wf[i] = fetch(sub_row(i) + lane % 32, h);
+            for (int i = 0; i < NI; i++)
+#pragma unroll
+                for (int j = 0; j < MJ; j++)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[i], xf[j], acc[i][j], 0, 0, 0, wc[i],
+                                                                                0, xc[j]);
+            __builtin_amdgcn_s_setprio(0);
+            if (!late) landed(t);
+            turn();
+        }
+        if (!late) turn();
+    } else {
+        for (int t = 0; t < stages; t++) {
+            // Stage t has landed, and the buffer of the one before has been read by every wave.
+            if (t + kStages - 1 <= stages)
+                stage_barrier<kLeft>();
+            else
+                stage_barrier<0>();
+            scales_at(t);
+            if (t + kStages - 1 < stages) stage(t + kStages - 1);
+            codes_at(t);
+            v8i xf[MJ];
+#pragma unroll
+            for (int j = 0; j < MJ; j++) xf[j] = fetch_x(t, j);
+            if constexpr (!S::kExact) {
+                v8i wf[NI];
+#pragma unroll
+                for (int i = 0; i < NI; i++) wf[i] = fetch_w(t, i);
 #pragma unroll
                 for (int i = 0; i < NI; i++)
 #pragma unroll
                     for (int j = 0; j < MJ; j++)
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[i], af[j], acc[i][j], 0, 0, 0,
-                                                                                    ws[i], 0, as[j]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < MJ; j++) {
-                v8bf af[8];
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const v8i q = fetch(BN + (wm * MJ + j) * 32 + lane % 32, h);
-#pragma unroll
-                    for (int c = 0; c < 4; c++) af[4 * h + c] = widen8(q[2 * c], q[2 * c + 1]);
-                }
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[i], xf[j], acc[i][j], 0, 0, 0,
+                                                                                    wc[i], 0, xc[j]);
+            } else {
 #pragma unroll
                 for (int i = 0; i < NI; i++) {
-                    v16f z;
+                    const v8i q = fetch_w(t, i);
+                    v8bf wf[4];
 #pragma unroll
-                    for (int r = 0; r < 16; r++) z[r] = 0.0f;
+                    for (int c = 0; c < 4; c++) wf[c] = widen8(q[2 * c], q[2 * c + 1]);
 #pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        const v8i q = fetch(sub_row(i) + lane % 32, h);
+                    for (int j = 0; j < MJ; j++) {
+                        v16f z;
+#pragma unroll
+                        for (int r = 0; r < 16; r++) z[r] = 0.0f;
 #pragma unroll
                         for (int c = 0; c < 4; c++)
-                            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(q[2 * c], q[2 * c + 1]), af[4 * h + c],
+                            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[c], widen8(xf[j][2 * c], xf[j][2 * c + 1]),
                                                                         z, 0, 0, 0);
-                    }
-                    const int shift = (int)(ws[i] & 255) + (int)(as[j] & 255) - 2 * kOne;
+                        const int e = (int)(wc[i] & 255) + (int)(xc[j] & 255) - 2 * kOne;
 #pragma unroll
-                    for (int r = 0; r < 16; r++) acc[i][j][r] += ldexpf(z[r], shift);
+                        for (int r = 0; r < 16; r++) acc[i][j][r] += ldexpf(z[r], e);
+                    }
                 }
             }
         }
-#pragma unroll
-        for (int j = 0; j < MJ; j++) as[j] >>= 8;
-#pragma unroll
-        for (int i = 0; i < NI; i++) ws[i] >>= 8;
     }
 
     // acc[i][j][4 q + v]: tile row (wm MJ + j) 32 + lane % 32, weight row sub_row(i) + 8 q + 4 (lane / 32) + v
@@ -231,9 +295,9 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
         constexpr int NP = NI / 2;
         constexpr int kPitch = kBlock + 16;  // LDS pitch of a row of codes: rows start in different banks
         static_assert(BN == 2 * kBlock, "a tile's outputs are one block of p");
-        static_assert(BM * kPitch + WN * BM * 4 <= S::kLds, "the epilogue's arrays fit the stages");
+        static_assert(BM * kPitch + WN * BM * 4 <= STAGES * S::kStage, "the epilogue's arrays fit the stages");
         float *red = (float *)(lds + BM * kPitch);
-        stage_barrier();  // the last stage has been read
+        stage_barrier<0>();  // the last stage has been read
 #pragma unroll
         for (int j = 0; j < MJ; j++) {
             float amax = 0.0f;
@@ -280,10 +344,14 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
     } else {
         // Through LDS, 32 rows of every wave at a time, so that whole lines leave for memory.
         constexpr int kCells = 16 / sizeof(T), kPitch = BN + kCells, kSlice = WM * 32;
-        static_assert(kSlice * kPitch * sizeof(T) + BN * 4 <= S::kLds, "a slice of the outputs fits the stages");
+        static_assert(kSlice * kPitch * sizeof(T) + BN * 4 <= STAGES * S::kStage, "a slice of the outputs fits the stages");
         T *out = (T *)lds;
         float *bias = (float *)(lds + kSlice * kPitch * sizeof(T));
-        stage_barrier();  // the last stage has been read
+        stage_barrier<0>();  // the last stage has been read
+        int *const slot = (int *)scales;
+        if constexpr (MODE == kTileExpertsOut)
+            for (int c = threadIdx.x; c < BM; c += S::kThreads)
+                slot[c] = min(max(x.order[row0 + min(c, rows - 1)], 0), (int)(x.tokens * x.chosen - 1));
         if constexpr (MODE == kTileProduct)
             for (int c = threadIdx.x; c < BN; c += S::kThreads)
                 bias[c] = a.bias && n0 + c < n_rows ? a.bias[n0 + c] : 0.0f;
@@ -313,7 +381,7 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
                 if constexpr (MODE == kTileProduct)
                     y = (T *)a.y + (row0 + r) * a.ldy;
                 else
-                    y = (T *)work.o + min(max((int64_t)x.order[row0 + r], (int64_t)0), x.tokens * x.chosen - 1) * n_rows;
+                    y = (T *)work.o + (int64_t)slot[r] * n_rows;
                 const T *from = out + lr * kPitch + col;
                 if (work.wide && n0 + col + kCells <= n_rows)
                     *(v4i *)(y + n0 + col) = *(const v4i *)from;
@@ -324,12 +392,12 @@ __global__ void __launch_bounds__(64 * WN * WM) product_tile_kernel(ProductArgs 
     }
 }
 
-template <int MODE, typename T, int BN, int BM, int WN, int WM>
+template <int MODE, typename T, int BN, int BM, int WN, int WM, int STAGES>
 hipError_t tile_go(const ProductArgs &a, const ExpertsArgs &x, TileWork work, int64_t m_tiles, int64_t outputs,
                    hipStream_t s) {
-    using S = Tile<MODE, T, BN, BM, WN, WM>;
+    using S = Tile<MODE, T, BN, BM, WN, WM, STAGES>;
     static std::atomic<unsigned long long> raised{0};
-    const auto kernel = product_tile_kernel<MODE, T, BN, BM, WN, WM>;
+    const auto kernel = product_tile_kernel<MODE, T, BN, BM, WN, WM, STAGES>;
     hipError_t e = raise_lds_limit((const void *)kernel, S::kLds, raised);
     if (e != hipSuccess) return e;
     constexpr int kOut = MODE == kTileExpertsIn ? BN / 2 : BN;
@@ -343,24 +411,25 @@ hipError_t tile_go(const ProductArgs &a, const ExpertsArgs &x, TileWork work, in
 template <typename T>
 hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
     const ExpertsArgs none{};
-    const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
     if constexpr (sizeof(T) == 2)
-        if (big >= 256) return tile_go<kTileProduct, T, 256, 256, 2, 4>(a, none, work, (a.m + 255) / 256, a.n, s);
-    return tile_go<kTileProduct, T, 128, 128, 2, 2>(a, none, work, (a.m + 127) / 128, a.n, s);
+        if (((a.m + 255) / 256) * ((a.n + 255) / 256) >= 256)
+            return tile_go<kTileProduct, T, 256, 256, 2, 4, 4>(a, none, work, (a.m + 255) / 256, a.n, s);
+    return tile_go<kTileProduct, T, 128, 128, 2, 2, 4>(a, none, work, (a.m + 127) / 128, a.n, s);
 }
 
 template <typename T>
 hipError_t experts_go(const ExpertsArgs &x, TileWork work, hipStream_t s) {
     const ProductArgs none{};
     const int64_t slots = x.tokens * x.chosen, busy = slots < x.experts ? slots : x.experts;
-    if constexpr (sizeof(T) == 2) if (slots >= 128 * busy) {
-        hipError_t e = tile_go<kTileExpertsIn, T, 256, 256, 2, 4>(none, x, work, busy + slots / 256, x.inner, s);
-        if (e != hipSuccess) return e;
-        return tile_go<kTileExpertsOut, T, 256, 256, 2, 4>(none, x, work, busy + slots / 256, x.width, s);
-    }
-    hipError_t e = tile_go<kTileExpertsIn, T, 256, 64, 2, 2>(none, x, work, busy + slots / 64, x.inner, s);
+    if constexpr (sizeof(T) == 2)
+        if (slots >= 128 * busy) {
+            hipError_t e = tile_go<kTileExpertsIn, T, 256, 256, 2, 4, 4>(none, x, work, busy + slots / 256, x.inner, s);
+            if (e != hipSuccess) return e;
+            return tile_go<kTileExpertsOut, T, 256, 128, 2, 2, 3>(none, x, work, busy + slots / 128, x.width, s);
+        }
+    hipError_t e = tile_go<kTileExpertsIn, T, 256, 64, 2, 2, 6>(none, x, work, busy + slots / 64, x.inner, s);
     if (e != hipSuccess) return e;
-    return tile_go<kTileExpertsOut, T, 128, 64, 2, 2>(none, x, work, busy + slots / 64, x.width, s);
+    return tile_go<kTileExpertsOut, T, 128, 64, 2, 2, 6>(none, x, work, busy + slots / 64, x.width, s);
 }
 
 }  // namespace
