@@ -1,15 +1,24 @@
 // Routing: the k best experts of each token, their weights, and the plan of the experts' products (the slots
 // t * k + j sorted by expert).
 //
-// One wave per token; a lane holds R neighbouring experts.  Scores are held in 64 bits, so that which expert is
-// chosen does not depend on how a 32-bit exponential or the order of a softmax's sum rounds; equal scores go to the
-// lower expert.
+// Which expert is chosen is defined by scores in 64 bits, so that it does not depend on how a 32-bit exponential or
+// the order of a softmax's sum rounds; equal scores go to the lower expert.  Nearly always 32 bits tell the same: a
+// token is first decided in fp32 with a bound on the error of its choices, and only where two choices that decide
+// something lie within that bound is it decided anew in fp64 (a few tokens in a thousand; exact ties, as bfloat16
+// logits have them, among these).  The weights of the chosen experts are computed in fp64 either way.
+//
+// 16 lanes take a token of up to 256 experts, a wave four tokens: a maximum over 16 lanes is four register-to-register
+// moves with the comparison built in, and what a choice costs is the search through a lane's own experts.
 #include "blocks8.h"
 
 namespace sdnn {
 namespace {
 
-constexpr int kRouteWaves = 4;  // tokens per workgroup
+constexpr int kScoreWaves = 4;  // waves of a workgroup of the scores
+constexpr int kPlanThreads = 512, kPlanWaves = kPlanThreads / 64;
+constexpr int64_t kChunk = 4096;      // slots that one workgroup sorts, up to kMaxChunks of them; then more each
+constexpr int64_t kMaxChunks = 256;
+constexpr int64_t kSmallTokens = 64;  // up to here one workgroup does everything
 
 // The largest (value, lowest index) pair of a wave, in every lane.
 __device__ __forceinline__ void wave_best(double &v, int &i) {
@@ -20,28 +29,64 @@ __device__ __forceinline__ void wave_best(double &v, int &i) {
     }
 }
 
+template <int N>
+__device__ __forceinline__ float ror16(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, true));
+}
+template <int N>
+__device__ __forceinline__ int ror16(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true);
+}
+
+// Reductions over the LANES (16 or 64) lanes of a token, in every lane of them.
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+    v = fmaxf(v, ror16<8>(v)), v = fmaxf(v, ror16<4>(v)), v = fmaxf(v, ror16<2>(v)), v = fmaxf(v, ror16<1>(v));
+    if (LANES == 64) v = fmaxf(v, __shfl_xor(v, 16)), v = fmaxf(v, __shfl_xor(v, 32));
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ int lanes_min(int v) {
+    v = min(v, ror16<8>(v)), v = min(v, ror16<4>(v)), v = min(v, ror16<2>(v)), v = min(v, ror16<1>(v));
+    if (LANES == 64) v = min(v, __shfl_xor(v, 16)), v = min(v, __shfl_xor(v, 32));
+    return v;
+}
+template <int LANES, typename V>
+__device__ __forceinline__ V lanes_sum(V v) {
+    for (int m = 1; m < LANES; m <<= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// A logit, -inf where the expert cannot be chosen (NaN, or past the last).
+template <typename T>
+__device__ __forceinline__ float logit_of(const RouteArgs &a, const T *row, int e) {
+    const float l = e < a.experts ? load_f32(row + e) : -INFINITY;
+    return l > -INFINITY ? l : -INFINITY;
+}
+
+__device__ __forceinline__ void put_choice(const RouteArgs &a, int64_t token, int j, int id, double score) {
+    a.ids[token * a.chosen + j] = id;
+    a.weight[token * a.chosen + j] = (float)(score * (double)a.factor);
+}
+
+// One token decided in fp64 by a whole wave; `shared` holds 64 R values of the wave's own.
 template <typename T, int R>
-__global__ void __launch_bounds__(64 * kRouteWaves) route_scores_kernel(RouteArgs a) {
-    __shared__ double choices[kRouteWaves][64 * R];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t token = (int64_t)blockIdx.x * kRouteWaves + wave;
-    const bool live = token < a.tokens;
-    const T *row = (const T *)a.logits + (live ? token : 0) * a.ld;
+__device__ __forceinline__ void route_exact(const RouteArgs &a, int64_t token, double *shared) {
+    const int lane = threadIdx.x % 64;
+    const T *row = (const T *)a.logits + token * a.ld;
     double score[R], choice[R];
     float l[R];
     float top = -INFINITY;
 #pragma unroll
     for (int r = 0; r < R; r++) {
-        const int e = lane * R + r;
-        l[r] = e < a.experts ? load_f32(row + e) : -INFINITY;
-        if (!(l[r] > -INFINITY)) l[r] = -INFINITY;  // NaN is never chosen
+        l[r] = logit_of(a, row, lane * R + r);
         top = fmaxf(top, l[r]);
     }
     if (a.sigmoid) {
 #pragma unroll
         for (int r = 0; r < R; r++) score[r] = 1.0 / (1.0 + exp(-(double)l[r]));
     } else {
-        for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        top = lanes_max<64>(top);
         double sum = 0.0;
 #pragma unroll
         for (int r = 0; r < R; r++) {
@@ -60,15 +105,15 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_scores_kernel(RouteArg
             choice[r] = a.bias ? score[r] + (double)a.bias[e] : score[r];
             if (!(choice[r] > -INFINITY)) choice[r] = -INFINITY;
         }
-        choices[wave][e] = choice[r];
+        shared[e] = choice[r];
     }
-    __syncthreads();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own LDS writes, read by its other lanes
     if (a.groups > 1) {
         const int size = a.experts / a.groups;
         double one = -INFINITY, two = -INFINITY;
         if (lane < a.groups)
             for (int i = 0; i < size; i++) {
-                const double c = choices[wave][lane * size + i];
+                const double c = shared[lane * size + i];
                 if (c > one) two = one, one = c;
                 else if (c > two) two = c;
             }
@@ -107,73 +152,359 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_scores_kernel(RouteArg
         const double sum = wave_sum(mine);
         mine = sum > 0.0 ? mine / sum : 0.0;
     }
-    if (live && lane < a.chosen) {
-        a.ids[token * a.chosen + lane] = id;
-        a.weight[token * a.chosen + lane] = (float)(mine * (double)a.factor);
+    if (lane < a.chosen) put_choice(a, token, lane, id, mine);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// The wave's 64 / LANES tokens from `token0` on.  A lane holds the R experts from lane * R on.  `shared`: 64 R floats
+// (or 64 R' doubles of the exact decision, whichever is more) of the wave's own.
+template <typename T, int LANES, int R>
+__device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0, double *shared) {
+    constexpr int RX = LANES == 64 ? R : (R + 3) / 4;  // experts of a lane where a wave takes one token
+    const int lane = threadIdx.x % LANES, sub = threadIdx.x % 64 / LANES;
+    const int64_t token = token0 + sub;
+    const bool live = token < a.tokens;
+    const T *row = (const T *)a.logits + (live ? token : 0) * a.ld;
+    bool sure = a.chosen <= LANES && a.groups <= LANES;
+    float c[R], top = -INFINITY;
+    const bool whole = lane * R + R <= a.experts && ((uintptr_t)(row + lane * R) & 15) == 0;
+    if (whole && R * sizeof(T) >= 16) {
+#pragma unroll
+        for (int r = 0; r < R; r += (int)(16 / sizeof(T))) {
+            if constexpr (R * sizeof(T) >= 16) {
+                const v4i bits = *(const v4i *)(row + lane * R + r);
+#pragma unroll
+                for (int i = 0; i < (int)(16 / sizeof(T)); i++) {
+                    float l;
+                    if constexpr (sizeof(T) == 4)
+                        l = __int_as_float(bits[i]);
+                    else
+                        l = __int_as_float(i % 2 ? bits[i / 2] & 0xffff0000 : bits[i / 2] << 16);
+                    c[r + i] = l > -INFINITY ? l : -INFINITY;
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; r++) c[r] = logit_of(a, row, lane * R + r);
+    }
+#pragma unroll
+    for (int r = 0; r < R; r++) top = fmaxf(top, c[r]);
+    top = lanes_max<LANES>(top);
+    sure = sure && top < INFINITY;
+
+    // Choices in fp32.  With e the relative error of exp(x), |e| <= 3e-7 + 2e-7 |x|, a sigmoid is off by at most
+    // s (1 - s) e + 1.2e-7 < 3e-7, and by 2e-5 of itself down to the smallest normal number; a softmax p, whose sum adds at
+    // most 2e-6 relative, by p e + 2e-6 p < 3e-6, and by 2.2e-5 of itself; adding the bias rounds by 6e-8 of the choice.
+    // Two choices further apart than twice that, with some room, are in the order of their 64-bit values.
+    const float slack = a.sigmoid ? 2e-6f : 8e-6f;
+    if (a.sigmoid) {
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            c[r] = c[r] > -INFINITY ? 1.0f / (1.0f + __expf(-c[r])) : -INFINITY;
+    } else {
+        float sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            c[r] = c[r] > -INFINITY ? __expf(c[r] - top) : -INFINITY;
+            sum += fmaxf(c[r], 0.0f);
+        }
+        sum = 1.0f / lanes_sum<LANES>(sum);
+#pragma unroll
+        for (int r = 0; r < R; r++) c[r] *= sum;
+    }
+    if (a.bias) {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const int e = lane * R + r;
+            if (e < a.experts) c[r] += a.bias[e];
+            if (!(c[r] > -INFINITY)) c[r] = -INFINITY;
+        }
+    }
+    auto apart = [&](float high, float low, float times) {  // high >= low; false as soon as anything is not finite
+        const float size = fmaxf(fabsf(high), fabsf(low));
+        float bound = slack * (1.0f + size);
+        if (!a.bias) bound = fminf(bound, 5e-5f * size);
+        return low == -INFINITY || high - low > times * bound;
+    };
+    if (a.groups > 1) {
+        float *mine = (float *)shared + sub * LANES * R;
+        const int size = a.experts / a.groups;
+#pragma unroll
+        for (int r = 0; r < R; r++) mine[lane * R + r] = c[r];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float one = -INFINITY, two = -INFINITY;
+        if (lane < a.groups) {
+            int at = lane % size;  // lanes start at different places, in different banks
+            for (int i = 0; i < size; i++) {
+                const float v = mine[lane * size + at];
+                two = fmaxf(two, fminf(one, v));
+                one = fmaxf(one, v);
+                at = at + 1 < size ? at + 1 : 0;
+            }
+        }
+        float worth = a.group_best == 2 && two > -INFINITY ? one + two : one;
+        uint64_t kept = 0;
+        float least = INFINITY;
+        for (int g = 0; g < a.groups_kept; g++) {
+            least = lanes_max<LANES>(worth);
+            const int i = lanes_min<LANES>(worth == least ? lane : LANES);
+            kept |= 1ull << (i & 63);
+            if (lane == i) worth = -INFINITY;
+        }
+        sure = sure && apart(least, lanes_max<LANES>(worth), 2.0f);
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const int e = lane * R + r;
+            if (e < a.experts && !(kept >> (e / size) & 1)) c[r] = -INFINITY;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    int id = -1;
+    float last = INFINITY;
+    for (int j = 0; j <= a.chosen; j++) {
+        float best = c[0];
+#pragma unroll
+        for (int r = 1; r < R; r++) best = fmaxf(best, c[r]);
+        best = lanes_max<LANES>(best);
+        if (j > 0) sure = sure && apart(last, best, 1.0f);
+        if (j == a.chosen || !(best > -INFINITY)) break;  // a token's lanes leave together
+        int found = LANES * R;
+#pragma unroll
+        for (int r = R - 1; r >= 0; r--)
+            if (c[r] == best) found = lane * R + r;
+        found = lanes_min<LANES>(found);
+        if (lane == j) id = found;
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            if (lane * R + r == found) c[r] = -INFINITY;
+        last = best;
+    }
+
+    // weights of the chosen, in fp64
+    double score = 0.0;
+    if (id >= 0) {
+        const double l = (double)load_f32(row + id);
+        score = a.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - (double)top);
+    }
+    if (a.normalize) {
+        const double sum = lanes_sum<LANES>(score);
+        score = sum > 0.0 ? score / sum : 0.0;
+    } else if (!a.sigmoid) {
+        double sum = 0.0;
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const float l = logit_of(a, row, lane * R + r);
+            if (l > -INFINITY) sum += exp((double)l - (double)top);
+        }
+        sum = lanes_sum<LANES>(sum);
+        score = sum > 0.0 ? score / sum : 0.0;
+    }
+    if (live && sure && lane < a.chosen) put_choice(a, token, lane, id, score);
+
+    uint64_t open = __ballot(live && !sure && lane == 0);
+    while (open) {
+        const int first = __ffsll((unsigned long long)open) - 1;
+        open &= open - 1;
+        route_exact<T, RX>(a, token0 + first / LANES, shared);
     }
 }
 
-// Workgroup e writes expert e's slots in ascending order behind those of the experts before it; workgroup E writes
-// the total and fills the rest of `order` with -1.
-__global__ void __launch_bounds__(1024) route_plan_kernel(RouteArgs a) {
-    __shared__ int sums[2][16];
-    const int e = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t slots = a.tokens * a.chosen;
-    int less = 0;
-    for (int64_t i = threadIdx.x; i < slots; i += 1024) {
-        const int id = a.ids[i];
-        less += id >= 0 && id < e;
+template <typename T, int LANES, int R>
+__global__ void __launch_bounds__(64 * kScoreWaves) route_scores_kernel(RouteArgs a) {
+    constexpr int RX = LANES == 64 ? R : (R + 3) / 4;
+    __shared__ double shared[kScoreWaves][64 * RX > 32 * R ? 64 * RX : 32 * R];
+    const int wave = threadIdx.x / 64;
+    const int64_t token0 = ((int64_t)blockIdx.x * kScoreWaves + wave) * (64 / LANES);
+    if (token0 < a.tokens) route_tokens<T, LANES, R>(a, token0, shared[wave]);
+}
+
+// ------------------------------------------------------------------------------------------------ the plan
+// A counting sort.  A workgroup takes a chunk of slots, its waves equal runs of it: each counts its run by expert (the
+// lanes that hold the same expert find each other bit by bit), the counts become first places, and each wave goes
+// through its run again and writes.  Everything is in order of the slots, so the sort is stable.
+
+// Lanes of the wave with this lane's expert.
+__device__ __forceinline__ uint64_t same_expert(int id, int bits) {
+    uint64_t mask = __ballot(id >= 0);
+    for (int b = 0; b < bits; b++) {
+        const uint64_t ones = __ballot(id >> b & 1);
+        mask &= id >> b & 1 ? ones : ~ones;
     }
-    for (int m = 1; m < 64; m <<= 1) less += __shfl_xor(less, m);
-    if (lane == 0) sums[0][wave] = less;
+    return mask;
+}
+
+// Slots of a chunk: whole rounds of 64 for every wave.
+__device__ __forceinline__ int64_t chunk_of(int64_t slots, int chunks) {
+    constexpr int64_t kRound = 64 * kPlanWaves;
+    return (slots + chunks * kRound - 1) / (chunks * kRound) * kRound;
+}
+
+struct PlanShared {
+    int count[kPlanWaves][kRouteMaxExperts];
+    int part[kPlanWaves];
+};
+
+// Counts each wave's run of the chunk into s.count.
+__device__ __forceinline__ void plan_count(const RouteArgs &a, int64_t begin, int64_t end, int64_t run, int bits,
+                                           PlanShared &s) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (int w = 0; w < kPlanWaves; w++)
+        for (int e = threadIdx.x; e < a.experts; e += kPlanThreads) s.count[w][e] = 0;
     __syncthreads();
-    int64_t at = 0;
-    for (int w = 0; w < 16; w++) at += sums[0][w];
-    __syncthreads();
-    if (threadIdx.x == 0) a.offsets[e] = (int)at;
-    if (e == a.experts) {
-        for (int64_t i = at + threadIdx.x; i < slots; i += 1024) a.order[i] = -1;
-        return;
+    const int64_t stop = min(begin + (wave + 1) * run, end);
+    for (int64_t i = begin + wave * run; i < stop; i += 64) {
+        const int id = i + lane < stop ? a.ids[i + lane] : -1;
+        const uint64_t mask = same_expert(id, bits);
+        if (id >= 0 && lane == __ffsll((unsigned long long)mask) - 1) s.count[wave][id] += __popcll(mask);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    int turn = 0;
-    for (int64_t i0 = 0; i0 < slots; i0 += 1024, turn ^= 1) {
-        const int64_t i = i0 + threadIdx.x;
-        const bool mine = i < slots && a.ids[i] == e;
-        const uint64_t mask = __ballot(mine);
-        if (lane == 0) sums[turn][wave] = __popcll(mask);
-        __syncthreads();
-        int before = 0, all = 0;
-        for (int w = 0; w < 16; w++) {
-            before += w < wave ? sums[turn][w] : 0;
-            all += sums[turn][w];
+    __syncthreads();
+}
+
+// `chunks` workgroups; counts: chunks x experts, of every chunk, or null where there is one.
+__device__ __forceinline__ void plan_chunk(const RouteArgs &a, int chunk, int chunks, const int32_t *counts, int bits,
+                                           PlanShared &s) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t slots = a.tokens * a.chosen, each = chunk_of(slots, chunks);
+    const int64_t begin = chunk * each, end = min(begin + each, slots), run = each / kPlanWaves;
+    plan_count(a, begin, end, run, bits, s);
+    int before = 0;  // slots of the experts below this thread's
+    for (int e0 = 0; e0 < a.experts; e0 += kPlanThreads) {
+        const int e = e0 + threadIdx.x;
+        int all = 0, earlier = 0;
+        if (e < a.experts) {
+            if (counts) {
+#pragma unroll 8
+                for (int c = 0; c < chunks; c++) {
+                    const int n = counts[(int64_t)c * a.experts + e];
+                    all += n;
+                    earlier += c < chunk ? n : 0;
+                }
+            } else {
+                for (int w = 0; w < kPlanWaves; w++) all += s.count[w][e];
+            }
         }
-        if (mine) a.order[at + before + __popcll(mask & ((1ull << lane) - 1))] = (int)i;
-        at += all;
+        int upto = all;
+        for (int m = 1; m < 64; m <<= 1) {
+            const int o = __shfl_up(upto, m);
+            if (lane >= m) upto += o;
+        }
+        if (lane == 63) s.part[wave] = upto;
+        __syncthreads();
+        int total = 0;
+        for (int w = 0; w < kPlanWaves; w++) {
+            if (w < wave) upto += s.part[w];
+            total += s.part[w];
+        }
+        __syncthreads();
+        if (e < a.experts) {
+            int at = before + upto - all;
+            if (chunk == 0) a.offsets[e] = at;
+            at += earlier;
+            for (int w = 0; w < kPlanWaves; w++) {
+                const int n = s.count[w][e];
+                s.count[w][e] = at;
+                at += n;
+            }
+        }
+        before += total;
     }
+    if (chunk == 0 && threadIdx.x == 0) a.offsets[a.experts] = before;
+    __syncthreads();
+    const int64_t stop = min(begin + (wave + 1) * run, end);
+    for (int64_t i = begin + wave * run; i < stop; i += 64) {
+        const int id = i + lane < stop ? a.ids[i + lane] : -1;
+        const uint64_t mask = same_expert(id, bits);
+        int at = 0;
+        if (id >= 0) at = s.count[wave][id];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (id >= 0) {
+            const int rank = __popcll(mask & ((1ull << lane) - 1));
+            a.order[at + rank] = (int)(i + lane);
+            if (rank == 0) s.count[wave][id] = at + __popcll(mask);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    for (int64_t i = before + (int64_t)chunk * kPlanThreads + threadIdx.x; i < slots;
+         i += (int64_t)chunks * kPlanThreads)
+        a.order[i] = -1;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) route_count_kernel(RouteArgs a, int32_t *counts, int bits) {
+    __shared__ PlanShared s;
+    const int64_t slots = a.tokens * a.chosen, each = chunk_of(slots, (int)gridDim.x), begin = blockIdx.x * each;
+    plan_count(a, begin, min(begin + each, slots), each / kPlanWaves, bits, s);
+    for (int e = threadIdx.x; e < a.experts; e += kPlanThreads) {
+        int n = 0;
+        for (int w = 0; w < kPlanWaves; w++) n += s.count[w][e];
+        counts[(int64_t)blockIdx.x * a.experts + e] = n;
+    }
+}
+
+__global__ void __launch_bounds__(kPlanThreads) route_plan_kernel(RouteArgs a, const int32_t *counts, int bits) {
+    __shared__ PlanShared s;
+    plan_chunk(a, (int)blockIdx.x, (int)gridDim.x, counts, bits, s);
+}
+
+// A few tokens: scores and plan in one launch.
+template <typename T, int LANES, int R>
+__global__ void __launch_bounds__(kPlanThreads) route_small_kernel(RouteArgs a, int bits) {
+    constexpr int RX = LANES == 64 ? R : (R + 3) / 4;
+    constexpr int kEach = 64 * RX > 32 * R ? 64 * RX : 32 * R;
+    __shared__ union {
+        PlanShared plan;
+        double scores[kPlanWaves][kEach];
+    } s;
+    const int wave = threadIdx.x / 64;
+    for (int64_t t = wave * (64 / LANES); t < a.tokens; t += kPlanWaves * (64 / LANES))
+        route_tokens<T, LANES, R>(a, t, s.scores[wave]);
+    __threadfence_block();
+    __syncthreads();
+    plan_chunk(a, 0, 1, nullptr, bits, s.plan);
+}
+
+int chunks_of(int64_t slots) {
+    const int64_t chunks = (slots + kChunk - 1) / kChunk;
+    return chunks <= 2 ? 1 : (int)(chunks < kMaxChunks ? chunks : kMaxChunks);
+}
+
+template <typename T, int LANES, int R>
+hipError_t route_go(const RouteArgs &a, hipStream_t s) {
+    int bits = 0;
+    while ((1 << bits) < a.experts) bits++;
+    if (a.tokens <= kSmallTokens) {
+        route_small_kernel<T, LANES, R><<<1, kPlanThreads, 0, s>>>(a, bits);
+        return hipGetLastError();
+    }
+    constexpr int64_t kTokens = kScoreWaves * (64 / LANES);
+    route_scores_kernel<T, LANES, R><<<(unsigned)((a.tokens + kTokens - 1) / kTokens), 64 * kScoreWaves, 0, s>>>(a);
+    const int chunks = chunks_of(a.tokens * a.chosen);
+    int32_t *counts = chunks > 1 ? (int32_t *)a.ws : nullptr;
+    if (chunks > 1) route_count_kernel<<<chunks, kPlanThreads, 0, s>>>(a, counts, bits);
+    route_plan_kernel<<<chunks, kPlanThreads, 0, s>>>(a, counts, bits);
+    return hipGetLastError();
 }
 
 template <typename T>
-hipError_t route_go(const RouteArgs &a, hipStream_t s) {
-    const unsigned grid = (unsigned)((a.tokens + kRouteWaves - 1) / kRouteWaves);
-    const int r = (a.experts + 63) / 64;
-    if (r <= 1) route_scores_kernel<T, 1><<<grid, 64 * kRouteWaves, 0, s>>>(a);
-    else if (r <= 2) route_scores_kernel<T, 2><<<grid, 64 * kRouteWaves, 0, s>>>(a);
-    else if (r <= 4) route_scores_kernel<T, 4><<<grid, 64 * kRouteWaves, 0, s>>>(a);
-    else if (r <= 8) route_scores_kernel<T, 8><<<grid, 64 * kRouteWaves, 0, s>>>(a);
-    else route_scores_kernel<T, 16><<<grid, 64 * kRouteWaves, 0, s>>>(a);
-    return hipGetLastError();
+hipError_t route_type(const RouteArgs &a, hipStream_t s) {
+    if (a.experts <= 16) return route_go<T, 16, 1>(a, s);
+    if (a.experts <= 64) return route_go<T, 16, 4>(a, s);
+    if (a.experts <= 128) return route_go<T, 16, 8>(a, s);
+    if (a.experts <= 256) return route_go<T, 16, 16>(a, s);
+    if (a.experts <= 512) return route_go<T, 64, 8>(a, s);
+    return route_go<T, 64, 16>(a, s);
 }
 
 }  // namespace
 
-size_t route_workspace(int64_t, int32_t, int32_t) { return 0; }
+size_t route_workspace(int64_t tokens, int32_t experts, int32_t chosen) {
+    const int chunks = chunks_of(tokens * chosen);
+    return chunks > 1 ? (size_t)chunks * experts * sizeof(int32_t) : 0;
+}
 
 hipError_t launch_route(const RouteArgs &a, bool bf16, hipStream_t stream) {
-    hipError_t e = hipSuccess;
-    if (a.tokens > 0) e = bf16 ? route_go<__bf16>(a, stream) : route_go<float>(a, stream);
-    if (e != hipSuccess) return e;
-    route_plan_kernel<<<a.experts + 1, 1024, 0, stream>>>(a);
-    return hipGetLastError();
+    return bf16 ? route_type<__bf16>(a, stream) : route_type<float>(a, stream);
 }
 
 }  // namespace sdnn
