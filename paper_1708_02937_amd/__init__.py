@@ -454,4 +454,15 @@ def net_from_problem(problem, device: str = "cuda:0", dense=0, bias_mode: int = 
     return net
 
 
-from .experts import Routes, experts_forward, norm_quantize, product_blocks, quantize_blocks, route  # noqa: E402
+_EXPERTS = ("Routes", "experts_forward", "norm_quantize", "product_blocks", "quantize_blocks", "route")
+
+
+def __getattr__(name):
+    """The layer of experts on torch tensors, imported with torch when first used."""
+    if name in _EXPERTS:
+        from . import experts
+
+        for n in _EXPERTS:
+            globals()[n] = getattr(experts, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -20,15 +20,6 @@ constexpr int64_t kChunk = 4096;      // slots that one workgroup sorts, up to k
 constexpr int64_t kMaxChunks = 256;
 constexpr int64_t kSmallTokens = 64;  // up to here one workgroup does everything
 
-// The largest (value, lowest index) pair of a wave, in every lane.
-__device__ __forceinline__ void wave_best(double &v, int &i) {
-    for (int m = 1; m < 64; m <<= 1) {
-        const double ov = __shfl_xor(v, m);
-        const int oi = __shfl_xor(i, m);
-        if (ov > v || (ov == v && oi < i)) v = ov, i = oi;
-    }
-}
-
 template <int N>
 __device__ __forceinline__ float ror16(float v) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, true));
@@ -38,17 +29,61 @@ __device__ __forceinline__ int ror16(int v) {
     return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true);
 }
 
+// Each half of the wave's (or of every 32 lanes') 32-bit values beside the other's: a reduction over lanes i and i ^ 32
+// (i ^ 16) is an operation on the pair, the same in both.
+struct Two {
+    uint32_t a, b;
+};
+__device__ __forceinline__ Two across32(uint32_t v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return {r[0], r[1]};
+}
+__device__ __forceinline__ Two across16(uint32_t v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return {r[0], r[1]};
+}
+
+// The largest (value, lowest index) pair of a wave, in every lane.
+__device__ __forceinline__ void better(double &v, int &i, double ov, int oi) {
+    if (ov > v || (ov == v && oi < i)) v = ov, i = oi;
+}
+__device__ __forceinline__ double join64(uint32_t lo, uint32_t hi) { return __hiloint2double((int)hi, (int)lo); }
+template <int N>
+__device__ __forceinline__ void best_ror(double &v, int &i) {
+    better(v, i, join64(ror16<N>(__double2loint(v)), ror16<N>(__double2hiint(v))), ror16<N>(i));
+}
+template <typename F>
+__device__ __forceinline__ void best_across(double &v, int &i, F across) {
+    const Two lo = across(__double2loint(v)), hi = across(__double2hiint(v)), at = across(i);
+    v = join64(lo.a, hi.a), i = (int)at.a;
+    better(v, i, join64(lo.b, hi.b), (int)at.b);
+}
+__device__ __forceinline__ void wave_best(double &v, int &i) {
+    best_ror<8>(v, i), best_ror<4>(v, i), best_ror<2>(v, i), best_ror<1>(v, i);
+    best_across(v, i, across16), best_across(v, i, across32);
+}
+
 // Reductions over the LANES (16 or 64) lanes of a token, in every lane of them.
 template <int LANES>
 __device__ __forceinline__ float lanes_max(float v) {
     v = fmaxf(v, ror16<8>(v)), v = fmaxf(v, ror16<4>(v)), v = fmaxf(v, ror16<2>(v)), v = fmaxf(v, ror16<1>(v));
-    if (LANES == 64) v = fmaxf(v, __shfl_xor(v, 16)), v = fmaxf(v, __shfl_xor(v, 32));
+    if (LANES == 64) {
+        Two t = across16(__float_as_uint(v));
+        v = fmaxf(__uint_as_float(t.a), __uint_as_float(t.b));
+        t = across32(__float_as_uint(v));
+        v = fmaxf(__uint_as_float(t.a), __uint_as_float(t.b));
+    }
     return v;
 }
 template <int LANES>
 __device__ __forceinline__ int lanes_min(int v) {
     v = min(v, ror16<8>(v)), v = min(v, ror16<4>(v)), v = min(v, ror16<2>(v)), v = min(v, ror16<1>(v));
-    if (LANES == 64) v = min(v, __shfl_xor(v, 16)), v = min(v, __shfl_xor(v, 32));
+    if (LANES == 64) {
+        Two t = across16(v);
+        v = min((int)t.a, (int)t.b);
+        t = across32(v);
+        v = min((int)t.a, (int)t.b);
+    }
     return v;
 }
 template <int LANES, typename V>
@@ -112,10 +147,11 @@ __device__ __forceinline__ void route_exact(const RouteArgs &a, int64_t token, d
         const int size = a.experts / a.groups;
         double one = -INFINITY, two = -INFINITY;
         if (lane < a.groups)
+#pragma unroll 8
             for (int i = 0; i < size; i++) {
                 const double c = shared[lane * size + i];
-                if (c > one) two = one, one = c;
-                else if (c > two) two = c;
+                two = fmax(two, fmin(one, c));
+                one = fmax(one, c);
             }
         double best = a.group_best == 2 && two > -INFINITY ? one + two : one;
         uint64_t kept = 0;
@@ -201,7 +237,7 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
     if (a.sigmoid) {
 #pragma unroll
         for (int r = 0; r < R; r++)
-            c[r] = c[r] > -INFINITY ? 1.0f / (1.0f + __expf(-c[r])) : -INFINITY;
+            c[r] = c[r] > -INFINITY ? __builtin_amdgcn_rcpf(1.0f + __expf(-c[r])) : -INFINITY;
     } else {
         float sum = 0.0f;
 #pragma unroll
@@ -214,10 +250,21 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
         for (int r = 0; r < R; r++) c[r] *= sum;
     }
     if (a.bias) {
+        float b[R];
+        if (R % 4 == 0 && lane * R + R <= a.experts && ((uintptr_t)a.bias & 15) == 0) {
+#pragma unroll
+            for (int r = 0; r < R; r += 4) {
+                const v4f four = *(const v4f *)(a.bias + lane * R + r);
+#pragma unroll
+                for (int i = 0; i < 4 && r + i < R; i++) b[r + i] = four[i];
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; r++) b[r] = lane * R + r < a.experts ? a.bias[lane * R + r] : 0.0f;
+        }
 #pragma unroll
         for (int r = 0; r < R; r++) {
-            const int e = lane * R + r;
-            if (e < a.experts) c[r] += a.bias[e];
+            c[r] += b[r];
             if (!(c[r] > -INFINITY)) c[r] = -INFINITY;
         }
     }
@@ -228,37 +275,54 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
         return low == -INFINITY || high - low > times * bound;
     };
     if (a.groups > 1) {
-        float *mine = (float *)shared + sub * LANES * R;
         const int size = a.experts / a.groups;
-#pragma unroll
-        for (int r = 0; r < R; r++) mine[lane * R + r] = c[r];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int span = size / R;  // lanes of a group, where groups begin and end with lanes
+        const bool by_lanes = size % R == 0 && (span & (span - 1)) == 0;
         float one = -INFINITY, two = -INFINITY;
-        if (lane < a.groups) {
-            int at = lane % size;  // lanes start at different places, in different banks
-            for (int i = 0; i < size; i++) {
-                const float v = mine[lane * size + at];
-                two = fmaxf(two, fminf(one, v));
-                one = fmaxf(one, v);
-                at = at + 1 < size ? at + 1 : 0;
+        auto take = [&](float v) {
+            two = fmaxf(two, fminf(one, v));
+            one = fmaxf(one, v);
+        };
+        if (by_lanes) {
+#pragma unroll
+            for (int r = 0; r < R; r++) take(c[r]);
+            for (int m = 1; m < span; m <<= 1) {
+                const float u = __shfl_xor(one, m), v = __shfl_xor(two, m);
+                two = fmaxf(fmaxf(two, v), fminf(one, u));
+                one = fmaxf(one, u);
             }
+        } else {
+            float *mine = (float *)shared + sub * LANES * R;
+#pragma unroll
+            for (int r = 0; r < R; r++) mine[lane * R + r] = c[r];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (lane < a.groups) {
+                int at = lane % size;  // lanes start at different places, in different banks
+                for (int i = 0; i < size; i++) {
+                    take(mine[lane * size + at]);
+                    at = at + 1 < size ? at + 1 : 0;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
+        // A lane holds the worth of its own group (by_lanes: shared with the others of the group), or of group `lane`.
+        const int own = by_lanes ? lane / span : lane;
         float worth = a.group_best == 2 && two > -INFINITY ? one + two : one;
         uint64_t kept = 0;
         float least = INFINITY;
         for (int g = 0; g < a.groups_kept; g++) {
             least = lanes_max<LANES>(worth);
-            const int i = lanes_min<LANES>(worth == least ? lane : LANES);
+            const int i = lanes_min<LANES>(worth == least ? own : LANES);
             kept |= 1ull << (i & 63);
-            if (lane == i) worth = -INFINITY;
+            if (own == i) worth = -INFINITY;
         }
         sure = sure && apart(least, lanes_max<LANES>(worth), 2.0f);
+        int g = lane * R / size, end = (g + 1) * size - lane * R;
 #pragma unroll
         for (int r = 0; r < R; r++) {
-            const int e = lane * R + r;
-            if (e < a.experts && !(kept >> (e / size) & 1)) c[r] = -INFINITY;
+            if (r == end) g++, end += size;
+            if (!(kept >> (g & 63) & 1)) c[r] = -INFINITY;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     int id = -1;
     float last = INFINITY;
@@ -269,15 +333,25 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
         best = lanes_max<LANES>(best);
         if (j > 0) sure = sure && apart(last, best, 1.0f);
         if (j == a.chosen || !(best > -INFINITY)) break;  // a token's lanes leave together
+        // Every expert with that choice leaves; if there is more than one, the token is not sure anyway.
         int found = LANES * R;
+        uint64_t seen = 0, twice = 0;
 #pragma unroll
-        for (int r = R - 1; r >= 0; r--)
-            if (c[r] == best) found = lane * R + r;
+        for (int r = 0; r < R; r++) {
+            const bool equal = c[r] == best;
+            const uint64_t mask = __ballot(equal);
+            twice |= seen & mask;
+            seen |= mask;
+            if (equal) found = lane * R + r, c[r] = -INFINITY;
+        }
         found = lanes_min<LANES>(found);
+        if (LANES == 64) {
+            sure = sure && !twice && __popcll(seen) == 1;
+        } else {
+            const uint32_t ours = (uint32_t)(seen >> (threadIdx.x & 48)) & 0xffff;
+            sure = sure && !(twice >> (threadIdx.x & 48) & 0xffff) && (ours & (ours - 1)) == 0;
+        }
         if (lane == j) id = found;
-#pragma unroll
-        for (int r = 0; r < R; r++)
-            if (lane * R + r == found) c[r] = -INFINITY;
         last = best;
     }
 
@@ -345,6 +419,20 @@ struct PlanShared {
     int part[kPlanWaves];
 };
 
+// f(slot, expert) for the slots [begin, end), 64 at a time in order, eight loads ahead; expert -1 past the end.
+template <typename F>
+__device__ __forceinline__ void each_round(const RouteArgs &a, int64_t begin, int64_t end, F f) {
+    const int lane = threadIdx.x % 64;
+    for (int64_t i = begin; i < end; i += 512) {
+        int id[8];
+#pragma unroll
+        for (int b = 0; b < 8; b++) id[b] = i + 64 * b + lane < end ? a.ids[i + 64 * b + lane] : -1;
+#pragma unroll
+        for (int b = 0; b < 8; b++)
+            if (i + 64 * b < end) f(i + 64 * b + lane, id[b]);
+    }
+}
+
 // Counts each wave's run of the chunk into s.count.
 __device__ __forceinline__ void plan_count(const RouteArgs &a, int64_t begin, int64_t end, int64_t run, int bits,
                                            PlanShared &s) {
@@ -352,13 +440,11 @@ __device__ __forceinline__ void plan_count(const RouteArgs &a, int64_t begin, in
     for (int w = 0; w < kPlanWaves; w++)
         for (int e = threadIdx.x; e < a.experts; e += kPlanThreads) s.count[w][e] = 0;
     __syncthreads();
-    const int64_t stop = min(begin + (wave + 1) * run, end);
-    for (int64_t i = begin + wave * run; i < stop; i += 64) {
-        const int id = i + lane < stop ? a.ids[i + lane] : -1;
+    each_round(a, begin + wave * run, min(begin + (wave + 1) * run, end), [&](int64_t, int id) {
         const uint64_t mask = same_expert(id, bits);
         if (id >= 0 && lane == __ffsll((unsigned long long)mask) - 1) s.count[wave][id] += __popcll(mask);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
+    });
     __syncthreads();
 }
 
@@ -375,7 +461,7 @@ __device__ __forceinline__ void plan_chunk(const RouteArgs &a, int chunk, int ch
         int all = 0, earlier = 0;
         if (e < a.experts) {
             if (counts) {
-#pragma unroll 8
+#pragma unroll 32
                 for (int c = 0; c < chunks; c++) {
                     const int n = counts[(int64_t)c * a.experts + e];
                     all += n;
@@ -412,20 +498,18 @@ __device__ __forceinline__ void plan_chunk(const RouteArgs &a, int chunk, int ch
     }
     if (chunk == 0 && threadIdx.x == 0) a.offsets[a.experts] = before;
     __syncthreads();
-    const int64_t stop = min(begin + (wave + 1) * run, end);
-    for (int64_t i = begin + wave * run; i < stop; i += 64) {
-        const int id = i + lane < stop ? a.ids[i + lane] : -1;
+    each_round(a, begin + wave * run, min(begin + (wave + 1) * run, end), [&](int64_t slot, int id) {
         const uint64_t mask = same_expert(id, bits);
         int at = 0;
         if (id >= 0) at = s.count[wave][id];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (id >= 0) {
             const int rank = __popcll(mask & ((1ull << lane) - 1));
-            a.order[at + rank] = (int)(i + lane);
+            a.order[at + rank] = (int)slot;
             if (rank == 0) s.count[wave][id] = at + __popcll(mask);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
+    });
     for (int64_t i = before + (int64_t)chunk * kPlanThreads + threadIdx.x; i < slots;
          i += (int64_t)chunks * kPlanThreads)
         a.order[i] = -1;

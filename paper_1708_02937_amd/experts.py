@@ -19,6 +19,7 @@ CODES = torch.float8_e4m3fn
 SCALES = torch.float8_e8m0fnu
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}  # SDNN_TYPE_*
 _SCORES = {"softmax": 0, "sigmoid": 1}  # SDNN_SCORE_*
+_SMALL_PLAN = 8192  # slots up to which sdnn_route needs no workspace
 
 
 class Routes(NamedTuple):
@@ -36,21 +37,29 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _dense(t, name, dtype=None, device=None, shape=None):
-    """Checks a matrix whose rows are contiguous; returns its row stride."""
-    _need(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{name} must be a matrix with contiguous rows")
-    _need(t.is_cuda, f"{name} must be on the GPU")
-    _need(t.dtype == dtype if dtype is not None else t.dtype in _TYPES, f"{name}: unsupported type {t.dtype}")
-    _need(device is None or t.device == device, f"{name} is on another device")
-    _need(shape is None or tuple(t.shape) == shape, f"{name} must have shape {shape}, not {tuple(t.shape)}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _dense(t, name, dtype, device, shape):
+    """Checks a matrix of that type and shape on that device, with contiguous rows; returns its row stride."""
+    if t.dtype is not dtype or t.device != device or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {shape} on {device}, not {t.dtype} of shape "
+                         f"{tuple(t.shape)} on {t.device}")
+    rows, cols = t.stride()
+    if cols != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return rows if shape[0] > 1 else max(rows, shape[1])
 
 
 def _packed(t, name, dtype, device, shape):
-    _need(t.is_cuda and t.device == device, f"{name} must be on the other tensors' device")
-    _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
-    _need(t.is_contiguous() and tuple(t.shape) == shape, f"{name} must be contiguous with shape {shape}, not "
-          f"{tuple(t.shape)}")
+    """Checks a contiguous tensor of that type and shape on that device; returns its address."""
+    if t.dtype is not dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, {dtype} of shape {shape} on {device}, not {t.dtype} of shape "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _type(dtype, name):
+    if dtype not in _TYPES:
+        raise ValueError(f"{name}: float32 or bfloat16, not {dtype}")
+    return _TYPES[dtype]
 
 
 def _pitches(k):
@@ -63,18 +72,28 @@ def _on_device(f):
 
     @functools.wraps(f)
     def call(x, *args, **kw):
-        if not x.is_cuda:
+        index = x.get_device()  # -1 on the host
+        if index < 0:
             raise ValueError(f"{f.__name__} needs tensors on the GPU")
-        if x.device.index == torch.cuda.current_device():
+        if index == _current():
             return f(x, *args, **kw)
-        with torch.cuda.device(x.device):
+        with torch.cuda.device(index):
             return f(x, *args, **kw)
 
     return call
 
 
+def _current():
+    return torch.cuda.current_device()
+
+
 def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _call(status):
+    if status:
+        sd._check(status)
 
 
 @_on_device
@@ -82,14 +101,14 @@ def quantize_blocks(x, block_rows: int = 1):
     """(codes, scales) of a float32 or bfloat16 tensor (..., rows, k), contiguous, in blocks of block_rows x 128:
     1 for activations, 128 for weights."""
     _need(x.dim() >= 2 and x.is_contiguous(), "x must be contiguous, (..., rows, k)")
-    _need(x.dtype in _TYPES, f"x: unsupported type {x.dtype}")
+    kind = _type(x.dtype, "x")
     rows, k = x.shape[-2:]
     pitch, spitch = _pitches(k)
     count = x.numel() // (rows * k) if rows * k else 0
     scale_rows = rows if block_rows == 1 else -(-rows // 128)
     codes = torch.empty((*x.shape[:-1], pitch), dtype=CODES, device=x.device)
     scales = torch.empty((*x.shape[:-2], scale_rows, spitch), dtype=SCALES, device=x.device)
-    sd.sdnn_quantize_blocks(count, rows, k, block_rows, _TYPES[x.dtype], x, k, codes, scales, _stream(x.device))
+    sd.sdnn_quantize_blocks(count, rows, k, block_rows, kind, x, k, codes, scales, _stream(x.device))
     return codes, scales
 
 
@@ -99,22 +118,33 @@ def norm_quantize(x, gamma, eps: float = 1e-6, residual=None, normed: bool = Fal
 
     sum is x + residual in x's type (None without a residual; written to out_sum if given, which may be x or residual
     itself); normed is the normalised row in x's type (None unless asked for)."""
-    device, (rows, k) = x.device, x.shape
-    ldx = _dense(x, "x")
-    _packed(gamma, "gamma", torch.float32, device, (k,))
+    shape, dtype, device = x.shape, x.dtype, x.device
+    _need(len(shape) == 2, "x must be a matrix")
+    rows, k = shape
+    kind = _type(dtype, "x")
+    ldx = _dense(x, "x", dtype, device, shape)
+    g = _packed(gamma, "gamma", torch.float32, device, (k,))
     pitch, spitch = _pitches(k)
     codes = torch.empty((rows, pitch), dtype=CODES, device=device)
     scales = torch.empty((rows, spitch), dtype=SCALES, device=device)
+    r = s = z = None
     ldr = lds = 0
     if residual is not None:
-        ldr = _dense(residual, "residual", x.dtype, device, (rows, k))
+        ldr, r = _dense(residual, "residual", dtype, device, shape), residual.data_ptr()
         if out_sum is None:
-            out_sum = torch.empty((rows, k), dtype=x.dtype, device=device)
-        lds = _dense(out_sum, "out_sum", x.dtype, device, (rows, k))
-    z = torch.empty((rows, k), dtype=x.dtype, device=device) if normed else None
-    sd.sdnn_norm_quantize(rows, k, _TYPES[x.dtype], x, ldx, residual, ldr, gamma, eps, out_sum, lds, z, k, codes,
-                          scales, _stream(device))
-    return codes, scales, out_sum, z
+            out_sum, lds = torch.empty(shape, dtype=dtype, device=device), k
+        else:
+            lds = _dense(out_sum, "out_sum", dtype, device, shape)
+        s = out_sum.data_ptr()
+    else:
+        _need(out_sum is None, "out_sum without a residual")
+    out_normed = None
+    if normed:
+        out_normed = torch.empty(shape, dtype=dtype, device=device)
+        z = out_normed.data_ptr()
+    _call(sd.lib.sdnn_norm_quantize(rows, k, kind, x.data_ptr(), ldx, r, ldr, g, eps, s, lds, z, k, codes.data_ptr(),
+                                    scales.data_ptr(), _stream(device)))
+    return codes, scales, out_sum, out_normed
 
 
 @_on_device
@@ -123,18 +153,18 @@ def product_blocks(a, a_scale, w, w_scale, k: int, bias=None, ymax=None, dtype=t
     are.  dtype float32 keeps every product exact; bfloat16 takes the 8-bit matrix instructions."""
     device, m, n = a.device, a.shape[0], w.shape[0]
     pitch, spitch = _pitches(k)
-    _packed(a, "a", CODES, device, (m, pitch))
-    _packed(a_scale, "a_scale", SCALES, device, (m, spitch))
-    _packed(w, "w", CODES, device, (n, pitch))
-    _packed(w_scale, "w_scale", SCALES, device, (-(-n // 128), spitch))
-    if bias is not None:
-        _packed(bias, "bias", torch.float32, device, (n,))
-    _need(dtype in _TYPES, f"unsupported output type {dtype}")
+    kind = _type(dtype, "dtype")
+    pa = _packed(a, "a", CODES, device, (m, pitch))
+    psa = _packed(a_scale, "a_scale", SCALES, device, (m, spitch))
+    pw = _packed(w, "w", CODES, device, (n, pitch))
+    psw = _packed(w_scale, "w_scale", SCALES, device, (-(-n // 128), spitch))
+    pb = None if bias is None else _packed(bias, "bias", torch.float32, device, (n,))
     if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=device)
-    ldy = _dense(out, "out", dtype, device, (m, n))
-    sd.sdnn_product_blocks(m, n, k, a, a_scale, w, w_scale, bias, ymax is not None, 0.0 if ymax is None else ymax,
-                           _TYPES[dtype], out, ldy, _stream(device))
+        out, ldy = torch.empty((m, n), dtype=dtype, device=device), n
+    else:
+        ldy = _dense(out, "out", dtype, device, (m, n))
+    _call(sd.lib.sdnn_product_blocks(m, n, k, pa, psa, pw, psw, pb, ymax is not None, 0.0 if ymax is None else ymax,
+                                     kind, out.data_ptr(), ldy, _stream(device)))
     return out
 
 
@@ -142,19 +172,26 @@ def product_blocks(a, a_scale, w, w_scale, k: int, bias=None, ymax=None, dtype=t
 def route(logits, k: int, score: str = "softmax", bias=None, groups: int = 1, groups_kept: int = 1,
           group_best: int = 1, normalize: bool = True, factor: float = 1.0) -> Routes:
     """The k best experts of each token (logits: tokens x experts, float32 or bfloat16); see sdnn_route."""
-    device, (tokens, experts) = logits.device, logits.shape
-    ldl = _dense(logits, "logits")
+    device, shape = logits.device, logits.shape
+    _need(len(shape) == 2, "logits must be tokens x experts")
+    tokens, experts = shape
+    kind = _type(logits.dtype, "logits")
+    ldl = _dense(logits, "logits", logits.dtype, device, shape)
     _need(score in _SCORES, "score must be 'softmax' or 'sigmoid'")
-    if bias is not None:
-        _packed(bias, "bias", torch.float32, device, (experts,))
+    _need(k >= 1, "k must be at least 1")
+    b = None if bias is None else _packed(bias, "bias", torch.float32, device, (experts,))
     ids = torch.empty((tokens, k), dtype=torch.int32, device=device)
     weight = torch.empty((tokens, k), dtype=torch.float32, device=device)
     offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
     order = torch.empty(tokens * k, dtype=torch.int32, device=device)
-    need = sd.sdnn_route_workspace_size(tokens, experts, k)
-    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    sd.sdnn_route(tokens, experts, k, _SCORES[score], _TYPES[logits.dtype], logits, ldl, bias, groups, groups_kept,
-                  group_best, bool(normalize), factor, ids, weight, offsets, order, ws, need, _stream(device))
+    ws, need = None, 0
+    if tokens * k > _SMALL_PLAN:
+        need = sd.sdnn_route_workspace_size(tokens, experts, k)
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    _call(sd.lib.sdnn_route(tokens, experts, k, _SCORES[score], kind, logits.data_ptr(), ldl, b, groups, groups_kept,
+                            group_best, bool(normalize), factor, ids.data_ptr(), weight.data_ptr(),
+                            offsets.data_ptr(), order.data_ptr(), None if ws is None else ws.data_ptr(), need,
+                            _stream(device)))
     return Routes(ids, weight, offsets, order)
 
 
@@ -170,32 +207,32 @@ def experts_forward(a, a_scale, routes: Routes, w_in, w_in_scale, w_out, w_out_s
     ids, weight, offsets, order = routes
     _need(ids.dim() == 2, "ids must be tokens x chosen")
     chosen = ids.shape[1]
+    kind = _type(dtype, "dtype")
     pitch, spitch = _pitches(width)
     pitch_f, spitch_f = _pitches(inner)
-    _packed(a, "a", CODES, device, (tokens, pitch))
-    _packed(a_scale, "a_scale", SCALES, device, (tokens, spitch))
-    _packed(ids, "ids", torch.int32, device, (tokens, chosen))
-    _packed(weight, "weight", torch.float32, device, (tokens, chosen))
-    _packed(offsets, "offsets", torch.int32, device, (experts + 1,))
-    _packed(order, "order", torch.int32, device, (tokens * chosen,))
-    _packed(w_in, "w_in", CODES, device, (experts, 2, inner, pitch))
-    _packed(w_in_scale, "w_in_scale", SCALES, device, (experts, 2, -(-inner // 128), spitch))
-    _packed(w_out, "w_out", CODES, device, (experts, width, pitch_f))
-    _packed(w_out_scale, "w_out_scale", SCALES, device, (experts, -(-width // 128), spitch_f))
-    _need(dtype in _TYPES, f"unsupported output type {dtype}")
-    ldr = 0
+    pa = _packed(a, "a", CODES, device, (tokens, pitch))
+    psa = _packed(a_scale, "a_scale", SCALES, device, (tokens, spitch))
+    pi = _packed(ids, "ids", torch.int32, device, (tokens, chosen))
+    pw = _packed(weight, "weight", torch.float32, device, (tokens, chosen))
+    pf = _packed(offsets, "offsets", torch.int32, device, (experts + 1,))
+    po = _packed(order, "order", torch.int32, device, (tokens * chosen,))
+    p1 = _packed(w_in, "w_in", CODES, device, (experts, 2, inner, pitch))
+    ps1 = _packed(w_in_scale, "w_in_scale", SCALES, device, (experts, 2, -(-inner // 128), spitch))
+    p2 = _packed(w_out, "w_out", CODES, device, (experts, width, pitch_f))
+    ps2 = _packed(w_out_scale, "w_out_scale", SCALES, device, (experts, -(-width // 128), spitch_f))
+    pr, ldr = None, 0
     if residual is not None:
-        ldr = _dense(residual, "residual", dtype, device, (tokens, width))
+        ldr, pr = _dense(residual, "residual", dtype, device, (tokens, width)), residual.data_ptr()
     if out is None:
-        out = torch.empty((tokens, width), dtype=dtype, device=device)
-    ldo = _dense(out, "out", dtype, device, (tokens, width))
+        out, ldo = torch.empty((tokens, width), dtype=dtype, device=device), width
+    else:
+        ldo = _dense(out, "out", dtype, device, (tokens, width))
     if ws is None:
-        need = sd.sdnn_experts_workspace_size(tokens, width, inner, experts, chosen, _TYPES[dtype])
+        need = sd.sdnn_experts_workspace_size(tokens, width, inner, experts, chosen, kind)
         ws = torch.empty(need, dtype=torch.uint8, device=device)
     else:
-        _need(ws.is_cuda and ws.device == device and ws.dtype == torch.uint8 and ws.is_contiguous(),
+        _need(ws.device == device and ws.dtype is torch.uint8 and ws.is_contiguous(),
               "ws must be a contiguous uint8 tensor on the same device")
-    sd.sdnn_experts_forward(tokens, width, inner, experts, chosen, a, a_scale, ids, weight, offsets, order, w_in,
-                            w_in_scale, w_out, w_out_scale, _TYPES[dtype], residual, ldr, out, ldo, ws, ws.numel(),
-                            _stream(device))
+    _call(sd.lib.sdnn_experts_forward(tokens, width, inner, experts, chosen, pa, psa, pi, pw, pf, po, p1, ps1, p2, ps2,
+                                      kind, pr, ldr, out.data_ptr(), ldo, ws.data_ptr(), ws.numel(), _stream(device)))
     return out
