@@ -83,7 +83,8 @@ struct TileWork {
     bool wide;        // output rows start at multiples of 16 bytes
     const uint8_t *p_codes, *p_scales;  // the experts' inner rows, one per sorted slot
     uint8_t *p_codes_out, *p_scales_out;
-    void *o;  // the experts' output rows, one per slot
+    void *o;  // the experts' output rows, one per slot, o_pitch values apart
+    int64_t o_pitch;
 };
 
 hipError_t launch_product_tile(const ProductArgs &a, const TileWork &work, bool bf16, hipStream_t s);

@@ -30,70 +30,115 @@ __device__ __forceinline__ v8i load32(const uint8_t *p) {
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
-// 16 outputs x 16 rows per workgroup, whose waves share the blocks of the inner dimension and join their sums in LDS.
-constexpr int kSplit = 4;
+// 16 outputs x up to 64 rows per workgroup, straight from memory to registers: the weights are read once, which is what
+// bounds these calls.  The waves share the blocks of the inner dimension and join their sums in LDS.
+constexpr int kSplit = 8;
 
-__device__ __forceinline__ v4f stream_tile(const uint8_t *w, const uint8_t *ws, const uint8_t *x, const uint8_t *xs,
-                                           int64_t kb, int wave) {
-    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+// acc[v][m] += this wave's blocks of NW weight tiles times MT activation tiles.  BATCH blocks are loaded before the
+// first is multiplied, so that a wave has several kilobytes on their way.
+template <int NW, int MT, int BATCH>
+__device__ __forceinline__ void stream_tiles(v4f (&acc)[NW][MT], const uint8_t *const (&w)[NW],
+                                             const uint8_t *const (&ws)[NW], const uint8_t *const (&x)[MT],
+                                             const uint8_t *const (&xs)[MT], int kb, int first, int step) {
     const int part = (threadIdx.x % 64) / 16 * 32;
-    for (int64_t b = wave; b < kb; b += kSplit)
-        acc = block16(load32(w + b * kBlock + part), load32(x + b * kBlock + part), acc, ws[b], xs[b]);
-    return acc;
+    for (int b0 = first; b0 < kb; b0 += step * BATCH) {
+        v8i wq[BATCH][NW], xq[BATCH][MT];
+        int wc[BATCH][NW], xc[BATCH][MT];
+#pragma unroll
+        for (int u = 0; u < BATCH; u++) {
+            const int b = min(b0 + u * step, kb - 1);
+#pragma unroll
+            for (int v = 0; v < NW; v++) wq[u][v] = load32(w[v] + (int64_t)b * kBlock + part), wc[u][v] = ws[v][b];
+#pragma unroll
+            for (int m = 0; m < MT; m++) xq[u][m] = load32(x[m] + (int64_t)b * kBlock + part), xc[u][m] = xs[m][b];
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; u++)
+            if (b0 + u * step < kb)
+#pragma unroll
+                for (int v = 0; v < NW; v++)
+#pragma unroll
+                    for (int m = 0; m < MT; m++)
+                        acc[v][m] = block16(wq[u][v], xq[u][m], acc[v][m], wc[u][v], xc[u][m]);
+    }
 }
 
-__device__ __forceinline__ v4f join(v4f acc, v4f (*part)[64]) {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    part[wave][lane] = acc;
-    __syncthreads();
+// The waves' sums of a tile.
+__device__ __forceinline__ v4f total(const v4f (*part)[64]) {
+    const int lane = threadIdx.x % 64;
     v4f s = part[0][lane];
     for (int i = 1; i < kSplit; i++) s += part[i][lane];
     return s;
 }
 
-template <typename T>
+template <typename T, int MT>
 __global__ void __launch_bounds__(64 * kSplit) product_stream_kernel(ProductArgs a) {
-    __shared__ v4f part[kSplit][64];
+    __shared__ v4f part[MT][kSplit][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t n_tiles = (a.n + 15) / 16;
-    const int64_t n0 = blockIdx.x % n_tiles * 16, m0 = blockIdx.x / n_tiles * 16;
-    const int64_t n = min(n0 + lane % 16, a.n - 1), m = min(m0 + lane % 16, a.m - 1);
+    const int64_t n0 = blockIdx.x % n_tiles * 16, m0 = blockIdx.x / n_tiles * (16 * MT);
     const int64_t pitch = code_pitch(a.k), spitch = scale_pitch(a.k);
-    v4f acc = stream_tile(a.w + n * pitch, a.w_scale + n0 / kBlock * spitch, a.a + m * pitch,
-                                  a.a_scale + m * spitch, blocks_of(a.k), wave);
-    acc = join(acc, part);
-    if (wave != 0 || m0 + lane % 16 >= a.m) return;
+    const uint8_t *w[1] = {a.w + min(n0 + lane % 16, a.n - 1) * pitch}, *ws[1] = {a.w_scale + n0 / kBlock * spitch};
+    const uint8_t *x[MT], *xs[MT];
+    v4f acc[1][MT];
+#pragma unroll
+    for (int t = 0; t < MT; t++) {
+        const int64_t m = min(m0 + t * 16 + lane % 16, a.m - 1);
+        x[t] = a.a + m * pitch, xs[t] = a.a_scale + m * spitch;
+        acc[0][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    stream_tiles<1, MT, MT == 1 ? 4 : 2>(acc, w, ws, x, xs, (int)blocks_of(a.k), wave, kSplit);
+#pragma unroll
+    for (int t = 0; t < MT; t++) part[t][wave][lane] = acc[0][t];
+    __syncthreads();
+    const int64_t m = m0 + wave * 16 + lane % 16;  // a wave for each tile of rows
+    if (wave >= MT || m >= a.m) return;
+    const v4f s = total(part[wave]);
     T *y = (T *)a.y + m * a.ldy;
     for (int i = 0; i < 4; i++) {
         const int64_t col = n0 + lane / 16 * 4 + i;
         if (col >= a.n) break;
-        float z = acc[i];
+        float z = s[i];
         if (a.bias) z += a.bias[col];
         if (a.activate) z = relu_clamp(z, a.ymax);
         store_out(y + col, z);
     }
 }
 
-// p(slot, f) = silu(gate) * up in fp32, one row of `pitch` values per sorted slot.
+// p = silu(gate) * up in fp32, a row of code_pitch(inner) values per slot.  BY_SLOT: a workgroup takes one slot, and p's
+// rows are the slots; otherwise 16 sorted slots of one expert, and p's rows are in their order.
+template <bool BY_SLOT>
 __global__ void __launch_bounds__(64 * kSplit) experts_in_stream_kernel(ExpertsArgs a, float *p) {
     __shared__ v4f part[2][kSplit][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t f_tiles = (a.inner + 15) / 16, slots = a.tokens * a.chosen;
     const int64_t f0 = blockIdx.x % f_tiles * 16;
-    int64_t row0;
-    int rows;
-    const int e = find_tile(a.offsets, a.experts, slots, (int)(blockIdx.x / f_tiles), 16, row0, rows);
-    if (e < 0) return;
-    const int64_t at = row0 + min(lane % 16, rows - 1);
-    const int64_t slot = min(max((int64_t)a.order[at], (int64_t)0), slots - 1), token = slot / a.chosen;
+    int64_t at, token;
+    int rows = 1, e;
+    if constexpr (BY_SLOT) {
+        at = blockIdx.x / f_tiles;
+        e = a.ids[at];
+        if (e < 0 || e >= a.experts) return;
+        token = at / a.chosen;
+    } else {
+        int64_t row0;
+        e = find_tile(a.offsets, a.experts, slots, (int)(blockIdx.x / f_tiles), 16, row0, rows);
+        if (e < 0) return;
+        at = row0 + min(lane % 16, rows - 1);
+        token = min(max((int64_t)a.order[at], (int64_t)0), slots - 1) / a.chosen;
+    }
     const int64_t f = min(f0 + lane % 16, a.inner - 1);
     const int64_t pitch = code_pitch(a.width), spitch = scale_pitch(a.width), fb = blocks_of(a.inner);
-    const uint8_t *x = a.a + token * pitch, *xs = a.a_scale + token * spitch;
-    const uint8_t *gate = a.w_in + ((int64_t)e * 2 * a.inner + f) * pitch, *up = gate + a.inner * pitch;
-    const uint8_t *gate_s = a.w_in_scale + ((int64_t)e * 2 * fb + f0 / kBlock) * spitch, *up_s = gate_s + fb * spitch;
-    const v4f g = join(stream_tile(gate, gate_s, x, xs, blocks_of(a.width), wave), part[0]);
-    const v4f u = join(stream_tile(up, up_s, x, xs, blocks_of(a.width), wave), part[1]);
+    const uint8_t *gate = a.w_in + ((int64_t)e * 2 * a.inner + f) * pitch;
+    const uint8_t *gate_s = a.w_in_scale + ((int64_t)e * 2 * fb + f0 / kBlock) * spitch;
+    const uint8_t *w[2] = {gate, gate + a.inner * pitch}, *ws[2] = {gate_s, gate_s + fb * spitch};
+    const uint8_t *x[1] = {a.a + token * pitch}, *xs[1] = {a.a_scale + token * spitch};
+    v4f acc[2][1] = {};
+    stream_tiles<2, 1, 2>(acc, w, ws, x, xs, (int)blocks_of(a.width), wave, kSplit);
+    part[0][wave][lane] = acc[0][0], part[1][wave][lane] = acc[1][0];
+    __syncthreads();
     if (wave != 0 || lane % 16 >= rows) return;
+    const v4f g = total(part[0]), u = total(part[1]);
     for (int i = 0; i < 4; i++) {
         const int64_t col = f0 + lane / 16 * 4 + i;
         if (col < a.inner) p[at * code_pitch(a.inner) + col] = silu_times(g[i], u[i]);
@@ -103,11 +148,18 @@ __global__ void __launch_bounds__(64 * kSplit) experts_in_stream_kernel(ExpertsA
 // One block of 128 columns of p (fp32) rounded to 8 bits in registers: the same codes as if it had been stored so.
 __device__ __forceinline__ v8i quantize_row(const float *p, int64_t col, int64_t k, int &code) {
     float v[32], amax = 0.0f;
+    if (col + 32 <= k) {  // rows of p start at multiples of 16 bytes
 #pragma unroll
-    for (int i = 0; i < 32; i++) {
-        v[i] = col + i < k ? p[col + i] : 0.0f;
-        amax = fmaxf(amax, finite_abs(v[i]));
+        for (int i = 0; i < 32; i += 4) {
+            const v4f four = *(const v4f *)(p + col + i);
+            for (int j = 0; j < 4; j++) v[i + j] = four[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; i++) v[i] = col + i < k ? p[col + i] : 0.0f;
     }
+#pragma unroll
+    for (int i = 0; i < 32; i++) amax = fmaxf(amax, finite_abs(v[i]));
     amax = fmaxf(amax, __shfl_xor(amax, 16));
     amax = fmaxf(amax, __shfl_xor(amax, 32));
     code = scale_code(amax);
@@ -118,8 +170,35 @@ __device__ __forceinline__ v8i quantize_row(const float *p, int64_t col, int64_t
     return q;
 }
 
+// This wave's blocks of p's row times 16 rows of an expert's second matrix.
+__device__ __forceinline__ v4f stream_out(const uint8_t *w, const uint8_t *ws, const float *p, int64_t k, int first,
+                                          int step) {
+    constexpr int kBatch = 4;
+    const int part = (threadIdx.x % 64) / 16 * 32, kb = (int)blocks_of(k);
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int b0 = first; b0 < kb; b0 += step * kBatch) {
+        v8i wq[kBatch];
+        int wc[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            const int b = min(b0 + u * step, kb - 1);
+            wq[u] = load32(w + (int64_t)b * kBlock + part), wc[u] = ws[b];
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            const int b = b0 + u * step;
+            if (b >= kb) break;
+            int code;
+            const v8i x = quantize_row(p, (int64_t)b * kBlock + part, k, code);
+            acc = block16(wq[u], x, acc, wc[u], code);
+        }
+    }
+    return acc;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(64 * kSplit) experts_out_stream_kernel(ExpertsArgs a, const float *p, T *o) {
+__global__ void __launch_bounds__(64 * kSplit) experts_out_stream_kernel(ExpertsArgs a, const float *p, T *o,
+                                                                         int64_t o_pitch) {
     __shared__ v4f part[kSplit][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t n_tiles = (a.width + 15) / 16, slots = a.tokens * a.chosen;
@@ -130,29 +209,91 @@ __global__ void __launch_bounds__(64 * kSplit) experts_out_stream_kernel(Experts
     if (e < 0) return;
     const int64_t at = row0 + min(lane % 16, rows - 1);
     const int64_t n = min(n0 + lane % 16, a.width - 1);
-    const int64_t pitch = code_pitch(a.inner), spitch = scale_pitch(a.inner), kb = blocks_of(a.inner);
-    const uint8_t *w = a.w_out + ((int64_t)e * a.width + n) * pitch;
-    const uint8_t *ws = a.w_out_scale + ((int64_t)e * blocks_of(a.width) + n0 / kBlock) * spitch;
-    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t b = wave; b < kb; b += kSplit) {
-        const int64_t col = b * kBlock + lane / 16 * 32;
-        int code;
-        const v8i x = quantize_row(p + at * pitch, col, a.inner, code);
-        acc = block16(load32(w + col), x, acc, ws[b], code);
-    }
-    acc = join(acc, part);
+    const int64_t pitch = code_pitch(a.inner);
+    const uint8_t *ws = a.w_out_scale + ((int64_t)e * blocks_of(a.width) + n0 / kBlock) * scale_pitch(a.inner);
+    part[wave][lane] =
+        stream_out(a.w_out + ((int64_t)e * a.width + n) * pitch, ws, p + at * pitch, a.inner, wave, kSplit);
+    __syncthreads();
     if (wave != 0 || lane % 16 >= rows) return;
+    const v4f s = total(part);
     const int64_t slot = min(max((int64_t)a.order[at], (int64_t)0), slots - 1);
     for (int i = 0; i < 4; i++) {
         const int64_t col = n0 + lane / 16 * 4 + i;
-        if (col < a.width) store_out(o + slot * a.width + col, acc[i]);
+        if (col < a.width) store_out(o + slot * o_pitch + col, s[i]);
     }
 }
 
+// A few tokens: 16 outputs of one token per workgroup, all its experts at once, each taken by one wave or by several
+// that share its blocks, and the weighted sum in the same place.  A wave rounds four blocks of p at a time, 16 lanes to
+// a block, while their weights are on the way.
+template <typename T>
+__global__ void __launch_bounds__(64 * kSplit) experts_out_slot_kernel(ExpertsArgs a, const float *p, int share) {
+    constexpr int kPass = 4;
+    __shared__ __align__(16) float part[kRouteMaxChosen][16];
+    __shared__ __align__(16) float shared_part[kSplit][16];
+    __shared__ __align__(16) uint8_t codes[kSplit][kPass * kBlock];
+    __shared__ int scale[kSplit][kPass];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t n_tiles = (a.width + 15) / 16;
+    const int64_t n0 = blockIdx.x % n_tiles * 16, token = blockIdx.x / n_tiles;
+    const int64_t n = min(n0 + lane % 16, a.width - 1), pitch = code_pitch(a.inner);
+    const int kb = (int)blocks_of(a.inner);
+    for (int u = wave; u < a.chosen * share; u += kSplit) {
+        const int64_t slot = token * a.chosen + u / share;
+        const int e = a.ids[slot];
+        if (e < 0 || e >= a.experts) continue;
+        const uint8_t *w = a.w_out + ((int64_t)e * a.width + n) * pitch + lane / 16 * 32;
+        const uint8_t *ws = a.w_out_scale + ((int64_t)e * blocks_of(a.width) + n0 / kBlock) * scale_pitch(a.inner);
+        const float *row = p + slot * pitch;
+        v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b0 = u % share * kPass; b0 < kb; b0 += share * kPass) {
+            const int64_t col = (int64_t)b0 * kBlock + lane * 8;
+            float v[8];
+            load8<float, true>(row, col, a.inner, v);
+            v8i wq[kPass];
+            int wc[kPass];
+#pragma unroll
+            for (int i = 0; i < kPass; i++) {
+                const int b = min(b0 + i, kb - 1);
+                wq[i] = load32(w + (int64_t)b * kBlock), wc[i] = ws[b];
+            }
+            float amax = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) amax = fmaxf(amax, finite_abs(v[i]));
+            const int code = scale_code(row16_max(amax));
+            const float inv = inverse_scale(code);
+            *(int2 *)(codes[wave] + lane * 8) =
+                make_int2(pack_e4m3(v[0], v[1], v[2], v[3], inv), pack_e4m3(v[4], v[5], v[6], v[7], inv));
+            if (lane % 16 == 0) scale[wave][lane / 16] = code;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own LDS, read by its other lanes
+#pragma unroll
+            for (int i = 0; i < kPass; i++)
+                if (b0 + i < kb)
+                    acc = block16(wq[i], load32(codes[wave] + i * kBlock + lane / 16 * 32), acc, wc[i],
+                                  scale[wave][i]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        if (lane % 16 == 0) *(v4f *)(share > 1 ? &shared_part[u][lane / 4] : &part[u][lane / 4]) = acc;
+    }
+    __syncthreads();
+    const int64_t col = n0 + threadIdx.x;
+    if (threadIdx.x >= 16 || col >= a.width) return;
+    float s = a.residual ? load_f32((const T *)a.residual + token * a.ldr + col) : 0.0f;
+    for (int j = 0; j < a.chosen; j++) {
+        const int e = a.ids[token * a.chosen + j];
+        if (e < 0 || e >= a.experts) continue;
+        float o = share > 1 ? 0.0f : part[j][threadIdx.x];
+        if (share > 1)
+            for (int i = 0; i < share; i++) o += shared_part[j * share + i][threadIdx.x];
+        s = fmaf(a.weight[token * a.chosen + j], o, s);
+    }
+    store_out((T *)a.out + token * a.ldo + col, s);
+}
+
 // out(t) = residual(t) + sum_j weight(t, j) o(t k + j), in fp32, in the order of j.  A thread takes 8 columns of one
-// token; VEC: every row starts at a multiple of 16 bytes.
+// token; VEC: the rows of out and residual start at multiples of 16 bytes.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, const T *o, int parts) {
+__global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, const T *o, int64_t o_pitch, int parts) {
     const int64_t cells = a.tokens * parts;
     for (int64_t g = blockIdx.x; g < cells; g += gridDim.x) {
         const int64_t t = g / parts, c = (g % parts * 256 + threadIdx.x) * 8;
@@ -168,7 +309,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, con
             if (a.ids[slot] < 0) continue;
             const float w = a.weight[slot];
             float v[8];
-            load8<T, VEC>(o + slot * a.width, c, a.width, v);
+            load8<T, true>(o + slot * o_pitch, c, o_pitch, v);
             for (int i = 0; i < 8; i++) s[i] = fmaf(w, v[i], s[i]);
         }
         store8<T, VEC>((T *)a.out + t * a.ldo, c, a.width, s);
@@ -176,21 +317,27 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, con
 }
 
 template <typename T>
-void combine_go(const ExpertsArgs &a, const T *o, hipStream_t s) {
+void combine_go(const ExpertsArgs &a, const T *o, int64_t o_pitch, hipStream_t s) {
     const int parts = (int)((a.width + 2047) / 2048);
     const int64_t cells = a.tokens * parts;
     const unsigned grid = (unsigned)(cells < (1 << 20) ? cells : (1 << 20));
     const int size = sizeof(T);
-    const bool vec = a.width * size % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.ldo * size % 16 == 0 &&
+    const bool vec = ((uintptr_t)a.out & 15) == 0 && a.ldo * size % 16 == 0 &&
                      (!a.residual || (((uintptr_t)a.residual & 15) == 0 && a.ldr * size % 16 == 0));
     if (vec)
-        experts_combine_kernel<T, true><<<grid, 256, 0, s>>>(a, o, parts);
+        experts_combine_kernel<T, true><<<grid, 256, 0, s>>>(a, o, o_pitch, parts);
     else
-        experts_combine_kernel<T, false><<<grid, 256, 0, s>>>(a, o, parts);
+        experts_combine_kernel<T, false><<<grid, 256, 0, s>>>(a, o, o_pitch, parts);
 }
 
 // Few rows, or many: an average of fewer than 16 slots to a busy expert.
 bool few_slots(int64_t slots, int32_t experts) { return slots < 16 * (slots < experts ? slots : (int64_t)experts); }
+
+// So few tokens that each slot's weights are read for it alone.
+bool by_slot(int64_t tokens) { return tokens <= 4; }
+
+// Values from one row of the experts' outputs to the next: rows start at multiples of 16 bytes.
+int64_t out_pitch(int64_t width) { return (width + 7) / 8 * 8; }
 
 struct ExpertsPlan {
     size_t p, scales, o, bytes;
@@ -201,10 +348,10 @@ ExpertsPlan experts_plan(int64_t tokens, int64_t width, int64_t inner, int32_t e
     ExpertsPlan e;
     e.p = 0;
     e.scales = slots * code_pitch(inner);
-    e.o = few_slots((int64_t)slots, experts) ? slots * code_pitch(inner) * 4
+    e.o = by_slot(tokens) || few_slots((int64_t)slots, experts) ? slots * code_pitch(inner) * 4
                                              : e.scales + slots * scale_pitch(inner);
     e.o = align_up(e.o);
-    e.bytes = e.o + slots * width * (bf16 ? 2 : 4);
+    e.bytes = e.o + slots * out_pitch(width) * (bf16 ? 2 : 4);
     return e;
 }
 
@@ -213,21 +360,49 @@ hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
     const ExpertsPlan plan = experts_plan(a.tokens, a.width, a.inner, a.experts, a.chosen, sizeof(T) == 2);
     T *o = (T *)((char *)a.ws + plan.o);
     const int64_t slots = a.tokens * a.chosen;
+    const int64_t o_pitch = out_pitch(a.width);
+    float *p = (float *)((char *)a.ws + plan.p);
+    const int64_t f_tiles = (a.inner + 15) / 16, n_tiles = (a.width + 15) / 16;
+    if (by_slot(a.tokens)) {
+        if ((slots * f_tiles > a.tokens * n_tiles ? slots * f_tiles : a.tokens * n_tiles) * 64 * kSplit >=
+            (int64_t)1 << 32)
+            return hipErrorInvalidConfiguration;
+        int share = 1;
+        while (share * 2 * a.chosen <= kSplit) share *= 2;
+        experts_in_stream_kernel<true><<<(unsigned)(slots * f_tiles), 64 * kSplit, 0, s>>>(a, p);
+        experts_out_slot_kernel<T><<<(unsigned)(a.tokens * n_tiles), 64 * kSplit, 0, s>>>(a, p, share);
+        return hipGetLastError();
+    }
     if (few_slots(slots, a.experts)) {
-        float *p = (float *)((char *)a.ws + plan.p);
         const int64_t tiles = (slots < a.experts ? slots : a.experts) + slots / 16;
-        experts_in_stream_kernel<<<(unsigned)(tiles * ((a.inner + 15) / 16)), 64 * kSplit, 0, s>>>(a, p);
-        experts_out_stream_kernel<T><<<(unsigned)(tiles * ((a.width + 15) / 16)), 64 * kSplit, 0, s>>>(a, p, o);
+        if (tiles * (f_tiles > n_tiles ? f_tiles : n_tiles) * 64 * kSplit >= (int64_t)1 << 32)
+            return hipErrorInvalidConfiguration;
+        experts_in_stream_kernel<false><<<(unsigned)(tiles * f_tiles), 64 * kSplit, 0, s>>>(a, p);
+        experts_out_stream_kernel<T><<<(unsigned)(tiles * n_tiles), 64 * kSplit, 0, s>>>(a, p, o, o_pitch);
     } else {
         TileWork work{};
-        work.wide = a.width % (16 / (int)sizeof(T)) == 0;
+        work.wide = true;
+        work.o_pitch = o_pitch;
         work.p_codes = work.p_codes_out = (uint8_t *)a.ws + plan.p;
         work.p_scales = work.p_scales_out = (uint8_t *)a.ws + plan.scales;
         work.o = o;
         const hipError_t e = launch_experts_tile(a, work, sizeof(T) == 2, s);
         if (e != hipSuccess) return e;
     }
-    combine_go<T>(a, o, s);
+    combine_go<T>(a, o, o_pitch, s);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t product_few(const ProductArgs &a, hipStream_t s) {
+    const int64_t tiles = (a.n + 15) / 16;
+    if (tiles * 64 * kSplit >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
+    if (a.m <= 16)
+        product_stream_kernel<T, 1><<<(unsigned)tiles, 64 * kSplit, 0, s>>>(a);
+    else if (a.m <= 32)
+        product_stream_kernel<T, 2><<<(unsigned)tiles, 64 * kSplit, 0, s>>>(a);
+    else
+        product_stream_kernel<T, 4><<<(unsigned)tiles, 64 * kSplit, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -239,16 +414,13 @@ size_t experts_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t e
 
 hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
     if (a.m == 0 || a.n == 0) return hipSuccess;
-    if (a.m > 32) {
+    if (a.m > 64) {
         TileWork work{};
         const int size = bf16 ? 2 : 4;
         work.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy * size % 16 == 0;
         return launch_product_tile(a, work, bf16, stream);
     }
-    const unsigned grid = (unsigned)((a.n + 15) / 16 * ((a.m + 15) / 16));
-    if (bf16) product_stream_kernel<__bf16><<<grid, 64 * kSplit, 0, stream>>>(a);
-    else product_stream_kernel<float><<<grid, 64 * kSplit, 0, stream>>>(a);
-    return hipGetLastError();
+    return bf16 ? product_few<__bf16>(a, stream) : product_few<float>(a, stream);
 }
 
 hipError_t launch_experts(const ExpertsArgs &a, bool bf16, hipStream_t stream) {

@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
                 if constexpr (MODE == kTileProduct)
                     y = (T *)a.y + (row0 + r) * a.ldy;
                 else
-                    y = (T *)work.o + (int64_t)slot[r] * n_rows;
+                    y = (T *)work.o + (int64_t)slot[r] * work.o_pitch;
                 const T *from = out + lr * kPitch + col;
                 if (work.wide && n0 + col + kCells <= n_rows)
                     *(v4i *)(y + n0 + col) = *(const v4i *)from;
