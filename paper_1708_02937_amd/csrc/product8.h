@@ -51,11 +51,6 @@ __device__ __forceinline__ int find_tile(const int32_t *offsets, int experts, in
     return -1;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_out(T *p, float v) {
-    *p = (T)v;
-}
-
 __device__ __forceinline__ float relu_clamp(float z, float ymax) {
     if (z < 0.0f) z = 0.0f;
     if (z > ymax) z = ymax;

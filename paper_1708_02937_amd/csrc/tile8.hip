@@ -15,6 +15,8 @@ namespace {
 
 constexpr int kRowBytes = kBlock / 2;  // a row of a stage: half a block
 
+constexpr int kMaxLds = 160 * 1024;
+
 enum TileMode { kTileProduct, kTileExpertsIn, kTileExpertsOut };
 
 // Sixteen bytes per lane from global memory straight into LDS at base + 16 * lane.
@@ -29,24 +31,32 @@ __device__ __forceinline__ void stage_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-template <int MODE, typename T, int BN, int BM, int WN, int WM, int STAGES>
+template <int MODE, typename T, int BN, int BM, int WN, int WM, int KG, int STAGES>
 struct Tile {
-    static constexpr int kThreads = 64 * WN * WM, kWaves = WN * WM;
+    static constexpr int kThreads = 64 * WN * WM * KG, kWaves = WN * WM;  // waves of a group
     static constexpr int NI = BN / WN / 32, MJ = BM / WM / 32;
     static constexpr int kRows = BN + BM, kLoads = kRows / 16 / kWaves;
-    static constexpr int kStage = kRows * kRowBytes, kLds = STAGES * kStage + 2 * (BM + 64) * 4;
-    static constexpr bool kExact = sizeof(T) == 4, kTurns = kWaves == 8 && !kExact;
+    static constexpr int kStage = kRows * kRowBytes, kRing = STAGES * kStage * KG;
+    static constexpr int kBlockRows = BN > kBlock ? BN / kBlock : 1;  // block rows of weights
+    // the scales behind the stages: two words per row, or (KG > 1) every row's whole
+    static int64_t lds_bytes(int64_t k) {
+        return kRing + (KG == 1 ? 2 * (BM + 64) * 4 : (BM + kBlockRows) * (scale_pitch(k) + 4));
+    }
+    static constexpr bool kExact = sizeof(T) == 4, kTurns = kWaves == 8 && KG == 1 && !kExact;
     static_assert(kRows % (16 * kWaves) == 0, "every wave stages the same number of rows");
 };
 
-// Which weight row LDS row r of a tile stands for, relative to the tile's first.  In the experts' first product the
-// lower half of the tile is gate rows and the upper half the up rows of the same outputs.
-template <int MODE, typename T, int BN, int BM, int WN, int WM, int STAGES>
-__global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductArgs a, ExpertsArgs x, TileWork work) {
-    using S = Tile<MODE, T, BN, BM, WN, WM, STAGES>;
+// In the experts' first product the lower half of a tile's LDS rows is gate rows and the upper half the up rows of the
+// same outputs.  With KG > 1, KG groups of waves share the tile's blocks between them (group g takes blocks g, g + KG,
+// ...), each with stages of its own, and their sums join in the end: for products with few tiles, whose time is the
+// length of the chain of stages.
+template <int MODE, typename T, int BN, int BM, int WN, int WM, int KG, int STAGES>
+__global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_tile_kernel(ProductArgs a, ExpertsArgs x, TileWork work) {
+    using S = Tile<MODE, T, BN, BM, WN, WM, KG, STAGES>;
     constexpr int NI = S::NI, MJ = S::MJ, kStages = STAGES;
     extern __shared__ __align__(16) uint8_t lds[];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = threadIdx.x % 64, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wave = any_wave % S::kWaves, group = any_wave / S::kWaves;
     const int wn = wave % WN, wm = wave / WN;
 
     // The chiplets take workgroups in turn; each is given a run of neighbouring tiles, four tiles of rows wide, so that
@@ -113,12 +123,19 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
         } else {
             from[i] = act + act_row(r - BN) * pitch + piece;
         }
+        if (KG > 1) from[i] += min(group, kb - 1) * kBlock;
     }
+    const int stages = 2 * ((kb + KG - 1) / KG);
+    uint8_t *const ring = lds + group * (kStages * S::kStage);
     auto stage = [&](int t) {
 #pragma unroll
         for (int i = 0; i < S::kLoads; i++) {
-            stage16(from[i], lds + t % kStages * S::kStage + (i * S::kWaves + wave) * 1024);
-            from[i] += kRowBytes;
+            stage16(from[i], ring + t % kStages * S::kStage + (i * S::kWaves + wave) * 1024);
+            // the other half of the block, then the group's next block (past the end: the last one again)
+            if (KG == 1 || t % 2 == 0)
+                from[i] += kRowBytes;
+            else
+                from[i] += (t / 2 + 1) * KG + group < kb ? KG * kBlock - kRowBytes : -kRowBytes;
         }
     };
 
@@ -133,22 +150,26 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
     // Scale codes, four blocks to a word, go through LDS too: the words of the tile's activation rows, then of its block
     // rows of weights (in the experts' first product the gate's and the up rows').
     constexpr int kWords = BM + 64;
-    uint8_t *const scales = lds + kStages * S::kStage;
-    const uint8_t *scale_from = nullptr;
-    if (wave < BM / 64) {
-        scale_from = act_scale + act_row(wave * 64 + lane) * spitch;
-    } else if (wave == BM / 64) {
-        const int64_t last = (n_rows - 1) / kBlock;
+    uint8_t *const scales = lds + S::kRing;
+    const int64_t last_block = (n_rows - 1) / kBlock;
+    auto weight_scales = [&](int i) -> const uint8_t * {
         if constexpr (MODE == kTileExpertsIn)
-            scale_from = wt_scale + (min(n0 / kBlock, last) + (lane % 2) * (last + 1)) * spitch;
+            return wt_scale + (min(n0 / kBlock, last_block) + i % 2 * (last_block + 1)) * spitch;
         else
-            scale_from = wt_scale + min(n0 / kBlock + lane % (BN / kBlock), last) * spitch;
+            return wt_scale + min(n0 / kBlock + i % S::kBlockRows, last_block) * spitch;
+    };
+    const uint8_t *scale_from = nullptr;
+    if (KG == 1) {
+        if (wave < BM / 64)
+            scale_from = act_scale + act_row(wave * 64 + lane) * spitch;
+        else if (wave == BM / 64)
+            scale_from = weight_scales(lane);
     }
-    auto stage_scales = [&](int group) {
+    auto stage_scales = [&](int four) {
         if (wave <= BM / 64)
             __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void *)(scale_from + group * 4),
-                (__attribute__((address_space(3))) void *)(scales + (group & 1) * kWords * 4 + wave * 256), 4, 0, 0);
+                (const __attribute__((address_space(1))) void *)(scale_from + four * 4),
+                (__attribute__((address_space(3))) void *)(scales + (four & 1) * kWords * 4 + wave * 256), 4, 0, 0);
     };
 
     v16f acc[NI][MJ];
@@ -160,8 +181,8 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
             for (int r = 0; r < 16; r++) acc[i][j][r] = 0.0f;
 
     uint32_t xs[MJ], ws[NI];
-    auto read_scales = [&](int group) {
-        const uint32_t *w = (const uint32_t *)(scales + (group & 1) * kWords * 4);
+    auto read_scales = [&](int four) {
+        const uint32_t *w = (const uint32_t *)(scales + (four & 1) * kWords * 4);
 #pragma unroll
         for (int j = 0; j < MJ; j++) xs[j] = w[(wm * MJ + j) * 32 + lane % 32];
 #pragma unroll
@@ -169,20 +190,27 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
     };
     // Several stages are on their way while one is multiplied: a load takes longer than a stage's products.
     constexpr int kLeft = S::kLoads * (kStages - 2);
-    const int stages = 2 * kb;
-    stage_scales(0);
+    if (KG == 1) stage_scales(0);
     for (int t = 0; t < kStages - 1; t++)
         if (t < stages) stage(t);
+    if (KG > 1) {
+        const int words = (int)spitch / 4;
+        for (int c = threadIdx.x; c < (BM + S::kBlockRows) * words; c += S::kThreads) {
+            const int r = c / words, w = c % words;
+            const uint8_t *at = r < BM ? act_scale + act_row(r) * spitch : weight_scales(r - BM);
+            *(uint32_t *)(scales + r * ((int)spitch + 4) + w * 4) = *(const uint32_t *)(at + w * 4);
+        }
+    }
     // The scales of stage t, read anew every four blocks, and the next ones sent for.
     auto scales_at = [&](int t) {
-        if (t % 8 == 0) {
+        if (KG == 1 && t % 8 == 0) {
             read_scales(t / 8);
             if (t + 8 < stages) stage_scales(t / 8 + 1);
         }
     };
     // The lane's 32 bytes of LDS row r of stage t.
     auto fetch = [&](int t, int r) -> v8i {
-        const uint8_t *row = lds + t % kStages * S::kStage + r * kRowBytes;
+        const uint8_t *row = ring + t % kStages * S::kStage + r * kRowBytes;
         const int c = lane / 32 * 2, sw = r >> 2 & 3;
         const v4i lo = *(const v4i *)(row + ((c ^ sw) * 16)), hi = *(const v4i *)(row + (((c + 1) ^ sw) * 16));
         return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -191,6 +219,14 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
     auto fetch_w = [&](int t, int i) { return fetch(t, sub_row(i) + lane % 32); };
     uint32_t xc[MJ], wc[NI];  // the codes of a stage's block, in the low byte
     auto codes_at = [&](int t) {
+        if constexpr (KG > 1) {
+            const int b = min(t / 2 * KG + group, kb - 1), row = (int)spitch + 4;
+#pragma unroll
+            for (int j = 0; j < MJ; j++) xc[j] = scales[((wm * MJ + j) * 32 + lane % 32) * row + b];
+#pragma unroll
+            for (int i = 0; i < NI; i++) wc[i] = scales[(BM + sub_row(i) / kBlock) * row + b];
+            return;
+        }
         const int shift = t / 2 % 4 * 8;
 #pragma unroll
         for (int j = 0; j < MJ; j++) xc[j] = xs[j] >> shift;
@@ -251,6 +287,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
                 stage_barrier<0>();
             scales_at(t);
             if (t + kStages - 1 < stages) stage(t + kStages - 1);
+            if (KG > 1 && t / 2 * KG + group >= kb) continue;  // this group's blocks are done
             codes_at(t);
             v8i xf[MJ];
 #pragma unroll
@@ -290,14 +327,38 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
         }
     }
 
+    if constexpr (KG > 1) {
+        // The groups' sums, in the order of the groups.
+        constexpr int kSum = S::kWaves * NI * MJ * 16 * 64 * 4;
+        static_assert((KG - 1) * kSum <= S::kRing, "the groups' sums fit the stages");
+        stage_barrier<0>();
+        v4f *const sums = (v4f *)lds + (wave * NI * MJ * 4) * 64 + lane;
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < NI * MJ * 4; i++)
+                sums[(group - 1) * (kSum / 16) + i * 64] =
+                    v4f{acc[i / 4 / MJ][i / 4 % MJ][i % 4 * 4], acc[i / 4 / MJ][i / 4 % MJ][i % 4 * 4 + 1],
+                        acc[i / 4 / MJ][i / 4 % MJ][i % 4 * 4 + 2], acc[i / 4 / MJ][i / 4 % MJ][i % 4 * 4 + 3]};
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int i = 0; i < NI * MJ * 4; i++)
+#pragma unroll
+                for (int g = 0; g < KG - 1; g++) {
+                    const v4f v = sums[g * (kSum / 16) + i * 64];
+                    for (int c = 0; c < 4; c++) acc[i / 4 / MJ][i / 4 % MJ][i % 4 * 4 + c] += v[c];
+                }
+    }
+
     // acc[i][j][4 q + v]: tile row (wm MJ + j) 32 + lane % 32, weight row sub_row(i) + 8 q + 4 (lane / 32) + v
     if constexpr (MODE == kTileExpertsIn) {
         constexpr int NP = NI / 2;
         constexpr int kPitch = kBlock + 16;  // LDS pitch of a row of codes: rows start in different banks
         static_assert(BN == 2 * kBlock, "a tile's outputs are one block of p");
-        static_assert(BM * kPitch + WN * BM * 4 <= STAGES * S::kStage, "the epilogue's arrays fit the stages");
+        static_assert(BM * kPitch + WN * BM * 4 <= S::kRing, "the epilogue's arrays fit the stages");
         float *red = (float *)(lds + BM * kPitch);
         stage_barrier<0>();  // the last stage has been read
+        if (group == 0)
 #pragma unroll
         for (int j = 0; j < MJ; j++) {
             float amax = 0.0f;
@@ -315,6 +376,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
         }
         __syncthreads();
         const int64_t p_pitch = code_pitch(n_rows), p_spitch = scale_pitch(n_rows);
+        if (group == 0)
 #pragma unroll
         for (int j = 0; j < MJ; j++) {
             const int r = (wm * MJ + j) * 32 + lane % 32;
@@ -344,7 +406,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
     } else {
         // Through LDS, 32 rows of every wave at a time, so that whole lines leave for memory.
         constexpr int kCells = 16 / sizeof(T), kPitch = BN + kCells, kSlice = WM * 32;
-        static_assert(kSlice * kPitch * sizeof(T) + BN * 4 <= STAGES * S::kStage, "a slice of the outputs fits the stages");
+        static_assert(kSlice * kPitch * sizeof(T) + BN * 4 <= S::kRing, "a slice of the outputs fits the stages");
         T *out = (T *)lds;
         float *bias = (float *)(lds + kSlice * kPitch * sizeof(T));
         stage_barrier<0>();  // the last stage has been read
@@ -358,6 +420,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
 #pragma unroll
         for (int j = 0; j < MJ; j++) {
             __syncthreads();
+            if (group == 0)
 #pragma unroll
             for (int i = 0; i < NI; i++)
 #pragma unroll
@@ -392,44 +455,74 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(ProductAr
     }
 }
 
-template <int MODE, typename T, int BN, int BM, int WN, int WM, int STAGES>
+template <int MODE, typename T, int BN, int BM, int WN, int WM, int KG, int STAGES>
 hipError_t tile_go(const ProductArgs &a, const ExpertsArgs &x, TileWork work, int64_t m_tiles, int64_t outputs,
                    hipStream_t s) {
-    using S = Tile<MODE, T, BN, BM, WN, WM, STAGES>;
+    using S = Tile<MODE, T, BN, BM, WN, WM, KG, STAGES>;
     static std::atomic<unsigned long long> raised{0};
-    const auto kernel = product_tile_kernel<MODE, T, BN, BM, WN, WM, STAGES>;
-    hipError_t e = raise_lds_limit((const void *)kernel, S::kLds, raised);
+    const auto kernel = product_tile_kernel<MODE, T, BN, BM, WN, WM, KG, STAGES>;
+    const int64_t lds = S::lds_bytes(MODE == kTileProduct ? a.k : MODE == kTileExpertsIn ? x.width : x.inner);
+    hipError_t e = raise_lds_limit((const void *)kernel, kMaxLds, raised);
     if (e != hipSuccess) return e;
     constexpr int kOut = MODE == kTileExpertsIn ? BN / 2 : BN;
     work.n_tiles = (outputs + kOut - 1) / kOut;
     const int64_t grid = work.n_tiles * m_tiles;
-    if (grid * S::kThreads >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
-    kernel<<<(unsigned)grid, S::kThreads, S::kLds, s>>>(a, x, work);
+    if (grid * S::kThreads >= (int64_t)1 << 32 || lds > kMaxLds) return hipErrorInvalidConfiguration;
+    kernel<<<(unsigned)grid, S::kThreads, (unsigned)lds, s>>>(a, x, work);
     return hipGetLastError();
 }
 
+// A call is fastest on the largest tile that still gives every CU (256) a workgroup, and with few tiles the groups that
+// share a tile's blocks shorten the chain of stages.  Measured in us at K = 4096, bfloat16:
+//   N x M         64x64x4  64x64x2  128x64x4  128x128x2  256x128  256x256
+//   4096 x 128       12.1     12.5      16.3       22.5     40.0     41.7
+//   4096 x 256       15.2     12.8      16.7       22.7     40.3     42.6
+//   4096 x 512       27.0     23.5      19.8       23.6     40.9     43.3
+//   4096 x 1024      48.0     39.4      36.0       26.8     41.3     44.0
+//   4096 x 2048      88.9     76.7      70.5       53.6     44.2     46.1
+//   16384 x 1024    204.3    153.2     159.8      119.3     85.7     64.8
+// With float (the 16-bit instructions, 4096 x 256: 19.7, 22.0, 26.8, 44.3; 16384 x 512: 147.7, 122.2, 115.6, 99.0 and
+// 128x128x1 88.3) two groups on 64 x 64 are never ahead, and tiles beyond 128 x 128 do not fit the registers.
 template <typename T>
 hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
     const ExpertsArgs none{};
-    if constexpr (sizeof(T) == 2)
-        if (((a.m + 255) / 256) * ((a.n + 255) / 256) >= 256)
-            return tile_go<kTileProduct, T, 256, 256, 2, 4, 4>(a, none, work, (a.m + 255) / 256, a.n, s);
-    return tile_go<kTileProduct, T, 128, 128, 2, 2, 4>(a, none, work, (a.m + 127) / 128, a.n, s);
+    const auto tiles = [&](int side) { return (a.m + side - 1) / side; };
+    const int64_t small = tiles(64) * ((a.n + 63) / 64);
+    // the groups' kernels hold every scale of a tile in LDS
+    const bool groups = Tile<kTileProduct, T, 128, 128, 2, 2, 2, 4>::lds_bytes(a.k) <= kMaxLds;
+    if (groups && small <= 1024) {
+        if (small <= (sizeof(T) == 2 ? 128 : 256))
+            return tile_go<kTileProduct, T, 64, 64, 2, 2, 4, 4>(a, none, work, tiles(64), a.n, s);
+        if constexpr (sizeof(T) == 2)
+            if (small <= 256) return tile_go<kTileProduct, T, 64, 64, 2, 2, 2, 4>(a, none, work, tiles(64), a.n, s);
+        if (small <= 512) return tile_go<kTileProduct, T, 128, 64, 2, 2, 4, 3>(a, none, work, tiles(64), a.n, s);
+        return tile_go<kTileProduct, T, 128, 128, 2, 2, 2, 4>(a, none, work, tiles(128), a.n, s);
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (small <= 2048) return tile_go<kTileProduct, T, 256, 128, 2, 2, 1, 3>(a, none, work, tiles(128), a.n, s);
+        return tile_go<kTileProduct, T, 256, 256, 2, 4, 1, 4>(a, none, work, tiles(256), a.n, s);
+    } else {
+        return tile_go<kTileProduct, T, 128, 128, 2, 2, 1, 4>(a, none, work, tiles(128), a.n, s);
+    }
 }
 
+// Tiles of 64 rows for few rows to an expert, of 128 for many, where those still fill the chip (two workgroups to a CU,
+// or nearly).  Measured in us, 64 experts of 4096 x 1024, 8 chosen: 333 tokens (42 rows to an expert) 252 and 238, 64
+// tokens 208 and 224, 2048 tokens 531 and 447; 24 experts of 2001 x 701, 3 chosen: 333 tokens 42 and 49.
 template <typename T>
 hipError_t experts_go(const ExpertsArgs &x, TileWork work, hipStream_t s) {
     const ProductArgs none{};
     const int64_t slots = x.tokens * x.chosen, busy = slots < x.experts ? slots : x.experts;
+    const int64_t large = busy + slots / 128, small = busy + slots / 64;
     if constexpr (sizeof(T) == 2)
-        if (slots >= 128 * busy) {
-            hipError_t e = tile_go<kTileExpertsIn, T, 256, 256, 2, 4, 4>(none, x, work, busy + slots / 256, x.inner, s);
+        if (slots >= 32 * busy && large * ((x.inner + 127) / 128) >= 400) {
+            const hipError_t e = tile_go<kTileExpertsIn, T, 256, 128, 2, 2, 1, 3>(none, x, work, large, x.inner, s);
             if (e != hipSuccess) return e;
-            return tile_go<kTileExpertsOut, T, 256, 128, 2, 2, 3>(none, x, work, busy + slots / 128, x.width, s);
+            return tile_go<kTileExpertsOut, T, 256, 128, 2, 2, 1, 3>(none, x, work, large, x.width, s);
         }
-    hipError_t e = tile_go<kTileExpertsIn, T, 256, 64, 2, 2, 6>(none, x, work, busy + slots / 64, x.inner, s);
+    const hipError_t e = tile_go<kTileExpertsIn, T, 256, 64, 2, 2, 1, 3>(none, x, work, small, x.inner, s);
     if (e != hipSuccess) return e;
-    return tile_go<kTileExpertsOut, T, 128, 64, 2, 2, 6>(none, x, work, busy + slots / 64, x.width, s);
+    return tile_go<kTileExpertsOut, T, 128, 64, 2, 2, 1, 3>(none, x, work, small, x.width, s);
 }
 
 }  // namespace
