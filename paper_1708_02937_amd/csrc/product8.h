@@ -10,13 +10,18 @@ namespace sdnn {
 
 constexpr int kOne = 127;  // the scale code of 1
 
-__device__ __forceinline__ v8bf widen8(int lo, int hi) {
-    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false),
-               b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
-               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false),
-               d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// Eight codes times 2^(code - 127) as bfloat16.
+__device__ __forceinline__ v8bf widen8(int lo, int hi, int code) {
+    const float s = __int_as_float(code << 23);
+    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false),
+               b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false),
+               d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
     return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+
+// Whether every code times that scale, 2^-9 to 448 times 2^(code - 127), is a normal bfloat16: widening is then exact.
+__device__ __forceinline__ bool widens(int code) { return code >= 10 && code <= 245; }
 
 // Which expert's tile of `rows_per_tile` sorted slots number `tile` is; tiles are numbered expert by expert.  Returns the expert (-1 past the
 // last tile) and the tile's first row and row count among the sorted slots.

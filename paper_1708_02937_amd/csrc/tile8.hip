@@ -6,8 +6,8 @@
 //   bfloat16  the scaled 8-bit instructions, which multiply by both blocks' powers of two themselves.  Within an
 //             instruction they align products to the largest one and keep about 14 bits, 1.5e-5 of a sum of normal
 //             values (measured), a hundredth of the output's own rounding; between instructions the sum is fp32.
-//   float     codes widened to bfloat16, which is exact, and the 16-bit instructions, whose products and sums are
-//             fp32; each block's sum is scaled as it joins the total.  Half the matrix rate.
+//   float     codes widened to bfloat16 with their scales, which is exact, and the 16-bit instructions, whose products
+//             and sums are fp32.  Half the matrix rate.
 #include "product8.h"
 
 namespace sdnn {
@@ -303,24 +303,44 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
                         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[i], xf[j], acc[i][j], 0, 0, 0,
                                                                                     wc[i], 0, xc[j]);
             } else {
+                bool plain = true;  // every code of the stage lets its block be widened with its scale
+#pragma unroll
+                for (int j = 0; j < MJ; j++) plain = plain && widens((int)(xc[j] & 255));
+#pragma unroll
+                for (int i = 0; i < NI; i++) plain = plain && widens((int)(wc[i] & 255));
+                plain = __all(plain);
+                v8bf xw[MJ][4];
+#pragma unroll
+                for (int j = 0; j < MJ; j++)
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+                        xw[j][c] = widen8(xf[j][2 * c], xf[j][2 * c + 1], plain ? (int)(xc[j] & 255) : kOne);
 #pragma unroll
                 for (int i = 0; i < NI; i++) {
                     const v8i q = fetch_w(t, i);
                     v8bf wf[4];
 #pragma unroll
-                    for (int c = 0; c < 4; c++) wf[c] = widen8(q[2 * c], q[2 * c + 1]);
+                    for (int c = 0; c < 4; c++)
+                        wf[c] = widen8(q[2 * c], q[2 * c + 1], plain ? (int)(wc[i] & 255) : kOne);
+                    if (plain) {
 #pragma unroll
-                    for (int j = 0; j < MJ; j++) {
-                        v16f z;
+                        for (int j = 0; j < MJ; j++)
 #pragma unroll
-                        for (int r = 0; r < 16; r++) z[r] = 0.0f;
+                            for (int c = 0; c < 4; c++)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[c], xw[j][c], acc[i][j], 0, 0, 0);
+                    } else {
 #pragma unroll
-                        for (int c = 0; c < 4; c++)
-                            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[c], widen8(xf[j][2 * c], xf[j][2 * c + 1]),
-                                                                        z, 0, 0, 0);
-                        const int e = (int)(wc[i] & 255) + (int)(xc[j] & 255) - 2 * kOne;
+                        for (int j = 0; j < MJ; j++) {
+                            v16f z;
 #pragma unroll
-                        for (int r = 0; r < 16; r++) acc[i][j][r] += ldexpf(z[r], e);
+                            for (int r = 0; r < 16; r++) z[r] = 0.0f;
+#pragma unroll
+                            for (int c = 0; c < 4; c++)
+                                z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[c], xw[j][c], z, 0, 0, 0);
+                            const int e = (int)(wc[i] & 255) + (int)(xc[j] & 255) - 2 * kOne;
+#pragma unroll
+                            for (int r = 0; r < 16; r++) acc[i][j][r] += ldexpf(z[r], e);
+                        }
                     }
                 }
             }
@@ -435,21 +455,35 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
                     put4(out + (wm * 32 + lane % 32) * kPitch + c, z);
                 }
             __syncthreads();
-            constexpr int kPieces = BN / kCells;
-#pragma unroll
-            for (int c = threadIdx.x; c < kSlice * kPieces; c += S::kThreads) {
-                const int lr = c / kPieces, r = (lr / 32 * MJ + j) * 32 + lr % 32, col = c % kPieces * kCells;
-                if (r >= rows || n0 + col >= n_rows) continue;
-                T *y;
+            // Row lr of the slice, in tile row (lr / 32 MJ + j) 32 + lr % 32.
+            auto row_of = [&](int lr) -> T * {
+                const int r = (lr / 32 * MJ + j) * 32 + lr % 32;
+                if (r >= rows) return nullptr;
                 if constexpr (MODE == kTileProduct)
-                    y = (T *)a.y + (row0 + r) * a.ldy;
+                    return (T *)a.y + (row0 + r) * a.ldy + n0;
                 else
-                    y = (T *)work.o + (int64_t)slot[r] * work.o_pitch;
-                const T *from = out + lr * kPitch + col;
-                if (work.wide && n0 + col + kCells <= n_rows)
-                    *(v4i *)(y + n0 + col) = *(const v4i *)from;
-                else
-                    for (int v = 0; v < kCells && n0 + col + v < n_rows; v++) y[n0 + col + v] = from[v];
+                    return (T *)work.o + (int64_t)slot[r] * work.o_pitch + n0;
+            };
+            const int cols = (int)min((int64_t)BN, n_rows - n0);
+            if (work.wide) {
+                constexpr int kPieces = BN / kCells;
+#pragma unroll
+                for (int c = threadIdx.x; c < kSlice * kPieces; c += S::kThreads) {
+                    const int lr = c / kPieces, col = c % kPieces * kCells;
+                    T *const y = row_of(lr);
+                    const T *const from = out + lr * kPitch + col;
+                    if (!y || col >= cols) continue;
+                    if (col + kCells <= cols)
+                        *(v4i *)(y + col) = *(const v4i *)from;
+                    else
+                        for (int v = 0; col + v < cols; v++) y[col + v] = from[v];
+                }
+            } else {  // rows at any address: a value per lane, neighbours side by side
+                static_assert(S::kThreads % BN == 0 || BN % S::kThreads == 0, "a thread keeps its columns");
+                for (int col = threadIdx.x % BN; col < cols; col += S::kThreads)
+#pragma unroll 4
+                    for (int lr = threadIdx.x / BN; lr < kSlice; lr += S::kThreads > BN ? S::kThreads / BN : 1)
+                        if (T *const y = row_of(lr)) y[col] = out[lr * kPitch + col];
             }
         }
     }
