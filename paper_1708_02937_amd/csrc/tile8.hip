@@ -507,16 +507,17 @@ hipError_t tile_go(const ProductArgs &a, const ExpertsArgs &x, TileWork work, in
 }
 
 // A call is fastest on the largest tile that still gives every CU (256) a workgroup, and with few tiles the groups that
-// share a tile's blocks shorten the chain of stages.  Measured in us at K = 4096, bfloat16:
-//   N x M         64x64x4  64x64x2  128x64x4  128x128x2  256x128  256x256
-//   4096 x 128       12.1     12.5      16.3       22.5     40.0     41.7
-//   4096 x 256       15.2     12.8      16.7       22.7     40.3     42.6
-//   4096 x 512       27.0     23.5      19.8       23.6     40.9     43.3
-//   4096 x 1024      48.0     39.4      36.0       26.8     41.3     44.0
-//   4096 x 2048      88.9     76.7      70.5       53.6     44.2     46.1
-//   16384 x 1024    204.3    153.2     159.8      119.3     85.7     64.8
-// With float (the 16-bit instructions, 4096 x 256: 19.7, 22.0, 26.8, 44.3; 16384 x 512: 147.7, 122.2, 115.6, 99.0 and
-// 128x128x1 88.3) two groups on 64 x 64 are never ahead, and tiles beyond 128 x 128 do not fit the registers.
+// share a tile's blocks shorten the chain of stages.  Measured in us at K = 4096, bfloat16 (x 4: four groups):
+//   N x M         64x64 x4  64x64 x2  128x64 x2  128x128 x2  256x128  256x256
+//   4096 x 128        12.1      12.5       16.3        22.5     40.0     41.7
+//   4096 x 256        16.1      13.3       17.0        22.7     40.3     42.6
+//   4096 x 512        25.5      23.0       18.8        23.2     40.9     43.3
+//   4096 x 1024       47.6      40.8       31.6        26.8     41.3     44.0
+//   4096 x 2048       88.9      76.7                   53.6     44.2     46.1
+//   16384 x 1024     208.9     155.0      129.2       115.6     85.7     64.8
+// With float (the 16-bit instructions) four groups are ahead for longer: 4096 x 256 20.4, 22.5 and 31.4, 4096 x 512 on
+// 128 x 64 with four groups 30.1 and with two 32.6; and tiles beyond 128 x 128 do not fit the registers.  Over short rows
+// the chain is short anyway: 777 x 2999 x 1001 on 64 x 64 with one group 11.6 (float 17.2), on 128 x 128 x2 13.6 (19.7).
 template <typename T>
 hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
     const ExpertsArgs none{};
@@ -527,9 +528,13 @@ hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
     if (groups && small <= 1024) {
         if (small <= (sizeof(T) == 2 ? 128 : 256))
             return tile_go<kTileProduct, T, 64, 64, 2, 2, 4, 4>(a, none, work, tiles(64), a.n, s);
-        if constexpr (sizeof(T) == 2)
+        if constexpr (sizeof(T) == 2) {
             if (small <= 256) return tile_go<kTileProduct, T, 64, 64, 2, 2, 2, 4>(a, none, work, tiles(64), a.n, s);
-        if (small <= 512) return tile_go<kTileProduct, T, 128, 64, 2, 2, 4, 3>(a, none, work, tiles(64), a.n, s);
+            if (small <= 512) return tile_go<kTileProduct, T, 128, 64, 2, 2, 2, 3>(a, none, work, tiles(64), a.n, s);
+        } else {
+            if (small <= 512) return tile_go<kTileProduct, T, 128, 64, 2, 2, 4, 3>(a, none, work, tiles(64), a.n, s);
+        }
+        if (a.k <= 2048) return tile_go<kTileProduct, T, 64, 64, 2, 2, 1, 4>(a, none, work, tiles(64), a.n, s);
         return tile_go<kTileProduct, T, 128, 128, 2, 2, 2, 4>(a, none, work, tiles(128), a.n, s);
     }
     if constexpr (sizeof(T) == 2) {
