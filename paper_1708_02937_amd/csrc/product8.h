@@ -72,6 +72,11 @@ __device__ __forceinline__ void put4(__bf16 *p, const v4f &z) {
     *(v4bf *)p = v4bf{(__bf16)z[0], (__bf16)z[1], (__bf16)z[2], (__bf16)z[3]};
 }
 
+__device__ __forceinline__ void put4(_Float16 *p, const v4f &z) {
+    typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+    *(v4h *)p = v4h{(_Float16)z[0], (_Float16)z[1], (_Float16)z[2], (_Float16)z[3]};
+}
+
 // Workgroup `id` of `count` goes to chiplet id % 8: the tile that gives every chiplet a run of neighbours.
 __device__ __forceinline__ int64_t chiplet_order(int64_t id, int64_t count) {
     const int64_t each = count / 8, more = count % 8, x = id % 8;
@@ -85,9 +90,11 @@ struct TileWork {
     uint8_t *p_codes_out, *p_scales_out;
     void *o;  // the experts' output rows, one per slot, o_pitch values apart
     int64_t o_pitch;
+    uint8_t *o_scales;  // with bfloat16 outputs they are half precision, and this the code of each row's tile's scale
 };
 
 hipError_t launch_product_tile(const ProductArgs &a, const TileWork &work, bool bf16, hipStream_t s);
-hipError_t launch_experts_tile(const ExpertsArgs &x, const TileWork &work, bool bf16, hipStream_t s);
+// run: receives how many columns of an output row share a scale
+hipError_t launch_experts_tile(const ExpertsArgs &x, const TileWork &work, bool bf16, int *run, hipStream_t s);
 
 }  // namespace sdnn

@@ -188,9 +188,10 @@ __global__ void __launch_bounds__(64 * kSplit) experts_out_slot_kernel(ExpertsAr
 }
 
 // out(t) = residual(t) + sum_j weight(t, j) o(t k + j), in fp32, in the order of j.  A thread takes 8 columns of one
-// token; VEC: the rows of out and residual start at multiples of 16 bytes.
+// token; VEC: the rows of out and residual start at multiples of 16 bytes.  o is float, or half precision with a scale
+// for each run of `run` columns.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, const T *o, int64_t o_pitch, int parts) {
+__global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, TileWork work, int run, int parts) {
     const int64_t cells = a.tokens * parts;
     for (int64_t g = blockIdx.x; g < cells; g += gridDim.x) {
         const int64_t t = g / parts, c = (g % parts * 256 + threadIdx.x) * 8;
@@ -205,16 +206,24 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, con
             const int64_t slot = t * a.chosen + j;
             if (a.ids[slot] < 0) continue;
             const float w = a.weight[slot];
-            float v[8];
-            load8<T, true>(o + slot * o_pitch, c, o_pitch, v);
-            for (int i = 0; i < 8; i++) s[i] = fmaf(w, v[i], s[i]);
+            if constexpr (sizeof(T) == 4) {
+                float v[8];
+                load8<float, true>((const float *)work.o + slot * work.o_pitch, c, work.o_pitch, v);
+                for (int i = 0; i < 8; i++) s[i] = fmaf(w, v[i], s[i]);
+            } else {
+                typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+                const v8h v = *(const v8h *)((const _Float16 *)work.o + slot * work.o_pitch + c);
+                const int code = work.o_scales[slot * work.n_tiles + c / run];
+                const float scale = __int_as_float(code << 23);
+                for (int i = 0; i < 8; i++) s[i] = fmaf(w, (float)v[i] * scale, s[i]);
+            }
         }
         store8<T, VEC>((T *)a.out + t * a.ldo, c, a.width, s);
     }
 }
 
 template <typename T>
-void combine_go(const ExpertsArgs &a, const T *o, int64_t o_pitch, hipStream_t s) {
+void combine_go(const ExpertsArgs &a, const TileWork &work, int run, hipStream_t s) {
     const int parts = (int)((a.width + 2047) / 2048);
     const int64_t cells = a.tokens * parts;
     const unsigned grid = (unsigned)(cells < (1 << 20) ? cells : (1 << 20));
@@ -222,9 +231,9 @@ void combine_go(const ExpertsArgs &a, const T *o, int64_t o_pitch, hipStream_t s
     const bool vec = ((uintptr_t)a.out & 15) == 0 && a.ldo * size % 16 == 0 &&
                      (!a.residual || (((uintptr_t)a.residual & 15) == 0 && a.ldr * size % 16 == 0));
     if (vec)
-        experts_combine_kernel<T, true><<<grid, 256, 0, s>>>(a, o, o_pitch, parts);
+        experts_combine_kernel<T, true><<<grid, 256, 0, s>>>(a, work, run, parts);
     else
-        experts_combine_kernel<T, false><<<grid, 256, 0, s>>>(a, o, o_pitch, parts);
+        experts_combine_kernel<T, false><<<grid, 256, 0, s>>>(a, work, run, parts);
 }
 
 // No more slots than experts, a few tokens: each slot's weights are read for it alone, in two launches.  Measured in us
@@ -236,19 +245,20 @@ bool by_slot(int64_t slots, int32_t experts) { return slots <= experts; }
 int64_t out_pitch(int64_t width) { return (width + 7) / 8 * 8; }
 
 struct ExpertsPlan {
-    size_t scales, o, bytes;  // p itself lies at the start
+    size_t scales, o, o_scales, bytes;  // p itself lies at the start
 };
 
 ExpertsPlan experts_plan(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen, bool bf16) {
     const size_t slots = (size_t)tokens * chosen, codes = slots * code_pitch(inner);
     ExpertsPlan e;
     if (by_slot((int64_t)slots, experts)) {  // p in fp32, and nothing else
-        e.scales = e.o = e.bytes = codes * 4;
+        e.scales = e.o = e.o_scales = e.bytes = codes * 4;
         return e;
     }
     e.scales = codes;
     e.o = align_up(codes + slots * scale_pitch(inner));
-    e.bytes = e.o + slots * out_pitch(width) * (bf16 ? 2 : 4);
+    e.o_scales = e.o + slots * out_pitch(width) * (bf16 ? 2 : 4);
+    e.bytes = e.o_scales + (bf16 ? slots * blocks_of(width) : 0);
     return e;
 }
 
@@ -272,9 +282,12 @@ hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
     work.p_codes = work.p_codes_out = (uint8_t *)a.ws;
     work.p_scales = work.p_scales_out = (uint8_t *)a.ws + plan.scales;
     work.o = (char *)a.ws + plan.o;
-    const hipError_t e = launch_experts_tile(a, work, sizeof(T) == 2, s);
+    work.o_scales = (uint8_t *)a.ws + plan.o_scales;
+    int run = 0;
+    const hipError_t e = launch_experts_tile(a, work, sizeof(T) == 2, &run, s);
     if (e != hipSuccess) return e;
-    combine_go<T>(a, (const T *)work.o, work.o_pitch, s);
+    work.n_tiles = (a.width + run - 1) / run;
+    combine_go<T>(a, work, run, s);
     return hipGetLastError();
 }
 
