@@ -20,8 +20,17 @@ __device__ __forceinline__ v8bf widen8(int lo, int hi, int code) {
     return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Whether every code times that scale, 2^-9 to 448 times 2^(code - 127), is a normal bfloat16: widening is then exact.
-__device__ __forceinline__ bool widens(int code) { return code >= 10 && code <= 245; }
+// Whether every one of these codes times 2^(code - 127) is a bfloat16, so that widening is exact: normal ones are between
+// 2^-9 and 448 times the scale; beyond that range of scales only zeros (blocks of zeros have the least scale) and NaN.
+__device__ __forceinline__ bool widens(int code, const v8i &q) {
+    if (code >= 10 && code <= 245) return true;
+    for (int i = 0; i < 8; i++)
+        for (int b = 0; b < 32; b += 8) {
+            const int m = q[i] >> b & 0x7f;
+            if (m != 0 && m != 0x7f) return false;
+        }
+    return true;
+}
 
 // Which expert's tile of `rows_per_tile` sorted slots number `tile` is; tiles are numbered expert by expert.  Returns the expert (-1 past the
 // last tile) and the tile's first row and row count among the sorted slots.
@@ -62,8 +71,15 @@ __device__ __forceinline__ float relu_clamp(float z, float ymax) {
     return z;
 }
 
-// silu(gate) * up
-__device__ __forceinline__ float silu_times(float gate, float up) { return gate / (1.0f + expf(-gate)) * up; }
+// silu(gate) * up.  FAST: the hardware's exponential and reciprocal, 1e-7 (1 + |gate|) off, under what the products
+// before it and the rounding to 8 bits behind it leave.
+template <bool FAST>
+__device__ __forceinline__ float silu_times(float gate, float up) {
+    if constexpr (FAST)
+        return gate * __builtin_amdgcn_rcpf(1.0f + __expf(-gate)) * up;
+    else
+        return gate / (1.0f + expf(-gate)) * up;
+}
 
 // Four values as T at an address that is a multiple of their size.
 __device__ __forceinline__ void put4(float *p, const v4f &z) { *(v4f *)p = z; }

@@ -14,7 +14,7 @@ namespace {
 // Lane l holds columns 32 (l / 16) .. + 31 of weight row and activation row l % 16; acc[i] is output 4 (l / 16) + i of
 // row l % 16, so the activation's scale code is the lane's own and the weight rows share one.
 __device__ __forceinline__ v4f block16(const v8i &w, const v8i &x, v4f acc, int w_code, int x_code) {
-    const bool plain = __all(widens(w_code) && widens(x_code));
+    const bool plain = __all(widens(w_code, w) && widens(x_code, x));
     v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
     if (plain) z = acc;
 #pragma unroll
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(64 * kSplit) product_stream_kernel(ProductArgs
 }
 
 // p = silu(gate) * up in fp32, a row of code_pitch(inner) values per slot; a workgroup takes 16 of one slot's.
-__global__ void __launch_bounds__(64 * kSplit) experts_in_slot_kernel(ExpertsArgs a, float *p) {
+__global__ void __launch_bounds__(64 * kSplit, 4) experts_in_slot_kernel(ExpertsArgs a, float *p) {
     __shared__ v4f part[2][kSplit][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t f_tiles = (a.inner + 15) / 16;
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(64 * kSplit) experts_in_slot_kernel(ExpertsArg
     const v4f g = total(part[0]), u = total(part[1]);
     for (int i = 0; i < 4; i++) {
         const int64_t col = f0 + lane / 16 * 4 + i;
-        if (col < a.inner) p[slot * code_pitch(a.inner) + col] = silu_times(g[i], u[i]);
+        if (col < a.inner) p[slot * code_pitch(a.inner) + col] = silu_times<false>(g[i], u[i]);
     }
 }
 

@@ -31,7 +31,7 @@ __device__ __forceinline__ void stage_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-template <int MODE, typename T, int BN, int BM, int WN, int WM, int KG, int STAGES>
+template <int MODE, typename T, bool EXACT, int BN, int BM, int WN, int WM, int KG, int STAGES>
 struct Tile {
     static constexpr int kThreads = 64 * WN * WM * KG, kWaves = WN * WM;  // waves of a group
     static constexpr int NI = BN / WN / 32, MJ = BM / WM / 32;
@@ -42,7 +42,7 @@ struct Tile {
     static int64_t lds_bytes(int64_t k) {
         return kRing + (KG == 1 ? 2 * (BM + 64) * 4 : (BM + kBlockRows) * (scale_pitch(k) + 4));
     }
-    static constexpr bool kExact = sizeof(T) == 4, kTurns = kWaves == 8 && KG == 1 && !kExact;
+    static constexpr bool kTurns = kWaves == 8 && KG == 1 && !EXACT;
     static_assert(KG == 1 || MODE != kTileExpertsOut, "the experts' rows are rounded by one group");
     static_assert(kRows % (16 * kWaves) == 0, "every wave stages the same number of rows");
 };
@@ -51,9 +51,9 @@ struct Tile {
 // same outputs.  With KG > 1, KG groups of waves share the tile's blocks between them (group g takes blocks g, g + KG,
 // ...), each with stages of its own, and their sums join in the end: for products with few tiles, whose time is the
 // length of the chain of stages.
-template <int MODE, typename T, int BN, int BM, int WN, int WM, int KG, int STAGES>
+template <int MODE, typename T, bool EXACT, int BN, int BM, int WN, int WM, int KG, int STAGES>
 __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_tile_kernel(ProductArgs a, ExpertsArgs x, TileWork work) {
-    using S = Tile<MODE, T, BN, BM, WN, WM, KG, STAGES>;
+    using S = Tile<MODE, T, EXACT, BN, BM, WN, WM, KG, STAGES>;
     constexpr int NI = S::NI, MJ = S::MJ, kStages = STAGES;
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x % 64, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -293,10 +293,10 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
             v8i xf[MJ];
 #pragma unroll
             for (int j = 0; j < MJ; j++) xf[j] = fetch_x(t, j);
-            if constexpr (!S::kExact) {
-                v8i wf[NI];
+            v8i wf[NI];
 #pragma unroll
-                for (int i = 0; i < NI; i++) wf[i] = fetch_w(t, i);
+            for (int i = 0; i < NI; i++) wf[i] = fetch_w(t, i);
+            if constexpr (!EXACT) {
 #pragma unroll
                 for (int i = 0; i < NI; i++)
 #pragma unroll
@@ -304,11 +304,11 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
                         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[i], xf[j], acc[i][j], 0, 0, 0,
                                                                                     wc[i], 0, xc[j]);
             } else {
-                bool plain = true;  // every code of the stage lets its block be widened with its scale
+                bool plain = true;
 #pragma unroll
-                for (int j = 0; j < MJ; j++) plain = plain && widens((int)(xc[j] & 255));
+                for (int j = 0; j < MJ; j++) plain = plain && widens((int)(xc[j] & 255), xf[j]);
 #pragma unroll
-                for (int i = 0; i < NI; i++) plain = plain && widens((int)(wc[i] & 255));
+                for (int i = 0; i < NI; i++) plain = plain && widens((int)(wc[i] & 255), wf[i]);
                 plain = __all(plain);
                 v8bf xw[MJ][4];
 #pragma unroll
@@ -318,17 +318,16 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
                         xw[j][c] = widen8(xf[j][2 * c], xf[j][2 * c + 1], plain ? (int)(xc[j] & 255) : kOne);
 #pragma unroll
                 for (int i = 0; i < NI; i++) {
-                    const v8i q = fetch_w(t, i);
-                    v8bf wf[4];
+                    v8bf ww[4];
 #pragma unroll
                     for (int c = 0; c < 4; c++)
-                        wf[c] = widen8(q[2 * c], q[2 * c + 1], plain ? (int)(wc[i] & 255) : kOne);
+                        ww[c] = widen8(wf[i][2 * c], wf[i][2 * c + 1], plain ? (int)(wc[i] & 255) : kOne);
                     if (plain) {
 #pragma unroll
                         for (int j = 0; j < MJ; j++)
 #pragma unroll
                             for (int c = 0; c < 4; c++)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[c], xw[j][c], acc[i][j], 0, 0, 0);
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ww[c], xw[j][c], acc[i][j], 0, 0, 0);
                     } else {
 #pragma unroll
                         for (int j = 0; j < MJ; j++) {
@@ -337,7 +336,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
                             for (int r = 0; r < 16; r++) z[r] = 0.0f;
 #pragma unroll
                             for (int c = 0; c < 4; c++)
-                                z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[c], xw[j][c], z, 0, 0, 0);
+                                z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ww[c], xw[j][c], z, 0, 0, 0);
                             const int e = (int)(wc[i] & 255) + (int)(xc[j] & 255) - 2 * kOne;
 #pragma unroll
                             for (int r = 0; r < 16; r++) acc[i][j][r] += ldexpf(z[r], e);
@@ -388,10 +387,18 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
                     const int64_t f = n0 + sub_row(i) + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-                    const float p = f < n_rows ? silu_times(acc[i][j][r], acc[i + NP][j][r]) : 0.0f;
+                    float p = silu_times<sizeof(T) == 2>(acc[i][j][r], acc[i + NP][j][r]);
+                    p = f < n_rows ? p : 0.0f;
                     acc[i][j][r] = p;
-                    amax = fmaxf(amax, finite_abs(p));
+                    amax = fmaxf(amax, fabsf(p));  // NaN is passed over
                 }
+            if (__any(amax == INFINITY)) {
+                amax = 0.0f;
+#pragma unroll
+                for (int i = 0; i < NP; i++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) amax = fmaxf(amax, finite_abs(acc[i][j][r]));
+            }
             amax = fmaxf(amax, __shfl_xor(amax, 32));
             if (lane < 32) red[wn * BM + (wm * MJ + j) * 32 + lane] = amax;
         }
@@ -454,7 +461,14 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
 #pragma unroll
                 for (int i = 0; i < NI; i++)
 #pragma unroll
-                    for (int r = 0; r < 16; r++) amax = fmaxf(amax, finite_abs(acc[i][j][r]));
+                    for (int r = 0; r < 16; r++) amax = fmaxf(amax, fabsf(acc[i][j][r]));  // NaN is passed over
+                if (__any(amax == INFINITY)) {
+                    amax = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < NI; i++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++) amax = fmaxf(amax, finite_abs(acc[i][j][r]));
+                }
                 amax = fmaxf(amax, __shfl_xor(amax, 32));
                 if (lane < 32) red[wn * BM + (wm * MJ + j) * 32 + lane] = amax;
             }
@@ -523,12 +537,12 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
     }
 }
 
-template <int MODE, typename T, int BN, int BM, int WN, int WM, int KG, int STAGES>
+template <int MODE, typename T, bool EXACT, int BN, int BM, int WN, int WM, int KG, int STAGES>
 hipError_t tile_go(const ProductArgs &a, const ExpertsArgs &x, TileWork work, int64_t m_tiles, int64_t outputs,
                    hipStream_t s) {
-    using S = Tile<MODE, T, BN, BM, WN, WM, KG, STAGES>;
+    using S = Tile<MODE, T, EXACT, BN, BM, WN, WM, KG, STAGES>;
     static std::atomic<unsigned long long> raised{0};
-    const auto kernel = product_tile_kernel<MODE, T, BN, BM, WN, WM, KG, STAGES>;
+    const auto kernel = product_tile_kernel<MODE, T, EXACT, BN, BM, WN, WM, KG, STAGES>;
     const int64_t lds = S::lds_bytes(MODE == kTileProduct ? a.k : MODE == kTileExpertsIn ? x.width : x.inner);
     hipError_t e = raise_lds_limit((const void *)kernel, kMaxLds, raised);
     if (e != hipSuccess) return e;
@@ -554,28 +568,30 @@ hipError_t tile_go(const ProductArgs &a, const ExpertsArgs &x, TileWork work, in
 // the chain is short anyway: 777 x 2999 x 1001 on 64 x 64 with one group 11.6 (float 17.2), on 128 x 128 x2 13.6 (19.7).
 template <typename T>
 hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
+    constexpr bool kExact = sizeof(T) == 4;
     const ExpertsArgs none{};
     const auto tiles = [&](int side) { return (a.m + side - 1) / side; };
     const int64_t small = tiles(64) * ((a.n + 63) / 64);
-    // the groups' kernels hold every scale of a tile in LDS
-    const bool groups = Tile<kTileProduct, T, 128, 128, 2, 2, 2, 4>::lds_bytes(a.k) <= kMaxLds;
+    // the groups' kernels hold every scale of a tile in LDS; these two need the most
+    const bool groups = Tile<kTileProduct, T, kExact, 128, 128, 2, 2, 2, 4>::lds_bytes(a.k) <= kMaxLds &&
+                        Tile<kTileProduct, T, kExact, 128, 64, 2, 2, 4, 3>::lds_bytes(a.k) <= kMaxLds;
     if (groups && small <= 1024) {
         if (small <= (sizeof(T) == 2 ? 128 : 256))
-            return tile_go<kTileProduct, T, 64, 64, 2, 2, 4, 4>(a, none, work, tiles(64), a.n, s);
+            return tile_go<kTileProduct, T, kExact, 64, 64, 2, 2, 4, 4>(a, none, work, tiles(64), a.n, s);
         if constexpr (sizeof(T) == 2) {
-            if (small <= 256) return tile_go<kTileProduct, T, 64, 64, 2, 2, 2, 4>(a, none, work, tiles(64), a.n, s);
-            if (small <= 512) return tile_go<kTileProduct, T, 128, 64, 2, 2, 2, 3>(a, none, work, tiles(64), a.n, s);
+            if (small <= 256) return tile_go<kTileProduct, T, kExact, 64, 64, 2, 2, 2, 4>(a, none, work, tiles(64), a.n, s);
+            if (small <= 512) return tile_go<kTileProduct, T, kExact, 128, 64, 2, 2, 2, 3>(a, none, work, tiles(64), a.n, s);
         } else {
-            if (small <= 512) return tile_go<kTileProduct, T, 128, 64, 2, 2, 4, 3>(a, none, work, tiles(64), a.n, s);
+            if (small <= 512) return tile_go<kTileProduct, T, kExact, 128, 64, 2, 2, 4, 3>(a, none, work, tiles(64), a.n, s);
         }
-        if (a.k <= 2048) return tile_go<kTileProduct, T, 64, 64, 2, 2, 1, 4>(a, none, work, tiles(64), a.n, s);
-        return tile_go<kTileProduct, T, 128, 128, 2, 2, 2, 4>(a, none, work, tiles(128), a.n, s);
+        if (a.k <= 2048) return tile_go<kTileProduct, T, kExact, 64, 64, 2, 2, 1, 4>(a, none, work, tiles(64), a.n, s);
+        return tile_go<kTileProduct, T, kExact, 128, 128, 2, 2, 2, 4>(a, none, work, tiles(128), a.n, s);
     }
     if constexpr (sizeof(T) == 2) {
-        if (small <= 2048) return tile_go<kTileProduct, T, 256, 128, 2, 2, 1, 3>(a, none, work, tiles(128), a.n, s);
-        return tile_go<kTileProduct, T, 256, 256, 2, 4, 1, 4>(a, none, work, tiles(256), a.n, s);
+        if (small <= 2048) return tile_go<kTileProduct, T, kExact, 256, 128, 2, 2, 1, 3>(a, none, work, tiles(128), a.n, s);
+        return tile_go<kTileProduct, T, kExact, 256, 256, 2, 4, 1, 4>(a, none, work, tiles(256), a.n, s);
     } else {
-        return tile_go<kTileProduct, T, 128, 128, 2, 2, 1, 4>(a, none, work, tiles(128), a.n, s);
+        return tile_go<kTileProduct, T, kExact, 128, 128, 2, 2, 1, 4>(a, none, work, tiles(128), a.n, s);
     }
 }
 
@@ -584,20 +600,26 @@ hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
 // tokens 208 and 224, 2048 tokens 531 and 447; 24 experts of 2001 x 701, 3 chosen: 333 tokens 42 and 49.
 template <typename T>
 hipError_t experts_go(const ExpertsArgs &x, TileWork work, int *run, hipStream_t s) {
+    constexpr bool kExact = sizeof(T) == 4;
     const ProductArgs none{};
     const int64_t slots = x.tokens * x.chosen, busy = slots < x.experts ? slots : x.experts;
     const int64_t large = busy + slots / 128, small = busy + slots / 64;
     if constexpr (sizeof(T) == 2)
         if (slots >= 32 * busy && large * ((x.inner + 127) / 128) >= 400) {
-            const hipError_t e = tile_go<kTileExpertsIn, T, 256, 128, 2, 2, 1, 3>(none, x, work, large, x.inner, s);
+            const hipError_t e = tile_go<kTileExpertsIn, T, kExact, 256, 128, 2, 2, 1, 3>(none, x, work, large, x.inner, s);
             if (e != hipSuccess) return e;
             *run = 256;
-            return tile_go<kTileExpertsOut, T, 256, 128, 2, 2, 1, 3>(none, x, work, large, x.width, s);
+            return tile_go<kTileExpertsOut, T, kExact, 256, 128, 2, 2, 1, 3>(none, x, work, large, x.width, s);
         }
-    const hipError_t e = tile_go<kTileExpertsIn, T, 256, 64, 2, 2, 1, 3>(none, x, work, small, x.inner, s);
+    // Few rows wait for weights, so they take the exact arithmetic whatever the type: a sum that is 5e-5 off moves values
+    // of p over a boundary of their 8 bits, up to 1.9e-3 of the result (333 tokens as above: 53 us, 49 without).
+    const hipError_t e =
+        Tile<kTileExpertsIn, T, true, 256, 64, 4, 1, 2, 3>::lds_bytes(x.width) <= kMaxLds
+            ? tile_go<kTileExpertsIn, T, true, 256, 64, 4, 1, 2, 3>(none, x, work, small, x.inner, s)
+            : tile_go<kTileExpertsIn, T, true, 256, 64, 4, 1, 1, 3>(none, x, work, small, x.inner, s);
     if (e != hipSuccess) return e;
     *run = 128;
-    return tile_go<kTileExpertsOut, T, 128, 64, 2, 2, 1, 3>(none, x, work, small, x.width, s);
+    return tile_go<kTileExpertsOut, T, kExact, 128, 64, 2, 2, 1, 3>(none, x, work, small, x.width, s);
 }
 
 }  // namespace

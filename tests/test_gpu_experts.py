@@ -311,6 +311,22 @@ def test_product_of_integers_is_exact(torch, sd):
             assert np.array_equal(got, _to(torch, av @ wv.T, dt)), (m, n, k, dt)
 
 
+@pytest.mark.parametrize("m,n,k", [(20, 70, 33000), (3, 8200, 300), (16, 40, 70000), (300, 200, 31900), (70, 300, 65600)])
+def test_product_long_rows(torch, sd, m, n, k):
+    """Rows whose scales do not all fit in LDS, and the few-row kernel on both sides of its width: exact integers."""
+    rng = np.random.default_rng(m)
+    g = torch.Generator(device="cuda").manual_seed(m)
+    x = torch.randint(-2, 3, (m, k), generator=g, device="cuda").float()
+    y = torch.randint(-2, 3, (n, k), generator=g, device="cuda").float()
+    a, sa = sd.quantize_blocks(x)
+    w, sw = sd.quantize_blocks(y, 128)
+    want = (x.double() @ y.double().t()).cpu().numpy()
+    for dt in (torch.float32, torch.bfloat16):
+        _say("long rows", m, n, k, dt)
+        got = sd.product_blocks(a, sa, w, sw, k, dtype=dt).double().cpu().numpy()
+        assert np.array_equal(got, _to(torch, want, dt))
+
+
 def test_product_extremes(torch, sd):
     """Scales at both ends of their range, NaN codes in one row and one column only, outputs in a strided view."""
     m, n, k = 40, 150, 300
@@ -424,6 +440,58 @@ def test_experts(torch, sd, T, H, F, E, k, masked, dtype, res):
         assert np.linalg.norm(got - want) <= 4e-3 * np.linalg.norm(want)
     dead = (host[3] < 0).all(axis=1)
     assert np.array_equal(got[dead], residual[dead] if res else np.zeros((dead.sum(), H)))
+
+
+@pytest.mark.parametrize("T,H,F,E,k", [(64, 129, 33000, 2, 2), (70, 80000, 130, 2, 1), (2, 33000, 70, 4, 2),
+                                       (1500, 260, 900, 8, 2)])
+def test_experts_of_any_shape(torch, sd, T, H, F, E, k):
+    """Long inner and outer rows, and enough tiles for the largest kind, against float64 on the GPU (2-norm, as above)."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    a, sa = sd.quantize_blocks(rand(T, H))
+    w1, s1 = sd.quantize_blocks(rand(E, 2, F, H) / H ** 0.5, 128)
+    w2, s2 = sd.quantize_blocks(rand(E, H, F) / F ** 0.5, 128)
+    routes = sd.route(rand(T, E), k)
+    _say("experts", T, H, F, E, k)
+    got = sd.experts_forward(a, sa, routes, w1, s1, w2, s2, H, F).double()
+
+    def value(c, s, rows, n, m):
+        e = torch.exp2(s.view(torch.uint8).double() - 127).repeat_interleave(rows, 0)[:n]
+        return (c.double().unflatten(1, (-1, 128)) * e[:, :c.shape[1] // 128, None]).flatten(1)[:, :m]
+
+    x, want = value(a, sa, 1, T, H), torch.zeros(T, H, dtype=torch.float64, device="cuda")
+    for e in range(E):
+        t, j = (routes.ids == e).nonzero(as_tuple=True)
+        if t.numel() == 0:
+            continue
+        gate, up = (x[t] @ value(w1[e, i], s1[e, i], 128, F, H).t() for i in (0, 1))
+        p = (gate * torch.sigmoid(gate) * up).cpu().numpy()
+        q = torch.from_numpy(ref.values(*ref.quantize(p), F)).cuda()
+        want.index_add_(0, t, (q @ value(w2[e], s2[e], 128, H, F).t()) * routes.weight[t, j].double()[:, None])
+    assert float((got - want).norm() / want.norm()) <= 4e-3
+
+
+def test_experts_rows_that_are_not_finite(torch, sd):
+    """A NaN code in one token's row, and weights so large that one expert's products overflow: the token and the
+    expert's tokens are lost, the others do not notice."""
+    for T in (2, 200):
+        H, F, E = 256, 256, 4
+        args, host, _ = _experts_case(torch, sd, T, H, F, E, 1, 0.0, seed=7)
+        for dt in (torch.float32, torch.bfloat16):
+            want = sd.experts_forward(*args, H, F, dtype=dt)
+            a = args[0].clone()
+            a.view(torch.uint8)[1, 3] = 0x7F
+            got = sd.experts_forward(a, *args[1:], H, F, dtype=dt)
+            rest = torch.arange(T, device="cuda") != 1
+            assert torch.isnan(got[1]).all() and torch.equal(got[rest], want[rest])
+            s_out = args[6].clone()
+            hit = int(host[3][0, 0])
+            s_out.view(torch.uint8)[hit, 1] = 254  # outputs 128 on of that expert: 2^127 times the codes
+            got = sd.experts_forward(*args[:6], s_out, H, F, dtype=dt)
+            other = (args[2].ids != hit).all(dim=1)
+            assert torch.equal(got[other], want[other])
+            assert torch.equal(got[:, :128], want[:, :128])
+            assert not torch.isfinite(got[~other][:, 128:]).all()
 
 
 def test_experts_in_place_and_workspace(torch, sd):
