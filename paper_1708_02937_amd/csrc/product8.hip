@@ -3,8 +3,8 @@
 //   Y(m, n) = sum_b 2^(Ea(m, b) + Ew(n / 128, b)) sum_{i in block b} qa(m, i) qw(n, i)
 //
 // The weights are the matrix instruction's first operand and the activations its second, so a lane ends with four
-// consecutive outputs of one row.  e4m3 codes are widened to bfloat16 with their scales, which is exact, for the 16-bit
-// matrix instructions, whose products and sums are fp32.
+// consecutive outputs of one row.  e4m3 codes are widened to bfloat16, which is exact, for the 16-bit matrix
+// instructions, whose products and sums are fp32; each block's sum is scaled as it joins the total.
 #include "product8.h"
 
 namespace sdnn {
@@ -14,14 +14,11 @@ namespace {
 // Lane l holds columns 32 (l / 16) .. + 31 of weight row and activation row l % 16; acc[i] is output 4 (l / 16) + i of
 // row l % 16, so the activation's scale code is the lane's own and the weight rows share one.
 __device__ __forceinline__ v4f block16(const v8i &w, const v8i &x, v4f acc, int w_code, int x_code) {
-    const bool plain = __all(widens(w_code, w) && widens(x_code, x));
     v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (plain) z = acc;
 #pragma unroll
     for (int i = 0; i < 4; i++)
-        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * i], w[2 * i + 1], plain ? w_code : kOne),
-                                                    widen8(x[2 * i], x[2 * i + 1], plain ? x_code : kOne), z, 0, 0, 0);
-    if (plain) return z;
+        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * i], w[2 * i + 1], kOne),
+                                                    widen8(x[2 * i], x[2 * i + 1], kOne), z, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < 4; i++) acc[i] += ldexpf(z[i], w_code + x_code - 2 * kOne);
     return acc;
@@ -96,7 +93,7 @@ __global__ void __launch_bounds__(64 * kSplit) product_stream_kernel(ProductArgs
 }
 
 // p = silu(gate) * up in fp32, a row of code_pitch(inner) values per slot; a workgroup takes 16 of one slot's.
-__global__ void __launch_bounds__(64 * kSplit, 4) experts_in_slot_kernel(ExpertsArgs a, float *p) {
+__global__ void __launch_bounds__(64 * kSplit) experts_in_slot_kernel(ExpertsArgs a, float *p) {
     __shared__ v4f part[2][kSplit][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t f_tiles = (a.inner + 15) / 16;
