@@ -10,12 +10,13 @@
 // 16 lanes take a token of up to 256 experts, a wave four tokens: a maximum over 16 lanes is four register-to-register
 // moves with the comparison built in, and what a choice costs is the search through a lane's own experts.
 #include "blocks8.h"
+#include "common.h"
 
 namespace sdnn {
 namespace {
 
 constexpr int kScoreWaves = 4;  // waves of a workgroup of the scores
-constexpr int kPlanThreads = 512, kPlanWaves = kPlanThreads / 64;
+constexpr int kSmallWaves = 8, kPlanWaves = 16;  // waves of the workgroup of a small call, and of the plan's
 constexpr int64_t kChunk = 4096;      // slots that one workgroup sorts, up to kMaxChunks of them; then more each
 constexpr int64_t kMaxChunks = 256;
 constexpr int64_t kSmallTokens = 64;  // up to here one workgroup does everything
@@ -409,15 +410,11 @@ __device__ __forceinline__ uint64_t same_expert(int id, int bits) {
 }
 
 // Slots of a chunk: whole rounds of 64 for every wave.
+template <int WAVES>
 __device__ __forceinline__ int64_t chunk_of(int64_t slots, int chunks) {
-    constexpr int64_t kRound = 64 * kPlanWaves;
+    constexpr int64_t kRound = 64 * WAVES;
     return (slots + chunks * kRound - 1) / (chunks * kRound) * kRound;
 }
-
-struct PlanShared {
-    int count[kPlanWaves][kRouteMaxExperts];
-    int part[kPlanWaves];
-};
 
 // f(slot, expert) for the slots [begin, end), 64 at a time in order, eight loads ahead; expert -1 past the end.
 template <typename F>
@@ -433,34 +430,57 @@ __device__ __forceinline__ void each_round(const RouteArgs &a, int64_t begin, in
     }
 }
 
-// Counts each wave's run of the chunk into s.count.
+// Counts each wave's run of the chunk into count (WAVES x experts).
+template <int WAVES>
 __device__ __forceinline__ void plan_count(const RouteArgs &a, int64_t begin, int64_t end, int64_t run, int bits,
-                                           PlanShared &s) {
+                                           int *count) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (int w = 0; w < kPlanWaves; w++)
-        for (int e = threadIdx.x; e < a.experts; e += kPlanThreads) s.count[w][e] = 0;
+    for (int c = threadIdx.x; c < WAVES * a.experts; c += 64 * WAVES) count[c] = 0;
     __syncthreads();
     each_round(a, begin + wave * run, min(begin + (wave + 1) * run, end), [&](int64_t, int id) {
         const uint64_t mask = same_expert(id, bits);
-        if (id >= 0 && lane == __ffsll((unsigned long long)mask) - 1) s.count[wave][id] += __popcll(mask);
+        if (id >= 0 && lane == __ffsll((unsigned long long)mask) - 1) count[wave * a.experts + id] += __popcll(mask);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     });
     __syncthreads();
 }
 
 // `chunks` workgroups; counts: chunks x experts, of every chunk, or null where there is one.
+template <int WAVES>
 __device__ __forceinline__ void plan_chunk(const RouteArgs &a, int chunk, int chunks, const int32_t *counts, int bits,
-                                           PlanShared &s) {
+                                           int *count) {
+    constexpr int kThreads = 64 * WAVES;
+    __shared__ int part[WAVES];
+    __shared__ int sums[2][kThreads];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t slots = a.tokens * a.chosen, each = chunk_of(slots, chunks);
-    const int64_t begin = chunk * each, end = min(begin + each, slots), run = each / kPlanWaves;
-    plan_count(a, begin, end, run, bits, s);
+    const int64_t slots = a.tokens * a.chosen, each = chunk_of<WAVES>(slots, chunks);
+    const int64_t begin = chunk * each, end = min(begin + each, slots), run = each / WAVES;
+    plan_count<WAVES>(a, begin, end, run, bits, count);
+    const int ways = counts ? max(kThreads / a.experts, 1) : 1;  // threads that share an expert's sum over the chunks
+    if (ways > 1) {
+        int all = 0, earlier = 0;
+        if (threadIdx.x < ways * a.experts) {
+#pragma unroll 16
+            for (int c = threadIdx.x / a.experts; c < chunks; c += ways) {
+                const int n = counts[(int64_t)c * a.experts + threadIdx.x % a.experts];
+                all += n;
+                earlier += c < chunk ? n : 0;
+            }
+        }
+        sums[0][threadIdx.x] = all, sums[1][threadIdx.x] = earlier;
+        __syncthreads();
+    }
     int before = 0;  // slots of the experts below this thread's
-    for (int e0 = 0; e0 < a.experts; e0 += kPlanThreads) {
+    for (int e0 = 0; e0 < a.experts; e0 += kThreads) {
         const int e = e0 + threadIdx.x;
         int all = 0, earlier = 0;
         if (e < a.experts) {
-            if (counts) {
+            if (ways > 1) {  // then every expert has a thread in the first turn
+                for (int w = 0; w < ways; w++) {
+                    all += sums[0][w * a.experts + e];
+                    earlier += sums[1][w * a.experts + e];
+                }
+            } else if (counts) {
 #pragma unroll 32
                 for (int c = 0; c < chunks; c++) {
                     const int n = counts[(int64_t)c * a.experts + e];
@@ -468,7 +488,7 @@ __device__ __forceinline__ void plan_chunk(const RouteArgs &a, int chunk, int ch
                     earlier += c < chunk ? n : 0;
                 }
             } else {
-                for (int w = 0; w < kPlanWaves; w++) all += s.count[w][e];
+                for (int w = 0; w < WAVES; w++) all += count[w * a.experts + e];
             }
         }
         int upto = all;
@@ -476,21 +496,21 @@ __device__ __forceinline__ void plan_chunk(const RouteArgs &a, int chunk, int ch
             const int o = __shfl_up(upto, m);
             if (lane >= m) upto += o;
         }
-        if (lane == 63) s.part[wave] = upto;
+        if (lane == 63) part[wave] = upto;
         __syncthreads();
         int total = 0;
-        for (int w = 0; w < kPlanWaves; w++) {
-            if (w < wave) upto += s.part[w];
-            total += s.part[w];
+        for (int w = 0; w < WAVES; w++) {
+            if (w < wave) upto += part[w];
+            total += part[w];
         }
         __syncthreads();
         if (e < a.experts) {
             int at = before + upto - all;
             if (chunk == 0) a.offsets[e] = at;
             at += earlier;
-            for (int w = 0; w < kPlanWaves; w++) {
-                const int n = s.count[w][e];
-                s.count[w][e] = at;
+            for (int w = 0; w < WAVES; w++) {
+                const int n = count[w * a.experts + e];
+                count[w * a.experts + e] = at;
                 at += n;
             }
         }
@@ -501,51 +521,51 @@ __device__ __forceinline__ void plan_chunk(const RouteArgs &a, int chunk, int ch
     each_round(a, begin + wave * run, min(begin + (wave + 1) * run, end), [&](int64_t slot, int id) {
         const uint64_t mask = same_expert(id, bits);
         int at = 0;
-        if (id >= 0) at = s.count[wave][id];
+        if (id >= 0) at = count[wave * a.experts + id];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (id >= 0) {
             const int rank = __popcll(mask & ((1ull << lane) - 1));
             a.order[at + rank] = (int)slot;
-            if (rank == 0) s.count[wave][id] = at + __popcll(mask);
+            if (rank == 0) count[wave * a.experts + id] = at + __popcll(mask);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     });
-    for (int64_t i = before + (int64_t)chunk * kPlanThreads + threadIdx.x; i < slots;
-         i += (int64_t)chunks * kPlanThreads)
+    for (int64_t i = before + (int64_t)chunk * kThreads + threadIdx.x; i < slots; i += (int64_t)chunks * kThreads)
         a.order[i] = -1;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) route_count_kernel(RouteArgs a, int32_t *counts, int bits) {
-    __shared__ PlanShared s;
-    const int64_t slots = a.tokens * a.chosen, each = chunk_of(slots, (int)gridDim.x), begin = blockIdx.x * each;
-    plan_count(a, begin, min(begin + each, slots), each / kPlanWaves, bits, s);
-    for (int e = threadIdx.x; e < a.experts; e += kPlanThreads) {
+__global__ void __launch_bounds__(64 * kPlanWaves) route_count_kernel(RouteArgs a, int32_t *counts, int bits) {
+    extern __shared__ int count[];
+    const int64_t slots = a.tokens * a.chosen, each = chunk_of<kPlanWaves>(slots, (int)gridDim.x);
+    const int64_t begin = blockIdx.x * each;
+    plan_count<kPlanWaves>(a, begin, min(begin + each, slots), each / kPlanWaves, bits, count);
+    for (int e = threadIdx.x; e < a.experts; e += 64 * kPlanWaves) {
         int n = 0;
-        for (int w = 0; w < kPlanWaves; w++) n += s.count[w][e];
+        for (int w = 0; w < kPlanWaves; w++) n += count[w * a.experts + e];
         counts[(int64_t)blockIdx.x * a.experts + e] = n;
     }
 }
 
-__global__ void __launch_bounds__(kPlanThreads) route_plan_kernel(RouteArgs a, const int32_t *counts, int bits) {
-    __shared__ PlanShared s;
-    plan_chunk(a, (int)blockIdx.x, (int)gridDim.x, counts, bits, s);
+__global__ void __launch_bounds__(64 * kPlanWaves) route_plan_kernel(RouteArgs a, const int32_t *counts, int bits) {
+    extern __shared__ int count[];
+    plan_chunk<kPlanWaves>(a, (int)blockIdx.x, (int)gridDim.x, counts, bits, count);
 }
 
 // A few tokens: scores and plan in one launch.
 template <typename T, int LANES, int R>
-__global__ void __launch_bounds__(kPlanThreads) route_small_kernel(RouteArgs a, int bits) {
+__global__ void __launch_bounds__(64 * kSmallWaves) route_small_kernel(RouteArgs a, int bits) {
     constexpr int RX = LANES == 64 ? R : (R + 3) / 4;
     constexpr int kEach = 64 * RX > 32 * R ? 64 * RX : 32 * R;
     __shared__ union {
-        PlanShared plan;
-        double scores[kPlanWaves][kEach];
+        int count[kSmallWaves * LANES * R];
+        double scores[kSmallWaves][kEach];
     } s;
     const int wave = threadIdx.x / 64;
-    for (int64_t t = wave * (64 / LANES); t < a.tokens; t += kPlanWaves * (64 / LANES))
+    for (int64_t t = wave * (64 / LANES); t < a.tokens; t += kSmallWaves * (64 / LANES))
         route_tokens<T, LANES, R>(a, t, s.scores[wave]);
     __threadfence_block();
     __syncthreads();
-    plan_chunk(a, 0, 1, nullptr, bits, s.plan);
+    plan_chunk<kSmallWaves>(a, 0, 1, nullptr, bits, s.count);
 }
 
 int chunks_of(int64_t slots) {
@@ -558,15 +578,21 @@ hipError_t route_go(const RouteArgs &a, hipStream_t s) {
     int bits = 0;
     while ((1 << bits) < a.experts) bits++;
     if (a.tokens <= kSmallTokens) {
-        route_small_kernel<T, LANES, R><<<1, kPlanThreads, 0, s>>>(a, bits);
+        route_small_kernel<T, LANES, R><<<1, 64 * kSmallWaves, 0, s>>>(a, bits);
         return hipGetLastError();
     }
     constexpr int64_t kTokens = kScoreWaves * (64 / LANES);
     route_scores_kernel<T, LANES, R><<<(unsigned)((a.tokens + kTokens - 1) / kTokens), 64 * kScoreWaves, 0, s>>>(a);
     const int chunks = chunks_of(a.tokens * a.chosen);
     int32_t *counts = chunks > 1 ? (int32_t *)a.ws : nullptr;
-    if (chunks > 1) route_count_kernel<<<chunks, kPlanThreads, 0, s>>>(a, counts, bits);
-    route_plan_kernel<<<chunks, kPlanThreads, 0, s>>>(a, counts, bits);
+    static std::atomic<unsigned long long> raised[2];
+    constexpr size_t kMostLds = kPlanWaves * kRouteMaxExperts * sizeof(int);
+    const size_t lds = (size_t)kPlanWaves * a.experts * sizeof(int);
+    hipError_t e = raise_lds_limit((const void *)route_count_kernel, kMostLds, raised[0]);
+    if (e == hipSuccess) e = raise_lds_limit((const void *)route_plan_kernel, kMostLds, raised[1]);
+    if (e != hipSuccess) return e;
+    if (chunks > 1) route_count_kernel<<<chunks, 64 * kPlanWaves, lds, s>>>(a, counts, bits);
+    route_plan_kernel<<<chunks, 64 * kPlanWaves, lds, s>>>(a, counts, bits);
     return hipGetLastError();
 }
 

@@ -75,7 +75,7 @@ def _on_device(f):
         index = x.get_device()  # -1 on the host
         if index < 0:
             raise ValueError(f"{f.__name__} needs tensors on the GPU")
-        if index == _current():
+        if index == torch.cuda.current_device():
             return f(x, *args, **kw)
         with torch.cuda.device(index):
             return f(x, *args, **kw)
@@ -83,8 +83,9 @@ def _on_device(f):
     return call
 
 
-def _current():
-    return torch.cuda.current_device()
+def _like(x, ld, shape):
+    """An empty contiguous matrix of x's type and shape."""
+    return torch.empty_like(x) if ld == shape[1] else torch.empty(shape, dtype=x.dtype, device=x.device)
 
 
 def _stream(device):
@@ -132,7 +133,7 @@ def norm_quantize(x, gamma, eps: float = 1e-6, residual=None, normed: bool = Fal
     if residual is not None:
         ldr, r = _dense(residual, "residual", dtype, device, shape), residual.data_ptr()
         if out_sum is None:
-            out_sum, lds = torch.empty(shape, dtype=dtype, device=device), k
+            out_sum, lds = _like(x, ldx, shape), k
         else:
             lds = _dense(out_sum, "out_sum", dtype, device, shape)
         s = out_sum.data_ptr()
@@ -140,7 +141,7 @@ def norm_quantize(x, gamma, eps: float = 1e-6, residual=None, normed: bool = Fal
         _need(out_sum is None, "out_sum without a residual")
     out_normed = None
     if normed:
-        out_normed = torch.empty(shape, dtype=dtype, device=device)
+        out_normed = _like(x, ldx, shape)
         z = out_normed.data_ptr()
     _call(sd.lib.sdnn_norm_quantize(rows, k, kind, x.data_ptr(), ldx, r, ldr, g, eps, s, lds, z, k, codes.data_ptr(),
                                     scales.data_ptr(), _stream(device)))
