@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(64 * kSplit) experts_out_slot_kernel(ExpertsAr
         for (int b0 = u % share * kPass; b0 < kb; b0 += share * kPass) {
             const int64_t col = (int64_t)b0 * kBlock + lane * 8;
             float v[8];
-            load8<float, true>(row, col, a.inner, v);
+            load8<float, true, false>(row, col, a.inner, v);
             v8i wq[kPass];
             int wc[kPass];
 #pragma unroll
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, Til
                 for (int i = 0; i < 8; i++) s[i] = fmaf(w, v[i], s[i]);
             } else {
                 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-                const v8h v = *(const v8h *)((const _Float16 *)work.o + slot * work.o_pitch + c);
+                const v8h v = __builtin_nontemporal_load((const v8h *)((const _Float16 *)work.o + slot * work.o_pitch + c));
                 const int code = work.o_scales[slot * work.n_tiles + c / run];
                 const float scale = __int_as_float(code << 23);
                 for (int i = 0; i < 8; i++) s[i] = fmaf(w, (float)v[i] * scale, s[i]);

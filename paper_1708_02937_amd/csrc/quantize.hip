@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads)
     for (int c = 0; c < CHUNKS; c++) {
         const int64_t col = ((int64_t)c * TPR + t) * 8;
         float gm[8], odd[8], zf[8];
-        load8<float, VEC>(a.gamma, col, a.k, gm);
+        load8<float, VEC, false>(a.gamma, col, a.k, gm);
         float amax = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; i++) {

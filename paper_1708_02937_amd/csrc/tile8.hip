@@ -432,7 +432,8 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
             *(v4i *)(work.p_codes_out + (row0 + c / 8) * p_pitch + n0 + c % 8 * 16) =
                 *(const v4i *)(lds + c / 8 * kPitch + c % 8 * 16);
     } else {
-        // Through LDS, 32 rows of every wave at a time, so that whole lines leave for memory.
+        // Through LDS, 32 rows of every wave at a time, so that whole lines leave for memory, and past the caches, which
+        // the operands of the tiles to come fill better (8192 x 16384 x 4096: 516 us without that, 495 with it).
         constexpr bool kHalf = MODE == kTileExpertsOut && sizeof(T) == 2;  // the experts' rows in half precision
         using Out = typename std::conditional<kHalf, _Float16, T>::type;
         constexpr int kCells = 16 / sizeof(T), kPitch = BN + kCells, kSlice = WM * 32;
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
                     const Out *const from = out + lr * kPitch + col;
                     if (!y || col >= cols) continue;
                     if (col + kCells <= cols)
-                        *(v4i *)(y + col) = *(const v4i *)from;
+                        __builtin_nontemporal_store(*(const v4i *)from, (v4i *)(y + col));
                     else
                         for (int v = 0; col + v < cols; v++) y[col + v] = from[v];
                 }
