@@ -547,6 +547,17 @@ def test_layer_on_a_side_stream_and_in_a_graph(torch, sd, T):
         assert torch.equal(out, want), i
 
 
+def test_example(torch, sd, capsys):
+    """The example's prompt and its captured single token: the token's row is the prompt's.  Each of the two layers rounds
+    its input to 8 bits, where a difference of one bfloat16 rounding (2^-9) moves about one code in twenty by a step of a
+    sixteenth to an eighth: 1 to 2% of a layer's result."""
+    import examples.experts_layer as example
+
+    far = example.main(["--width", "512", "--inner", "256", "--experts", "8", "--chosen", "2", "--prompt", "200"])
+    assert far <= 0.05
+    assert "tokens/s" in capsys.readouterr().out
+
+
 def test_same_inputs_same_bits(torch, sd):
     T, H, F, E, k = 130, 512, 256, 6, 3
     args, _, _ = _experts_case(torch, sd, T, H, F, E, k, 0.0)
