@@ -20,6 +20,10 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+// 16-byte accesses at any address of the element: rows need not start at multiples of 16 bytes
+typedef v4f v4f_any __attribute__((aligned(4)));
+typedef v8bf v8bf_any __attribute__((aligned(2)));
+typedef v4i v4i_any __attribute__((aligned(2)));
 
 // The scale code of a block whose largest finite magnitude is `amax`: the least power of two, 2^-126 at least, that
 // brings it to 448 = 1.75 * 2^8 or less.
@@ -84,19 +88,19 @@ __device__ __forceinline__ float load_f32<__bf16>(const __bf16 *p) {
     return (float)*p;
 }
 
-// Eight consecutive elements of a row starting at column c of k, zeros past the end.  VEC: 16-byte loads are aligned.
+// Eight consecutive elements of a row starting at column c of k, zeros past the end.
 // ONCE: nobody reads them again soon, so they need not stay in the caches (16384 rows of 4096 through the norm 121 us
 // without that, 115 with it).
-template <typename T, bool VEC, bool ONCE = true>
+template <typename T, bool ONCE = true>
 __device__ __forceinline__ void load8(const T *row, int64_t c, int64_t k, float (&v)[8]) {
-    if (VEC && c + 8 <= k) {
+    if (c + 8 <= k) {
         if constexpr (sizeof(T) == 4) {
-            const v4f *p = (const v4f *)(row + c);
+            const v4f_any *p = (const v4f_any *)(row + c);
             const v4f a = ONCE ? __builtin_nontemporal_load(p) : p[0],
                       b = ONCE ? __builtin_nontemporal_load(p + 1) : p[1];
             for (int i = 0; i < 4; i++) v[i] = a[i], v[4 + i] = b[i];
         } else {
-            const v8bf *p = (const v8bf *)(row + c);
+            const v8bf_any *p = (const v8bf_any *)(row + c);
             const v8bf a = ONCE ? __builtin_nontemporal_load(p) : *p;
             for (int i = 0; i < 8; i++) v[i] = (float)a[i];
         }
@@ -106,16 +110,16 @@ __device__ __forceinline__ void load8(const T *row, int64_t c, int64_t k, float 
 }
 
 // The store to match; values past column k are dropped.
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void store8(T *row, int64_t c, int64_t k, const float (&v)[8]) {
-    if (VEC && c + 8 <= k) {
+    if (c + 8 <= k) {
         if constexpr (sizeof(T) == 4) {
-            __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, (v4f *)(row + c));
-            __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, (v4f *)(row + c + 4));
+            __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, (v4f_any *)(row + c));
+            __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, (v4f_any *)(row + c + 4));
         } else {
             v8bf a;
             for (int i = 0; i < 8; i++) a[i] = (__bf16)v[i];
-            __builtin_nontemporal_store(a, (v8bf *)(row + c));
+            __builtin_nontemporal_store(a, (v8bf_any *)(row + c));
         }
     } else {
         for (int i = 0; i < 8; i++)

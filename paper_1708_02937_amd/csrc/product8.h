@@ -101,7 +101,6 @@ __device__ __forceinline__ int64_t chiplet_order(int64_t id, int64_t count) {
 
 struct TileWork {
     int64_t n_tiles;  // tiles along the outputs
-    bool wide;        // output rows start at multiples of 16 bytes
     const uint8_t *p_codes, *p_scales;  // the experts' inner rows, one per sorted slot
     uint8_t *p_codes_out, *p_scales_out;
     void *o;  // the experts' output rows, one per slot, o_pitch values apart

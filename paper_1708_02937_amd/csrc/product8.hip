@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(64 * kSplit) experts_out_slot_kernel(ExpertsAr
         for (int b0 = u % share * kPass; b0 < kb; b0 += share * kPass) {
             const int64_t col = (int64_t)b0 * kBlock + lane * 8;
             float v[8];
-            load8<float, true, false>(row, col, a.inner, v);
+            load8<float, false>(row, col, a.inner, v);
             v8i wq[kPass];
             int wc[kPass];
 #pragma unroll
@@ -185,9 +185,8 @@ __global__ void __launch_bounds__(64 * kSplit) experts_out_slot_kernel(ExpertsAr
 }
 
 // out(t) = residual(t) + sum_j weight(t, j) o(t k + j), in fp32, in the order of j.  A thread takes 8 columns of one
-// token; VEC: the rows of out and residual start at multiples of 16 bytes.  o is float, or half precision with a scale
-// for each run of `run` columns.
-template <typename T, bool VEC>
+// token.  o is float, or half precision with a scale for each run of `run` columns.
+template <typename T>
 __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, TileWork work, int run, int parts) {
     const int64_t cells = a.tokens * parts;
     for (int64_t g = blockIdx.x; g < cells; g += gridDim.x) {
@@ -195,7 +194,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, Til
         if (c >= a.width) continue;
         float s[8];
         if (a.residual)
-            load8<T, VEC>((const T *)a.residual + t * a.ldr, c, a.width, s);
+            load8<T>((const T *)a.residual + t * a.ldr, c, a.width, s);
         else
             for (int i = 0; i < 8; i++) s[i] = 0.0f;
 #pragma unroll 4
@@ -205,7 +204,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, Til
             const float w = a.weight[slot];
             if constexpr (sizeof(T) == 4) {
                 float v[8];
-                load8<float, true>((const float *)work.o + slot * work.o_pitch, c, work.o_pitch, v);
+                load8<float>((const float *)work.o + slot * work.o_pitch, c, work.o_pitch, v);
                 for (int i = 0; i < 8; i++) s[i] = fmaf(w, v[i], s[i]);
             } else {
                 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
@@ -215,7 +214,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, Til
                 for (int i = 0; i < 8; i++) s[i] = fmaf(w, (float)v[i] * scale, s[i]);
             }
         }
-        store8<T, VEC>((T *)a.out + t * a.ldo, c, a.width, s);
+        store8<T>((T *)a.out + t * a.ldo, c, a.width, s);
     }
 }
 
@@ -224,13 +223,7 @@ void combine_go(const ExpertsArgs &a, const TileWork &work, int run, hipStream_t
     const int parts = (int)((a.width + 2047) / 2048);
     const int64_t cells = a.tokens * parts;
     const unsigned grid = (unsigned)(cells < (1 << 20) ? cells : (1 << 20));
-    const int size = sizeof(T);
-    const bool vec = ((uintptr_t)a.out & 15) == 0 && a.ldo * size % 16 == 0 &&
-                     (!a.residual || (((uintptr_t)a.residual & 15) == 0 && a.ldr * size % 16 == 0));
-    if (vec)
-        experts_combine_kernel<T, true><<<grid, 256, 0, s>>>(a, work, run, parts);
-    else
-        experts_combine_kernel<T, false><<<grid, 256, 0, s>>>(a, work, run, parts);
+    experts_combine_kernel<T><<<grid, 256, 0, s>>>(a, work, run, parts);
 }
 
 // No more slots than experts, a few tokens: each slot's weights are read for it alone, in two launches.  Measured in us
@@ -274,7 +267,6 @@ hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
     }
     const ExpertsPlan plan = experts_plan(a.tokens, a.width, a.inner, a.experts, a.chosen, sizeof(T) == 2);
     TileWork work{};
-    work.wide = true;
     work.o_pitch = out_pitch(a.width);
     work.p_codes = work.p_codes_out = (uint8_t *)a.ws;
     work.p_scales = work.p_scales_out = (uint8_t *)a.ws + plan.scales;
@@ -306,9 +298,7 @@ hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
             product_stream_kernel<float><<<grid, 64 * kSplit, 0, stream>>>(a);
         return hipGetLastError();
     }
-    TileWork work{};
-    work.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy * (bf16 ? 2 : 4) % 16 == 0;
-    return launch_product_tile(a, work, bf16, stream);
+    return launch_product_tile(a, TileWork{}, bf16, stream);
 }
 
 hipError_t launch_experts(const ExpertsArgs &a, bool bf16, hipStream_t stream) {

@@ -15,7 +15,7 @@ namespace {
 constexpr int kNormThreads = 256;  // least threads of a workgroup
 
 // TPR threads per row, each with CHUNKS runs of 8 columns (a block of 128 columns is 16 neighbouring lanes).
-template <typename T, bool RES, bool VEC, int TPR, int CHUNKS>
+template <typename T, bool RES, int TPR, int CHUNKS>
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads)
     norm_quantize_kernel(NormArgs a) {
     constexpr int kRows = TPR >= kNormThreads ? 1 : kNormThreads / TPR;
@@ -32,8 +32,8 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads)
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
         const int64_t col = ((int64_t)c * TPR + t) * 8;
-        load8<T, VEC>(x, col, a.k, xv[c]);
-        if (RES) load8<T, VEC>(r, col, a.k, rv[c]);
+        load8<T>(x, col, a.k, xv[c]);
+        if (RES) load8<T>(r, col, a.k, rv[c]);
     }
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++)
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads)
     for (int c = 0; c < CHUNKS; c++) {
         const int64_t col = ((int64_t)c * TPR + t) * 8;
         float gm[8], odd[8], zf[8];
-        load8<float, VEC, false>(a.gamma, col, a.k, gm);
+        load8<float, false>(a.gamma, col, a.k, gm);
         float amax = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
@@ -67,8 +67,8 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads)
             amax = fmaxf(amax, finite_abs(odd[i]));
             if (RES) xv[c][i] = (float)v;
         }
-        if (RES && a.sum) store8<T, VEC>((T *)a.sum + row * a.lds, col, a.k, xv[c]);
-        if (a.normed) store8<T, VEC>((T *)a.normed + row * a.ldn, col, a.k, zf);
+        if (RES && a.sum) store8<T>((T *)a.sum + row * a.lds, col, a.k, xv[c]);
+        if (a.normed) store8<T>((T *)a.normed + row * a.ldn, col, a.k, zf);
         const int code = scale_code(row16_max(amax));
         const float inv = inverse_scale(code);
         if (col < pitch) {
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads)
     }
 }
 
-template <typename T, bool RES, bool VEC, int TPR, int CHUNKS>
+template <typename T, bool RES, int TPR, int CHUNKS>
 hipError_t norm_go(const NormArgs &a, hipStream_t s) {
     constexpr int rows = TPR >= kNormThreads ? 1 : kNormThreads / TPR;
     // at most 2^22 workgroups of 512 threads in one launch
@@ -94,39 +94,25 @@ hipError_t norm_go(const NormArgs &a, hipStream_t s) {
         p.normed = a.normed ? (T *)a.normed + r0 * a.ldn : nullptr;
         p.codes = a.codes + r0 * code_pitch(a.k);
         p.scales = a.scales + r0 * scale_pitch(a.k);
-        norm_quantize_kernel<T, RES, VEC, TPR, CHUNKS>
+        norm_quantize_kernel<T, RES, TPR, CHUNKS>
             <<<(unsigned)((p.rows + rows - 1) / rows), TPR > kNormThreads ? TPR : kNormThreads, 0, s>>>(p);
     }
     return hipGetLastError();
 }
 
-template <typename T, bool RES, bool VEC>
+template <typename T, bool RES>
 hipError_t norm_width(const NormArgs &a, hipStream_t s) {
-    if (a.k <= 512) return norm_go<T, RES, VEC, 64, 1>(a, s);
-    if (a.k <= 1024) return norm_go<T, RES, VEC, 128, 1>(a, s);
-    if (a.k <= 2048) return norm_go<T, RES, VEC, 256, 1>(a, s);
-    if (a.k <= 4096) return norm_go<T, RES, VEC, 512, 1>(a, s);
-    if (a.k <= 8192) return norm_go<T, RES, VEC, 512, 2>(a, s);
-    if (a.k <= 16384) return norm_go<T, RES, VEC, 512, 4>(a, s);
-    return norm_go<T, RES, VEC, 512, 8>(a, s);
-}
-
-bool aligned16(const void *p, int64_t ld, size_t size) {
-    return ((uintptr_t)p & 15) == 0 && (ld * (int64_t)size) % 16 == 0;
-}
-
-template <typename T>
-hipError_t norm_type(const NormArgs &a, hipStream_t s) {
-    const bool vec = aligned16(a.x, a.ldx, sizeof(T)) && aligned16(a.gamma, 0, 4) &&
-                     (!a.residual || aligned16(a.residual, a.ldr, sizeof(T))) &&
-                     (!a.sum || aligned16(a.sum, a.lds, sizeof(T))) &&
-                     (!a.normed || aligned16(a.normed, a.ldn, sizeof(T)));
-    if (a.residual) return vec ? norm_width<T, true, true>(a, s) : norm_width<T, true, false>(a, s);
-    return vec ? norm_width<T, false, true>(a, s) : norm_width<T, false, false>(a, s);
+    if (a.k <= 512) return norm_go<T, RES, 64, 1>(a, s);
+    if (a.k <= 1024) return norm_go<T, RES, 128, 1>(a, s);
+    if (a.k <= 2048) return norm_go<T, RES, 256, 1>(a, s);
+    if (a.k <= 4096) return norm_go<T, RES, 512, 1>(a, s);
+    if (a.k <= 8192) return norm_go<T, RES, 512, 2>(a, s);
+    if (a.k <= 16384) return norm_go<T, RES, 512, 4>(a, s);
+    return norm_go<T, RES, 512, 8>(a, s);
 }
 
 // A tile of 128 rows x 128 columns: thread t holds columns 8 (t % 16) .. + 7 of rows t / 16 + 16 i.
-template <typename T, bool VEC, bool SQUARE>
+template <typename T, bool SQUARE>
 __global__ void __launch_bounds__(256) quantize_blocks_kernel(QuantizeArgs a, int64_t tiles) {
     __shared__ float part[4];
     const int64_t kb = blocks_of(a.k), rb = (a.rows + kBlock - 1) / kBlock, pitch = code_pitch(a.k),
@@ -139,7 +125,7 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(QuantizeArgs a, in
         for (int i = 0; i < 8; i++) {
             const int64_t row = rt * kBlock + r0 + 16 * i;
             if (row < a.rows)
-                load8<T, VEC>((const T *)a.x + (m * a.rows + row) * a.ld, col, a.k, v[i]);
+                load8<T>((const T *)a.x + (m * a.rows + row) * a.ld, col, a.k, v[i]);
             else
                 for (int j = 0; j < 8; j++) v[i][j] = 0.0f;
             float big = 0.0f;
@@ -178,15 +164,20 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(QuantizeArgs a, in
     }
 }
 
-template <typename T, bool VEC>
+template <typename T>
 hipError_t quantize_go(const QuantizeArgs &a, hipStream_t s) {
     const int64_t tiles = a.count * ((a.rows + kBlock - 1) / kBlock) * blocks_of(a.k);
     const unsigned grid = (unsigned)(tiles < (1 << 20) ? tiles : (1 << 20));
     if (a.block_rows == 1)
-        quantize_blocks_kernel<T, VEC, false><<<grid, 256, 0, s>>>(a, tiles);
+        quantize_blocks_kernel<T, false><<<grid, 256, 0, s>>>(a, tiles);
     else
-        quantize_blocks_kernel<T, VEC, true><<<grid, 256, 0, s>>>(a, tiles);
+        quantize_blocks_kernel<T, true><<<grid, 256, 0, s>>>(a, tiles);
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t norm_type(const NormArgs &a, hipStream_t s) {
+    return a.residual ? norm_width<T, true>(a, s) : norm_width<T, false>(a, s);
 }
 
 }  // namespace
@@ -198,9 +189,7 @@ hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t stream) {
 
 hipError_t launch_quantize(const QuantizeArgs &a, bool bf16, hipStream_t stream) {
     if (a.count == 0 || a.rows == 0) return hipSuccess;
-    const bool vec = aligned16(a.x, a.ld, bf16 ? 2 : 4);
-    if (bf16) return vec ? quantize_go<__bf16, true>(a, stream) : quantize_go<__bf16, false>(a, stream);
-    return vec ? quantize_go<float, true>(a, stream) : quantize_go<float, false>(a, stream);
+    return bf16 ? quantize_go<__bf16>(a, stream) : quantize_go<float>(a, stream);
 }
 
 }  // namespace sdnn

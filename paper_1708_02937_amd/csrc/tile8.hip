@@ -504,35 +504,23 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, KG == 1 ? 2 : KG) product_t
                     put4(out + (wm * 32 + lane % 32) * kPitch + c, z);
                 }
             __syncthreads();
-            // Row lr of the slice, in tile row (lr / 32 MJ + j) 32 + lr % 32.
-            auto row_of = [&](int lr) -> Out * {
-                const int r = (lr / 32 * MJ + j) * 32 + lr % 32;
-                if (r >= rows) return nullptr;
-                if constexpr (MODE == kTileProduct)
-                    return (Out *)a.y + (row0 + r) * a.ldy + n0;
-                else
-                    return (Out *)work.o + (int64_t)slot[r] * work.o_pitch + n0;
-            };
             const int cols = (int)min((int64_t)BN, n_rows - n0);
-            if (work.wide) {
-                constexpr int kPieces = BN / kCells;
+            constexpr int kPieces = BN / kCells;
 #pragma unroll
-                for (int c = threadIdx.x; c < kSlice * kPieces; c += S::kThreads) {
-                    const int lr = c / kPieces, col = c % kPieces * kCells;
-                    Out *const y = row_of(lr);
-                    const Out *const from = out + lr * kPitch + col;
-                    if (!y || col >= cols) continue;
-                    if (col + kCells <= cols)
-                        __builtin_nontemporal_store(*(const v4i *)from, (v4i *)(y + col));
-                    else
-                        for (int v = 0; col + v < cols; v++) y[col + v] = from[v];
-                }
-            } else {  // rows at any address: a value per lane, neighbours side by side
-                static_assert(S::kThreads % BN == 0 || BN % S::kThreads == 0, "a thread keeps its columns");
-                for (int col = threadIdx.x % BN; col < cols; col += S::kThreads)
-#pragma unroll 4
-                    for (int lr = threadIdx.x / BN; lr < kSlice; lr += S::kThreads > BN ? S::kThreads / BN : 1)
-                        if (Out *const y = row_of(lr)) y[col] = out[lr * kPitch + col];
+            for (int c = threadIdx.x; c < kSlice * kPieces; c += S::kThreads) {
+                const int lr = c / kPieces, col = c % kPieces * kCells;
+                const int r = (lr / 32 * MJ + j) * 32 + lr % 32;  // row lr of the slice, in the tile
+                if (r >= rows || col >= cols) continue;
+                Out *y;
+                if constexpr (MODE == kTileProduct)
+                    y = (Out *)a.y + (row0 + r) * a.ldy + n0 + col;
+                else
+                    y = (Out *)work.o + (int64_t)slot[r] * work.o_pitch + n0 + col;
+                const Out *const from = out + lr * kPitch + col;
+                if (col + kCells <= cols)
+                    __builtin_nontemporal_store(*(const v4i *)from, (v4i_any *)y);
+                else
+                    for (int v = 0; col + v < cols; v++) y[v] = from[v];
             }
         }
     }
