@@ -8,7 +8,7 @@
 namespace sdnn {
 
 constexpr int kBlock = 128;             // columns (and, for weights, rows) that share a scale
-constexpr int64_t kNormMaxK = 32768;    // widest row of the norm: 512 threads hold it in registers
+constexpr int64_t kNormMaxK = 32768;    // widest row of the norm: 1024 threads hold it in registers
 constexpr int kRouteMaxExperts = 1024;  // 16 scores per lane of a wave
 constexpr int kRouteMaxChosen = 64;     // one chosen expert per lane
 constexpr int kRouteMaxGroups = 64;
