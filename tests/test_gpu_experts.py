@@ -261,6 +261,43 @@ def test_route_near_ties(torch, sd):
         _check_route(torch, sd, l.astype(np.float64), torch.float32, 4, score, bias, 8, 3, 2, True, 1.0)
 
 
+@pytest.mark.parametrize("T", [5, 40])
+@pytest.mark.parametrize("E", [24, 70, 200, 300, 600])
+def test_route_without_bias_by_logits(torch, sd, E, T):
+    """Without a bias: logits one float apart, and different logits whose scores are the same in 64 bits too (a sigmoid
+    of 1, scores of 0), which are ties."""
+    rng = np.random.default_rng(E + T)
+    l = np.repeat(rng.standard_normal((T, 1)).astype(np.float32), E, axis=1)
+    for t in range(T):
+        for step, e in enumerate(rng.permutation(E)[:5]):
+            for _ in range(step + 1):
+                l[t, e] = np.nextafter(l[t, e], np.float32(np.inf))
+    l[1] = 45 + rng.permutation(E)  # sigmoids of 1
+    l[2] = -2000 - rng.permutation(E)  # sigmoids of 0
+    l[3] = -5000 - rng.permutation(E)  # softmax: 0 next to the first two
+    l[3, [E - 1, E // 2]] = [1.0, 0.5]
+    for score in ("softmax", "sigmoid"):
+        for groups, kept, best in ((1, 1, 1), (2, 1, 2)):
+            _say("route by logits", T, E, score, groups)
+            with np.errstate(over="ignore"):
+                _check_route(torch, sd, l.astype(np.float64), torch.float32, 4, score, None, groups, kept, best, True, 1.0)
+
+
+@pytest.mark.parametrize("T,E,k,score,use_bias,groups,kept,best", [
+    (8, 300, 8, "sigmoid", True, 4, 2, 2), (100, 300, 8, "sigmoid", True, 4, 2, 2), (100, 512, 8, "softmax", True, 8, 4, 2),
+    (33, 1000, 5, "softmax", False, 8, 3, 2), (70, 1024, 8, "sigmoid", True, 8, 4, 2), (19, 513, 17, "softmax", False, 1, 1, 1),
+])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_route_many_experts(torch, sd, T, E, k, score, use_bias, groups, kept, best, dtype):
+    rng = np.random.default_rng(T * E)
+    dt = getattr(torch, dtype)
+    logits = _to(torch, 1.5 * rng.standard_normal((T, E)), dt)
+    logits[rng.random((T, E)) < 0.1] = -np.inf
+    bias = (rng.integers(-100, 101, E) * np.float32(1e-3)).astype(np.float32) if use_bias else None
+    _say("route", T, E, k, score, groups, dtype)
+    _check_route(torch, sd, logits, dt, k, score, bias, groups, kept, best, True, 2.5)
+
+
 def test_route_strides_and_empty(torch, sd):
     big = torch.randn(50, 90, device="cuda")
     a, b = sd.route(big[3:40, 7:67], 3), sd.route(big[3:40, 7:67].contiguous(), 3)
