@@ -375,9 +375,11 @@ sdnn_status sdnn_norm_quantize(int64_t rows, int64_t k, int32_t type, const void
  * Y = h(A W^T + bias) for blocked 8-bit A (m x k, block_rows 1) and W (n x k, block_rows 128: row j holds output j's
  * weights): Y (m x n, of the type) in fp32 sums, rounded once.  bias: n fp32 values or NULL.  activate 0: h is the
  * identity; 1: h(z) = min(max(z, 0), ymax), ymax > 0 (+INFINITY for plain ReLU; NaN stays NaN).
- * With SDNN_TYPE_F32 every product is exact and sums are fp32.  With SDNN_TYPE_BF16 the 8-bit matrix instructions are
- * used, which align the products of an instruction to their largest and drop what is below about 2^-14 of it: a
- * relative error near 1.5e-5 for normally distributed values, well under the output's rounding of 2^-9.
+ * With SDNN_TYPE_F32 every product is exact and sums are fp32.  With SDNN_TYPE_BF16 that is so for m <= 16 with n <= 8192;
+ * elsewhere the 8-bit matrix instructions are used, which align the products of an instruction to their largest and
+ * drop what is below about 2^-14 of it: a relative error near 1.5e-5 for normally distributed values (5e-5 where some
+ * columns are far larger than the others), well under the output's rounding of 2^-9.  The order of the sums goes by m, n
+ * and k alone.
  * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED (more tiles than a launch holds), DEVICE.
  */
 sdnn_status sdnn_product_blocks(int64_t m, int64_t n, int64_t k, const uint8_t *a, const uint8_t *a_scale,
@@ -398,7 +400,7 @@ sdnn_status sdnn_route_workspace_size(int64_t tokens, int32_t experts, int32_t c
  * score(e) + bias(e) (bias: `experts` fp32 values for balance, or NULL); with groups > 1 the experts form that many
  * equal runs, a run's worth is the sum of its group_best (1 or 2) largest choices, and only the groups_kept
  * worthiest runs stay; of the experts that stay the `chosen` with the largest choice are taken, largest first.
- * Scores and choices are held in fp64, and ties go to the lower index.  A weight is the expert's score, divided by the
+ * Scores and choices are those of fp64 and ties go to the lower index.  A weight is the expert's score, divided by the
  * sum of the chosen scores if normalize is 1, times factor.  An expert whose logit is -inf or NaN, or whose choice is
  * -inf or NaN, is never taken; +inf logits share a softmax among themselves.  Places without an expert have id -1 and
  * weight 0, so a row that is masked whole has no expert.
@@ -426,8 +428,9 @@ sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t i
  * Weights are stacks of blocked matrices with block_rows 128: w_in holds, for each expert, the gate's and then the
  * up-projection's inner x width matrix (2 * experts matrices), w_out each expert's width x inner matrix.
  * ids, weight, offsets and order as sdnn_route writes them; residual (tokens x width, of the type) may be NULL and may
- * be out itself.  With SDNN_TYPE_F32 and SDNN_TYPE_BF16 the two products have the arithmetic that sdnn_product_blocks
- * has with that type.  The sum over j is fp32 in the order of j.
+ * be out itself.  With SDNN_TYPE_F32 every product is exact and sums are fp32, the sum over j in the order of j.  With
+ * SDNN_TYPE_BF16 o may be rounded to 11 bits before it is weighted (to those of the largest of the 128 or 256 values next
+ * to it), and with many rows to an expert both products use the 8-bit instructions as in sdnn_product_blocks.
  * Entries of offsets and order outside their ranges are brought into them, so no access leaves the arrays, but the
  * result is then undefined.
  * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED, WORKSPACE_TOO_SMALL, DEVICE.
