@@ -2,12 +2,12 @@
 // LDS one block of 128 columns at a time.
 //
 // The weights are the first operand of the 32 x 32 matrix instructions and the activations the second, so a lane ends
-// with runs of four consecutive outputs of one activation row.  Two arithmetics, by the output's type:
-//   bfloat16  the scaled 8-bit instructions, which multiply by both blocks' powers of two themselves.  Within an
-//             instruction they align products to the largest one and keep about 14 bits, 1.5e-5 of a sum of normal
-//             values (measured), a hundredth of the output's own rounding; between instructions the sum is fp32.
-//   float     codes widened to bfloat16 with their scales, which is exact, and the 16-bit instructions, whose products
-//             and sums are fp32.  Half the matrix rate.
+// with runs of four consecutive outputs of one activation row.  Two arithmetics:
+//   8 bits  (bfloat16 outputs) the scaled 8-bit instructions, which multiply by both blocks' powers of two themselves.
+//           Within an instruction they align products to the largest one and keep about 14 bits, 1.5e-5 of a sum of
+//           normal values (measured), a hundredth of the output's own rounding; between instructions the sum is fp32.
+//   EXACT   (float outputs, and the first of the experts' products for few rows) codes widened to bfloat16 with their
+//           scales, which is exact, and the 16-bit instructions, whose products and sums are fp32.  Half the matrix rate.
 #include "product8.h"
 
 namespace sdnn {
