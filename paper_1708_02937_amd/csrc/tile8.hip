@@ -584,9 +584,15 @@ hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
     }
 }
 
-// Tiles of 64 rows for few rows to an expert, of 128 for many, where those still fill the chip (two workgroups to a CU,
-// or nearly).  Measured in us, 64 experts of 4096 x 1024, 8 chosen: 333 tokens (42 rows to an expert) 252 and 238, 64
-// tokens 208 and 224, 2048 tokens 531 and 447; 24 experts of 2001 x 701, 3 chosen: 333 tokens 42 and 49.
+// Tiles of 64 rows with the first product exact; of 128 with the 8-bit instructions for many rows to an expert, where
+// tiles are enough to fill the chip more than once.  Both measured in us (64 rows | 128 rows):
+//   64 experts of 4096 x 1024, 8 chosen:   64 tokens 262 | 225,  333 tokens 312 | 226,  2048 tokens 739 | 429
+//   8 experts of 4096 x 1024, 2 chosen:    128 tokens 69 | 61,   512 tokens 80 | 70,    2048 tokens 216 | 122
+//   24 experts of 2001 x 701, 3 chosen:    333 tokens 51 | 47,   600 tokens 81 | 53,    1000 tokens 89 | 69
+// What the exact product is for: a sum that is 5e-5 off (a column in a hundred ten times as wide as the others) moves some
+// values of p over a boundary of their 8 bits.  Without a residual the result is then 1.3 to 1.5 times as far from the
+// exact one as its own rounding to bfloat16 brings it, with one 1.03 to 1.3 times.  That is paid for the halved time of
+// long calls, not for a few us of short ones.  (The exact product on tiles of 128 rows: 8192 tokens as above 2.2 ms, 1.3.)
 template <typename T>
 hipError_t experts_go(const ExpertsArgs &x, TileWork work, int *run, hipStream_t s) {
     constexpr bool kExact = sizeof(T) == 4;
@@ -600,8 +606,6 @@ hipError_t experts_go(const ExpertsArgs &x, TileWork work, int *run, hipStream_t
             *run = 256;
             return tile_go<kTileExpertsOut, T, kExact, 256, 128, 2, 2, 1, 3>(none, x, work, large, x.width, s);
         }
-    // Few rows wait for weights, so they take the exact arithmetic whatever the type: a sum that is 5e-5 off moves values
-    // of p over a boundary of their 8 bits, up to 1.9e-3 of the result (333 tokens as above: 53 us, 49 without).
     const hipError_t e =
         Tile<kTileExpertsIn, T, true, 256, 64, 4, 1, 2, 3>::lds_bytes(x.width) <= kMaxLds
             ? tile_go<kTileExpertsIn, T, true, 256, 64, 4, 1, 2, 3>(none, x, work, small, x.inner, s)
