@@ -3,7 +3,8 @@
 The functions below carry the C names and only marshal arguments: every step of the
 forward pass runs in the library's HIP kernels.  PyTorch supplies device memory and
 the stream.  Importing this package fails if libsdnn.so has not been built
-(``python paper_1708_02937_amd/build.py``); there is no fallback.
+(``python paper_1708_02937_amd/build.py``); there is no fallback.  The layer of experts also has calls on torch
+tensors (experts.py over _tensors.so, built beside the library).
 
 The paper computes Y_{k+1} = h(W_k Y_k + B_k) with ReLU h (Kepner et al.,
 arXiv:1708.02937, Sec. III) via the GraphBLAS loop of Fig. 4 (Sec. IV); here the

@@ -15,6 +15,7 @@ Tolerances, fixed before any run:
 """
 
 import math
+import sys
 
 import numpy as np
 import pytest
@@ -601,3 +602,73 @@ def test_same_inputs_same_bits(torch, sd):
     a = sd.experts_forward(*args, H, F)
     for _ in range(3):
         assert torch.equal(sd.experts_forward(*args, H, F), a)
+
+
+# ------------------------------------------------------------------------------------------------ tensor arguments
+
+
+def test_tensor_arguments_are_checked(torch, sd):
+    """Wrong types, shapes, devices and strides are ValueErrors (TypeError where no tensor is given); what only the C call
+    refuses carries its status."""
+    x = torch.randn(6, 200, device="cuda")
+    gamma = torch.ones(200, device="cuda")
+    a, sa = sd.quantize_blocks(x)
+    w, sw = sd.quantize_blocks(torch.randn(70, 200, device="cuda"), 128)
+    logits = torch.randn(6, 8, device="cuda")
+    routes = sd.route(logits, 2)
+    w_in, s_in = sd.quantize_blocks(torch.randn(8, 2, 40, 200, device="cuda"), 128)
+    w_out, s_out = sd.quantize_blocks(torch.randn(8, 200, 40, device="cuda"), 128)
+
+    def experts(**kw):
+        args = dict(a=a, a_scale=sa, routes=routes, w_in=w_in, w_in_scale=s_in, w_out=w_out, w_out_scale=s_out, width=200,
+                    inner=40)
+        return sd.experts_forward(**{**args, **kw})
+
+    assert experts().shape == (6, 200)
+    wrong = [
+        lambda: sd.norm_quantize(x.half(), gamma), lambda: sd.norm_quantize(x[0], gamma),
+        lambda: sd.norm_quantize(x, gamma[1:]), lambda: sd.norm_quantize(x, gamma.double()),
+        lambda: sd.norm_quantize(x, gamma.cpu()), lambda: sd.norm_quantize(x.t(), torch.ones(6, device="cuda")),
+        lambda: sd.norm_quantize(x, gamma, residual=x.bfloat16()), lambda: sd.norm_quantize(x, gamma, residual=x[1:]),
+        lambda: sd.norm_quantize(x, gamma, out_sum=x), lambda: sd.quantize_blocks(x.t()),
+        lambda: sd.quantize_blocks(x[0]), lambda: sd.product_blocks(a, sa, w, sw, 300),
+        lambda: sd.product_blocks(a[:5], sa, w, sw, 200), lambda: sd.product_blocks(a, sa, w, sw[:, :2], 200),
+        lambda: sd.product_blocks(a.view(torch.uint8), sa, w, sw, 200),
+        lambda: sd.product_blocks(a, sa, w, sw, 200, bias=gamma), lambda: sd.product_blocks(a, sa, w, sw, 200, out=x),
+        lambda: sd.product_blocks(a, sa, w, sw, 200, dtype=torch.float16), lambda: sd.route(logits, 0),
+        lambda: sd.route(logits, 2, score="best"), lambda: sd.route(logits.long(), 2),
+        lambda: sd.route(logits, 2, bias=gamma), lambda: experts(a=a[:3]), lambda: experts(w_out=w_out[:4]),
+        lambda: experts(residual=x), lambda: experts(ws=torch.empty(9, device="cuda")), lambda: experts(width=201),
+        lambda: experts(routes=routes._replace(order=routes.order[1:])),
+    ]
+    for i, call in enumerate(wrong):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"case {i} was taken")
+    for call in (lambda: sd.norm_quantize(x, None), lambda: sd.route(logits, 2.5), lambda: sd.route(logits, 2, bias=3)):
+        with pytest.raises(TypeError):
+            call()
+    for status, call in ((2, lambda: sd.route(logits, 9)), (2, lambda: sd.norm_quantize(x, gamma, eps=-1.0)),
+                         (2, lambda: sd.quantize_blocks(x, 64)), (2, lambda: sd.route(logits, 2, groups=3)),
+                         (6, lambda: experts(ws=torch.empty(16, dtype=torch.uint8, device="cuda")))):
+        with pytest.raises(sd.SdnnError) as e:
+            call()
+        assert e.value.status == status
+
+
+def test_tensor_results_are_owned(torch, sd):
+    """Results are freed when they are dropped, out tensors come back as themselves, refused calls keep nothing."""
+    x = torch.randn(64, 500, device="cuda")
+    gamma = torch.ones(500, device="cuda")
+    same = sd.norm_quantize(x, gamma, residual=x.clone(), out_sum=x)
+    assert same[2] is x and same[3] is None
+    del same
+    torch.cuda.synchronize()
+    before, refs = torch.cuda.memory_allocated(), sys.getrefcount(x)
+    for _ in range(20):
+        sd.norm_quantize(x, gamma, residual=x, normed=True)
+        sd.route(x, 3)
+        sd.product_blocks(*sd.quantize_blocks(x), *sd.quantize_blocks(x, 128), 500)
+        with pytest.raises(sd.SdnnError):
+            sd.route(x, 501)
+    assert torch.cuda.memory_allocated() == before and sys.getrefcount(x) == refs
