@@ -375,7 +375,8 @@ sdnn_status sdnn_norm_quantize(int64_t rows, int64_t k, int32_t type, const void
  * Y = h(A W^T + bias) for blocked 8-bit A (m x k, block_rows 1) and W (n x k, block_rows 128: row j holds output j's
  * weights): Y (m x n, of the type) in fp32 sums, rounded once.  bias: n fp32 values or NULL.  activate 0: h is the
  * identity; 1: h(z) = min(max(z, 0), ymax), ymax > 0 (+INFINITY for plain ReLU; NaN stays NaN).
- * With SDNN_TYPE_F32 every product is exact and sums are fp32.  With SDNN_TYPE_BF16 that is so for m <= 16 with n <= 8192;
+ * With SDNN_TYPE_F32 every product is exact and sums are fp32.  With SDNN_TYPE_BF16 that is so for few outputs (up
+ * to 256 tiles of 16 x 16, 512 with m <= 8);
  * elsewhere the 8-bit matrix instructions are used, which align the products of an instruction to their largest and
  * drop what is below about 2^-14 of it: a relative error near 1.5e-5 for normally distributed values (5e-5 where some
  * columns are far larger than the others), well under the output's rounding of 2^-9.  The order of the sums goes by m, n

@@ -30,8 +30,9 @@ __device__ __forceinline__ v8i load32(const uint8_t *p) {
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
-// 16 outputs x up to 16 rows per workgroup, straight from memory to registers: the weights are read once, which is what
-// bounds these calls.  The waves share the blocks of the inner dimension and join their sums in LDS.
+// 16 outputs x 16 rows per workgroup, straight from memory to registers: with up to 16 rows the weights are read once,
+// which is what bounds those calls.  The waves share the blocks of the inner dimension and join their sums in LDS.  (16
+// waves in place of 8: 11.4 us against 7.1 at 116 x 271 x 4000, the same at 16000.)
 constexpr int kSplit = 8;
 
 // acc[v] += this wave's blocks of NW weight tiles times the activation tile.  Four blocks are loaded before the first is
@@ -72,14 +73,14 @@ template <typename T>
 __global__ void __launch_bounds__(64 * kSplit) product_stream_kernel(ProductArgs a) {
     __shared__ v4f part[kSplit][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, m = min((int64_t)lane % 16, a.m - 1);
+    const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16, m = min(m0 + lane % 16, a.m - 1);
     const int64_t pitch = code_pitch(a.k), spitch = scale_pitch(a.k);
     const uint8_t *w[1] = {a.w + min(n0 + lane % 16, a.n - 1) * pitch}, *ws[1] = {a.w_scale + n0 / kBlock * spitch};
     v4f acc[1] = {};
     stream_tiles<1>(acc, w, ws, a.a + m * pitch, a.a_scale + m * spitch, (int)blocks_of(a.k), wave);
     part[wave][lane] = acc[0];
     __syncthreads();
-    if (wave != 0 || lane % 16 >= a.m) return;
+    if (wave != 0 || m0 + lane % 16 >= a.m) return;
     const v4f s = total(part);
     T *y = (T *)a.y + m * a.ldy;
     for (int i = 0; i < 4; i++) {
@@ -288,10 +289,14 @@ size_t experts_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t e
 
 hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
     if (a.m == 0 || a.n == 0) return hipSuccess;
-    // Up to 16 rows and 512 workgroups; measured at K = 4096, M = 16 against tiles: N = 4096 8.1 and 10.0 us, N = 16384 21.5
-    // and 14.9.
-    if (a.m <= 16 && a.n <= 512 * 16) {
-        const unsigned grid = (unsigned)((a.n + 15) / 16);
+    // Few outputs: 16 x 16 of them per workgroup; tiles would leave most CUs empty.  Measured in us (this | tiles):
+    //   bfloat16, K = 4000:  116 x 271 7.1 | 10.3,  64 x 1000 7.4 | 10.2,  128 x 1000 (504) 12.3 | 10.3,
+    //                        1 x 8192 (512) 8.0 | 10.4,  8 x 5000 9.8 | 10.2,  16 x 8192 12.3 | 10.5
+    //   float, K = 4000:     116 x 271 7.2 | 17.8,  128 x 1000 12.4 | 17.9,  64 x 4000 (1000) 21.8 | 18.1
+    //   K = 16000, 116 x 271:  bfloat16 21 | 26,  float 21 | 56
+    const int64_t across = (a.n + 15) / 16, cells = (a.m + 15) / 16 * across;
+    if (cells <= (bf16 && a.m > 8 ? 256 : 512)) {
+        const dim3 grid((unsigned)across, (unsigned)((a.m + 15) / 16));
         if (bf16)
             product_stream_kernel<__bf16><<<grid, 64 * kSplit, 0, stream>>>(a);
         else

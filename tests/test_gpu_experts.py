@@ -365,6 +365,25 @@ def test_product_long_rows(torch, sd, m, n, k):
         assert np.array_equal(got, _to(torch, want, dt))
 
 
+@pytest.mark.parametrize("m,n,k", [(33, 1000, 3999), (116, 271, 1287), (250, 250, 640), (8, 8192, 130), (9, 4097, 257),
+                                   (64, 4200, 1001), (257, 1000, 4000), (500, 900, 333), (1000, 2000, 2500),
+                                   (400, 700, 33000), (600, 260, 66000)])
+def test_product_between_few_rows_and_tiles(torch, sd, m, n, k):
+    """Both sides of the bound between 16 x 16 outputs per workgroup and larger tiles, rows too long for their scales to
+    lie in LDS among these: exact integers."""
+    g = torch.Generator(device="cuda").manual_seed(m + n)
+    x = torch.randint(-2, 3, (m, k), generator=g, device="cuda").float()
+    y = torch.randint(-2, 3, (n, k), generator=g, device="cuda").float()
+    a, sa = sd.quantize_blocks(x)
+    w, sw = sd.quantize_blocks(y, 128)
+    bias = torch.randint(-9, 10, (n,), generator=g, device="cuda").float()
+    want = (x.double() @ y.double().t()).cpu().numpy() + bias.double().cpu().numpy()
+    for dt in (torch.float32, torch.bfloat16):
+        _say("few rows or tiles", m, n, k, dt)
+        got = sd.product_blocks(a, sa, w, sw, k, bias=bias, ymax=150.0, dtype=dt).double().cpu().numpy()
+        assert np.array_equal(got, _to(torch, np.clip(want, 0, 150.0), dt))
+
+
 def test_product_extremes(torch, sd):
     """Scales at both ends of their range, NaN codes in one row and one column only, outputs in a strided view."""
     m, n, k = 40, 150, 300
