@@ -108,6 +108,13 @@ __device__ __forceinline__ void put_choice(const RouteArgs &a, int64_t token, in
     a.weight[token * a.chosen + j] = (float)(score * (double)a.factor);
 }
 
+// Lanes that share a group where `lanes` of them take `groups` groups: a power of two.
+__device__ __forceinline__ int span_of(int lanes, int groups) {
+    int span = 1;
+    while (span * 2 * groups <= lanes) span *= 2;
+    return span;
+}
+
 // One token decided in fp64 by a whole wave; `shared` holds 64 R values of the wave's own.
 template <typename T, int R>
 __device__ __forceinline__ void route_exact(const RouteArgs &a, int64_t token, double *shared) {
@@ -149,22 +156,27 @@ __device__ __forceinline__ void route_exact(const RouteArgs &a, int64_t token, d
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own LDS writes, read by its other lanes
     if (a.groups > 1) {
         const int size = a.experts / a.groups;
+        const int span = span_of(64, a.groups), own = lane / span;
         double one = -INFINITY, two = -INFINITY;
-        if (lane < a.groups)
-#pragma unroll 8
-            for (int i = 0; i < size; i++) {
-                const double c = shared[lane * size + i];
+        if (own < a.groups)
+            for (int i = lane % span; i < size; i += span) {
+                const double c = shared[own * size + i];
                 two = fmax(two, fmin(one, c));
                 one = fmax(one, c);
             }
+        for (int m = 1; m < span; m <<= 1) {
+            const double u = __shfl_xor(one, m), v = __shfl_xor(two, m);
+            two = fmax(fmax(two, v), fmin(one, u));
+            one = fmax(one, u);
+        }
         double best = a.group_best == 2 && two > -INFINITY ? one + two : one;
         uint64_t kept = 0;
         for (int g = 0; g < a.groups_kept; g++) {
             double v = best;
-            int i = lane;
+            int i = own;
             wave_best(v, i);
             kept |= 1ull << i;
-            if (lane == i) best = -INFINITY;
+            if (own == i) best = -INFINITY;
         }
 #pragma unroll
         for (int r = 0; r < R; r++) {
@@ -287,8 +299,9 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
     uint64_t kept = ~0ull;
     const int size = a.experts / a.groups;
     if (a.groups > 1) {
-        const int span = size / R;  // lanes of a group, where groups begin and end with lanes
-        const bool by_lanes = size % R == 0 && (span & (span - 1)) == 0;
+        // A group is held by whole lanes, or scanned in LDS; `span` lanes share it, a power of two.
+        const bool by_lanes = size % R == 0 && (size / R & (size / R - 1)) == 0;
+        const int span = by_lanes ? size / R : span_of(LANES, a.groups), own = lane / span;
         float one = -INFINITY, two = -INFINITY;
         auto take = [&](float v) {
             two = fmaxf(two, fminf(one, v));
@@ -297,27 +310,20 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
         if (by_lanes) {
 #pragma unroll
             for (int r = 0; r < R; r++) take(c[r]);
-            for (int m = 1; m < span; m <<= 1) {
-                const float u = __shfl_xor(one, m), v = __shfl_xor(two, m);
-                two = fmaxf(fmaxf(two, v), fminf(one, u));
-                one = fmaxf(one, u);
-            }
         } else {
             float *mine = (float *)shared + sub * LANES * R;
 #pragma unroll
             for (int r = 0; r < R; r++) mine[lane * R + r] = c[r];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (lane < a.groups) {
-                int at = lane % size;  // lanes start at different places, in different banks
-                for (int i = 0; i < size; i++) {
-                    take(mine[lane * size + at]);
-                    at = at + 1 < size ? at + 1 : 0;
-                }
-            }
+            if (own < a.groups)
+                for (int i = lane % span; i < size; i += span) take(mine[own * size + i]);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        // A lane holds the worth of its own group (by_lanes: shared with the others of the group), or of group `lane`.
-        const int own = by_lanes ? lane / span : lane;
+        for (int m = 1; m < span; m <<= 1) {
+            const float u = __shfl_xor(one, m), v = __shfl_xor(two, m);
+            two = fmaxf(fmaxf(two, v), fminf(one, u));
+            one = fmaxf(one, u);
+        }
         float worth = a.group_best == 2 && two > -INFINITY ? one + two : one;
         kept = 0;
         float least = INFINITY;
