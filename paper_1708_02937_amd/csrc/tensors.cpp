@@ -1,7 +1,7 @@
 // The layer of experts on torch tensors: shapes and addresses are read from the tensors, outputs and workspaces come
 // from torch's allocator on the stream given, and the C entry is called.  The Python functions of experts.py choose
 // device and stream and hand their arguments over in order.  A small call's time is spent on the host: one token of 4096
-// columns through the norm, whose kernel takes 3.2 us, is 7.4 us a call, 11.4 with the same steps in Python (four
+// columns through the norm, whose kernel takes 3.1 us, is 7.4 us a call, 11.4 with the same steps in Python (four
 // tensors of torch's at about 0.9 us, the launch 2.5).
 //
 // Every function returns its tensors, or the status of the C call where that is not SDNN_OK.
