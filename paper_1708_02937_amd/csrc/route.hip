@@ -290,11 +290,9 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
             if (!(c[r] > -INFINITY)) c[r] = -INFINITY;
         }
     }
-    auto apart = [&](float high, float low, float times) {  // high >= low; false as soon as anything is not finite
+    auto apart = [&](float high, float low) {  // high >= low; false as soon as anything is not finite
         const float size = fmaxf(fabsf(high), fabsf(low));
-        float bound = slack + 2.5e-7f * size;
-        if (!BIAS) bound = fminf(bound, 5e-5f * size);
-        return low == -INFINITY || high - low > times * bound;
+        return low == -INFINITY || high - low > slack + 2.5e-7f * size;
     };
     uint64_t kept = ~0ull;
     const int size = a.experts / a.groups;
@@ -324,16 +322,30 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
             two = fmaxf(fmaxf(two, v), fminf(one, u));
             one = fmaxf(one, u);
         }
-        float worth = a.group_best == 2 && two > -INFINITY ? one + two : one;
+        // A group's worth is off by what its choices are, twice their bound, and by its own rounding, which go by the
+        // choices' size and not by the sum's: choices of opposite signs cancel.  The groups that stay have to lie above the
+        // others by both errors.  Half a worth is held where a bias could make the whole one overflow: a group whose
+        // choices are near the lowest value is not an empty one.  Without a bias the error is a share of the worth, down to
+        // the smallest normal number, below which a choice may be 0.
+        constexpr float kPart = BIAS ? 0.5f : 1.0f;
+        const bool both = a.group_best == 2 && two > -INFINITY;
+        float worth = both ? kPart * one + kPart * two : kPart * one;
+        const float largest = both ? fmaxf(fabsf(one), fabsf(two)) : fabsf(one);
+        float off = kPart * (slack + 4e-7f * largest);
+        if (!BIAS) off = fminf(off, 5e-5f * worth + 2.4e-38f);
+        const bool empty = !(worth > -INFINITY), finite = largest < INFINITY;
+        const float low = empty ? INFINITY : finite ? worth - off : -INFINITY;
+        const float high = empty ? -INFINITY : finite ? worth + off : INFINITY;
         kept = 0;
-        float least = INFINITY;
         for (int g = 0; g < a.groups_kept; g++) {
-            least = lanes_max<LANES>(worth);
-            const int i = lanes_min<LANES>(worth == least ? own : LANES);
+            const float best = lanes_max<LANES>(worth);
+            const int i = lanes_min<LANES>(worth == best ? own : LANES);
             kept |= 1ull << (i & 63);
             if (own == i) worth = -INFINITY;
         }
-        sure = sure && apart(least, lanes_max<LANES>(worth), 2.0f);
+        const bool stays = kept >> (own & 63) & 1;
+        const float lowest = -lanes_max<LANES>(stays ? -low : -INFINITY), others = lanes_max<LANES>(stays ? -INFINITY : high);
+        sure = sure && (others == -INFINITY || lowest > others);
     }
     // what the experts are ordered by, those of other groups out of it
     float (&key)[R] = BIAS ? c : l;
@@ -354,7 +366,7 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
         best = lanes_max<LANES>(best);
         if (j > 0) {
             if constexpr (BIAS) {
-                sure = sure && apart(last, best, 1.0f);
+                sure = sure && apart(last, best);
             } else if (last > best && best > -INFINITY) {
                 // different logits, and scores that differ in 64 bits too: by 2e-15 of the larger one or more
                 const float gap = last - best;

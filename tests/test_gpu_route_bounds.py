@@ -1,0 +1,70 @@
+"""Routing at the edges of what 32 bits can decide and of what one launch holds, against tests/blocks_ref.py.
+
+Tolerances as in tests/test_gpu_experts.py: ids, offsets and order equal, weights within one rounding to fp32.
+"""
+
+import numpy as np
+import pytest
+
+from tests import blocks_ref as ref
+from tests.test_gpu_experts import _check_route, _say, sd, torch  # noqa: F401  (the last two are fixtures)
+
+pytestmark = pytest.mark.gpu
+
+LOWEST = float(np.finfo(np.float32).min)
+
+
+@pytest.mark.parametrize("T", [8, 1500])
+@pytest.mark.parametrize("groups,size", [(4, 2), (8, 3), (8, 4), (4, 150)])
+@pytest.mark.parametrize("B", [100.0, 1000.0])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_groups_whose_two_best_cancel(torch, sd, score, B, groups, size, T):  # noqa: F811
+    """Biases of +B and -B on a group's two best experts: the choices are rounded at B's magnitude in 32 bits, and their
+    sums, which decide the groups, differ by far less than that rounding."""
+    rng = np.random.default_rng(int(B) + groups * size + T)
+    bias = np.full((groups, size), -2 * B, np.float32)
+    mine = B * (1 + np.arange(groups) / 64)  # so far apart that the experts' own order is never in doubt
+    bias[:, 0], bias[:, size - 1] = mine, -mine
+    near = 10.0 ** rng.uniform(-6, -3, (T, 1, 1)) * rng.standard_normal((T, groups, 1))
+    l = (rng.standard_normal((T, 1, size)) + near).reshape(T, groups * size).astype(np.float32)
+    _say("groups that cancel", score, B, groups, size, T)
+    _check_route(torch, sd, l.astype(np.float64), torch.float32, 2, score, bias.reshape(-1), groups, 2, 2, True, 1.0)
+
+
+@pytest.mark.parametrize("T", [3, 200])
+@pytest.mark.parametrize("low", [LOWEST, -3e38])
+@pytest.mark.parametrize("spread", [1.0, 0.75])
+@pytest.mark.parametrize("best", [1, 2])
+def test_groups_masked_by_a_bias_of_the_lowest_value(torch, sd, best, spread, low, T):  # noqa: F811
+    """A bias of the type's lowest value puts experts last and leaves them choosable: the sum of two such choices is a
+    finite 64-bit number, so their group stays where fewer others do than groups_kept, and only -inf takes it out."""
+    rng = np.random.default_rng(T)
+    for groups, size in ((4, 4), (8, 3)):
+        bias = (rng.integers(-100, 101, (groups, size)) * np.float32(1e-3)).astype(np.float32)
+        # masks of one value, and masks that differ, which 32 bits can tell apart
+        bias[[0, groups - 1]] = low * np.linspace(1, spread, 2 * size, dtype=np.float32).reshape(2, size)
+        bias[1, 1:] = low * np.linspace(spread, 1, size - 1, dtype=np.float32)  # an open expert beside masked ones
+        bias[2] = -np.inf
+        l = rng.standard_normal((T, groups * size)).astype(np.float32)
+        for score in ("softmax", "sigmoid"):
+            for kept in (1, groups - 2, groups - 1, groups):
+                _say("groups masked", best, spread, low, T, groups, score, kept)
+                with np.errstate(over="ignore"):
+                    _check_route(torch, sd, l.astype(np.float64), torch.float32, min(6, size * kept), score,
+                                 bias.reshape(-1), groups, kept, best, True, 1.0)
+
+
+@pytest.mark.parametrize("high", [-LOWEST, 3e38, np.inf])
+def test_groups_raised_by_a_bias_of_the_largest_value(torch, sd, high):  # noqa: F811
+    rng = np.random.default_rng(6)
+    bias = np.zeros((8, 4), np.float32)
+    bias[3, 1:3] = high
+    bias[5] = high
+    bias[6, 2] = high
+    l = rng.standard_normal((50, 32)).astype(np.float32)
+    for score in ("softmax", "sigmoid"):
+        for best in (1, 2):
+            for kept in (1, 2, 4):
+                with np.errstate(over="ignore", invalid="ignore"):
+                    _check_route(torch, sd, l.astype(np.float64), torch.float32, 4, score, bias.reshape(-1), 8, kept,
+                                 best, True, 1.0)
