@@ -263,6 +263,8 @@ hipError_t experts_go(const ExpertsArgs &a, hipStream_t s) {
         while (share * 2 * a.chosen <= kSplit) share *= 2;
         float *p = (float *)a.ws;
         experts_in_slot_kernel<<<(unsigned)in, 64 * kSplit, 0, s>>>(a, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
         experts_out_slot_kernel<T><<<(unsigned)out, 64 * kSplit, 0, s>>>(a, p, share);
         return hipGetLastError();
     }

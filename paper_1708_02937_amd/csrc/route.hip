@@ -637,16 +637,31 @@ hipError_t route_go(const RouteArgs &a, hipStream_t s) {
         return hipGetLastError();
     }
     constexpr int64_t kTokens = kScoreWaves * (64 / LANES);
-    route_scores_kernel<T, LANES, R, BIAS><<<(unsigned)((a.tokens + kTokens - 1) / kTokens), 64 * kScoreWaves, 0, s>>>(a);
+    constexpr int64_t kStep = kTokens << 22;  // tokens of a launch, which holds fewer than 2^32 threads
+    for (int64_t t0 = 0; t0 < a.tokens; t0 += kStep) {
+        RouteArgs p = a;
+        p.tokens = a.tokens - t0 < kStep ? a.tokens - t0 : kStep;
+        p.logits = (const T *)a.logits + t0 * a.ld;
+        p.ids = a.ids + t0 * a.chosen;
+        p.weight = a.weight + t0 * a.chosen;
+        route_scores_kernel<T, LANES, R, BIAS>
+            <<<(unsigned)((p.tokens + kTokens - 1) / kTokens), 64 * kScoreWaves, 0, s>>>(p);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;  // the plan reads the ids
     const int chunks = chunks_of(a.tokens * a.chosen);
     int32_t *counts = chunks > 1 ? (int32_t *)a.ws : nullptr;
     static std::atomic<unsigned long long> raised[2];
     constexpr size_t kMostLds = kPlanWaves * kRouteMaxExperts * sizeof(int);
     const size_t lds = (size_t)kPlanWaves * a.experts * sizeof(int);
-    hipError_t e = raise_lds_limit((const void *)route_count_kernel, kMostLds, raised[0]);
+    e = raise_lds_limit((const void *)route_count_kernel, kMostLds, raised[0]);
     if (e == hipSuccess) e = raise_lds_limit((const void *)route_plan_kernel, kMostLds, raised[1]);
     if (e != hipSuccess) return e;
-    if (chunks > 1) route_count_kernel<<<chunks, 64 * kPlanWaves, lds, s>>>(a, counts, bits);
+    if (chunks > 1) {
+        route_count_kernel<<<chunks, 64 * kPlanWaves, lds, s>>>(a, counts, bits);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     route_plan_kernel<<<chunks, 64 * kPlanWaves, lds, s>>>(a, counts, bits);
     return hipGetLastError();
 }

@@ -68,3 +68,30 @@ def test_groups_raised_by_a_bias_of_the_largest_value(torch, sd, high):  # noqa:
                 with np.errstate(over="ignore", invalid="ignore"):
                     _check_route(torch, sd, l.astype(np.float64), torch.float32, 4, score, bias.reshape(-1), 8, kept,
                                  best, True, 1.0)
+
+
+def test_more_tokens_than_one_launch_holds(torch, sd):  # noqa: F811
+    """2^28 tokens and a few, at 16 lanes each: 2^32 threads and more.  Two experts, so that the definition is one
+    comparison and one exponential for a token."""
+    T = (1 << 28) + 5
+    g = torch.Generator(device="cuda").manual_seed(9)
+    logits = torch.randn(T, 2, generator=g, device="cuda", dtype=torch.bfloat16)
+    logits[-3, 1] = -float("inf")
+    logits[T // 2] = -float("inf")
+    _say("many tokens", T)
+    got = sd.route(logits, 1, normalize=False)
+    part = 1 << 24
+    for t in range(0, T, part):
+        l = logits[t:t + part].double()
+        one = l[:, 1] > l[:, 0]
+        there = l.amax(dim=1) > -float("inf")
+        assert torch.equal(got.ids[t:t + part, 0], torch.where(there, one.int(), -1))
+        want = torch.where(there, 1 / (1 + torch.exp(-(l[:, 1] - l[:, 0]).abs())), 0.0)
+        assert bool(((got.weight[t:t + part, 0].double() - want).abs() <= 2.0 ** -23 * want).all())
+    ones = int((got.ids == 1).sum())
+    zeros = T - 1 - ones
+    assert got.offsets.tolist() == [0, zeros, T - 1] and int(got.order[-1]) == -1
+    order = got.order[:T - 1].long()
+    assert bool((got.ids[order[:zeros], 0] == 0).all()) and bool((got.ids[order[zeros:], 0] == 1).all())
+    for run in (order[:zeros], order[zeros:]):  # ascending within an expert, so each slot once
+        assert bool((run[1:] > run[:-1]).all())
