@@ -422,7 +422,8 @@ sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t i
 
 /*
  * The chosen experts' gated feed-forward networks and their weighted sum.  With a_t row t of A (tokens x width,
- * blocked, block_rows 1), for each slot (t, j) with expert e = ids(t, j) >= 0:
+ * blocked, block_rows 1), for each slot (t, j) with expert e = ids(t, j), 0 <= e < experts (any other id is a place
+ * without an expert, whose weight is not read):
  *   g = W_gate(e) a_t,  u = W_up(e) a_t,  p = g / (1 + exp(-g)) * u   (inner values)
  *   o = W_out(e) q(p)   (width values; q rounds p to 8 bits by the rule of sdnn_quantize_blocks, block_rows 1)
  *   out_t = residual_t + sum_j weight(t, j) o(t, j)

@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(ExpertsArgs a, Til
 #pragma unroll 4
         for (int j = 0; j < a.chosen; j++) {
             const int64_t slot = t * a.chosen + j;
-            if (a.ids[slot] < 0) continue;
+            if ((uint32_t)a.ids[slot] >= (uint32_t)a.experts) continue;  // its row of o is not written
             const float w = a.weight[slot];
             if constexpr (sizeof(T) == 4) {
                 float v[8];
