@@ -393,7 +393,10 @@ enum {
     SDNN_SCORE_SIGMOID = 1  /* 1 / (1 + exp(-l_e)) */
 };
 
-/* Bytes of device workspace sdnn_route needs.  Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED. */
+/*
+ * Bytes of device workspace sdnn_route needs for any call of up to `tokens` tokens.
+ * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED.
+ */
 sdnn_status sdnn_route_workspace_size(int64_t tokens, int32_t experts, int32_t chosen, int64_t *bytes);
 
 /*
@@ -416,7 +419,10 @@ sdnn_status sdnn_route(int64_t tokens, int32_t experts, int32_t chosen, int32_t 
                        int32_t group_best, int32_t normalize, float factor, int32_t *ids, float *weight,
                        int32_t *offsets, int32_t *order, void *ws, int64_t ws_bytes, void *stream);
 
-/* Bytes of device workspace sdnn_experts_forward needs.  Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED. */
+/*
+ * Bytes of device workspace sdnn_experts_forward needs for any call of up to `tokens` tokens.
+ * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED.
+ */
 sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t inner, int32_t experts,
                                         int32_t chosen, int32_t type, int64_t *bytes);
 

@@ -174,7 +174,7 @@ sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t i
     sdnn::set_error(SDNN_OK, "");
     if (!bytes) return fail(SDNN_ERR_NULL_POINTER, "bytes is NULL");
     SDNN_CHECK(check_experts(tokens, width, inner, experts, chosen, type));
-    *bytes = (int64_t)sdnn::experts_workspace(tokens, width, inner, experts, chosen, type == SDNN_TYPE_BF16);
+    *bytes = (int64_t)sdnn::experts_workspace_upto(tokens, width, inner, experts, chosen, type == SDNN_TYPE_BF16);
     return SDNN_OK;
 }
 

@@ -81,7 +81,9 @@ hipError_t launch_route(const RouteArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_experts(const ExpertsArgs &a, bool bf16, hipStream_t stream);
 size_t route_workspace(int64_t tokens, int32_t experts, int32_t chosen);
+// what a call needs, and what every call of up to so many tokens does
 size_t experts_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen,
                          bool bf16);
+size_t experts_workspace_upto(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen, bool bf16);
 
 }  // namespace sdnn

@@ -289,6 +289,14 @@ size_t experts_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t e
     return experts_plan(tokens, width, inner, experts, chosen, bf16).bytes;
 }
 
+// A call of few slots holds p in fp32, four times the bytes of the codes that a few more slots bring it to.
+size_t experts_workspace_upto(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen, bool bf16) {
+    const int64_t most = experts / chosen;  // tokens of such a call
+    const size_t all = experts_workspace(tokens, width, inner, experts, chosen, bf16),
+                 few = experts_workspace(tokens < most ? tokens : most, width, inner, experts, chosen, bf16);
+    return all > few ? all : few;
+}
+
 hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
     if (a.m == 0 || a.n == 0) return hipSuccess;
     // Few outputs: 16 x 16 of them per workgroup; tiles would leave most CUs empty.  Measured in us (this | tiles):

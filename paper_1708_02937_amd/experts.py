@@ -104,7 +104,7 @@ def experts_forward(a, a_scale, routes: Routes, w_in, w_in_scale, w_out, w_out_s
 
     w_in: codes (experts, 2, inner, pitch of width), gate then up; w_out: codes (experts, width, pitch of inner); both
     with 128-row blocks, as quantize_blocks(w, 128) gives them.  ws: a uint8 tensor of at least
-    sdnn_experts_workspace_size bytes (allocated if absent)."""
+    sdnn_experts_workspace_size bytes (allocated if absent); one of the most tokens' size serves smaller calls."""
     device = a.get_device()
     if device < 0 or device != _current():
         return _elsewhere(experts_forward, device, a, a_scale, routes, w_in, w_in_scale, w_out, w_out_scale, width,

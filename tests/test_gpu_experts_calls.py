@@ -28,3 +28,18 @@ def test_ids_past_the_last_expert_have_none(torch, sd, dtype, T, E):  # noqa: F8
     _say("ids past the last", T, E, dtype)
     want = sd.experts_forward(*args, H, F, dtype=dt)
     assert torch.equal(sd.experts_forward(*args[:2], other, *args[3:], H, F, dtype=dt, ws=ws), want)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_one_workspace_for_calls_of_several_sizes(torch, sd, dtype):  # noqa: F811
+    """A workspace of the size for 9 tokens, which takes other kernels, for 1 to 9: same results as with one made for the
+    call, nothing written past its end."""
+    H, F, E, k = 130, 300, 24, 3
+    dt = getattr(torch, dtype)
+    need = sd.sdnn_experts_workspace_size(9, H, F, E, k, int(dt == torch.bfloat16))
+    room = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")
+    for T in (9, 8, 1, 5):
+        args, _, _ = _experts_case(torch, sd, T, H, F, E, k, 0.0)
+        _say("one workspace", T, dtype)
+        assert torch.equal(sd.experts_forward(*args, H, F, dtype=dt, ws=room[:need]), sd.experts_forward(*args, H, F, dtype=dt))
+    assert bool((room[need:] == 255).all())
