@@ -6,6 +6,7 @@
 //
 // Every function returns its tensors, or the status of the C call where that is not SDNN_OK.
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -32,7 +33,12 @@ void count(Py_ssize_t given, Py_ssize_t wanted) {
 
 const Tensor &tensor(PyObject *o, const char *name) {
     TORCH_CHECK_TYPE(THPVariable_Check(o), name, " must be a tensor");
-    return THPVariable_Unpack(o);
+    const Tensor &t = THPVariable_Unpack(o);
+    // Results know nothing of what they were made from: a gradient would stop here without a word.
+    TORCH_CHECK_VALUE(!(t.requires_grad() && c10::GradMode::is_enabled()) && !t._fw_grad(0).defined(), name,
+                      " requires a gradient, and a layer of experts has none: call it under torch.no_grad(), or detach ",
+                      name);
+    return t;
 }
 
 int64_t integer(PyObject *o) {

@@ -3,7 +3,8 @@ tensors and their outputs allocated.
 
 Codes are ``torch.float8_e4m3fn`` tensors of ``sdnn_blocks_pitch(k)`` columns and scales ``torch.float8_e8m0fnu``
 tensors of ``sdnn_blocks_scale_pitch(k)`` columns.  Work goes to the current stream of the tensors' device; outputs and
-workspaces come from torch's allocator on that stream.  Every function may be called while a graph is captured.
+workspaces come from torch's allocator on that stream.  Every function may be called while a graph is captured.  There
+are no gradients: a tensor that requires one is a ValueError, unless the call is made under torch.no_grad().
 Arguments are checked against each other, and the C calls made, in csrc/tensors.cpp.
 """
 

@@ -43,3 +43,46 @@ def test_one_workspace_for_calls_of_several_sizes(torch, sd, dtype):  # noqa: F8
         _say("one workspace", T, dtype)
         assert torch.equal(sd.experts_forward(*args, H, F, dtype=dt, ws=room[:need]), sd.experts_forward(*args, H, F, dtype=dt))
     assert bool((room[need:] == 255).all())
+
+
+def test_inputs_that_ask_for_gradients_are_refused(torch, sd):  # noqa: F811
+    """The layer has no gradients: an input that requires one is a ValueError while gradients are recorded, and so is one
+    with a tangent; results are not silently cut off from it.  Under no_grad and inference_mode, and detached, the same
+    tensors are ordinary inputs."""
+    x, gamma = torch.randn(6, 200, device="cuda"), torch.ones(200, device="cuda")
+    logits, bias = torch.randn(6, 8, device="cuda"), torch.zeros(8, device="cuda")
+    a, sa = sd.quantize_blocks(x)
+    w, sw = sd.quantize_blocks(torch.randn(70, 200, device="cuda"), 128)
+    routes = sd.route(logits, 2)
+    w_in, s_in = sd.quantize_blocks(torch.randn(8, 2, 40, 200, device="cuda"), 128)
+    w_out, s_out = sd.quantize_blocks(torch.randn(8, 200, 40, device="cuda"), 128)
+    out_bias = torch.zeros(70, device="cuda")
+
+    def experts(weight, residual):
+        return sd.experts_forward(a, sa, routes._replace(weight=weight), w_in, s_in, w_out, s_out, 200, 40,
+                                  residual=residual, dtype=torch.float32)
+
+    calls = [
+        (lambda t: sd.quantize_blocks(t), x), (lambda t: sd.norm_quantize(t, gamma), x),
+        (lambda t: sd.norm_quantize(x, t), gamma), (lambda t: sd.norm_quantize(x, gamma, residual=t), x),
+        (lambda t: sd.norm_quantize(x, gamma, residual=x, out_sum=t), x.clone()), (lambda t: sd.route(t, 2), logits),
+        (lambda t: sd.route(logits, 2, bias=t), bias),
+        (lambda t: sd.product_blocks(a, sa, w, sw, 200, bias=t), out_bias),
+        (lambda t: sd.product_blocks(t, sa, w, sw, 200), a), (lambda t: experts(t, None), routes.weight),
+        (lambda t: experts(routes.weight, t), x),
+    ]
+    for i, (call, t) in enumerate(calls):
+        _say("gradient", i)
+        asks = t.detach().clone().requires_grad_()
+        with pytest.raises(ValueError, match="gradient"):
+            call(asks)
+            pytest.fail(f"case {i} was taken")
+        call(asks.detach())
+        with torch.no_grad():
+            call(asks)
+        with torch.inference_mode():
+            call(asks)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        with pytest.raises(ValueError, match="gradient"):
+            sd.norm_quantize(dual, gamma)
