@@ -405,7 +405,7 @@ sdnn_status sdnn_route_workspace_size(int64_t tokens, int32_t experts, int32_t c
  * equal runs, a run's worth is the sum of its group_best (1 or 2) largest choices, and only the groups_kept
  * worthiest runs stay; of the experts that stay the `chosen` with the largest choice are taken, largest first.
  * Scores and choices are those of fp64 and ties go to the lower index.  A weight is the expert's score, divided by the
- * sum of the chosen scores if normalize is 1, times factor.  An expert whose logit is -inf or NaN, or whose choice is
+ * sum of the chosen scores if normalize is 1 (0 where that sum is 0), times factor.  An expert whose logit is -inf or NaN, or whose choice is
  * -inf or NaN, is never taken; +inf logits share a softmax among themselves.  Places without an expert have id -1 and
  * weight 0, so a row that is masked whole has no expert.
  * Outputs: ids and weight (tokens x chosen); the plan of the experts' products: a slot is t * chosen + j, offsets
@@ -437,8 +437,12 @@ sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t i
  * up-projection's inner x width matrix (2 * experts matrices), w_out each expert's width x inner matrix.
  * ids, weight, offsets and order as sdnn_route writes them; residual (tokens x width, of the type) may be NULL and may
  * be out itself.  With SDNN_TYPE_F32 every product is exact and sums are fp32, the sum over j in the order of j.  With
- * SDNN_TYPE_BF16 o may be rounded to 11 bits before it is weighted (to those of the largest of the 128 or 256 values next
- * to it), and with many rows to an expert both products use the 8-bit instructions as in sdnn_product_blocks.
+ * SDNN_TYPE_BF16 that is so where there are no more slots than experts.  With more, the second product uses the 8-bit
+ * instructions as in sdnn_product_blocks, and o is rounded to 11 bits before it is weighted (to those of the largest of
+ * the 128 values next to it): the result is up to 1.03 times as far from the exact one as its own rounding brings it.
+ * From 32 rows to an expert on, and 400 tiles of 128 rows x 128 inner values, the first product uses them too (and the
+ * run is 256 values): 1.03 to 1.3 times with a residual, 1.17 to 1.55 without.  A caller who wants neither takes
+ * SDNN_TYPE_F32.
  * Entries of offsets and order outside their ranges are brought into them, so no access leaves the arrays, but the
  * result is then undefined.
  * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED, WORKSPACE_TOO_SMALL, DEVICE.

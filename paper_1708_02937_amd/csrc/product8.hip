@@ -304,6 +304,10 @@ hipError_t launch_product(const ProductArgs &a, bool bf16, hipStream_t stream) {
     //                        1 x 8192 (512) 8.0 | 10.4,  8 x 5000 9.8 | 10.2,  16 x 8192 12.3 | 10.5
     //   float, K = 4000:     116 x 271 7.2 | 17.8,  128 x 1000 12.4 | 17.9,  64 x 4000 (1000) 21.8 | 18.1
     //   K = 16000, 116 x 271:  bfloat16 21 | 26,  float 21 | 56
+    //   K = 4096, 1 x 16384 (1024) and 1 x 32000 (2000):  bfloat16 13.9 | 13.5, 26 | 34,  float 13.9 | 19.3, 26 | 39
+    //   K = 4096, 16 x 12000 (750) and 16 x 16384 (1024): bfloat16 16.6 | 12.5, 21 | 15,  float 16.5 | 18.3, 21 | 20
+    //   K = 1024, 1 x 8192 (512) and 1 x 16384 (1024):    bfloat16 6.0 | 5.8, 10.0 | 6.9,  float 5.9 | 7.7, 9.9 | 9.0
+    // Past the bound one row in float, and one row of very many outputs, would still be ahead here, by up to a third.
     const int64_t across = (a.n + 15) / 16, cells = (a.m + 15) / 16 * across;
     if (cells <= (bf16 && a.m > 8 ? 256 : 512)) {
         const dim3 grid((unsigned)across, (unsigned)((a.m + 15) / 16));

@@ -6,8 +6,9 @@
 //   8 bits  (bfloat16 outputs) the scaled 8-bit instructions, which multiply by both blocks' powers of two themselves.
 //           Within an instruction they align products to the largest one and keep about 14 bits, 1.5e-5 of a sum of
 //           normal values (measured), a hundredth of the output's own rounding; between instructions the sum is fp32.
-//   EXACT   (float outputs, and the first of the experts' products for few rows) codes widened to bfloat16 with their
-//           scales, which is exact, and the 16-bit instructions, whose products and sums are fp32.  Half the matrix rate.
+//   EXACT   (float outputs, and the first of the experts' products where tiles are few) codes widened to bfloat16 with
+//           their scales, which is exact, and the 16-bit instructions, whose products and sums are fp32.  Half the matrix
+//           rate.
 #include "product8.h"
 
 namespace sdnn {
@@ -553,8 +554,17 @@ hipError_t tile_go(const ProductArgs &a, const ExpertsArgs &x, TileWork work, in
 //   4096 x 2048       88.9      76.7                   53.6     44.2     46.1
 //   16384 x 1024     208.9     155.0      129.2       115.6     85.7     64.8
 // With float (the 16-bit instructions) four groups are ahead for longer: 4096 x 256 20.4, 22.5 and 31.4, 4096 x 512 on
-// 128 x 64 with four groups 30.1 and with two 32.6; and tiles beyond 128 x 128 do not fit the registers.  Over short rows
-// the chain is short anyway: 777 x 2999 x 1001 on 64 x 64 with one group 11.6 (float 17.2), on 128 x 128 x2 13.6 (19.7).
+// 128 x 64 with four groups 30.1 and with two 32.6; and tiles beyond 128 x 128 do not fit the registers.
+// Over short rows the chain of stages is short anyway, and 64 x 64 with one group comes before 128 x 128 x2.  One bound on K
+// stands for a line that falls as tiles rise, and is higher for float (64x64 | 128x128 x2, by tiles of 64 x 64):
+//   K        576 x 3700 (522)          1024 x 3900 (976)         float: 522              976
+//   1001      9.7 | 11.5                12.9 | 12.0              15.4 | 17.9             18.5 | 18.8
+//   1536     12.8 | 14.0                18.1 | 14.9              21.0 | 23.0             25.5 | 24.1
+//   2048     15.3 | 15.7                21.5 | 16.7              25.8 | 27.8             32.1 | 28.8
+//   2560     19.1 | 19.1                26.7 | 20.1              31.4 | 33.1             39.3 | 34.1
+//   4096     27.5 | 24.6                41.8 | 26.0              46.3 | 47.5             59.2 | 49.0
+// Float above 1024 tiles, 64x64 | 128x128: 1000 x 5000 x 2048 (1264) 41.3 | 44.7, 1024 x 8192 x 2048 (2048) 60.1 | 47.4,
+// 2048 x 16384 x 4096 (8192) 428 | 354.
 template <typename T>
 hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
     constexpr bool kExact = sizeof(T) == 4;
@@ -585,14 +595,16 @@ hipError_t product_go(const ProductArgs &a, TileWork work, hipStream_t s) {
 }
 
 // Tiles of 64 rows with the first product exact; of 128 with the 8-bit instructions for many rows to an expert, where
-// tiles are enough to fill the chip more than once.  Both measured in us (64 rows | 128 rows):
+// tiles are enough to fill the chip more than once.  Both measured in us (64 rows | 128 rows), at sizes on both sides of
+// the bound; the 8-bit instructions are ahead at all of them, so the bound is not where their time begins to pay:
 //   64 experts of 4096 x 1024, 8 chosen:   64 tokens 262 | 225,  333 tokens 312 | 226,  2048 tokens 739 | 429
 //   8 experts of 4096 x 1024, 2 chosen:    128 tokens 69 | 61,   512 tokens 80 | 70,    2048 tokens 216 | 122
 //   24 experts of 2001 x 701, 3 chosen:    333 tokens 51 | 47,   600 tokens 81 | 53,    1000 tokens 89 | 69
 // What the exact product is for: a sum that is 5e-5 off (a column in a hundred ten times as wide as the others) moves some
-// values of p over a boundary of their 8 bits.  Without a residual the result is then 1.3 to 1.5 times as far from the
-// exact one as its own rounding to bfloat16 brings it, with one 1.03 to 1.3 times.  That is paid for the halved time of
-// long calls, not for a few us of short ones.  (The exact product on tiles of 128 rows: 8192 tokens as above 2.2 ms, 1.3.)
+// values of p over a boundary of their 8 bits.  Without a residual the result is then 1.17 to 1.55 times as far from the
+// exact one as its own rounding to bfloat16 brings it, with one 1.03 to 1.3 times; with the exact product up to 1.03.
+// The bound goes by tiles alone, not by what a call saves: 333 tokens on 64 experts lie above it, 2048 on 8 below.  (The
+// exact product on tiles of 128 rows: 8192 tokens as above 2.2 ms, 1.3.)
 template <typename T>
 hipError_t experts_go(const ExpertsArgs &x, TileWork work, int *run, hipStream_t s) {
     constexpr bool kExact = sizeof(T) == 4;

@@ -79,8 +79,8 @@ def norm_quantize(x, gamma, eps: float = 1e-6, residual=None, normed: bool = Fal
 
 def product_blocks(a, a_scale, w, w_scale, k: int, bias=None, ymax=None, dtype=torch.bfloat16, out=None):
     """h(A W^T + bias) of blocked 8-bit A (m x k) and W (n x k); h clamps to [0, ymax], None leaves values as they
-    are.  dtype float32 keeps every product exact; bfloat16 takes the 8-bit matrix instructions for more than a few
-    rows."""
+    are.  dtype float32 keeps every product exact; bfloat16 does for few outputs (up to 256 tiles of 16 x 16, 512
+    with up to 8 rows) and takes the 8-bit matrix instructions for more."""
     device = a.get_device()
     if device < 0 or device != _current():
         return _elsewhere(product_blocks, device, a, a_scale, w, w_scale, k, bias, ymax, dtype, out)
@@ -102,6 +102,9 @@ def route(logits, k: int, score: str = "softmax", bias=None, groups: int = 1, gr
 def experts_forward(a, a_scale, routes: Routes, w_in, w_in_scale, w_out, w_out_scale, width: int, inner: int,
                     residual=None, dtype=torch.bfloat16, out=None, ws=None):
     """residual + the weighted sum of each token's experts (gated by SiLU) on its blocked 8-bit row of A.
+
+    dtype float32 keeps every product exact; bfloat16 does for up to as many slots as experts, then takes the 8-bit matrix
+    instructions for the second product, and with many rows to an expert for both (see sdnn_experts_forward).
 
     w_in: codes (experts, 2, inner, pitch of width), gate then up; w_out: codes (experts, width, pitch of inner); both
     with 128-row blocks, as quantize_blocks(w, 128) gives them.  ws: a uint8 tensor of at least

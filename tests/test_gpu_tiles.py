@@ -15,7 +15,7 @@ Tolerances, fixed before any run:
     1.7e-3, both as 2-norms and independent: 1.0001 times the rounding alone, and 1.01 for chance.
   * experts, bfloat16, first product exact: rows held at 11 bits until they are summed, 1.4e-4, and the second product's
     1.5e-5, beside the rounding: 1.004 times it, and 1.03 for chance.  With both products on the 8-bit instructions some
-    codes of p move over a boundary: 1.3 to 1.55 times the rounding without a residual over many calls, 1.03 to 1.31 with
+    codes of p move over a boundary: 1.17 to 1.55 times the rounding without a residual over many calls, 1.03 to 1.31 with
     one; 1.7 and 1.45.
   * experts, float: p is about 1e-6 off, which moves about 3e-5 of its codes by a step of 0.09: 5e-4 in the 2-norm; 1e-3.
 """
