@@ -367,11 +367,21 @@ __device__ __forceinline__ void route_tokens(const RouteArgs &a, int64_t token0,
         if (j > 0) {
             if constexpr (BIAS) {
                 sure = sure && apart(last, best);
-            } else if (last > best && best > -INFINITY) {
-                // different logits, and scores that differ in 64 bits too: by 2e-15 of the larger one or more
-                const float gap = last - best;
-                const float slope = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(last)) : 1.0f;  // of log(score)
-                sure = sure && slope * gap > 2e-15f && (a.sigmoid ? best > -700.0f : best - top > -700.0f);
+            } else {
+                // What comes next has a different logit and a score that differs in 64 bits too, by 2e-15 of the larger one
+                // or more; after the last choice that is the next lower logit, past those equal to the last one.
+                float next = best;
+                if (j == a.chosen && best == last) {
+                    next = -INFINITY;
+#pragma unroll
+                    for (int r = 0; r < R; r++) next = fmaxf(next, key[r] < last ? key[r] : -INFINITY);
+                    next = lanes_max<LANES>(next);
+                }
+                if (last > next && next > -INFINITY) {
+                    const float gap = last - next;
+                    const float slope = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(last)) : 1.0f;  // of log(score)
+                    sure = sure && slope * gap > 2e-15f && (a.sigmoid ? next > -700.0f : next - top > -700.0f);
+                }
             }
         }
         if (j == a.chosen || !(best > -INFINITY)) break;  // a token's lanes leave together

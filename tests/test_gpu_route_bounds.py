@@ -70,6 +70,28 @@ def test_groups_raised_by_a_bias_of_the_largest_value(torch, sd, high):  # noqa:
                                  best, True, 1.0)
 
 
+@pytest.mark.parametrize("T", [4, 70])
+@pytest.mark.parametrize("E,groups", [(12, 1), (88, 1), (88, 4), (300, 1), (700, 2)])
+def test_equal_logits_beside_others_of_the_same_score(torch, sd, E, groups, T):  # noqa: F811
+    """More experts with the largest logit than places, and lower logits whose 64-bit scores are the same: the lowest
+    experts of all of these are taken, not those of the larger logit."""
+    rng = np.random.default_rng(E + T)
+    for score, low, high in (("sigmoid", 50.0, np.nextafter(np.float32(50), np.float32(60))), ("sigmoid", 40.0, 300.0),
+                             ("sigmoid", -5000.0, -2000.0), ("softmax", -5000.0, -2000.0), ("softmax", 1e-30, 2e-30)):
+        l = np.full((T, E), low, np.float32)
+        for t in range(T):
+            l[t, rng.permutation(E)[:E // 3]] = high
+        if score == "softmax" and low < 0:
+            l[:, E // 2] = 1.0
+        l[1::3, 2] = -np.inf
+        l[2::3, 1] = low - abs(low) / 2  # lower still: of another score, or of the same one too
+        for k in (1, 2, E // 3 - 1, E // 3):
+            _say("equal logits", score, low, E, groups, T, k)
+            with np.errstate(over="ignore", invalid="ignore"):
+                _check_route(torch, sd, l.astype(np.float64), torch.float32, min(k, 64, E // groups), score, None, groups, 1, 1,
+                             True, 1.0)
+
+
 def test_more_tokens_than_one_launch_holds(torch, sd):  # noqa: F811
     """2^28 tokens and a few, at 16 lanes each: 2^32 threads and more.  Two experts, so that the definition is one
     comparison and one exponential for a token."""
