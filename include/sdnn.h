@@ -439,10 +439,10 @@ sdnn_status sdnn_experts_workspace_size(int64_t tokens, int64_t width, int64_t i
  * be out itself.  With SDNN_TYPE_F32 every product is exact and sums are fp32, the sum over j in the order of j.  With
  * SDNN_TYPE_BF16 that is so where there are no more slots than experts.  With more, the second product uses the 8-bit
  * instructions as in sdnn_product_blocks, and o is rounded to 11 bits before it is weighted (to those of the largest of
- * the 128 values next to it): the result is up to 1.03 times as far from the exact one as its own rounding brings it.
- * From 32 rows to an expert on, and 400 tiles of 128 rows x 128 inner values, the first product uses them too (and the
- * run is 256 values): 1.03 to 1.3 times with a residual, 1.17 to 1.55 without.  A caller who wants neither takes
- * SDNN_TYPE_F32.
+ * the 128 values next to it): over a whole result of many values the error is up to 1.03 times that of its rounding to
+ * bfloat16 (measured).  From 32 rows to an expert on, and 400 tiles of 128 rows x 128 inner values, the first product
+ * uses them too (and the run is 256 values): 1.03 to 1.3 times with a residual, 1.17 to 1.55 without.  A caller who wants
+ * neither takes SDNN_TYPE_F32.
  * Entries of offsets and order outside their ranges are brought into them, so no access leaves the arrays, but the
  * result is then undefined.
  * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED, WORKSPACE_TOO_SMALL, DEVICE.
