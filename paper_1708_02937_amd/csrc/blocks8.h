@@ -69,7 +69,8 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// A double as a float with round to odd: any later rounding to 22 bits or fewer is then the rounding of the double.
+// A double as a float with round to odd: any later rounding to 22 bits or fewer is then the rounding of the double.  (Below
+// 2^-126 the float is subnormal and rounded to nearest itself, a 2^14th of the last place that 8 bits have there.)
 __device__ __forceinline__ float round_odd(double z) {
     const uint64_t b = __double_as_longlong(z);
     uint32_t lo = (uint32_t)b;
