@@ -454,6 +454,57 @@ sdnn_status sdnn_experts_forward(int64_t tokens, int64_t width, int64_t inner, i
                                  int32_t type, const void *residual, int64_t ldr, void *out, int64_t ldo, void *ws,
                                  int64_t ws_bytes, void *stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------------
+ * Generating tokens: products with 4-bit weights, a layer of experts for a few tokens, and the next token.
+ *
+ * What is said above of the calls of a layer of experts holds for these: they belong to no net, work on the current
+ * device and the caller's stream, allocate nothing, never synchronise and may be recorded into a HIP graph.
+ *
+ * A 4-bit matrix of `rows` x k is a pair of device arrays:
+ *   codes   uint8, rows x sdnn_groups_pitch(k) (half of k rounded up to a multiple of 128), two e2m1 codes to a byte, the
+ *           lower column in the lower four bits.  Codes 0 to 7 are 0, 0.5, 1, 1.5, 2, 3, 4, 6, and 8 to 15 their
+ *           negatives; zeros from column k on;
+ *   scales  uint8, rows x sdnn_groups_scale_pitch(k) (a 32nd of k rounded up to a multiple of 128), code c (0 to 254)
+ *           standing for 2^(c - 127) and 255 for NaN.
+ * Element (r, i) is the value of its code times the scale scales[r][i / 32]; one past the float range is infinite.  Codes
+ * are 16-byte aligned, scales 4-byte aligned.  The zeros from column k on are read as operands, and so are their groups'
+ * scales: the quantizing call writes zeros with the scale of an empty group (code 1), and a caller who fills the arrays
+ * otherwise has to write zeros and a scale that is no NaN.
+ */
+
+/* Bytes of one row of codes, and of one row of scales, of a 4-bit matrix of k columns (0 if k is out of range). */
+int64_t sdnn_groups_pitch(int64_t k);
+int64_t sdnn_groups_scale_pitch(int64_t k);
+
+/*
+ * Round rows x k values to a 4-bit matrix.  A group's scale is the least power of two, 2^-126 at least, that brings its
+ * largest magnitude to 6 or less; codes are rounded to nearest even.  The type has no infinity and no NaN: a group that
+ * holds one is NaN as a whole (scale 255, codes 0).
+ * Errors: NULL_POINTER, INVALID_VALUE, DEVICE.
+ */
+sdnn_status sdnn_quantize_groups(int64_t rows, int64_t k, int32_t type, const void *x, int64_t ldx, uint8_t *codes,
+                                 uint8_t *scales, void *stream);
+
+/*
+ * The values of a 4-bit matrix as rows x k values of the type, which holds each of them exactly.
+ * Errors: NULL_POINTER, INVALID_VALUE, DEVICE.
+ */
+sdnn_status sdnn_widen_groups(int64_t rows, int64_t k, const uint8_t *codes, const uint8_t *scales, int32_t type,
+                              void *y, int64_t ldy, void *stream);
+
+/*
+ * Y = h(X W^T + bias) for dense X (m x k) and 4-bit W (n x k: row j holds output j's weights): Y (m x n).  X and Y have
+ * types of their own.  bias: n fp32 values or NULL.  activate 0: h is the identity; 1: h(z) = min(max(z, 0), ymax),
+ * ymax > 0 (+INFINITY for plain ReLU; NaN stays NaN).  Every product is exact (but for what a
+ * float of X has below 2^-133), sums are fp32 and rounded once, and their order goes by m, n and k alone.  Made for few rows: the weights are read once for each 64 rows, and with up to that
+ * many they are what a call costs.
+ * Errors: NULL_POINTER, INVALID_VALUE, DEVICE.
+ */
+sdnn_status sdnn_product_groups(int64_t m, int64_t n, int64_t k, int32_t x_type, const void *x, int64_t ldx,
+                                const uint8_t *w, const uint8_t *w_scale, const float *bias, int32_t activate,
+                                float ymax, int32_t y_type, void *y, int64_t ldy, void *stream);
+
 /* Static text for a status code. */
 const char *sdnn_status_string(sdnn_status status);
 

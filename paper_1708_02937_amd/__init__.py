@@ -3,8 +3,8 @@
 The functions below carry the C names and only marshal arguments: every step of the
 forward pass runs in the library's HIP kernels.  PyTorch supplies device memory and
 the stream.  Importing this package fails if libsdnn.so has not been built
-(``python paper_1708_02937_amd/build.py``); there is no fallback.  The layer of experts also has calls on torch
-tensors (experts.py over _tensors.so, built beside the library).
+(``python paper_1708_02937_amd/build.py``); there is no fallback.  The layer of experts and what generates
+tokens with it also have calls on torch tensors (experts.py and generate.py over _tensors.so, built beside the library).
 
 The paper computes Y_{k+1} = h(W_k Y_k + B_k) with ReLU h (Kepner et al.,
 arXiv:1708.02937, Sec. III) via the GraphBLAS loop of Fig. 4 (Sec. IV); here the
@@ -88,6 +88,9 @@ _sig = {
     "sdnn_quantize_blocks": [_I64, _I64, _I64, _I32, _I32, _P, _I64, _P, _P, _P],
     "sdnn_norm_quantize": [_I64, _I64, _I32, _P, _I64, _P, _I64, _P, _c.c_float, _P, _I64, _P, _I64, _P, _P, _P],
     "sdnn_product_blocks": [_I64, _I64, _I64, _P, _P, _P, _P, _P, _I32, _c.c_float, _I32, _P, _I64, _P],
+    "sdnn_quantize_groups": [_I64, _I64, _I32, _P, _I64, _P, _P, _P],
+    "sdnn_widen_groups": [_I64, _I64, _P, _P, _I32, _P, _I64, _P],
+    "sdnn_product_groups": [_I64, _I64, _I64, _I32, _P, _I64, _P, _P, _P, _I32, _c.c_float, _I32, _P, _I64, _P],
     "sdnn_route_workspace_size": [_I64, _I32, _I32, _c.POINTER(_I64)],
     "sdnn_route": [_I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _I32, _I32, _I32, _I32, _c.c_float, _P, _P, _P, _P,
                    _P, _I64, _P],
@@ -109,7 +112,7 @@ lib.sdnn_net_read_profile.argtypes = lib_read_profile_args
 lib.sdnn_net_read_profile.restype = _c.c_int
 lib.sdnn_noalloc_scratch_bytes.argtypes = []
 lib.sdnn_noalloc_scratch_bytes.restype = _I64
-for _name in ("sdnn_blocks_pitch", "sdnn_blocks_scale_pitch"):
+for _name in ("sdnn_blocks_pitch", "sdnn_blocks_scale_pitch", "sdnn_groups_pitch", "sdnn_groups_scale_pitch"):
     getattr(lib, _name).argtypes = [_I64]
     getattr(lib, _name).restype = _I64
 lib.sdnn_status_string.argtypes = [_c.c_int]
@@ -280,6 +283,28 @@ def sdnn_experts_forward(tokens: int, width: int, inner: int, experts: int, chos
                                     _ptr(weight), _ptr(offsets), _ptr(order), _ptr(w_in), _ptr(w_in_scale),
                                     _ptr(w_out), _ptr(w_out_scale), type, _ptr(residual), ldr, _ptr(out), ldo,
                                     _ptr(ws), ws_bytes, _ptr(stream)))
+
+
+def sdnn_groups_pitch(k: int) -> int:
+    return lib.sdnn_groups_pitch(k)
+
+
+def sdnn_groups_scale_pitch(k: int) -> int:
+    return lib.sdnn_groups_scale_pitch(k)
+
+
+def sdnn_quantize_groups(rows: int, k: int, type: int, x, ldx: int, codes, scales, stream=None):
+    _check(lib.sdnn_quantize_groups(rows, k, type, _ptr(x), ldx, _ptr(codes), _ptr(scales), _ptr(stream)))
+
+
+def sdnn_widen_groups(rows: int, k: int, codes, scales, type: int, y, ldy: int, stream=None):
+    _check(lib.sdnn_widen_groups(rows, k, _ptr(codes), _ptr(scales), type, _ptr(y), ldy, _ptr(stream)))
+
+
+def sdnn_product_groups(m: int, n: int, k: int, x_type: int, x, ldx: int, w, w_scale, bias, activate: int, ymax: float,
+                        y_type: int, y, ldy: int, stream=None):
+    _check(lib.sdnn_product_groups(m, n, k, x_type, _ptr(x), ldx, _ptr(w), _ptr(w_scale), _ptr(bias), activate, ymax,
+                                   y_type, _ptr(y), ldy, _ptr(stream)))
 
 
 class Net:
@@ -456,14 +481,21 @@ def net_from_problem(problem, device: str = "cuda:0", dense=0, bias_mode: int = 
 
 
 _EXPERTS = ("Routes", "experts_forward", "norm_quantize", "product_blocks", "quantize_blocks", "route")
+_GENERATE = ("product_groups", "quantize_groups", "widen_groups")
 
 
 def __getattr__(name):
-    """The layer of experts on torch tensors, imported with torch when first used."""
+    """The calls on torch tensors, imported with torch when first used."""
     if name in _EXPERTS:
         from . import experts
 
         for n in _EXPERTS:
             globals()[n] = getattr(experts, n)
+        return globals()[name]
+    if name in _GENERATE:
+        from . import generate
+
+        for n in _GENERATE:
+            globals()[n] = getattr(generate, n)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,4 +1,4 @@
-// Host side of the operators on 8-bit operands: argument checks of the C ABI, then the launchers of operators.h.
+// Host side of the operators on 8-bit and 4-bit operands: argument checks of the C ABI, then the launchers of operators.h.
 // These calls hold no state: the device is the one current on the calling thread, the stream the caller's.
 #include "operators.h"
 
@@ -110,6 +110,61 @@ sdnn_status sdnn_product_blocks(int64_t m, int64_t n, int64_t k, const uint8_t *
     const hipError_t e = sdnn::launch_product(p, type == SDNN_TYPE_BF16, (hipStream_t)stream);
     if (e == hipErrorInvalidConfiguration) return fail(SDNN_ERR_UNSUPPORTED, "more tiles than one launch holds");
     return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_product_blocks");
+}
+
+int64_t sdnn_groups_pitch(int64_t k) { return k < 1 || k >= kMaxSide ? 0 : sdnn::group_pitch(k); }
+
+int64_t sdnn_groups_scale_pitch(int64_t k) { return k < 1 || k >= kMaxSide ? 0 : sdnn::group_scale_pitch(k); }
+
+// The arguments that a 4-bit matrix and a dense one of its shape share.
+static sdnn_status check_groups(int64_t rows, int64_t k, int32_t type, const void *x, int64_t ldx, const uint8_t *codes,
+                                const uint8_t *scales) {
+    if (!side(rows, 0) || !side(k, 1)) return fail(SDNN_ERR_INVALID_VALUE, "rows or k out of range");
+    if (!known_type(type)) return fail(SDNN_ERR_INVALID_VALUE, "unknown element type");
+    if (rows == 0) return SDNN_OK;
+    if (!x) return fail(SDNN_ERR_NULL_POINTER, "the dense matrix is NULL");
+    SDNN_CHECK(check_codes(codes, scales, "4-bit matrix"));
+    if (bad_dense(x, type, ldx, k))
+        return fail(SDNN_ERR_INVALID_VALUE, "the dense matrix is misaligned or its row stride below k");
+    return SDNN_OK;
+}
+
+sdnn_status sdnn_quantize_groups(int64_t rows, int64_t k, int32_t type, const void *x, int64_t ldx, uint8_t *codes,
+                                 uint8_t *scales, void *stream) {
+    sdnn::set_error(SDNN_OK, "");
+    SDNN_CHECK(check_groups(rows, k, type, x, ldx, codes, scales));
+    const sdnn::GroupsArgs a{rows, k, const_cast<void *>(x), ldx, codes, scales};
+    const hipError_t e = sdnn::launch_quantize_groups(a, type == SDNN_TYPE_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_quantize_groups");
+}
+
+sdnn_status sdnn_widen_groups(int64_t rows, int64_t k, const uint8_t *codes, const uint8_t *scales, int32_t type, void *y,
+                              int64_t ldy, void *stream) {
+    sdnn::set_error(SDNN_OK, "");
+    SDNN_CHECK(check_groups(rows, k, type, y, ldy, codes, scales));
+    const sdnn::GroupsArgs a{rows, k, y, ldy, const_cast<uint8_t *>(codes), const_cast<uint8_t *>(scales)};
+    const hipError_t e = sdnn::launch_widen_groups(a, type == SDNN_TYPE_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_widen_groups");
+}
+
+sdnn_status sdnn_product_groups(int64_t m, int64_t n, int64_t k, int32_t x_type, const void *x, int64_t ldx,
+                                const uint8_t *w, const uint8_t *w_scale, const float *bias, int32_t activate,
+                                float ymax, int32_t y_type, void *y, int64_t ldy, void *stream) {
+    sdnn::set_error(SDNN_OK, "");
+    if (!side(m, 0) || !side(n, 0) || !side(k, 1)) return fail(SDNN_ERR_INVALID_VALUE, "m, n or k out of range");
+    if (!known_type(x_type) || !known_type(y_type)) return fail(SDNN_ERR_INVALID_VALUE, "unknown element type");
+    if (activate != 0 && activate != 1) return fail(SDNN_ERR_INVALID_VALUE, "activate must be 0 or 1");
+    if (activate && !(ymax > 0.0f)) return fail(SDNN_ERR_INVALID_VALUE, "ymax must be > 0");
+    if (m == 0 || n == 0) return SDNN_OK;
+    if (!x || !y) return fail(SDNN_ERR_NULL_POINTER, "x or y is NULL");
+    SDNN_CHECK(check_codes(w, w_scale, "w"));
+    if (bad_dense(x, x_type, ldx, k)) return fail(SDNN_ERR_INVALID_VALUE, "x is misaligned or its row stride below k");
+    if (bad_dense(y, y_type, ldy, n) || misaligned(bias, 4))
+        return fail(SDNN_ERR_INVALID_VALUE, "y or bias is misaligned or y's row stride below n");
+    const sdnn::GroupProductArgs p{m, n, k, x, ldx, w, w_scale, bias, activate != 0, ymax, y, ldy};
+    const hipError_t e =
+        sdnn::launch_product_groups(p, x_type == SDNN_TYPE_BF16, y_type == SDNN_TYPE_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_product_groups");
 }
 
 static sdnn_status check_routes(int64_t tokens, int32_t experts, int32_t chosen) {

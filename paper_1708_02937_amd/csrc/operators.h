@@ -1,5 +1,6 @@
 // Launchers of the operators on 8-bit operands (the norm, the router, the block-scaled product and the experts'
-// products) and the sizes they share with the host checks.
+// products) and of those that generate tokens (products with 4-bit weights, the experts' layer of a few tokens, the next
+// token), and the sizes they share with the host checks.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -13,9 +14,14 @@ constexpr int kRouteMaxExperts = 1024;  // 16 scores per lane of a wave
 constexpr int kRouteMaxChosen = 64;     // one chosen expert per lane
 constexpr int kRouteMaxGroups = 64;
 
+constexpr int kGroup = 32;              // columns of a 4-bit matrix that share a scale
+
 constexpr int64_t blocks_of(int64_t k) { return (k + kBlock - 1) / kBlock; }
 constexpr int64_t code_pitch(int64_t k) { return blocks_of(k) * kBlock; }
 constexpr int64_t scale_pitch(int64_t k) { return (blocks_of(k) + 3) / 4 * 4; }
+// bytes of a row of a 4-bit matrix: rows are padded to 128 columns, so that they start at multiples of 16 bytes
+constexpr int64_t group_pitch(int64_t k) { return blocks_of(k) * (kBlock / 2); }
+constexpr int64_t group_scale_pitch(int64_t k) { return blocks_of(k) * (kBlock / kGroup); }
 
 struct NormArgs {
     int64_t rows, k;
@@ -74,7 +80,29 @@ struct ExpertsArgs {
     void *ws;
 };
 
+struct GroupsArgs {  // dense rows and 4-bit ones, in either direction
+    int64_t rows, k;
+    void *x;
+    int64_t ld;
+    uint8_t *codes, *scales;
+};
+
+struct GroupProductArgs {
+    int64_t m, n, k;
+    const void *x;
+    int64_t ldx;
+    const uint8_t *w, *w_scale;
+    const float *bias;  // may be null
+    bool activate;
+    float ymax;
+    void *y;
+    int64_t ldy;
+};
+
 // bf16: the dense tensors are bfloat16, otherwise float
+hipError_t launch_quantize_groups(const GroupsArgs &a, bool bf16, hipStream_t stream);
+hipError_t launch_widen_groups(const GroupsArgs &a, bool bf16, hipStream_t stream);
+hipError_t launch_product_groups(const GroupProductArgs &a, bool x_bf16, bool y_bf16, hipStream_t stream);
 hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_quantize(const QuantizeArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_route(const RouteArgs &a, bool bf16, hipStream_t stream);

@@ -1,5 +1,5 @@
-// The layer of experts on torch tensors: shapes and addresses are read from the tensors, outputs and workspaces come
-// from torch's allocator on the stream given, and the C entry is called.  The Python functions of experts.py choose
+// The layer of experts, and what generates tokens with it, on torch tensors: shapes and addresses are read from the tensors, outputs and workspaces come
+// from torch's allocator on the stream given, and the C entry is called.  The Python functions of experts.py and generate.py choose
 // device and stream and hand their arguments over in order.  A small call's time is spent on the host: one token of 4096
 // columns through the norm, whose kernel takes 3.1 us, is 7.4 us a call, 11.4 with the same steps in Python (four
 // tensors of torch's at about 0.9 us, the launch 2.5).
@@ -20,7 +20,8 @@ namespace {
 using at::ScalarType;
 using at::Tensor;
 
-constexpr ScalarType kCodes = ScalarType::Float8_e4m3fn, kScales = ScalarType::Float8_e8m0fnu;
+constexpr ScalarType kCodes = ScalarType::Float8_e4m3fn, kScales = ScalarType::Float8_e8m0fnu,
+                     kPairs = ScalarType::Float4_e2m1fn_x2;
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t pitch_of(int64_t k) { return up(k, 128) * 128; }
@@ -36,7 +37,7 @@ const Tensor &tensor(PyObject *o, const char *name) {
     const Tensor &t = THPVariable_Unpack(o);
     // Results know nothing of what they were made from: a gradient would stop here without a word.
     TORCH_CHECK_VALUE(!(t.requires_grad() && c10::GradMode::is_enabled()) && !t._fw_grad(0).defined(), name,
-                      " requires a gradient, and a layer of experts has none: call it under torch.no_grad(), or detach ",
+                      " requires a gradient, and this call has none: call it under torch.no_grad(), or detach ",
                       name);
     return t;
 }
@@ -323,9 +324,94 @@ PyObject *experts_forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// x, stream -> codes, scales
+PyObject *quantize_groups(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count(n, 2);
+    const Tensor &x = tensor(args[0], "x");
+    void *const stream = stream_of(args[1]);
+    TORCH_CHECK_VALUE(x.dim() >= 2, "x must be (..., rows, k)");
+    const int32_t kind = kind_of(x, "x");
+    const int64_t k = x.size(-1);
+    TORCH_CHECK_VALUE(x.dim() == 2 || x.is_contiguous(), "x of more than two dimensions must be contiguous");
+    int64_t rows = 1;
+    for (int64_t i = 0; i + 1 < x.dim(); i++) rows *= x.size(i);
+    const int64_t ldx = x.dim() == 2 ? dense(x, "x", x.scalar_type(), x.device(), rows, k) : k;
+    std::vector<int64_t> shape = x.sizes().vec();
+    shape.back() = sdnn_groups_pitch(k);
+    const Tensor codes = empty(shape, kPairs, x.device());
+    shape.back() = sdnn_groups_scale_pitch(k);
+    const Tensor scales = empty(shape, kScales, x.device());
+    sdnn_status s;
+    {
+        Unlocked u;
+        s = sdnn_quantize_groups(rows, k, kind, x.data_ptr(), ldx, (uint8_t *)codes.data_ptr(),
+                                 (uint8_t *)scales.data_ptr(), stream);
+    }
+    return s ? PyLong_FromLong(s) : tuple_of(codes, scales);
+    END_HANDLE_TH_ERRORS
+}
+
+// codes, scales, k, kind, stream -> y
+PyObject *widen_groups(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count(n, 5);
+    const Tensor &codes = tensor(args[0], "codes");
+    const int64_t k = integer(args[2]), kind = integer(args[3]);
+    void *const stream = stream_of(args[4]);
+    TORCH_CHECK_VALUE(codes.dim() >= 2, "codes must be (..., rows, pitch)");
+    std::vector<int64_t> shape = codes.sizes().vec();
+    int64_t rows = 1;
+    for (int64_t i = 0; i + 1 < codes.dim(); i++) rows *= codes.size(i);
+    shape.back() = sdnn_groups_pitch(k);
+    const uint8_t *pc = packed<uint8_t>(codes, "codes", kPairs, codes.device(), shape);
+    shape.back() = sdnn_groups_scale_pitch(k);
+    const uint8_t *ps = packed<uint8_t>(args[1], "scales", kScales, codes.device(), shape);
+    shape.back() = k;
+    const Tensor y = empty(shape, scalar_of(kind), codes.device());
+    sdnn_status s;
+    {
+        Unlocked u;
+        s = sdnn_widen_groups(rows, k, pc, ps, (int32_t)kind, y.data_ptr(), k, stream);
+    }
+    return s ? PyLong_FromLong(s) : wrapped(y);
+    END_HANDLE_TH_ERRORS
+}
+
+// x, w, w_scale, bias, ymax, kind (or None: x's), out, stream -> y
+PyObject *product_groups(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count(n, 8);
+    const Tensor &x = tensor(args[0], "x"), &w = tensor(args[1], "w");
+    const bool clamp = args[4] != Py_None;
+    const float ymax = clamp ? (float)real(args[4]) : 0.0f;
+    void *const stream = stream_of(args[7]);
+    TORCH_CHECK_VALUE(x.dim() == 2 && w.dim() == 2, "x and w must be matrices");
+    const int32_t x_kind = kind_of(x, "x"), kind = args[5] == Py_None ? x_kind : (int32_t)integer(args[5]);
+    const int64_t rows = x.size(0), k = x.size(1), cols = w.size(0);
+    const at::Device device = x.device();
+    const ScalarType type = scalar_of(kind);
+    const int64_t ldx = dense(x, "x", x.scalar_type(), device, rows, k);
+    const uint8_t *pw = packed<uint8_t>(w, "w", kPairs, device, {cols, sdnn_groups_pitch(k)});
+    const uint8_t *psw = packed<uint8_t>(args[2], "w_scale", kScales, device, {cols, sdnn_groups_scale_pitch(k)});
+    const float *bias =
+        args[3] == Py_None ? nullptr : packed<float>(args[3], "bias", ScalarType::Float, device, {cols});
+    const Tensor y = args[6] == Py_None ? empty({rows, cols}, type, device) : tensor(args[6], "out");
+    const int64_t ldy = args[6] == Py_None ? cols : dense(y, "out", type, device, rows, cols);
+    sdnn_status s;
+    {
+        Unlocked u;
+        s = sdnn_product_groups(rows, cols, k, x_kind, x.data_ptr(), ldx, pw, psw, bias, clamp, ymax, kind, y.data_ptr(),
+                                ldy, stream);
+    }
+    return s ? PyLong_FromLong(s) : wrapped(y);
+    END_HANDLE_TH_ERRORS
+}
+
 #define SDNN_CALL(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDNN_CALL(quantize_blocks), SDNN_CALL(norm_quantize),   SDNN_CALL(product_blocks),
-                         SDNN_CALL(route),           SDNN_CALL(experts_forward), {nullptr, nullptr, 0, nullptr}};
+                         SDNN_CALL(route),           SDNN_CALL(experts_forward), SDNN_CALL(quantize_groups),
+                         SDNN_CALL(widen_groups),    SDNN_CALL(product_groups),  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
