@@ -505,6 +505,36 @@ sdnn_status sdnn_product_groups(int64_t m, int64_t n, int64_t k, int32_t x_type,
                                 const uint8_t *w, const uint8_t *w_scale, const float *bias, int32_t activate,
                                 float ymax, int32_t y_type, void *y, int64_t ldy, void *stream);
 
+/*
+ * Bytes of device workspace sdnn_experts_layer needs for any call of up to `tokens` tokens.
+ * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED (more than 16 tokens).
+ */
+sdnn_status sdnn_experts_layer_workspace_size(int64_t tokens, int64_t width, int64_t inner, int32_t experts,
+                                              int32_t chosen, int64_t *bytes);
+
+/*
+ * A whole layer of experts for up to 16 tokens (more take the separate calls above, which compute the same):
+ *   s = x + residual (s = x where residual is NULL),  z = s / sqrt(mean(s^2) + eps) * gamma  over each row of width columns
+ *   logits(t, e) = z_t . router_e  (router: experts x width, of router_type, row stride ldw)
+ *   ids, weight = the choice of sdnn_route from these logits, with its score, bias, groups, normalize and factor
+ *   out_t = s_t + sum_j weight(t, j) o(t, j),  o as in sdnn_experts_forward from q(z), the blocked 8-bit rows of
+ *           sdnn_norm_quantize, and the same weights w_in and w_out
+ * s, the mean, z, the logits and the choice are carried in fp64; the experts' products are exact and their sums fp32; out (of
+ * x's type, which may be x or residual itself) is rounded once.  Sums have one order for given sizes and choices.  live
+ * (a byte for each token, or NULL): a token whose byte is 0 takes part in no expert: ids -1, weights 0, out_t = s_t; so
+ * does one whose logits are all -inf or NaN.  ids and weight (tokens x chosen) are written as sdnn_route writes them.
+ * tokens <= 16, experts <= 1024, chosen <= 64, groups <= 64, width below 2^27.
+ * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED, WORKSPACE_TOO_SMALL, DEVICE.
+ */
+sdnn_status sdnn_experts_layer(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen,
+                               int32_t type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                               const float *gamma, float eps, const uint8_t *live, int32_t router_type,
+                               const void *router, int64_t ldw, int32_t score, const float *bias, int32_t groups,
+                               int32_t groups_kept, int32_t group_best, int32_t normalize, float factor,
+                               const uint8_t *w_in, const uint8_t *w_in_scale, const uint8_t *w_out,
+                               const uint8_t *w_out_scale, void *out, int64_t ldo, int32_t *ids, float *weight, void *ws,
+                               int64_t ws_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *sdnn_status_string(sdnn_status status);
 

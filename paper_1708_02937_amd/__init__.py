@@ -91,6 +91,9 @@ _sig = {
     "sdnn_quantize_groups": [_I64, _I64, _I32, _P, _I64, _P, _P, _P],
     "sdnn_widen_groups": [_I64, _I64, _P, _P, _I32, _P, _I64, _P],
     "sdnn_product_groups": [_I64, _I64, _I64, _I32, _P, _I64, _P, _P, _P, _I32, _c.c_float, _I32, _P, _I64, _P],
+    "sdnn_experts_layer_workspace_size": [_I64, _I64, _I64, _I32, _I32, _c.POINTER(_I64)],
+    "sdnn_experts_layer": [_I64, _I64, _I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _c.c_float, _P, _I32, _P, _I64,
+                           _I32, _P, _I32, _I32, _I32, _I32, _c.c_float, _P, _P, _P, _P, _P, _I64, _P, _P, _P, _I64, _P],
     "sdnn_route_workspace_size": [_I64, _I32, _I32, _c.POINTER(_I64)],
     "sdnn_route": [_I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _I32, _I32, _I32, _I32, _c.c_float, _P, _P, _P, _P,
                    _P, _I64, _P],
@@ -307,6 +310,23 @@ def sdnn_product_groups(m: int, n: int, k: int, x_type: int, x, ldx: int, w, w_s
                                    y_type, _ptr(y), ldy, _ptr(stream)))
 
 
+def sdnn_experts_layer_workspace_size(tokens: int, width: int, inner: int, experts: int, chosen: int) -> int:
+    out = _I64()
+    _check(lib.sdnn_experts_layer_workspace_size(tokens, width, inner, experts, chosen, _c.byref(out)))
+    return out.value
+
+
+def sdnn_experts_layer(tokens: int, width: int, inner: int, experts: int, chosen: int, type: int, x, ldx: int, residual,
+                       ldr: int, gamma, eps: float, live, router_type: int, router, ldw: int, score: int, bias,
+                       groups: int, groups_kept: int, group_best: int, normalize: int, factor: float, w_in, w_in_scale,
+                       w_out, w_out_scale, out, ldo: int, ids, weight, ws, ws_bytes: int, stream=None):
+    _check(lib.sdnn_experts_layer(tokens, width, inner, experts, chosen, type, _ptr(x), ldx, _ptr(residual), ldr,
+                                  _ptr(gamma), eps, _ptr(live), router_type, _ptr(router), ldw, score, _ptr(bias), groups,
+                                  groups_kept, group_best, normalize, factor, _ptr(w_in), _ptr(w_in_scale),
+                                  _ptr(w_out), _ptr(w_out_scale), _ptr(out), ldo, _ptr(ids), _ptr(weight), _ptr(ws),
+                                  ws_bytes, _ptr(stream)))
+
+
 class Net:
     """Owns a net handle, its arena (a torch uint8 tensor) and the device tensors its layers reference (they
     must outlive it).  nnz_per_layer: the most entries each layer will hold (an int applies to every layer);
@@ -481,7 +501,7 @@ def net_from_problem(problem, device: str = "cuda:0", dense=0, bias_mode: int = 
 
 
 _EXPERTS = ("Routes", "experts_forward", "norm_quantize", "product_blocks", "quantize_blocks", "route")
-_GENERATE = ("product_groups", "quantize_groups", "widen_groups")
+_GENERATE = ("Layer", "experts_layer", "product_groups", "quantize_groups", "widen_groups")
 
 
 def __getattr__(name):

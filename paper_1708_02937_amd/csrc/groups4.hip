@@ -111,7 +111,7 @@ hipError_t each_slab(const GroupsArgs &a, F f) {
 //
 // A step is 128 columns: lane l holds the 32 columns from 32 (l / 16) on of weight row and activation row l % 16, one
 // group, in four instructions of eight columns a lane.  Any order of columns will do as long as both operands have it.
-constexpr int kSplit = 8;  // waves of a workgroup, which share the columns
+constexpr int kWaves = 8;  // waves of a workgroup, which share the columns
 
 template <typename TX>
 constexpr int kParts = sizeof(TX) == 4 ? 3 : 1;
@@ -173,11 +173,11 @@ struct Rows32<float> {
 
 // 16 NW outputs of 16 MT rows.  Each wave takes a run of steps and loads AHEAD of them before it multiplies the first.
 template <typename TX, typename TY, int MT, int NW, int AHEAD>
-__global__ void __launch_bounds__(64 * kSplit) product_groups_kernel(GroupProductArgs a) {
-    __shared__ v4f part[kSplit / 2][MT * NW][64];
+__global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProductArgs a) {
+    __shared__ v4f part[kWaves / 2][MT * NW][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
     const int64_t n0 = (int64_t)blockIdx.x * (16 * NW), m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int steps = (int)blocks_of(a.k), each = (steps + kSplit - 1) / kSplit;
+    const int steps = (int)blocks_of(a.k), each = (steps + kWaves - 1) / kWaves;
     const int begin = min(wave * each, steps), end = min(begin + each, steps);
     const uint8_t *w[NW], *ws[NW];
 #pragma unroll
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(64 * kSplit) product_groups_kernel(GroupProduc
     }
     // the waves' sums, pair by pair
 #pragma unroll
-    for (int half = kSplit / 2; half >= 1; half /= 2) {
+    for (int half = kWaves / 2; half >= 1; half /= 2) {
         if (wave >= half && wave < 2 * half)
 #pragma unroll
             for (int t = 0; t < MT; t++)
@@ -284,7 +284,7 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
             p.bias = a.bias ? a.bias + n0 : nullptr;
             p.y = (TY *)a.y + m0 * a.ldy + n0;
             const dim3 grid((unsigned)((p.n + 16 * NW - 1) / (16 * NW)), (unsigned)((p.m + 16 * MT - 1) / (16 * MT)));
-            product_groups_kernel<TX, TY, MT, NW, AHEAD><<<grid, 64 * kSplit, 0, s>>>(p);
+            product_groups_kernel<TX, TY, MT, NW, AHEAD><<<grid, 64 * kWaves, 0, s>>>(p);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

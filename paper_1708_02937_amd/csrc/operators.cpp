@@ -177,6 +177,20 @@ static sdnn_status check_routes(int64_t tokens, int32_t experts, int32_t chosen)
     return SDNN_OK;
 }
 
+static sdnn_status check_choice(int32_t experts, int32_t score, int32_t type, int32_t groups, int32_t groups_kept,
+                                int32_t group_best, int32_t normalize, float factor) {
+    if (score != SDNN_SCORE_SOFTMAX && score != SDNN_SCORE_SIGMOID)
+        return fail(SDNN_ERR_INVALID_VALUE, "unknown score");
+    if (!known_type(type)) return fail(SDNN_ERR_INVALID_VALUE, "unknown element type");
+    if (groups < 1 || groups > sdnn::kRouteMaxGroups || experts % groups != 0)
+        return fail(SDNN_ERR_INVALID_VALUE, "groups must be 1 to 64 and divide the experts");
+    if (groups_kept < 1 || groups_kept > groups) return fail(SDNN_ERR_INVALID_VALUE, "groups_kept out of range");
+    if (group_best != 1 && group_best != 2) return fail(SDNN_ERR_INVALID_VALUE, "group_best must be 1 or 2");
+    if (normalize != 0 && normalize != 1) return fail(SDNN_ERR_INVALID_VALUE, "normalize must be 0 or 1");
+    if (!std::isfinite(factor)) return fail(SDNN_ERR_INVALID_VALUE, "factor must be finite");
+    return SDNN_OK;
+}
+
 sdnn_status sdnn_route_workspace_size(int64_t tokens, int32_t experts, int32_t chosen, int64_t *bytes) {
     sdnn::set_error(SDNN_OK, "");
     if (!bytes) return fail(SDNN_ERR_NULL_POINTER, "bytes is NULL");
@@ -191,15 +205,7 @@ sdnn_status sdnn_route(int64_t tokens, int32_t experts, int32_t chosen, int32_t 
                        int32_t *offsets, int32_t *order, void *ws, int64_t ws_bytes, void *stream) {
     sdnn::set_error(SDNN_OK, "");
     SDNN_CHECK(check_routes(tokens, experts, chosen));
-    if (score != SDNN_SCORE_SOFTMAX && score != SDNN_SCORE_SIGMOID)
-        return fail(SDNN_ERR_INVALID_VALUE, "unknown score");
-    if (!known_type(type)) return fail(SDNN_ERR_INVALID_VALUE, "unknown element type");
-    if (groups < 1 || groups > sdnn::kRouteMaxGroups || experts % groups != 0)
-        return fail(SDNN_ERR_INVALID_VALUE, "groups must be 1 to 64 and divide the experts");
-    if (groups_kept < 1 || groups_kept > groups) return fail(SDNN_ERR_INVALID_VALUE, "groups_kept out of range");
-    if (group_best != 1 && group_best != 2) return fail(SDNN_ERR_INVALID_VALUE, "group_best must be 1 or 2");
-    if (normalize != 0 && normalize != 1) return fail(SDNN_ERR_INVALID_VALUE, "normalize must be 0 or 1");
-    if (!std::isfinite(factor)) return fail(SDNN_ERR_INVALID_VALUE, "factor must be finite");
+    SDNN_CHECK(check_choice(experts, score, type, groups, groups_kept, group_best, normalize, factor));
     if (!offsets || (tokens > 0 && (!logits || !ids || !weight || !order)))
         return fail(SDNN_ERR_NULL_POINTER, "logits or an output is NULL");
     if (bad_dense(logits, type, ldl, experts) || misaligned(bias, 4) || misaligned(ids, 4) || misaligned(weight, 4) ||
@@ -261,6 +267,62 @@ sdnn_status sdnn_experts_forward(int64_t tokens, int64_t width, int64_t inner, i
     const hipError_t e = sdnn::launch_experts(p, type == SDNN_TYPE_BF16, (hipStream_t)stream);
     if (e == hipErrorInvalidConfiguration) return fail(SDNN_ERR_UNSUPPORTED, "more tiles than one launch holds");
     return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_experts_forward");
+}
+
+static sdnn_status check_layer(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen) {
+    SDNN_CHECK(check_routes(tokens, experts, chosen));
+    if (!side(width, 1) || !side(inner, 1)) return fail(SDNN_ERR_INVALID_VALUE, "width or inner out of range");
+    if (tokens > sdnn::kLayerMaxTokens)
+        return fail(SDNN_ERR_UNSUPPORTED, "more than 16 tokens: sdnn_norm_quantize, sdnn_route and sdnn_experts_forward "
+                                          "take any number");
+    if (width >= sdnn::kLayerMaxWidth) return fail(SDNN_ERR_UNSUPPORTED, "rows of 2^27 columns or more");
+    return SDNN_OK;
+}
+
+sdnn_status sdnn_experts_layer_workspace_size(int64_t tokens, int64_t width, int64_t inner, int32_t experts,
+                                              int32_t chosen, int64_t *bytes) {
+    sdnn::set_error(SDNN_OK, "");
+    if (!bytes) return fail(SDNN_ERR_NULL_POINTER, "bytes is NULL");
+    SDNN_CHECK(check_layer(tokens, width, inner, experts, chosen));
+    *bytes = (int64_t)sdnn::layer_workspace(tokens, width, inner, experts, chosen);
+    return SDNN_OK;
+}
+
+sdnn_status sdnn_experts_layer(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen,
+                               int32_t type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                               const float *gamma, float eps, const uint8_t *live, int32_t router_type,
+                               const void *router, int64_t ldw, int32_t score, const float *bias, int32_t groups,
+                               int32_t groups_kept, int32_t group_best, int32_t normalize, float factor,
+                               const uint8_t *w_in, const uint8_t *w_in_scale, const uint8_t *w_out,
+                               const uint8_t *w_out_scale, void *out, int64_t ldo, int32_t *ids, float *weight, void *ws,
+                               int64_t ws_bytes, void *stream) {
+    sdnn::set_error(SDNN_OK, "");
+    SDNN_CHECK(check_layer(tokens, width, inner, experts, chosen));
+    SDNN_CHECK(check_choice(experts, score, type, groups, groups_kept, group_best, normalize, factor));
+    if (!known_type(router_type)) return fail(SDNN_ERR_INVALID_VALUE, "unknown element type of the router");
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(SDNN_ERR_INVALID_VALUE, "eps must be finite and >= 0");
+    if (tokens == 0) return SDNN_OK;
+    if (!x || !gamma || !router || !out || !ids || !weight)
+        return fail(SDNN_ERR_NULL_POINTER, "x, gamma, router or an output is NULL");
+    SDNN_CHECK(check_codes(w_in, w_in_scale, "w_in"));
+    SDNN_CHECK(check_codes(w_out, w_out_scale, "w_out"));
+    if (bad_dense(x, type, ldx, width) || (residual && bad_dense(residual, type, ldr, width)) ||
+        bad_dense(out, type, ldo, width) || bad_dense(router, router_type, ldw, width))
+        return fail(SDNN_ERR_INVALID_VALUE, "a dense tensor is misaligned or its row stride below width");
+    if (misaligned(gamma, 4) || misaligned(bias, 4) || misaligned(ids, 4) || misaligned(weight, 4))
+        return fail(SDNN_ERR_INVALID_VALUE, "gamma, bias, ids or weight is misaligned");
+    const size_t need = sdnn::layer_workspace(tokens, width, inner, experts, chosen);
+    if (!ws) return fail(SDNN_ERR_NULL_POINTER, "ws is NULL");
+    if (ws_bytes < 0 || (size_t)ws_bytes < need)
+        return fail(SDNN_ERR_WORKSPACE_TOO_SMALL, "ws_bytes below sdnn_experts_layer_workspace_size");
+    if (misaligned(ws, 16)) return fail(SDNN_ERR_INVALID_VALUE, "ws must be 16-byte aligned");
+    const sdnn::LayerArgs p{tokens,     width,  inner,      experts,     chosen, groups,   groups_kept,
+                            group_best, score == SDNN_SCORE_SIGMOID,     normalize != 0,   factor,
+                            x,          residual, ldx,      ldr,         gamma,  (double)eps, router,
+                            ldw,        bias,   live,       w_in,        w_in_scale, w_out, w_out_scale,
+                            out,        ldo,    ids,        weight,      ws};
+    const hipError_t e = sdnn::launch_layer(p, type == SDNN_TYPE_BF16, router_type == SDNN_TYPE_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_experts_layer");
 }
 
 }  // extern "C"

@@ -14,6 +14,8 @@ constexpr int kRouteMaxExperts = 1024;  // 16 scores per lane of a wave
 constexpr int kRouteMaxChosen = 64;     // one chosen expert per lane
 constexpr int kRouteMaxGroups = 64;
 
+constexpr int kLayerMaxTokens = 16;     // one row of the matrix instructions' tiles each
+constexpr int64_t kLayerMaxWidth = (int64_t)1 << 27;  // a launch holds fewer than 2^32 threads, 512 to 16 columns
 constexpr int kGroup = 32;              // columns of a 4-bit matrix that share a scale
 
 constexpr int64_t blocks_of(int64_t k) { return (k + kBlock - 1) / kBlock; }
@@ -99,10 +101,33 @@ struct GroupProductArgs {
     int64_t ldy;
 };
 
+struct LayerArgs {
+    int64_t tokens, width, inner;
+    int32_t experts, chosen, groups, groups_kept, group_best;
+    bool sigmoid, normalize;
+    float factor;
+    const void *x, *residual;  // residual may be null
+    int64_t ldx, ldr;
+    const float *gamma;
+    double eps;
+    const void *router;  // experts x width
+    int64_t ldw;
+    const float *bias;    // may be null
+    const uint8_t *live;  // may be null
+    const uint8_t *w_in, *w_in_scale, *w_out, *w_out_scale;
+    void *out;
+    int64_t ldo;
+    int32_t *ids;
+    float *weight;
+    void *ws;
+};
+
 // bf16: the dense tensors are bfloat16, otherwise float
 hipError_t launch_quantize_groups(const GroupsArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_widen_groups(const GroupsArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_product_groups(const GroupProductArgs &a, bool x_bf16, bool y_bf16, hipStream_t stream);
+hipError_t launch_layer(const LayerArgs &a, bool bf16, bool router_bf16, hipStream_t stream);
+size_t layer_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen);
 hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_quantize(const QuantizeArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_route(const RouteArgs &a, bool bf16, hipStream_t stream);

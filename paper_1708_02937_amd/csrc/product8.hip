@@ -10,25 +10,6 @@
 namespace sdnn {
 namespace {
 
-// acc += scaled product of 16 weight rows and 16 activation rows over one block of 128 columns, every product exact.
-// Lane l holds columns 32 (l / 16) .. + 31 of weight row and activation row l % 16; acc[i] is output 4 (l / 16) + i of
-// row l % 16, so the activation's scale code is the lane's own and the weight rows share one.
-__device__ __forceinline__ v4f block16(const v8i &w, const v8i &x, v4f acc, int w_code, int x_code) {
-    v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * i], w[2 * i + 1], kOne),
-                                                    widen8(x[2 * i], x[2 * i + 1], kOne), z, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 4; i++) acc[i] += ldexpf(z[i], w_code + x_code - 2 * kOne);
-    return acc;
-}
-
-__device__ __forceinline__ v8i load32(const uint8_t *p) {
-    const v4i a = *(const v4i *)p, b = *(const v4i *)(p + 16);
-    return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-
 // ------------------------------------------------------------------------------------------------ few rows
 // 16 outputs x 16 rows per workgroup, straight from memory to registers: with up to 16 rows the weights are read once,
 // which is what bounds those calls.  The waves share the blocks of the inner dimension and join their sums in LDS.  (16

@@ -11,6 +11,7 @@
 // moves with the comparison built in, and what a choice costs is the search through a lane's own experts.
 #include "blocks8.h"
 #include "common.h"
+#include "lanes.h"
 
 namespace sdnn {
 namespace {
@@ -19,82 +20,6 @@ constexpr int kScoreWaves = 4;  // waves of a workgroup of the scores
 constexpr int kSmallWaves = 8, kPlanWaves = 16;  // waves of the workgroup of a small call, one to a token, and of the plan's
 constexpr int64_t kChunk = 4096;      // slots that one workgroup sorts, up to kMaxChunks of them; then more each
 constexpr int64_t kMaxChunks = 256;
-
-template <int N>
-__device__ __forceinline__ float ror16(float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, true));
-}
-template <int N>
-__device__ __forceinline__ int ror16(int v) {
-    return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true);
-}
-
-// Each half of the wave's (or of every 32 lanes') 32-bit values beside the other's: a reduction over lanes i and i ^ 32
-// (i ^ 16) is an operation on the pair, the same in both.
-struct Two {
-    uint32_t a, b;
-};
-__device__ __forceinline__ Two across32(uint32_t v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return {r[0], r[1]};
-}
-__device__ __forceinline__ Two across16(uint32_t v) {
-    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    return {r[0], r[1]};
-}
-
-// The largest (value, lowest index) pair of a wave, in every lane.
-__device__ __forceinline__ void better(double &v, int &i, double ov, int oi) {
-    if (ov > v || (ov == v && oi < i)) v = ov, i = oi;
-}
-__device__ __forceinline__ double join64(uint32_t lo, uint32_t hi) { return __hiloint2double((int)hi, (int)lo); }
-template <int N>
-__device__ __forceinline__ void best_ror(double &v, int &i) {
-    better(v, i, join64(ror16<N>(__double2loint(v)), ror16<N>(__double2hiint(v))), ror16<N>(i));
-}
-template <typename F>
-__device__ __forceinline__ void best_across(double &v, int &i, F across) {
-    const Two lo = across(__double2loint(v)), hi = across(__double2hiint(v)), at = across(i);
-    v = join64(lo.a, hi.a), i = (int)at.a;
-    better(v, i, join64(lo.b, hi.b), (int)at.b);
-}
-__device__ __forceinline__ void wave_best(double &v, int &i) {
-    best_ror<8>(v, i), best_ror<4>(v, i), best_ror<2>(v, i), best_ror<1>(v, i);
-    best_across(v, i, across16), best_across(v, i, across32);
-}
-
-// Reductions over the LANES (16, 32 or 64) lanes of a token, in every lane of them.
-template <int LANES>
-__device__ __forceinline__ float lanes_max(float v) {
-    v = fmaxf(v, ror16<8>(v)), v = fmaxf(v, ror16<4>(v)), v = fmaxf(v, ror16<2>(v)), v = fmaxf(v, ror16<1>(v));
-    if (LANES > 16) {
-        const Two t = across16(__float_as_uint(v));
-        v = fmaxf(__uint_as_float(t.a), __uint_as_float(t.b));
-    }
-    if (LANES > 32) {
-        const Two t = across32(__float_as_uint(v));
-        v = fmaxf(__uint_as_float(t.a), __uint_as_float(t.b));
-    }
-    return v;
-}
-template <int LANES>
-__device__ __forceinline__ int lanes_min(int v) {
-    v = min(v, ror16<8>(v)), v = min(v, ror16<4>(v)), v = min(v, ror16<2>(v)), v = min(v, ror16<1>(v));
-    if (LANES > 16) {
-        const Two t = across16(v);
-        v = min((int)t.a, (int)t.b);
-    }
-    if (LANES > 32) {
-        const Two t = across32(v);
-        v = min((int)t.a, (int)t.b);
-    }
-    return v;
-}
-template <int LANES, typename V>
-__device__ __forceinline__ V lanes_sum(V v) {
-    for (int m = 1; m < LANES; m <<= 1) v += __shfl_xor(v, m);
-    return v;
-}
 
 // A logit, -inf where the expert cannot be chosen (NaN, or past the last).
 template <typename T>

@@ -408,10 +408,81 @@ PyObject *product_groups(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// x, gamma, router, k, w_in, w_in_scale, w_out, w_out_scale, inner, eps, residual, live, score, bias, groups, groups_kept,
+// group_best, normalize, factor, out, ws, stream -> out, ids, weight
+PyObject *experts_layer(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count(n, 22);
+    const Tensor &x = tensor(args[0], "x"), &router = tensor(args[2], "router"), &w_in = tensor(args[4], "w_in");
+    const int32_t chosen = small(integer(args[3]), "k");
+    const int64_t inner = integer(args[8]);
+    const float eps = (float)real(args[9]);
+    const int32_t score = (int32_t)integer(args[12]);
+    const int32_t groups = small(integer(args[14]), "groups"), kept = small(integer(args[15]), "groups_kept"),
+                  best = small(integer(args[16]), "group_best");
+    const int32_t normalize = PyObject_IsTrue(args[17]) == 1;
+    const float factor = (float)real(args[18]);
+    void *const stream = stream_of(args[21]);
+    TORCH_CHECK_VALUE(x.dim() == 2 && router.dim() == 2, "x and router must be matrices");
+    TORCH_CHECK_VALUE(chosen >= 1, "k must be at least 1");
+    TORCH_CHECK_VALUE(inner >= 1, "inner must be at least 1");
+    const at::Device device = x.device();
+    const ScalarType type = x.scalar_type();
+    const int32_t kind = kind_of(x, "x"), router_kind = kind_of(router, "router");
+    const int64_t tokens = x.size(0), width = x.size(1);
+    const int32_t experts = small(router.size(0), "experts");
+    const int64_t pitch = pitch_of(width), spitch = scale_pitch_of(width);
+    const int64_t pitch_f = pitch_of(inner), spitch_f = scale_pitch_of(inner);
+    const int64_t ldx = dense(x, "x", type, device, tokens, width);
+    const int64_t ldw = dense(router, "router", router.scalar_type(), device, experts, width);
+    const float *gamma = packed<float>(args[1], "gamma", ScalarType::Float, device, {width});
+    const uint8_t *p1 = packed<uint8_t>(w_in, "w_in", kCodes, device, {experts, 2, inner, pitch});
+    const uint8_t *ps1 = packed<uint8_t>(args[5], "w_in_scale", kScales, device, {experts, 2, up(inner, 128), spitch});
+    const uint8_t *p2 = packed<uint8_t>(args[6], "w_out", kCodes, device, {experts, width, pitch_f});
+    const uint8_t *ps2 = packed<uint8_t>(args[7], "w_out_scale", kScales, device, {experts, up(width, 128), spitch_f});
+    const void *residual = nullptr;
+    int64_t ldr = 0;
+    if (args[10] != Py_None) {
+        const Tensor &r = tensor(args[10], "residual");
+        ldr = dense(r, "residual", type, device, tokens, width);
+        residual = r.data_ptr();
+    }
+    const uint8_t *live =
+        args[11] == Py_None ? nullptr : packed<uint8_t>(args[11], "live", ScalarType::Bool, device, {tokens});
+    const float *bias =
+        args[13] == Py_None ? nullptr : packed<float>(args[13], "bias", ScalarType::Float, device, {experts});
+    const Tensor out = args[19] == Py_None ? empty({tokens, width}, type, device) : tensor(args[19], "out");
+    const int64_t ldo = args[19] == Py_None ? width : dense(out, "out", type, device, tokens, width);
+    Tensor ws;
+    sdnn_status s;
+    if (args[20] == Py_None) {
+        int64_t need = 0;
+        s = sdnn_experts_layer_workspace_size(tokens, width, inner, experts, chosen, &need);
+        if (s) return PyLong_FromLong(s);
+        ws = empty({need}, ScalarType::Byte, device);
+    } else {
+        ws = tensor(args[20], "ws");
+        TORCH_CHECK_VALUE(ws.device() == device && ws.scalar_type() == ScalarType::Byte && ws.is_contiguous(),
+                          "ws must be a contiguous uint8 tensor on the same device");
+    }
+    const Tensor ids = empty({tokens, chosen}, ScalarType::Int, device);
+    const Tensor weight = empty({tokens, chosen}, ScalarType::Float, device);
+    {
+        Unlocked u;
+        s = sdnn_experts_layer(tokens, width, inner, experts, chosen, kind, x.data_ptr(), ldx, residual, ldr, gamma, eps,
+                               live, router_kind, router.data_ptr(), ldw, score, bias, groups, kept, best, normalize,
+                               factor, p1, ps1, p2, ps2, out.data_ptr(), ldo, (int32_t *)ids.data_ptr(),
+                               (float *)weight.data_ptr(), ws.data_ptr(), ws.numel(), stream);
+    }
+    return s ? PyLong_FromLong(s) : tuple_of(out, ids, weight);
+    END_HANDLE_TH_ERRORS
+}
+
 #define SDNN_CALL(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDNN_CALL(quantize_blocks), SDNN_CALL(norm_quantize),   SDNN_CALL(product_blocks),
                          SDNN_CALL(route),           SDNN_CALL(experts_forward), SDNN_CALL(quantize_groups),
-                         SDNN_CALL(widen_groups),    SDNN_CALL(product_groups),  {nullptr, nullptr, 0, nullptr}};
+                         SDNN_CALL(widen_groups),    SDNN_CALL(product_groups),  SDNN_CALL(experts_layer),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -9,10 +9,20 @@ function may be called while a graph is captured, and a tensor that requires a g
 
 from __future__ import annotations
 
+from typing import NamedTuple
+
 import torch
 
 from . import _tensors
-from .experts import _checked, _current, _elsewhere, _kind, _stream
+from .experts import _SCORES, _checked, _current, _elsewhere, _kind, _stream
+
+
+class Layer(NamedTuple):
+    """A layer's result (tokens x width), and the experts that each token took (ids and weight as in Routes)."""
+
+    out: torch.Tensor
+    ids: torch.Tensor
+    weight: torch.Tensor
 
 
 def quantize_groups(x):
@@ -40,3 +50,23 @@ def product_groups(x, w, w_scale, bias=None, ymax=None, dtype=None, out=None):
         return _elsewhere(product_groups, device, x, w, w_scale, bias, ymax, dtype, out)
     return _checked(_tensors.product_groups(x, w, w_scale, bias, ymax, None if dtype is None else _kind(dtype), out,
                                             _stream(device)))
+
+
+def experts_layer(x, gamma, router, k: int, w_in, w_in_scale, w_out, w_out_scale, inner: int, eps: float = 1e-6,
+                  residual=None, live=None, score: str = "softmax", bias=None, groups: int = 1, groups_kept: int = 1,
+                  group_best: int = 1, normalize: bool = True, factor: float = 1.0, out=None, ws=None) -> Layer:
+    """A whole layer of experts for up to 16 tokens (x: tokens x width): s = x + residual, its RMS norm times gamma, the
+    router's logits (router: experts x width, float32 or bfloat16) and choice (k, score, bias, groups, ... as in route),
+    and s + the weighted sum of the chosen experts on the norm in 8 bits (weights as in experts_forward).
+
+    live: a bool for each token; one that is False takes part in no expert, and its result is s.  out may be x or residual
+    itself.  ws: a uint8 tensor of at least sdnn_experts_layer_workspace_size bytes (allocated if absent)."""
+    device = x.get_device()
+    if device < 0 or device != _current():
+        return _elsewhere(experts_layer, device, x, gamma, router, k, w_in, w_in_scale, w_out, w_out_scale, inner, eps,
+                          residual, live, score, bias, groups, groups_kept, group_best, normalize, factor, out, ws)
+    if score not in _SCORES:
+        raise ValueError("score must be 'softmax' or 'sigmoid'")
+    return Layer._make(_checked(_tensors.experts_layer(x, gamma, router, k, w_in, w_in_scale, w_out, w_out_scale, inner,
+                                                       eps, residual, live, _SCORES[score], bias, groups, groups_kept,
+                                                       group_best, normalize, factor, out, ws, _stream(device))))

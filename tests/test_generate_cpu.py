@@ -59,3 +59,35 @@ def test_reference_codes():
     codes, scales = gen.quantize4(np.array([[6.0, 3.0, 6.1], [-6.0, 0.0, 0.0]]))
     assert scales[0, 0] == 128 and scales[1, 0] == 127 and codes[0, 0] == 5 | 3 << 4 and codes[1, 0] == 15
     assert np.array_equal(gen.values4(codes, scales, 3), [[6.0, 3.0, 6.0], [-6.0, 0.0, 0.0]])
+
+
+def test_layer_refusals(sd):  # noqa: F811
+    good = dict(tokens=3, width=10, inner=20, experts=4, chosen=2, type=1, x=FAKE, ldx=10, residual=FAKE, ldr=10,
+                gamma=FAKE, eps=1e-6, live=FAKE + 1, router_type=0, router=FAKE, ldw=10, score=1, bias=FAKE, groups=2,
+                groups_kept=1, group_best=2, normalize=1, factor=1.0, w_in=FAKE, w_in_scale=FAKE, w_out=FAKE,
+                w_out_scale=FAKE, out=FAKE, ldo=10, ids=FAKE, weight=FAKE, ws=FAKE, ws_bytes=1 << 30)
+    changes = [(dict(tokens=-1), 2), (dict(tokens=17), 9), (dict(width=0), 2), (dict(inner=0), 2), (dict(experts=0), 2),
+               (dict(width=1 << 27, ldx=1 << 28, ldr=1 << 28, ldw=1 << 28, ldo=1 << 28), 9), (dict(chosen=5), 2),
+               (dict(chosen=0), 2), (dict(experts=1025, groups=1), 9), (dict(type=9), 2), (dict(router_type=2), 2),
+               (dict(eps=-1.0), 2), (dict(eps=math.nan), 2), (dict(score=2), 2), (dict(groups=3), 2),
+               (dict(groups_kept=3), 2), (dict(group_best=0), 2), (dict(normalize=2), 2), (dict(factor=math.inf), 2),
+               (dict(ldx=9), 2), (dict(ldr=9), 2), (dict(ldw=9), 2), (dict(ldo=9), 2), (dict(x=FAKE + 1), 2),
+               (dict(router=FAKE + 2), 2), (dict(gamma=FAKE + 2), 2), (dict(bias=FAKE + 1), 2), (dict(ids=FAKE + 2), 2),
+               (dict(weight=FAKE + 2), 2), (dict(ws=None), 1), (dict(ws_bytes=100), 6), (dict(ws_bytes=-1), 6),
+               (dict(ws=FAKE + 8), 2)]
+    changes += [({x: None}, 1) for x in ("x", "gamma", "router", "w_in", "w_in_scale", "w_out", "w_out_scale", "out",
+                                         "ids", "weight")]
+    changes += [({x: FAKE + 8}, 2) for x in ("w_in", "w_out")]
+    _refusals(sd, sd.sdnn_experts_layer, good, changes)
+    none = {k: (None if v in (FAKE, FAKE + 1) else v) for k, v in good.items()}
+    assert _status(sd, sd.sdnn_experts_layer, *{**none, "tokens": 0}.values()) == 0
+
+
+def test_layer_workspace_sizes(sd):  # noqa: F811
+    """One of the size for the most tokens serves every smaller call."""
+    for width, inner, experts, chosen in ((1, 1, 1, 1), (300, 70, 8, 3), (4096, 1024, 64, 8), (100, 33, 1024, 64)):
+        sizes = [sd.sdnn_experts_layer_workspace_size(t, width, inner, experts, chosen) for t in range(17)]
+        assert sizes == sorted(sizes) and sizes[1] >= chosen * inner * 4 + width
+    assert _status(sd, sd.sdnn_experts_layer_workspace_size, 17, 8, 8, 4, 2) == 9
+    assert _status(sd, sd.sdnn_experts_layer_workspace_size, 1, 8, 8, 4, 5) == 2
+    assert sd.lib.sdnn_experts_layer_workspace_size(1, 8, 8, 4, 2, None) == 1
