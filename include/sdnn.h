@@ -535,6 +535,34 @@ sdnn_status sdnn_experts_layer(int64_t tokens, int64_t width, int64_t inner, int
                                const uint8_t *w_out_scale, void *out, int64_t ldo, int32_t *ids, float *weight, void *ws,
                                int64_t ws_bytes, void *stream);
 
+/*
+ * Bytes of device workspace sdnn_sample needs for any call of up to `rows` rows of that vocabulary.
+ * Errors: NULL_POINTER, INVALID_VALUE.
+ */
+sdnn_status sdnn_sample_workspace_size(int64_t rows, int64_t vocab, int64_t *bytes);
+
+/*
+ * The next token of each row of logits (rows x vocab, of the type).  With p_i = exp((l_i - max l) / temperature), tokens
+ * in the order of their logits, the largest first and equal ones by index, a row keeps those that are all of
+ *   the first top_k (all, where top_k is 0 or less),
+ *   the shortest run of those from the first on whose mass is top_p or more of theirs (all, where top_p is 1 or more; the
+ *   first one at the least), and
+ *   p_i >= min_p (all, where min_p is 0 or less; the largest logit's at the least),
+ * and takes the first index i at which the sum of p over the kept tokens 0 .. i exceeds uniform times the sum over all kept
+ * ones.  temperature 0 or less: the largest logit's first index alone is kept.  A logit of -inf or NaN is no token; +inf ones
+ * share the row among themselves; a row without any token has id -1, prob 0 and kept 0.
+ * uniform: rows fp64 values in [0, 1), the caller's random numbers.  temperature, top_p, min_p (fp32) and top_k (int32): a
+ * value for each row, or NULL for 1, 1, 0 and 0; a NaN temperature is 0, a NaN share none.
+ * Outputs: ids (rows, int32), prob (rows, fp32: the token's share of what is kept) and kept (rows, int32: how many tokens
+ * are).  All of it is decided by sums in 64 bits, in an order that goes by the row alone; tokens whose p is below 2e-28 are
+ * counted but never drawn.
+ * Errors: NULL_POINTER, INVALID_VALUE, WORKSPACE_TOO_SMALL, DEVICE.
+ */
+sdnn_status sdnn_sample(int64_t rows, int64_t vocab, int32_t type, const void *logits, int64_t ldl,
+                        const double *uniform, const float *temperature, const int32_t *top_k, const float *top_p,
+                        const float *min_p, int32_t *ids, float *prob, int32_t *kept, void *ws, int64_t ws_bytes,
+                        void *stream);
+
 /* Static text for a status code. */
 const char *sdnn_status_string(sdnn_status status);
 

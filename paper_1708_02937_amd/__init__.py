@@ -94,6 +94,8 @@ _sig = {
     "sdnn_experts_layer_workspace_size": [_I64, _I64, _I64, _I32, _I32, _c.POINTER(_I64)],
     "sdnn_experts_layer": [_I64, _I64, _I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _c.c_float, _P, _I32, _P, _I64,
                            _I32, _P, _I32, _I32, _I32, _I32, _c.c_float, _P, _P, _P, _P, _P, _I64, _P, _P, _P, _I64, _P],
+    "sdnn_sample_workspace_size": [_I64, _I64, _c.POINTER(_I64)],
+    "sdnn_sample": [_I64, _I64, _I32, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _P],
     "sdnn_route_workspace_size": [_I64, _I32, _I32, _c.POINTER(_I64)],
     "sdnn_route": [_I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _I32, _I32, _I32, _I32, _c.c_float, _P, _P, _P, _P,
                    _P, _I64, _P],
@@ -327,6 +329,19 @@ def sdnn_experts_layer(tokens: int, width: int, inner: int, experts: int, chosen
                                   ws_bytes, _ptr(stream)))
 
 
+def sdnn_sample_workspace_size(rows: int, vocab: int) -> int:
+    out = _I64()
+    _check(lib.sdnn_sample_workspace_size(rows, vocab, _c.byref(out)))
+    return out.value
+
+
+def sdnn_sample(rows: int, vocab: int, type: int, logits, ldl: int, uniform, temperature, top_k, top_p, min_p, ids, prob,
+                kept, ws, ws_bytes: int, stream=None):
+    _check(lib.sdnn_sample(rows, vocab, type, _ptr(logits), ldl, _ptr(uniform), _ptr(temperature), _ptr(top_k),
+                           _ptr(top_p), _ptr(min_p), _ptr(ids), _ptr(prob), _ptr(kept), _ptr(ws), ws_bytes,
+                           _ptr(stream)))
+
+
 class Net:
     """Owns a net handle, its arena (a torch uint8 tensor) and the device tensors its layers reference (they
     must outlive it).  nnz_per_layer: the most entries each layer will hold (an int applies to every layer);
@@ -501,7 +516,7 @@ def net_from_problem(problem, device: str = "cuda:0", dense=0, bias_mode: int = 
 
 
 _EXPERTS = ("Routes", "experts_forward", "norm_quantize", "product_blocks", "quantize_blocks", "route")
-_GENERATE = ("Layer", "experts_layer", "product_groups", "quantize_groups", "widen_groups")
+_GENERATE = ("Layer", "Tokens", "experts_layer", "product_groups", "quantize_groups", "sample", "widen_groups")
 
 
 def __getattr__(name):

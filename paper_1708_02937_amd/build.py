@@ -15,7 +15,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsdnn.so")
 TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["setup.hip", "spmm.hip", "resident.hip", "gemm.hip", "spgemm.hip", "semiring.hip", "blocked.hip", "quantize.hip", "route.hip",
-           "product8.hip", "tile8.hip", "groups4.hip", "layer.hip", "api.cpp", "operators.cpp"]
+           "product8.hip", "tile8.hip", "groups4.hip", "layer.hip", "sample.hip",
+           "api.cpp", "operators.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")

@@ -325,4 +325,42 @@ sdnn_status sdnn_experts_layer(int64_t tokens, int64_t width, int64_t inner, int
     return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_experts_layer");
 }
 
+static sdnn_status check_sample(int64_t rows, int64_t vocab) {
+    if (!side(rows, 0) || !side(vocab, 1)) return fail(SDNN_ERR_INVALID_VALUE, "rows or vocab out of range");
+    return SDNN_OK;
+}
+
+sdnn_status sdnn_sample_workspace_size(int64_t rows, int64_t vocab, int64_t *bytes) {
+    sdnn::set_error(SDNN_OK, "");
+    if (!bytes) return fail(SDNN_ERR_NULL_POINTER, "bytes is NULL");
+    SDNN_CHECK(check_sample(rows, vocab));
+    *bytes = (int64_t)sdnn::sample_workspace(rows, vocab);
+    return SDNN_OK;
+}
+
+sdnn_status sdnn_sample(int64_t rows, int64_t vocab, int32_t type, const void *logits, int64_t ldl,
+                        const double *uniform, const float *temperature, const int32_t *top_k, const float *top_p,
+                        const float *min_p, int32_t *ids, float *prob, int32_t *kept, void *ws, int64_t ws_bytes,
+                        void *stream) {
+    sdnn::set_error(SDNN_OK, "");
+    SDNN_CHECK(check_sample(rows, vocab));
+    if (!known_type(type)) return fail(SDNN_ERR_INVALID_VALUE, "unknown element type");
+    if (rows == 0) return SDNN_OK;
+    if (!logits || !uniform || !ids || !prob || !kept)
+        return fail(SDNN_ERR_NULL_POINTER, "logits, uniform or an output is NULL");
+    if (bad_dense(logits, type, ldl, vocab))
+        return fail(SDNN_ERR_INVALID_VALUE, "logits are misaligned or their row stride below vocab");
+    if (misaligned(uniform, 8) || misaligned(temperature, 4) || misaligned(top_k, 4) || misaligned(top_p, 4) ||
+        misaligned(min_p, 4) || misaligned(ids, 4) || misaligned(prob, 4) || misaligned(kept, 4))
+        return fail(SDNN_ERR_INVALID_VALUE, "a setting or an output is misaligned");
+    const size_t need = sdnn::sample_workspace(rows, vocab);
+    if (need > 0 && !ws) return fail(SDNN_ERR_NULL_POINTER, "ws is NULL");
+    if (ws_bytes < 0 || (size_t)ws_bytes < need)
+        return fail(SDNN_ERR_WORKSPACE_TOO_SMALL, "ws_bytes below sdnn_sample_workspace_size");
+    if (misaligned(ws, 16)) return fail(SDNN_ERR_INVALID_VALUE, "ws must be 16-byte aligned");
+    const sdnn::SampleArgs p{rows, vocab, logits, ldl, uniform, temperature, top_k, top_p, min_p, ids, prob, kept, ws};
+    const hipError_t e = sdnn::launch_sample(p, type == SDNN_TYPE_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? SDNN_OK : fail_hip(e, "sdnn_sample");
+}
+
 }  // extern "C"

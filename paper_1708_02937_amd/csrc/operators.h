@@ -122,11 +122,27 @@ struct LayerArgs {
     void *ws;
 };
 
+struct SampleArgs {
+    int64_t rows, vocab;
+    const void *logits;
+    int64_t ld;
+    const double *uniform;
+    const float *temperature;  // this and the others may be null
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    int32_t *ids;
+    float *prob;
+    int32_t *kept;
+    void *ws;
+};
+
 // bf16: the dense tensors are bfloat16, otherwise float
 hipError_t launch_quantize_groups(const GroupsArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_widen_groups(const GroupsArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_product_groups(const GroupProductArgs &a, bool x_bf16, bool y_bf16, hipStream_t stream);
 hipError_t launch_layer(const LayerArgs &a, bool bf16, bool router_bf16, hipStream_t stream);
+hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t stream);
+size_t sample_workspace(int64_t rows, int64_t vocab);
 size_t layer_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen);
 hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_quantize(const QuantizeArgs &a, bool bf16, hipStream_t stream);

@@ -478,11 +478,53 @@ PyObject *experts_layer(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// logits, uniform, temperature, top_k, top_p, min_p, ws, stream -> ids, prob, kept
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count(n, 8);
+    const Tensor &logits = tensor(args[0], "logits");
+    void *const stream = stream_of(args[7]);
+    TORCH_CHECK_VALUE(logits.dim() == 2, "logits must be rows x vocabulary");
+    const int32_t kind = kind_of(logits, "logits");
+    const int64_t rows = logits.size(0), vocab = logits.size(1);
+    const at::Device device = logits.device();
+    const int64_t ldl = dense(logits, "logits", logits.scalar_type(), device, rows, vocab);
+    const double *uniform = packed<double>(args[1], "uniform", ScalarType::Double, device, {rows});
+    const auto setting = [&](int i, const char *name) {
+        return args[i] == Py_None ? nullptr : packed<float>(args[i], name, ScalarType::Float, device, {rows});
+    };
+    const float *temperature = setting(2, "temperature"), *top_p = setting(4, "top_p"), *min_p = setting(5, "min_p");
+    const int32_t *top_k = args[3] == Py_None ? nullptr : packed<int32_t>(args[3], "top_k", ScalarType::Int, device, {rows});
+    Tensor ws;
+    sdnn_status s;
+    if (args[6] == Py_None) {
+        int64_t need = 0;
+        s = sdnn_sample_workspace_size(rows, vocab, &need);
+        if (s) return PyLong_FromLong(s);
+        if (need) ws = empty({need}, ScalarType::Byte, device);
+    } else {
+        ws = tensor(args[6], "ws");
+        TORCH_CHECK_VALUE(ws.device() == device && ws.scalar_type() == ScalarType::Byte && ws.is_contiguous(),
+                          "ws must be a contiguous uint8 tensor on the same device");
+    }
+    const Tensor ids = empty({rows}, ScalarType::Int, device);
+    const Tensor prob = empty({rows}, ScalarType::Float, device);
+    const Tensor kept = empty({rows}, ScalarType::Int, device);
+    {
+        Unlocked u;
+        s = sdnn_sample(rows, vocab, kind, logits.data_ptr(), ldl, uniform, temperature, top_k, top_p, min_p,
+                        (int32_t *)ids.data_ptr(), (float *)prob.data_ptr(), (int32_t *)kept.data_ptr(),
+                        ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
+    }
+    return s ? PyLong_FromLong(s) : tuple_of(ids, prob, kept);
+    END_HANDLE_TH_ERRORS
+}
+
 #define SDNN_CALL(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDNN_CALL(quantize_blocks), SDNN_CALL(norm_quantize),   SDNN_CALL(product_blocks),
                          SDNN_CALL(route),           SDNN_CALL(experts_forward), SDNN_CALL(quantize_groups),
                          SDNN_CALL(widen_groups),    SDNN_CALL(product_groups),  SDNN_CALL(experts_layer),
-                         {nullptr, nullptr, 0, nullptr}};
+                         SDNN_CALL(sample),          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

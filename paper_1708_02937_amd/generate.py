@@ -25,6 +25,15 @@ class Layer(NamedTuple):
     weight: torch.Tensor
 
 
+class Tokens(NamedTuple):
+    """The next tokens: ids (int32, -1 where a row has none), prob (their share of what was kept) and kept (int32: how many
+    tokens were)."""
+
+    ids: torch.Tensor
+    prob: torch.Tensor
+    kept: torch.Tensor
+
+
 def quantize_groups(x):
     """(codes, scales) of a float32 or bfloat16 tensor (..., rows, k) rounded to 4 bits with a scale for each group of 32
     columns; a matrix may have any row stride, a stack of them has to be contiguous."""
@@ -70,3 +79,16 @@ def experts_layer(x, gamma, router, k: int, w_in, w_in_scale, w_out, w_out_scale
     return Layer._make(_checked(_tensors.experts_layer(x, gamma, router, k, w_in, w_in_scale, w_out, w_out_scale, inner,
                                                        eps, residual, live, _SCORES[score], bias, groups, groups_kept,
                                                        group_best, normalize, factor, out, ws, _stream(device))))
+
+
+def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, ws=None) -> Tokens:
+    """The next token of each row of logits (rows x vocabulary, float32 or bfloat16) for a uniform number each (float64,
+    in [0, 1)): of the top_k largest (int32; 0: all), of the shortest run of those whose mass is top_p of theirs, and of those
+    with at least min_p of the largest one's probability, all at that temperature (0: the largest logit); see sdnn_sample.
+
+    temperature, top_p and min_p are float32 tensors with a value for each row; what is None is off (temperature: 1).
+    ws: a uint8 tensor of at least sdnn_sample_workspace_size bytes (allocated if absent)."""
+    device = logits.get_device()
+    if device < 0 or device != _current():
+        return _elsewhere(sample, device, logits, uniform, temperature, top_k, top_p, min_p, ws)
+    return Tokens._make(_checked(_tensors.sample(logits, uniform, temperature, top_k, top_p, min_p, ws, _stream(device))))

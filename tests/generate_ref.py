@@ -56,3 +56,36 @@ def values4(codes, scales, k):
     index[:, 0::2], index[:, 1::2] = codes & 15, codes >> 4
     s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
     return (TABLE[index] * np.repeat(s, GROUP, axis=1))[:, :k]
+
+
+def sample(l, u, temperature, top_k, top_p, min_p):
+    """(index, share, kept, room) of one row of float64 logits, by sorting; room: how far, relative to all masses, the
+    decisions are from being other ones (0 where a sum is exactly a share)."""
+    order = np.lexsort((np.arange(l.size), -l))
+    order = order[l[order] > -np.inf]  # NaN sorts last and is dropped
+    if not order.size:
+        return -1, 0.0, 0, 1.0
+    if not temperature > 0:
+        return int(order[0]), 1.0, 1, 1.0
+    top = l[order[0]]
+    with np.errstate(invalid="ignore"):
+        x = np.where(l[order] == top, 0.0, (top - l[order]) / min(temperature, 1e300))
+    p = np.exp(-x.astype(np.longdouble))
+    k = top_k if 0 < top_k < order.size else order.size
+    keep, room = k, 1.0
+    if top_p < 1:
+        sums = np.cumsum(p[:k])
+        share = max(top_p, 0.0) * sums[-1]
+        keep = 1 + int(np.searchsorted(sums, share))
+        room = float(np.min(np.abs(sums - share)) / sums[-1])
+    if min_p > 0:
+        keep = min(keep, int(np.sum(x <= -np.log(min(min_p, 1.0)))))
+    kept = np.sort(order[:keep])
+    mass = np.zeros(l.size, np.longdouble)
+    mass[order[:keep]] = p[:keep]
+    sums = np.cumsum(mass[kept])
+    at = min(int(np.searchsorted(sums, u * sums[-1], side="right")), kept.size - 1)
+    while at > 0 and mass[kept[at]] == 0:
+        at -= 1
+    room = min(room, float(np.min(np.abs(sums - u * sums[-1])) / sums[-1]))
+    return int(kept[at]), float(mass[kept[at]] / sums[-1]), keep, room

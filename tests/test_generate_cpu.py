@@ -91,3 +91,36 @@ def test_layer_workspace_sizes(sd):  # noqa: F811
     assert _status(sd, sd.sdnn_experts_layer_workspace_size, 17, 8, 8, 4, 2) == 9
     assert _status(sd, sd.sdnn_experts_layer_workspace_size, 1, 8, 8, 4, 5) == 2
     assert sd.lib.sdnn_experts_layer_workspace_size(1, 8, 8, 4, 2, None) == 1
+
+
+def test_sample_refusals(sd):  # noqa: F811
+    good = dict(rows=3, vocab=40000, type=1, logits=FAKE, ldl=40000, uniform=FAKE, temperature=FAKE, top_k=FAKE,
+                top_p=FAKE, min_p=FAKE, ids=FAKE, prob=FAKE, kept=FAKE, ws=FAKE, ws_bytes=1 << 30)
+    changes = [(dict(rows=-1), 2), (dict(vocab=0), 2), (dict(vocab=1 << 31, ldl=1 << 31), 2), (dict(type=2), 2),
+               (dict(ldl=39999), 2), (dict(logits=FAKE + 1), 2), (dict(uniform=FAKE + 4), 2), (dict(ws=None), 1),
+               (dict(ws_bytes=100), 6), (dict(ws_bytes=-1), 6), (dict(ws=FAKE + 8), 2)]
+    changes += [({x: None}, 1) for x in ("logits", "uniform", "ids", "prob", "kept")]
+    changes += [({x: FAKE + 2}, 2) for x in ("temperature", "top_k", "top_p", "min_p", "ids", "prob", "kept")]
+    _refusals(sd, sd.sdnn_sample, good, changes)
+    assert _status(sd, sd.sdnn_sample, 0, 5, 0, None, 5, None, None, None, None, None, None, None, None, None, 0) == 0
+
+
+def test_sample_workspace_sizes(sd):  # noqa: F811
+    """One of the size for the most rows serves every smaller call."""
+    for vocab in (1, 100, 32768, 32769, 50021, 131072, 10**6, 5 * 10**6, 2**31 - 1):
+        sizes = [sd.sdnn_sample_workspace_size(r, vocab) for r in list(range(1100)) + [5000, 100000]]
+        assert sizes == sorted(sizes) and (sizes[1] == 0) == (vocab <= 32768)
+    assert _status(sd, sd.sdnn_sample_workspace_size, -1, 8) == 2
+    assert _status(sd, sd.sdnn_sample_workspace_size, 1, 0) == 2
+    assert sd.lib.sdnn_sample_workspace_size(1, 8, None) == 1
+
+
+def test_reference_sample():
+    """The reference by hand: four tokens of masses 8, 4, 2, 1 (in any order of the row)."""
+    l = np.log(np.array([2.0, 8.0, 1.0, 4.0]))
+    assert gen.sample(l, 0.0, 1.0, 0, 1.0, 0.0)[:3] == (0, pytest.approx(2 / 15), 4)
+    assert gen.sample(l, 0.5, 1.0, 0, 1.0, 0.0)[0] == 1 and gen.sample(l, 0.99, 1.0, 0, 1.0, 0.0)[0] == 3
+    assert gen.sample(l, 0.9, 1.0, 2, 1.0, 0.0)[:3] == (3, pytest.approx(4 / 12), 2)
+    assert gen.sample(l, 0.9, 1.0, 0, 0.75, 0.0)[2] == 2 and gen.sample(l, 0.9, 1.0, 0, 0.85, 0.0)[2] == 3
+    assert gen.sample(l, 0.9, 1.0, 0, 1.0, 0.2)[2] == 3 and gen.sample(l, 0.9, 0.0, 0, 1.0, 0.0)[:3] == (1, 1.0, 1)
+    assert gen.sample(np.full(3, -np.inf), 0.9, 1.0, 0, 1.0, 0.0)[:3] == (-1, 0.0, 0)
