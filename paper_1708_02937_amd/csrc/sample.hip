@@ -16,6 +16,7 @@
 #include "blocks8.h"
 #include "common.h"
 #include "lanes.h"
+#include "shared_memory.h"
 
 namespace sdnn {
 namespace {
@@ -24,6 +25,7 @@ constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kTile = kThreads * 8;   // tokens that a workgroup looks at in turn
 constexpr int kBuckets = 1024, kPerNat = 16;
 constexpr int kList = 4096;           // tokens of the last buckets that fit LDS; more are looked for in the row each time
+constexpr int kSorted = kThreads;     // up to so many are ranked by counting
 constexpr int kCountOnly = 1024;      // up to so many tokens kept by top_k, masses are not summed over the row
 constexpr int kBins = 2048;           // of one level of a selection by the bits of a logit: 11, 11 and 10 of them
 
@@ -70,8 +72,8 @@ struct SampleSpace {
     uint32_t *done;      // rows: chunks that are through with the last kernel
     uint32_t *counts;    // rows x buckets
     uint64_t *masses;    // rows x buckets
+    uint64_t *parts;     // rows x chunks x buckets: the chunk's masses
     double *whole;       // rows x chunks: mass of the chunk's tokens in buckets that are kept whole
-    uint32_t *kept;      // rows x chunks: how many they are
     uint32_t *listed;    // rows x chunks: tokens in the buckets that are looked at one by one
     uint32_t *list;      // rows x chunks x chunk / 8 of their indices
 };
@@ -84,7 +86,7 @@ int64_t chunk_of(int64_t rows, int64_t vocab) {
 }
 
 struct SampleSizes {
-    size_t done, counts, masses, whole, kept, listed, list, bytes;
+    size_t done, counts, masses, parts, whole, listed, list, bytes;
 };
 
 // Of bounds that grow with the rows, so that the space for the most rows holds any call of fewer.
@@ -93,10 +95,10 @@ SampleSizes sample_sizes(int64_t rows, int64_t vocab) {
     const size_t most = rows < 1024 ? 1024 : rows, chunks = (size_t)(rows < (int64_t)most / tiles ? rows * tiles : most);
     SampleSizes s;
     s.masses = align_up(chunks * 8);
-    s.whole = s.masses + align_up(rows * kBuckets * 8);
+    s.parts = s.masses + align_up(rows * kBuckets * 8);
+    s.whole = s.parts + align_up(chunks * kBuckets * 8);
     s.counts = s.whole + align_up(chunks * 8);
-    s.kept = s.counts + align_up(rows * kBuckets * 4);
-    s.listed = s.kept + align_up(chunks * 4);
+    s.listed = s.counts + align_up(rows * kBuckets * 4);
     s.list = s.listed + align_up(chunks * 4);
     s.done = s.list + align_up((size_t)rows * (tiles * kTile + chunk - kTile) / 8 * 4);
     s.bytes = s.done + align_up(rows * 4);
@@ -107,7 +109,7 @@ SampleSpace sample_space(void *ws, int64_t rows, int64_t vocab) {
     const SampleSizes s = sample_sizes(rows, vocab);
     char *p = (char *)ws;
     return {(uint64_t *)p,           (uint32_t *)(p + s.done), (uint32_t *)(p + s.counts), (uint64_t *)(p + s.masses),
-            (double *)(p + s.whole), (uint32_t *)(p + s.kept), (uint32_t *)(p + s.listed), (uint32_t *)(p + s.list)};
+            (uint64_t *)(p + s.parts), (double *)(p + s.whole), (uint32_t *)(p + s.listed), (uint32_t *)(p + s.list)};
 }
 
 // ------------------------------------------------------------------------------------------------ over a workgroup
@@ -234,13 +236,15 @@ __device__ __forceinline__ Row row_of(const SampleArgs &a, const Settings &s, fl
 }
 
 // What the buckets tell of a row.
+constexpr int kEach = kBuckets / kThreads;  // buckets of a thread
 struct Plan {
     int64_t k;          // tokens that top_k leaves
     bool cut_k, cut_p;  // whether there is anything to cut
-    int lo, hi;         // buckets that are looked at token by token; top_k and top_p keep those before whole
+    int lo, hi;         // buckets that are looked at token by token; those before are kept whole
     int64_t before;     // tokens of the buckets before lo, and their mass
     double above;
-    double all;         // the row's mass (0 where masses are not summed)
+    double all;          // the row's mass (0 where masses are not summed)
+    double unit[kEach];  // of the thread's buckets' masses
 };
 
 struct Shared {
@@ -250,20 +254,23 @@ struct Shared {
             uint64_t masses[kBins];
             uint32_t counts[kBins];
         } bins;
+        struct {
+            uint32_t key[kSorted], index[kSorted];
+            double mass[kSorted];
+            double upto[kSorted + 1];
+        } sorted;
     };
     uint32_t key[kList], index[kList];  // the list, in order of the indices
     double part[kWaves];
     uint64_t upart[kWaves];
     int64_t ipart[kWaves];
     int64_t found[4];
-    double value;
+    double value[2];
     uint32_t offset[kThreads + 1];  // of the chunks' parts of the list
     uint32_t last;
 };
 
 __device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared &sh) {
-    constexpr int kEach = kBuckets / kThreads;
-    const double unit = ldexp(1.0, -r.shift);
     Plan p;
     int64_t n[kEach], cells = 0;
     double m[kEach], sum = 0.0;
@@ -271,28 +278,28 @@ __device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared 
     for (int i = 0; i < kEach; i++) {
         const int b = threadIdx.x * kEach + i;
         n[i] = sh.hist.counts[b];
-        m[i] = s.masses ? (double)sh.hist.masses[b] * unit * exp(-(double)b / kPerNat) : 0.0;
+        p.unit[i] = s.masses ? ldexp(exp(-(double)b / kPerNat), -r.shift) : 0.0;
+        m[i] = s.masses ? (double)sh.hist.masses[b] * p.unit[i] : 0.0;
         cells += n[i], sum += m[i];
     }
     int64_t valid;
     const int64_t n0 = block_upto(cells, sh.ipart, valid) - cells;
-    const double m0 = block_upto(sum, sh.part, p.all) - sum;
+    p.all = 0.0;
+    const double m0 = s.masses ? block_upto(sum, sh.part, p.all) - sum : 0.0;
     p.k = s.top_k > 0 && s.top_k < valid ? s.top_k : valid;
     p.cut_k = p.k < valid;
     p.cut_p = s.top_p < 1.0;
     // the bucket of the k-th token, and the mass before and in it
-    if (threadIdx.x == 0) sh.found[0] = kBuckets - 1;
-    __syncthreads();
     int64_t c = n0;
     double q = m0;
 #pragma unroll
     for (int i = 0; i < kEach; i++) {
-        if (c < p.k && c + n[i] >= p.k) sh.found[0] = threadIdx.x * kEach + i, sh.value = q, sh.part[0] = m[i];
+        if (c < p.k && c + n[i] >= p.k) sh.found[0] = threadIdx.x * kEach + i, sh.value[0] = q, sh.value[1] = m[i];
         c += n[i], q += m[i];
     }
     __syncthreads();
     const int bucket_k = (int)sh.found[0];
-    const double before_k = sh.value, in_k = sh.part[0];
+    const double before_k = sh.value[0], in_k = sh.value[1];
     p.lo = kBuckets, p.hi = -1;
     if (!s.masses) {
         p.lo = 0, p.hi = bucket_k;
@@ -312,61 +319,56 @@ __device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared 
                     first = max64(first, kBuckets - b), last = max64(last, b + 1);
                 q += m[i];
             }
-            first = block_max(first, sh.upart), last = block_max(last, sh.upart);
-            if (first) {
-                p.lo = min(p.lo, kBuckets - (int)first);
-                if (!p.cut_k) p.hi = (int)last - 1;
+            first = block_max(first << 32 | last, sh.upart);  // the first bucket's `last` does not matter with one alone
+            if (first >> 32) {
+                p.lo = min(p.lo, kBuckets - (int)(first >> 32));
+                if (!p.cut_k) p.hi = (int)block_max(last, sh.upart) - 1;
             }
+        }
+        // where min_p cuts before
+        if (r.most_x < (double)INFINITY) {
+            const int bucket_m = Row::bucket(r.most_x);
+            if (bucket_m < p.lo) p.lo = p.hi = bucket_m, p.cut_k = p.cut_p = false;
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) sh.found[0] = valid, sh.value = p.all;  // of a row whose buckets are all kept whole
+    if (threadIdx.x == 0) sh.found[0] = valid, sh.value[0] = p.all;  // of a row whose buckets are all kept whole
     __syncthreads();
     c = n0, q = m0;
 #pragma unroll
     for (int i = 0; i < kEach; i++) {
-        if ((int)threadIdx.x * kEach + i == p.lo) sh.found[0] = c, sh.value = q;
+        if ((int)threadIdx.x * kEach + i == p.lo) sh.found[0] = c, sh.value[0] = q;
         c += n[i], q += m[i];
     }
     __syncthreads();
-    p.before = sh.found[0], p.above = sh.value;
+    p.before = sh.found[0], p.above = sh.value[0];
     __syncthreads();
     return p;
 }
 
-// Tokens [begin, end), a tile at a time: the mass and number of those in buckets kept whole, and the others' indices in
-// order to put(place, index, key).  Returns how many others there are.
+// The indices of the tokens in buckets lo to hi among [begin, end), in order, to put(place, index, key); returns how many
+// places there are then.
 template <typename T, typename F>
-__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Row &r, const Plan &p,
-                                            Shared &sh, uint32_t placed, double &whole, uint32_t &kept, F put) {
-    double sum = 0.0;
-    uint32_t count = 0;
+__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Row &r, const Plan &p, Shared &sh,
+                                            F put) {
+    uint32_t placed = 0;
     for (int64_t c0 = begin; c0 < end; c0 += kTile) {
         const int64_t c = c0 + threadIdx.x * 8;
         uint32_t k[8], mask = 0;
         keys8(row, c, end, k);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            if (!k[i]) continue;
-            const double x = r.x(logit_of_key(k[i]));
-            const int b = Row::bucket(x);
-            if (b < p.lo) {
-                if (x <= r.most_x) sum += mass(x), count++;
-            } else if (b <= p.hi) {
-                mask |= 1u << i;
-            }
+            const int b = k[i] ? Row::bucket(r.x(logit_of_key(k[i]))) : kBuckets;
+            if (b >= p.lo && b <= p.hi) mask |= 1u << i;
         }
-        if (p.hi < 0) continue;
-        int64_t all;
+        uint64_t all;
         const int mine = __popc(mask);
-        uint32_t at = placed + (uint32_t)(block_upto((int64_t)mine, sh.ipart, all) - mine);
+        uint32_t at = placed + (uint32_t)block_upto((uint64_t)mine, sh.upart, all) - mine;
 #pragma unroll
         for (int i = 0; i < 8; i++)
             if (mask >> i & 1) put(at++, (uint32_t)(c + i), k[i]);
         placed += (uint32_t)all;
     }
-    whole = block_sum(sum, sh.part);
-    kept = (uint32_t)block_sum((int64_t)count, sh.ipart);
     return placed;
 }
 
@@ -401,8 +403,22 @@ struct Listed {
 
 // The index of the rank-th token with that key (from 1 on) in order of the indices.
 template <typename T>
-__device__ __forceinline__ int64_t nth_equal(const T *row, int64_t vocab, uint32_t key, int64_t rank, Shared &sh) {
+__device__ __forceinline__ int64_t nth_equal(const Listed<T> &l, uint32_t key, int64_t rank, Shared &sh) {
     int64_t before = 0;
+    if (l.n >= 0) {
+        for (int c0 = 0; c0 < l.n; c0 += kThreads) {
+            const int i = c0 + threadIdx.x;
+            const bool equal = i < l.n && sh.key[i] == key;
+            int64_t all;
+            const int64_t upto = before + block_upto((int64_t)equal, sh.ipart, all);
+            if (equal && upto == rank) sh.found[0] = sh.index[i];
+            before += all;
+        }
+        __syncthreads();
+        return sh.found[0];
+    }
+    const T *row = l.row;
+    const int64_t vocab = l.r.vocab;
     for (int64_t c0 = 0; c0 < vocab; c0 += kTile) {
         const int64_t c = c0 + threadIdx.x * 8;
         uint32_t k[8];
@@ -489,153 +505,160 @@ __device__ __forceinline__ End select(const Listed<T> &l, uint64_t target, Share
     rank = rank < 1 ? 1 : rank;
     End end;
     end.key = prefix;
-    end.index = rank >= equal ? l.r.vocab : nth_equal(l.row, l.r.vocab, prefix, rank, sh);
+    end.index = rank >= equal ? l.r.vocab : nth_equal(l, prefix, rank, sh);
     __syncthreads();
     return end;
 }
 
-// The whole row's end, from the list and the chunks' sums (whole, kept: of the buckets kept whole, one value to a chunk).
+// What is kept of a row, and what is drawn of it.
+struct Kept {
+    End k, p;
+    double most_x;
+    int64_t count;
+    double total, drawn;
+    __device__ __forceinline__ bool holds(uint32_t key, int64_t index, double x) const {
+        return k.holds(key, index) && p.holds(key, index) && x <= most_x;
+    }
+};
+
+__device__ __forceinline__ Kept all_of(const Settings &s, const Row &r, const Plan &p) {
+    Kept k;
+    k.most_x = r.most_x, k.count = p.before, k.total = p.above, k.drawn = s.u * p.above;
+    return k;
+}
+
+__device__ __forceinline__ void answer(const SampleArgs &a, int64_t at, int64_t id, double prob, int64_t kept) {
+    a.ids[at] = (int32_t)id;
+    a.prob[at] = (float)prob;
+    a.kept[at] = (int32_t)kept;
+}
+
+// The token within [begin, end), whose kept tokens come after a mass of `before`: a thread takes a run of them.
 template <typename T>
-__device__ __forceinline__ void finish(const SampleArgs &a, int64_t at, const T *row, const Settings &s, const Row &r,
-                                       const Plan &p, int listed, Shared &sh, double *whole, uint32_t *kept,
-                                       const uint32_t *offset, int64_t chunks, int64_t chunk) {
-    const Listed<T> l{row, r, p, sh, listed};
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    End end_k, end_p;  // everything
-    if (p.cut_k && p.hi >= 0)
-        end_k = select<false>(l, (uint64_t)(p.k - p.before), sh, [](uint32_t, uint32_t) { return true; });
-    if (p.cut_p && p.hi >= 0) {
+__device__ __forceinline__ void draw_in(const SampleArgs &a, int64_t at, const T *row, const Row &r, const Kept &kept,
+                                        int64_t begin, int64_t end, double before, Shared &sh) {
+    const int64_t each = (end - begin + kTile - 1) / kTile * 8;
+    const int64_t from = min(begin + threadIdx.x * each, end), to = min(from + each, end);
+    double sum = 0.0;
+    for (int64_t c = from; c < to; c += 8) {
+        uint32_t k[8];
+        keys8(row, c, to, k);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (!k[i]) continue;
+            const double x = r.x(logit_of_key(k[i]));
+            if (kept.holds(k[i], c + i, x)) sum += mass(x);
+        }
+    }
+    double all;
+    const double upto = before + block_upto(sum, sh.part, all);
+    // the thread whose run passes the drawn share, or the last that has any mass
+    const uint64_t first = block_max(sum > 0.0 && upto > kept.drawn ? kThreads - threadIdx.x : 0, sh.upart);
+    const uint64_t any = block_max(sum > 0.0 ? threadIdx.x + 1 : 0, sh.upart);
+    if (!any) {
+        if (threadIdx.x == 0) answer(a, at, -1, 0.0, kept.count);
+        return;
+    }
+    if ((int64_t)threadIdx.x != (first ? kThreads - (int64_t)first : (int64_t)any - 1)) return;
+    double q = upto - sum, last = 0.0;
+    int64_t id = -1;
+    for (int64_t c = from; c < to; c++) {
+        const uint32_t k = key_of(load_f32(row + c));
+        if (!k) continue;
+        const double x = r.x(logit_of_key(k));
+        const double m = kept.holds(k, c, x) ? mass(x) : 0.0;
+        if (!(m > 0.0)) continue;
+        id = c, last = m;
+        q += m;
+        if (q > kept.drawn) break;
+    }
+    answer(a, at, id, last / kept.total, kept.count);
+}
+
+// A list of up to a token for each thread: each finds its rank by counting the larger ones, and everything goes by ranks from
+// there.  Leaves in sh.sorted.upto the mass of the kept ones among the list's first so many.  Returns true if the token is drawn
+// and answered, which it is where no bucket is kept whole.
+__device__ __forceinline__ bool by_rank(const SampleArgs &a, int64_t at, const Settings &s, const Row &r, const Plan &p, int n,
+                                        Shared &sh, Kept &kept) {
+    const int i = threadIdx.x;
+    const bool mine = i < n;
+    const uint32_t key = mine ? sh.key[i] : 0;
+    int rank = 0;
+    if ((i & ~63) < n) {  // equal ones before a token are larger, and equal ones after it are not
+        const int w0 = i & ~63, w1 = min(w0 + 64, n);
+#pragma unroll 8
+        for (int j = 0; j < w0; j++) rank += sh.key[j] >= key;
+        for (int j = w0; j < w1; j++) rank += sh.key[j] > key || (sh.key[j] == key && j < i);
+#pragma unroll 8
+        for (int j = w1; j < n; j++) rank += sh.key[j] > key;
+    }
+    double m = 0.0;
+    bool stays = false;
+    if (mine) {
+        const double x = r.x(logit_of_key(key));
+        m = mass(x);
+        stays = x <= r.most_x;
+        sh.sorted.key[rank] = key, sh.sorted.index[rank] = sh.index[i], sh.sorted.mass[rank] = m;
+    }
+    int64_t left = block_sum((int64_t)stays, sh.ipart);  // what min_p leaves; its barriers make the sorted list visible too
+    const int64_t left_k = p.cut_k ? p.k - p.before : n;
+    left = min(left, left_k);
+    if (p.cut_p) {
+        double all;
+        const double v = mine && i < left_k ? sh.sorted.mass[i] : 0.0, upto = block_upto(v, sh.part, all);
+        const double share = s.masses && !p.cut_k ? p.all : p.above + all, target = s.top_p * share - p.above;
+        // the first that reaches the share, if any does
+        const uint64_t reach = block_max(mine && upto >= target ? (uint64_t)(kThreads - i) : 0, sh.upart);
+        if (reach) left = min(left, (int64_t)kThreads - (int64_t)reach + 1);
+    }
+    kept.count = p.before + left;
+    if (!mine || rank >= left) m = 0.0;
+    double listed;
+    const double upto = block_upto(m, sh.part, listed);
+    kept.total = p.above + listed;
+    kept.drawn = s.u * kept.total;
+    if (p.lo == 0) {
+        const uint64_t first = block_max(m > 0.0 && upto > kept.drawn ? (uint64_t)(kThreads - i) : 0, sh.upart);
+        const uint64_t any = first ? 1 : block_max(m > 0.0 ? (uint64_t)(i + 1) : 0, sh.upart);
+        if (i == (first ? kThreads - (int)first : (int)any - 1)) answer(a, at, sh.index[i], m / kept.total, kept.count);
+        return true;
+    }
+    if (i == 0) sh.sorted.upto[0] = 0.0;
+    sh.sorted.upto[i + 1] = upto;
+    // the kept tokens of the list are those up to the last one's place in the order
+    kept.k.key = sh.sorted.key[left > 0 ? left - 1 : 0];
+    kept.k.index = (int64_t)sh.sorted.index[left > 0 ? left - 1 : 0] - (left > 0 ? 0 : 1);
+    __syncthreads();
+    return false;
+}
+
+// Longer lists.
+template <typename T>
+__device__ __forceinline__ void by_select(const Settings &s, const Row &r, const Plan &p, const Listed<T> &l, Shared &sh,
+                                          Kept &kept) {
+    if (p.cut_k) kept.k = select<false>(l, (uint64_t)(p.k - p.before), sh, [](uint32_t, uint32_t) { return true; });
+    if (p.cut_p) {
         double share = p.all;
         if (!s.masses || p.cut_k) {
             double sum = 0.0;
             l.each([&](uint32_t k, uint32_t i) {
-                if (end_k.holds(k, i)) sum += mass(r.x(logit_of_key(k)));
+                if (kept.k.holds(k, i)) sum += mass(r.x(logit_of_key(k)));
             });
-            share = (s.masses ? p.above : 0.0) + block_sum(sum, sh.part);
+            share = p.above + block_sum(sum, sh.part);
         }
-        const double rest = (s.top_p * share - (s.masses ? p.above : 0.0)) * exp((double)p.lo / kPerNat);
-        const double units = ceil(rest * ldexp(1.0, r.shift));
-        end_p = select<true>(l, units >= 1.0 ? (uint64_t)units : 1ull, sh,
-                             [&](uint32_t k, uint32_t i) { return end_k.holds(k, i); });
+        const double units = ceil((s.top_p * share - p.above) * exp((double)p.lo / kPerNat) * ldexp(1.0, r.shift));
+        kept.p = select<true>(l, units >= 1.0 ? (uint64_t)units : 1ull, sh,
+                              [&](uint32_t k, uint32_t i) { return kept.k.holds(k, i); });
     }
-    auto in = [&](uint32_t k, int64_t i, double x) { return end_k.holds(k, i) && end_p.holds(k, i) && x <= r.most_x; };
-    // each chunk's mass, and the number of all
+    double sum = 0.0;
     int64_t count = 0;
-    if (listed >= 0) {
-        for (int64_t c = wave; c < chunks; c += kWaves) {
-            double sum = 0.0;
-            if (listed > 0)
-                for (uint32_t i = offset[c] + lane; i < offset[c + 1]; i += 64) {
-                    const double x = r.x(logit_of_key(sh.key[i]));
-                    if (in(sh.key[i], sh.index[i], x)) sum += mass(x), count++;
-                }
-            sum = wave_sum(sum);
-            if (lane == 0) {
-                count += kept[c];
-                whole[c] += sum;
-            }
-        }
-    } else {
-        for (int64_t c = 0; c < chunks; c++) {
-            double sum = 0.0;
-            const int64_t end = min((c + 1) * chunk, r.vocab);
-            for (int64_t t = c * chunk + threadIdx.x * 8; t < end; t += kTile) {
-                uint32_t k[8];
-                keys8(row, t, end, k);
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    if (!k[i]) continue;
-                    const double x = r.x(logit_of_key(k[i]));
-                    if (in(k[i], t + i, x)) sum += mass(x), count++;
-                }
-            }
-            sum = block_sum(sum, sh.part);
-            if (threadIdx.x == 0) whole[c] = sum;
-        }
-    }
-    count = block_sum(count, sh.ipart);
-    // the chunk in which the mass exceeds the drawn share, or the last that has any
-    double total = 0.0;
-    for (int64_t c0 = 0; c0 < chunks; c0 += kThreads) {
-        double all;
-        block_upto(c0 + threadIdx.x < chunks ? whole[c0 + threadIdx.x] : 0.0, sh.part, all);
-        total += all;
-    }
-    const double drawn = s.u * total;
-    if (threadIdx.x == 0) sh.found[0] = -1;
-    __syncthreads();
-    double before = 0.0;
-    int64_t last = -1;
-    for (int64_t c0 = 0; c0 < chunks; c0 += kThreads) {
-        const int64_t c = c0 + threadIdx.x;
-        const double w = c < chunks ? whole[c] : 0.0;
-        double all;
-        const double upto = before + block_upto(w, sh.part, all);
-        const uint64_t hit = block_max(w > 0.0 && upto > drawn ? kThreads - threadIdx.x : 0, sh.upart);
-        const uint64_t any = block_max(w > 0.0 ? threadIdx.x + 1 : 0, sh.upart);
-        if (any) last = c0 + (int64_t)any - 1;
-        if (hit) {
-            last = c0 + kThreads - (int64_t)hit;
-            if (threadIdx.x == kThreads - hit) sh.value = upto - w;
-            break;
-        }
-        if (any && (int64_t)threadIdx.x == (int64_t)any - 1) sh.value = upto - w;
-        before += all;
-    }
-    __syncthreads();
-    before = sh.value;
-    // the token in that chunk
-    int64_t id = -1;
-    double prob = 0.0;
-    if (last >= 0) {
-        const int64_t end = min((last + 1) * chunk, r.vocab);
-        for (int64_t c0 = last * chunk; c0 < end; c0 += kTile) {
-            const int64_t c = c0 + threadIdx.x * 8;
-            uint32_t k[8];
-            double m[8], sum = 0.0;
-            keys8(row, c, end, k);
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                m[i] = 0.0;
-                if (!k[i]) continue;
-                const double x = r.x(logit_of_key(k[i]));
-                if (in(k[i], c + i, x)) m[i] = mass(x);
-                sum += m[i];
-            }
-            double all;
-            double upto = before + block_upto(sum, sh.part, all) - sum;
-            int hit = 8, some = -1;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                upto += m[i];
-                if (m[i] > 0.0) {
-                    some = i;
-                    if (hit == 8 && upto > drawn) hit = i;
-                }
-            }
-            const uint64_t first = block_max(hit < 8 ? kThreads - threadIdx.x : 0, sh.upart);
-            const uint64_t any = block_max(some >= 0 ? threadIdx.x + 1 : 0, sh.upart);
-            const int64_t owner = first ? kThreads - (int64_t)first : (int64_t)any - 1;
-            if ((int64_t)threadIdx.x == owner) {
-                const int i = first ? hit : some;
-                double v = 0.0;
-#pragma unroll
-                for (int j = 0; j < 8; j++)
-                    if (j == i) v = m[j];
-                sh.found[0] = c + i, sh.value = v;
-            }
-            __syncthreads();
-            if (any) id = sh.found[0], prob = sh.value / total;
-            __syncthreads();
-            if (first) break;
-            before += all;
-        }
-    }
-    if (threadIdx.x == 0) {
-        a.ids[at] = (int32_t)id;
-        a.prob[at] = (float)prob;
-        a.kept[at] = (int32_t)count;
-    }
+    l.each([&](uint32_t k, uint32_t i) {
+        const double x = r.x(logit_of_key(k));
+        if (kept.holds(k, i, x)) sum += mass(x), count++;
+    });
+    kept.total = p.above + block_sum(sum, sh.part);
+    kept.count = p.before + block_sum(count, sh.ipart);
+    kept.drawn = s.u * kept.total;
 }
 
 // A row without a token to take, or whose largest logit is taken: true if that is all.
@@ -643,22 +666,18 @@ __device__ __forceinline__ bool settled(const SampleArgs &a, int64_t at, const S
     const bool none = best == 0;
     if (!none && !s.greedy) return false;
     if (writes && threadIdx.x == 0) {
-        a.ids[at] = none ? -1 : (int32_t)~(uint32_t)best;
-        a.prob[at] = none ? 0.0f : 1.0f;
-        a.kept[at] = none ? 0 : 1;
+        answer(a, at, none ? -1 : (int32_t)~(uint32_t)best, none ? 0.0 : 1.0, none ? 0 : 1);
     }
     return true;
 }
 
 // ------------------------------------------------------------------------------------------------ kernels
 // A short row by one workgroup, in one launch.
-constexpr int kShortTiles = 8;
+constexpr int64_t kShort = 8 * kTile;
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, int shift) {
     __shared__ Shared sh;
-    __shared__ double whole[kShortTiles];
-    __shared__ uint32_t kept[kShortTiles];
     const int64_t at = blockIdx.x;
     const T *row = (const T *)a.logits + at * a.ld;
     const Settings s = settings_of(a, at);
@@ -670,20 +689,19 @@ __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, in
     count_buckets(row, 0, a.vocab, r, s.masses, sh.hist);
     __syncthreads();
     const Plan p = plan_of(s, r, sh);
-    uint32_t placed = 0;
-    const int64_t tiles = (a.vocab + kTile - 1) / kTile;
-    if (threadIdx.x == 0) sh.offset[0] = 0;
-    for (int64_t c = 0; c < tiles; c++) {
-        double w;
-        uint32_t n;
-        placed = collect(row, c * kTile, min((c + 1) * kTile, a.vocab), r, p, sh, placed, w, n,
-                         [&](uint32_t place, uint32_t index, uint32_t key) {
-                             if (place < kList) sh.key[place] = key, sh.index[place] = index;
-                         });
-        if (threadIdx.x == 0) whole[c] = w, kept[c] = n, sh.offset[c + 1] = placed;
-    }
+    uint32_t n = 0;
+    if (p.hi >= 0)
+        n = collect(row, 0, a.vocab, r, p, sh, [&](uint32_t place, uint32_t index, uint32_t key) {
+            if (place < kList) sh.key[place] = key, sh.index[place] = index;
+        });
     __syncthreads();
-    finish(a, at, row, s, r, p, placed <= kList ? (int)placed : -1, sh, whole, kept, sh.offset, tiles, kTile);
+    Kept kept = all_of(s, r, p);
+    if (n > 0 && n <= kSorted) {
+        if (by_rank(a, at, s, r, p, (int)n, sh, kept)) return;
+    } else if (n > 0) {
+        by_select(s, r, p, Listed<T>{row, r, p, sh, n <= kList ? (int)n : -1}, sh, kept);
+    }
+    draw_in(a, at, row, r, kept, 0, a.vocab, 0.0, sh);
 }
 
 // Longer ones in three: the largest logit of each chunk; the buckets; the list, and the row's end by whichever workgroup
@@ -724,6 +742,8 @@ __global__ void __launch_bounds__(kThreads) sample_count_kernel(SampleArgs a, Sa
         atomicAdd(&ws.counts[at * kBuckets + b], hist.counts[b]);
         if (s.masses) atomicAdd((unsigned long long *)&ws.masses[at * kBuckets + b], (unsigned long long)hist.masses[b]);
     }
+    if (s.masses)
+        for (int b = threadIdx.x; b < kBuckets; b += kThreads) ws.parts[blockIdx.x * (int64_t)kBuckets + b] = hist.masses[b];
 }
 
 template <typename T>
@@ -742,47 +762,128 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
     const Plan p = plan_of(s, r, sh);
     const uint32_t room = (uint32_t)(chunk / 8);
     uint32_t *const list = ws.list + (at * chunks + c) * room;
-    double whole;
-    uint32_t kept;
-    const uint32_t placed = collect(row, c * chunk, min((c + 1) * chunk, a.vocab), r, p, sh, 0, whole, kept,
-                                    [&](uint32_t place, uint32_t index, uint32_t) {
-                                        if (place < room) list[place] = index;
-                                    });
-    if (threadIdx.x == 0)
-        ws.whole[at * chunks + c] = whole, ws.kept[at * chunks + c] = kept, ws.listed[at * chunks + c] = placed;
-    __threadfence();
+    uint32_t placed = 0;
+    if (p.hi >= 0)
+        placed = collect(row, c * chunk, min((c + 1) * chunk, a.vocab), r, p, sh,
+                         [&](uint32_t place, uint32_t index, uint32_t) {
+                             if (place < room) put_shared(list + place, index);
+                         });
+    if (p.lo > 0 && s.masses) {
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kEach; i++) {
+            const int b = threadIdx.x * kEach + i;
+            if (b < p.lo) sum += (double)ws.parts[blockIdx.x * (int64_t)kBuckets + b] * p.unit[i];
+        }
+        sum = block_sum(sum, sh.part);
+        if (threadIdx.x == 0) put_shared(ws.whole + blockIdx.x, sum);
+    }
+    if (threadIdx.x == 0) put_shared(ws.listed + blockIdx.x, placed);
+    stores_arrived();
     __syncthreads();
     if (threadIdx.x == 0) sh.last = atomicAdd(&ws.done[at], 1u) == (uint32_t)chunks - 1;
     __syncthreads();
     if (!sh.last) return;
-    __threadfence();
     // the chunks' lists in LDS, where they fit
-    bool fits = chunks <= kThreads;
-    if (fits) {
-        const uint32_t mine = threadIdx.x < chunks ? ws.listed[at * chunks + threadIdx.x] : 0;
+    int64_t n = 0;
+    bool fits = true;
+    for (int64_t c0 = 0; c0 < chunks; c0 += kThreads) {
+        const uint32_t mine = c0 + threadIdx.x < chunks ? get_shared(ws.listed + at * chunks + c0 + threadIdx.x) : 0;
         int64_t all;
         const int64_t upto = block_upto((int64_t)mine, sh.ipart, all);
-        if ((int64_t)threadIdx.x < chunks) sh.offset[threadIdx.x + 1] = (uint32_t)upto;
-        if (threadIdx.x == 0) sh.offset[0] = 0;
-        fits = block_max(mine > room, sh.upart) == 0 && all <= kList;
-        __syncthreads();
+        if (c0 == 0) sh.offset[threadIdx.x + 1] = (uint32_t)upto;
+        if (c0 == 0 && threadIdx.x == 0) sh.offset[0] = 0;
+        fits = block_max(mine > room, sh.upart) == 0 && fits;
+        n += all;
     }
-    int listed = -1;
-    if (fits) {
-        const int lane = threadIdx.x % 64;
-        for (int64_t w = threadIdx.x / 64; w < chunks; w += kWaves)
-            for (uint32_t i = lane; i < sh.offset[w + 1] - sh.offset[w]; i += 64) {
-                const uint32_t index = ws.list[(at * chunks + w) * room + i];
-                sh.index[sh.offset[w] + i] = index;
-                sh.key[sh.offset[w] + i] = key_of(load_f32(row + index));
+    __syncthreads();
+    fits = fits && n <= kList && chunks <= kThreads;
+    if (fits && n > 0) {
+        // a thread finds the chunk of its place
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            int low = 0, high = (int)chunks;  // offset[low] <= i < offset[high]
+            while (high - low > 1) {
+                const int mid = (low + high) / 2;
+                if (sh.offset[mid] <= (uint32_t)i)
+                    low = mid;
+                else
+                    high = mid;
             }
-        listed = (int)sh.offset[chunks];
+            const uint32_t index = get_shared(ws.list + (at * chunks + low) * room + (i - sh.offset[low]));
+            sh.index[i] = index;
+            sh.key[i] = key_of(load_f32(row + index));
+        }
         __syncthreads();
     }
-    finish(a, at, row, s, r, p, listed, sh, ws.whole + at * chunks, ws.kept + at * chunks, sh.offset, chunks, chunk);
+    Kept kept = all_of(s, r, p);
+    const bool ranked = fits && n > 0 && n <= kSorted;
+    if (ranked) {
+        if (by_rank(a, at, s, r, p, (int)n, sh, kept)) return;
+    } else if (n > 0) {
+        const Listed<T> l{row, r, p, sh, fits ? (int)n : -1};
+        by_select(s, r, p, l, sh, kept);
+        // the list's part of each chunk's mass
+        if (fits) {
+            const int lane = threadIdx.x % 64;
+            for (int64_t w = threadIdx.x / 64; w < chunks; w += kWaves) {
+                double sum = 0.0;
+                for (uint32_t i = sh.offset[w] + lane; i < sh.offset[w + 1]; i += 64) {
+                    const double x = r.x(logit_of_key(sh.key[i]));
+                    if (kept.holds(sh.key[i], sh.index[i], x)) sum += mass(x);
+                }
+                sum = wave_sum(sum);
+                if (lane == 0) {
+                    double *const of = ws.whole + at * chunks + w;
+                    put_shared(of, (p.lo > 0 && s.masses ? get_shared(of) : 0.0) + sum);
+                }
+            }
+        } else {
+            for (int64_t w = 0; w < chunks; w++) {
+                double sum = 0.0;
+                const int64_t end = min((w + 1) * chunk, a.vocab);
+                for (int64_t t = w * chunk + threadIdx.x * 8; t < end; t += kTile) {
+                    uint32_t k[8];
+                    keys8(row, t, end, k);
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        if (!k[i]) continue;
+                        const double x = r.x(logit_of_key(k[i]));
+                        if (kept.holds(k[i], t + i, x)) sum += mass(x);
+                    }
+                }
+                sum = block_sum(sum, sh.part);
+                if (threadIdx.x == 0) put_shared(ws.whole + at * chunks + w, sum);
+            }
+        }
+        stores_arrived();
+        __syncthreads();
+    }
+    // the chunk whose tokens pass the drawn share, or the last that has any mass
+    int64_t chosen = 0;
+    double before = 0.0, start = 0.0;
+    for (int64_t c0 = 0; c0 < chunks; c0 += kThreads) {
+        const int64_t w = c0 + threadIdx.x;
+        double m = w < chunks ? get_shared(ws.whole + at * chunks + w) : 0.0;
+        if (ranked && w < chunks) m += sh.sorted.upto[sh.offset[w + 1]] - sh.sorted.upto[sh.offset[w]];
+        double all;
+        const double upto = before + block_upto(m, sh.part, all);
+        const uint64_t hit = block_max(m > 0.0 && upto > kept.drawn ? kThreads - threadIdx.x : 0, sh.upart);
+        const uint64_t any = hit ? 1 : block_max(m > 0.0 ? threadIdx.x + 1 : 0, sh.upart);
+        if (any) {
+            const int64_t owner = hit ? kThreads - (int64_t)hit : (int64_t)any - 1;
+            if ((int64_t)threadIdx.x == owner) sh.value[0] = upto - m;
+            chosen = c0 + owner;
+            __syncthreads();
+            start = sh.value[0];
+            __syncthreads();
+        }
+        if (hit) break;
+        before += all;
+    }
+    draw_in(a, at, row, r, kept, chosen * chunk, min((chosen + 1) * chunk, a.vocab), start, sh);
 }
 
-bool is_short(int64_t vocab) { return vocab <= kShortTiles * kTile; }
+bool is_short(int64_t vocab) { return vocab <= kShort; }
 
 template <typename T>
 hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
