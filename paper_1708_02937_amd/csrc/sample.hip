@@ -7,8 +7,11 @@
 //
 // Which token it is goes by sums in 64 bits: 32 do not tell the tokens of a large vocabulary apart.  Nothing is sorted.  A
 // row's tokens are counted in buckets of x, a 16th wide, with their mass as whole numbers, so that the order of the additions
-// does not matter; the buckets tell where the order ends, within a bucket or a few, and only the tokens of those are looked
-// at one by one.  Buckets above them are kept whole.
+// does not matter; the buckets tell where the order ends, within a bucket or a few, and only the tokens of those, the list, are
+// looked at one by one.  Buckets before them are kept whole.
+//
+// A token is a number: its logit's place in the order of floats above the complement of its index, so that a larger one
+// comes first and no two are equal.
 //
 // A bucket's masses are in units of exp(-b / 16) 2^-shift: e^-d for 0 <= d < 1/16 is a polynomial of degree 8 (the next term is
 // 4e-17), and the sum of a bucket is as exact as its values.  The last bucket is x >= 63.9: its tokens count, but their mass,
@@ -22,12 +25,11 @@ namespace sdnn {
 namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / 64;
-constexpr int kTile = kThreads * 8;   // tokens that a workgroup looks at in turn
-constexpr int kBuckets = 1024, kPerNat = 16;
-constexpr int kList = 4096;           // tokens of the last buckets that fit LDS; more are looked for in the row each time
-constexpr int kSorted = kThreads;     // up to so many are ranked by counting
-constexpr int kCountOnly = 1024;      // up to so many tokens kept by top_k, masses are not summed over the row
-constexpr int kBins = 2048;           // of one level of a selection by the bits of a logit: 11, 11 and 10 of them
+constexpr int kTile = kThreads * 8;  // tokens that a workgroup looks at in turn
+constexpr int kBuckets = 1024, kPerNat = 16, kEach = kBuckets / kThreads;
+constexpr int kList = 4096;          // tokens of the list that fit LDS; of a longer one they are looked for in the row each time
+constexpr int kRanked = kThreads;    // up to so many are ranked by counting
+constexpr int kCountOnly = 1024;     // up to so many tokens kept by top_k, masses are not summed over the row
 
 // The order of logits as numbers above 0; 0 for one that cannot be taken (-inf, NaN).
 __device__ __forceinline__ uint32_t key_of(float l) {
@@ -38,17 +40,54 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 __device__ __forceinline__ float logit_of_key(uint32_t k) {
     return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
+__device__ __forceinline__ uint64_t token_of(uint32_t key, int64_t index) {
+    return (uint64_t)key << 32 | (uint32_t)~(uint32_t)index;
+}
+__device__ __forceinline__ int64_t index_of(uint64_t token) { return (uint32_t)~(uint32_t)token; }
 
+// Settings of a row, and x of its logits.
 struct Row {
-    int64_t vocab;
+    double u, top_p, inverse;  // of the temperature
+    double most_x;             // x of min_p
+    int64_t top_k;
     float top;  // largest logit
-    double inverse;  // of the temperature
-    double most_x;   // x of min_p
-    int shift;
+    bool greedy, masses;
 
-    __device__ __forceinline__ double x(float l) const { return l == top ? 0.0 : ((double)top - (double)l) * inverse; }
-    __device__ __forceinline__ static int bucket(double x) { return (int)fmin(x * kPerNat, (double)(kBuckets - 1)); }
+    __device__ __forceinline__ double x(uint32_t key) const {
+        const float l = logit_of_key(key);
+        return l == top ? 0.0 : ((double)top - (double)l) * inverse;
+    }
 };
+
+__device__ __forceinline__ Row row_of(const SampleArgs &a, int64_t at) {
+    Row r;
+    double temperature = a.temperature ? (double)a.temperature[at] : 1.0;
+    const double min_p = a.min_p ? (double)a.min_p[at] : 0.0;
+    r.u = a.uniform[at];
+    r.top_k = a.top_k ? a.top_k[at] : 0;
+    r.top_p = a.top_p ? (double)a.top_p[at] : 1.0;
+    if (r.top_p < 0.0) r.top_p = 0.0;
+    r.greedy = !(temperature > 0.0);
+    if (temperature == (double)INFINITY) temperature = 1e300;  // every token alike
+    r.inverse = 1.0 / temperature;
+    r.most_x = min_p > 0.0 ? -log(fmin(min_p, 1.0)) : (double)INFINITY;
+    r.masses = !(r.top_k > 0 && r.top_k <= kCountOnly);
+    return r;
+}
+
+// Buckets of a range of x.  The whole row's are a 16th wide; the list's tokens are counted again in narrower ones.
+struct Level {
+    double start, width, inverse;  // of the width
+    __device__ __forceinline__ int bucket(double x) const {
+        return (int)fmin(fmax((x - start) * inverse, 0.0), (double)(kBuckets - 1));
+    }
+    __device__ __forceinline__ double from(int b) const { return fma((double)b, width, start); }
+};
+__device__ __forceinline__ Level row_level() { return {0.0, 1.0 / kPerNat, (double)kPerNat}; }
+__device__ __forceinline__ Level list_level(int lo, int hi) {
+    const double width = (double)(hi - lo + 1) / (kPerNat * kBuckets);
+    return {(double)lo / kPerNat, width, 1.0 / width};
+}
 
 // e^-d, 0 <= d <= 1/16.
 __device__ __forceinline__ double exp_small(double d) {
@@ -58,24 +97,45 @@ __device__ __forceinline__ double exp_small(double d) {
     return fma(-d, e, 1.0);
 }
 
-// The mass of x in its bucket's unit, a whole number of 2^-shift.
-__device__ __forceinline__ uint64_t whole_mass(const Row &r, double x, int b) {
-    if (b == kBuckets - 1) return 0;
-    const double magic = __hiloint2double((1023 + 52 - r.shift) << 20, 0);  // its last place is 2^-shift
-    return (uint64_t)__double_as_longlong(exp_small(x - (double)b / kPerNat) + magic) & ((1ull << 52) - 1);
+// Past this tokens have no mass: the row's last bucket.
+__device__ __forceinline__ bool weighs(double x) { return x * kPerNat < (double)(kBuckets - 1); }
+
+// e^-x from e^-(b / 16) of the bucket b that x is in.
+__device__ __forceinline__ double mass(double x, const double *table) {
+    if (!weighs(x)) return 0.0;
+    const int b = (int)(x * kPerNat);
+    return table[b] * exp_small(x - (double)b / kPerNat);
 }
 
-__device__ __forceinline__ double mass(double x) { return x * kPerNat < (double)(kBuckets - 1) ? exp(-x) : 0.0; }
+// The mass of x in the unit of its bucket, which starts at `from`: a whole number of 2^-shift.
+__device__ __forceinline__ uint64_t whole_mass(double x, double from, int shift) {
+    if (!weighs(x)) return 0;
+    const double magic = __hiloint2double((1023 + 52 - shift) << 20, 0);  // its last place is 2^-shift
+    return (uint64_t)__double_as_longlong(exp_small(x - from) + magic) & ((1ull << 52) - 1);
+}
+
+// What the buckets tell of a row.
+struct Plan {
+    int64_t k;       // tokens that top_k leaves
+    int64_t before;  // tokens of the buckets before lo, and their mass
+    double above;
+    double all;         // the row's mass (0 where masses are not summed)
+    int lo, hi;         // buckets of the list (hi < lo: none); those before are kept whole, those after not at all
+    bool cut_k, cut_p;  // whether there is anything to cut within the list
+    bool settled;       // the row has been answered
+    float top;
+};
 
 struct SampleSpace {
-    uint64_t *best;      // rows x chunks: largest key and the complement of its first index
-    uint32_t *done;      // rows: chunks that are through with the last kernel
-    uint32_t *counts;    // rows x buckets
-    uint64_t *masses;    // rows x buckets
-    uint64_t *parts;     // rows x chunks x buckets: the chunk's masses
-    double *whole;       // rows x chunks: mass of the chunk's tokens in buckets that are kept whole
-    uint32_t *listed;    // rows x chunks: tokens in the buckets that are looked at one by one
-    uint32_t *list;      // rows x chunks x chunk / 8 of their indices
+    uint64_t *best;    // rows x chunks: the first token
+    uint64_t *masses;  // rows x buckets
+    uint64_t *parts;   // rows x chunks x buckets: the chunk's masses
+    uint64_t *list;    // rows x chunks x chunk / 8 tokens
+    double *whole;     // rows x chunks: mass of the chunk's tokens in buckets that are kept whole
+    Plan *plan;        // rows
+    uint32_t *counts;  // rows x buckets
+    uint32_t *listed;  // rows x chunks: tokens in the list's buckets
+    uint32_t *done;    // rows: chunks that are counted
 };
 
 // Tokens of a chunk: whole tiles, so that a call has about 1024 workgroups.
@@ -85,34 +145,64 @@ int64_t chunk_of(int64_t rows, int64_t vocab) {
     return (tiles_of(vocab) + each - 1) / each * kTile;
 }
 
-struct SampleSizes {
-    size_t done, counts, masses, parts, whole, listed, list, bytes;
-};
-
 // Of bounds that grow with the rows, so that the space for the most rows holds any call of fewer.
-SampleSizes sample_sizes(int64_t rows, int64_t vocab) {
+size_t sample_sizes(int64_t rows, int64_t vocab, void *at, SampleSpace *ws) {
     const int64_t tiles = tiles_of(vocab), chunk = chunk_of(rows, vocab);
     const size_t most = rows < 1024 ? 1024 : rows, chunks = (size_t)(rows < (int64_t)most / tiles ? rows * tiles : most);
-    SampleSizes s;
-    s.masses = align_up(chunks * 8);
-    s.parts = s.masses + align_up(rows * kBuckets * 8);
-    s.whole = s.parts + align_up(chunks * kBuckets * 8);
-    s.counts = s.whole + align_up(chunks * 8);
-    s.listed = s.counts + align_up(rows * kBuckets * 4);
-    s.list = s.listed + align_up(chunks * 4);
-    s.done = s.list + align_up((size_t)rows * (tiles * kTile + chunk - kTile) / 8 * 4);
-    s.bytes = s.done + align_up(rows * 4);
-    return s;
-}
-
-SampleSpace sample_space(void *ws, int64_t rows, int64_t vocab) {
-    const SampleSizes s = sample_sizes(rows, vocab);
-    char *p = (char *)ws;
-    return {(uint64_t *)p,           (uint32_t *)(p + s.done), (uint32_t *)(p + s.counts), (uint64_t *)(p + s.masses),
-            (uint64_t *)(p + s.parts), (double *)(p + s.whole), (uint32_t *)(p + s.listed), (uint32_t *)(p + s.list)};
+    char *p = (char *)at;
+    auto take = [&](size_t bytes) {
+        char *const q = p;
+        p += align_up(bytes);
+        return q;
+    };
+    SampleSpace s;
+    s.best = (uint64_t *)take(chunks * 8);
+    s.masses = (uint64_t *)take(rows * kBuckets * 8);
+    s.parts = (uint64_t *)take(chunks * kBuckets * 8);
+    s.list = (uint64_t *)take((size_t)rows * (tiles * kTile + chunk - kTile) / 8 * 8);
+    s.whole = (double *)take(chunks * 8);
+    s.plan = (Plan *)take(rows * sizeof(Plan));
+    s.counts = (uint32_t *)take(rows * kBuckets * 4);
+    s.listed = (uint32_t *)take(chunks * 4);
+    s.done = (uint32_t *)take(rows * 4);
+    if (ws) *ws = s;
+    return (size_t)(p - (char *)at);
 }
 
 // ------------------------------------------------------------------------------------------------ over a workgroup
+struct Hist {
+    uint64_t masses[kBuckets];
+    uint32_t counts[kBuckets];
+};
+
+constexpr int kBins = 256;  // of one of the eight levels of a selection by the bits of a token
+
+struct Common {
+    union {
+        Hist hist;
+        struct {
+            uint64_t masses[kBins];
+            uint32_t counts[kBins];
+        } bins;
+        struct {
+            uint64_t token[kRanked];
+            double mass[kRanked];
+        } sorted;
+    };
+    double part[kWaves];
+    uint64_t upart[kWaves];
+    int64_t ipart[kWaves];
+    int64_t found[2];
+    double value[2];
+};
+
+struct Shared : Common {
+    uint64_t list[kList];  // in order of the indices; later the mass of what is kept of it up to there
+    uint64_t few[kRanked];
+    double table[kBuckets];  // e^-(b / 16)
+    uint32_t offset[kThreads + 1];  // of the chunks' parts of the list
+};
+
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 __device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *part) {
@@ -125,23 +215,16 @@ __device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *part) {
     return v;
 }
 
+// The sum of the threads' values up to this one's, and of all, in one order.
 template <typename V>
-__device__ __forceinline__ V wave_upto(V v) {
-    const int lane = threadIdx.x % 64;
+__device__ __forceinline__ V block_upto(V v, V *part, V &all) {
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     for (int m = 1; m < 64; m <<= 1) {
         const V o = __shfl_up(v, m);
         if (lane >= m) v += o;
     }
-    return v;
-}
-
-// The sum of the threads' values up to this one's, and of all.
-template <typename V>
-__device__ __forceinline__ V block_upto(V v, V *part, V &all) {
-    const int wave = threadIdx.x / 64;
-    V upto = wave_upto(v);
     __syncthreads();
-    if (threadIdx.x % 64 == 63) part[wave] = upto;
+    if (lane == 63) part[wave] = v;
     __syncthreads();
     all = V(0);
     V before = V(0);
@@ -149,7 +232,7 @@ __device__ __forceinline__ V block_upto(V v, V *part, V &all) {
         if (w == wave) before = all;
         all += part[w];
     }
-    return before + upto;
+    return before + v;
 }
 
 template <typename V>
@@ -159,7 +242,14 @@ __device__ __forceinline__ V block_sum(V v, V *part) {
     return all;
 }
 
-// Eight logits of a row from token c on, as keys.
+// The first thread with `hit`, or, where none has it, the last with `some`; -1 where none has either.
+__device__ __forceinline__ int elect(bool hit, bool some, Common &sh) {
+    const uint64_t first = block_max(hit ? kThreads - threadIdx.x : 0, sh.upart);
+    if (first) return kThreads - (int)first;
+    return (int)block_max(some ? threadIdx.x + 1 : 0, sh.upart) - 1;
+}
+
+// f(keys, first index) for the tokens [begin, end), eight at a time, the next ones on their way meanwhile.
 template <typename T>
 __device__ __forceinline__ void keys8(const T *row, int64_t c, int64_t end, uint32_t (&k)[8]) {
     float l[8];
@@ -167,110 +257,59 @@ __device__ __forceinline__ void keys8(const T *row, int64_t c, int64_t end, uint
 #pragma unroll
     for (int i = 0; i < 8; i++) k[i] = c + i < end ? key_of(l[i]) : 0;
 }
+template <typename T, typename F>
+__device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t end, F f) {
+    uint32_t next[8];
+    const int64_t own = threadIdx.x * 8;
+    keys8(row, begin + own, end, next);
+    for (int64_t c0 = begin; c0 < end; c0 += kTile) {
+        uint32_t k[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) k[i] = next[i];
+        if (c0 + kTile < end) keys8(row, c0 + kTile + own, end, next);
+        f(k, c0 + own);
+    }
+}
 
 // ------------------------------------------------------------------------------------------------ the parts of a row
 template <typename T>
 __device__ __forceinline__ uint64_t best_of(const T *row, int64_t begin, int64_t end, uint64_t *part) {
     uint64_t best = 0;
-    for (int64_t c = begin + threadIdx.x * 8; c < end; c += kTile) {
-        uint32_t k[8];
-        keys8(row, c, end, k);
+    each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t c) {
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (k[i]) best = max64(best, (uint64_t)k[i] << 32 | (uint32_t)~(uint32_t)(c + i));
-    }
+            if (k[i]) best = max64(best, token_of(k[i], c + i));
+    });
     return block_max(best, part);
 }
 
-struct Hist {
-    uint64_t masses[kBuckets];
-    uint32_t counts[kBuckets];
-};
-
 __device__ __forceinline__ void clear(Hist &h) {
     for (int b = threadIdx.x; b < kBuckets; b += kThreads) h.masses[b] = 0, h.counts[b] = 0;
+    __syncthreads();
 }
 
 template <typename T>
-__device__ __forceinline__ void count_buckets(const T *row, int64_t begin, int64_t end, const Row &r, bool masses, Hist &h) {
-    for (int64_t c = begin + threadIdx.x * 8; c < end; c += kTile) {
-        uint32_t k[8];
-        keys8(row, c, end, k);
+__device__ __forceinline__ void count_buckets(const T *row, int64_t begin, int64_t end, const Row &r, int shift, Hist &h) {
+    clear(h);
+    const Level level = row_level();
+    each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t) {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             if (!k[i]) continue;
-            const double x = r.x(logit_of_key(k[i]));
-            const int b = Row::bucket(x);
+            const double x = r.x(k[i]);
+            const int b = level.bucket(x);
             atomicAdd(&h.counts[b], 1u);
-            if (masses) atomicAdd((unsigned long long *)&h.masses[b], (unsigned long long)whole_mass(r, x, b));
+            if (r.masses)
+                atomicAdd((unsigned long long *)&h.masses[b], (unsigned long long)whole_mass(x, level.from(b), shift));
         }
-    }
+    });
+    __syncthreads();
 }
 
-// Settings of a row.
-struct Settings {
-    double temperature, top_p, min_p, u;
-    int64_t top_k;
-    bool greedy, masses;
-};
-
-__device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t row) {
-    Settings s;
-    s.temperature = a.temperature ? (double)a.temperature[row] : 1.0;
-    s.top_k = a.top_k ? a.top_k[row] : 0;
-    s.top_p = a.top_p ? (double)a.top_p[row] : 1.0;
-    s.min_p = a.min_p ? (double)a.min_p[row] : 0.0;
-    if (s.top_p < 0.0) s.top_p = 0.0;
-    s.u = a.uniform[row];
-    s.greedy = !(s.temperature > 0.0);
-    if (s.temperature == (double)INFINITY) s.temperature = 1e300;  // every token alike
-    s.masses = !(s.top_k > 0 && s.top_k <= kCountOnly);
-    return s;
-}
-
-__device__ __forceinline__ Row row_of(const SampleArgs &a, const Settings &s, float top, int shift) {
-    Row r;
-    r.vocab = a.vocab, r.top = top, r.inverse = 1.0 / s.temperature, r.shift = shift;
-    r.most_x = s.min_p > 0.0 ? -log(fmin(s.min_p, 1.0)) : (double)INFINITY;
-    return r;
-}
-
-// What the buckets tell of a row.
-constexpr int kEach = kBuckets / kThreads;  // buckets of a thread
-struct Plan {
-    int64_t k;          // tokens that top_k leaves
-    bool cut_k, cut_p;  // whether there is anything to cut
-    int lo, hi;         // buckets that are looked at token by token; those before are kept whole
-    int64_t before;     // tokens of the buckets before lo, and their mass
-    double above;
-    double all;          // the row's mass (0 where masses are not summed)
-    double unit[kEach];  // of the thread's buckets' masses
-};
-
-struct Shared {
-    union {
-        Hist hist;
-        struct {
-            uint64_t masses[kBins];
-            uint32_t counts[kBins];
-        } bins;
-        struct {
-            uint32_t key[kSorted], index[kSorted];
-            double mass[kSorted];
-            double upto[kSorted + 1];
-        } sorted;
-    };
-    uint32_t key[kList], index[kList];  // the list, in order of the indices
-    double part[kWaves];
-    uint64_t upart[kWaves];
-    int64_t ipart[kWaves];
-    int64_t found[4];
-    double value[2];
-    uint32_t offset[kThreads + 1];  // of the chunks' parts of the list
-    uint32_t last;
-};
-
-__device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared &sh) {
+// The plan by the buckets in sh.hist.  The row's own has no `outer` one; the one of a list takes from its row's what is known,
+// with the tokens and the mass before the list.  masses: whether sh.hist has them.
+__device__ __forceinline__ Plan plan_of(const Row &r, const Level &level, bool masses, const Plan *outer, int shift,
+                                        Common &sh) {
     Plan p;
     int64_t n[kEach], cells = 0;
     double m[kEach], sum = 0.0;
@@ -278,18 +317,25 @@ __device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared 
     for (int i = 0; i < kEach; i++) {
         const int b = threadIdx.x * kEach + i;
         n[i] = sh.hist.counts[b];
-        p.unit[i] = s.masses ? ldexp(exp(-(double)b / kPerNat), -r.shift) : 0.0;
-        m[i] = s.masses ? (double)sh.hist.masses[b] * p.unit[i] : 0.0;
+        m[i] = masses ? ldexp((double)sh.hist.masses[b] * exp(-level.from(b)), -shift) : 0.0;
         cells += n[i], sum += m[i];
     }
+    const int64_t base = outer ? outer->before : 0;
+    const double under = outer ? outer->above : 0.0;
     int64_t valid;
-    const int64_t n0 = block_upto(cells, sh.ipart, valid) - cells;
-    p.all = 0.0;
-    const double m0 = s.masses ? block_upto(sum, sh.part, p.all) - sum : 0.0;
-    p.k = s.top_k > 0 && s.top_k < valid ? s.top_k : valid;
-    p.cut_k = p.k < valid;
-    p.cut_p = s.top_p < 1.0;
+    const int64_t n0 = base + block_upto(cells, sh.ipart, valid) - cells;
+    double listed = 0.0;
+    const double m0 = masses ? under + block_upto(sum, sh.part, listed) - sum : 0.0;
+    valid += base;
+    p.settled = false;
+    p.top = r.top;
+    p.all = outer && r.masses ? outer->all : under + listed;
+    p.k = outer ? outer->k : r.top_k > 0 && r.top_k < valid ? r.top_k : valid;
+    p.cut_k = outer ? outer->cut_k : p.k < valid;
+    p.cut_p = outer ? outer->cut_p : r.top_p < 1.0;
     // the bucket of the k-th token, and the mass before and in it
+    if (threadIdx.x == 0) sh.found[0] = kBuckets - 1;
+    __syncthreads();
     int64_t c = n0;
     double q = m0;
 #pragma unroll
@@ -301,15 +347,15 @@ __device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared 
     const int bucket_k = (int)sh.found[0];
     const double before_k = sh.value[0], in_k = sh.value[1];
     p.lo = kBuckets, p.hi = -1;
-    if (!s.masses) {
+    if (!masses) {
         p.lo = 0, p.hi = bucket_k;
     } else {
         if (p.cut_k) p.lo = p.hi = bucket_k;
         if (p.cut_p) {
             // Buckets that may hold the end of the share, whatever part of its bucket the k-th token takes.  Sums by buckets
             // and by tokens differ by less than the slack.
-            const double slack = 1e-12 * p.all, least = s.top_p * (p.cut_k ? before_k : p.all),
-                         most = s.top_p * (p.cut_k ? before_k + in_k : p.all);
+            const double least = r.top_p * (p.cut_k ? before_k : p.all), slack = 1e-12 * (under + listed),
+                         most = r.top_p * (p.cut_k ? before_k + in_k : p.all);
             uint64_t first = 0, last = 0;
             q = m0;
 #pragma unroll
@@ -319,20 +365,20 @@ __device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared 
                     first = max64(first, kBuckets - b), last = max64(last, b + 1);
                 q += m[i];
             }
-            first = block_max(first << 32 | last, sh.upart);  // the first bucket's `last` does not matter with one alone
-            if (first >> 32) {
-                p.lo = min(p.lo, kBuckets - (int)(first >> 32));
+            first = block_max(first, sh.upart);
+            if (first) {
+                p.lo = min(p.lo, kBuckets - (int)first);
                 if (!p.cut_k) p.hi = (int)block_max(last, sh.upart) - 1;
             }
         }
         // where min_p cuts before
         if (r.most_x < (double)INFINITY) {
-            const int bucket_m = Row::bucket(r.most_x);
+            const int bucket_m = level.bucket(r.most_x);
             if (bucket_m < p.lo) p.lo = p.hi = bucket_m, p.cut_k = p.cut_p = false;
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) sh.found[0] = valid, sh.value[0] = p.all;  // of a row whose buckets are all kept whole
+    if (threadIdx.x == 0) sh.found[0] = valid, sh.value[0] = under + listed;  // where all buckets are kept whole
     __syncthreads();
     c = n0, q = m0;
 #pragma unroll
@@ -346,186 +392,38 @@ __device__ __forceinline__ Plan plan_of(const Settings &s, const Row &r, Shared 
     return p;
 }
 
-// The indices of the tokens in buckets lo to hi among [begin, end), in order, to put(place, index, key); returns how many
-// places there are then.
+// put(place, token) for the tokens of the list's buckets in [begin, end), in order of the indices; returns how many there are.
 template <typename T, typename F>
-__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Row &r, const Plan &p, Shared &sh,
-                                            F put) {
+__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Row &r, const Plan &p,
+                                            uint64_t *part, F put) {
     uint32_t placed = 0;
-    for (int64_t c0 = begin; c0 < end; c0 += kTile) {
-        const int64_t c = c0 + threadIdx.x * 8;
-        uint32_t k[8], mask = 0;
-        keys8(row, c, end, k);
+    const Level level = row_level();
+    each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t c) {
+        uint32_t mask = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const int b = k[i] ? Row::bucket(r.x(logit_of_key(k[i]))) : kBuckets;
+            const int b = k[i] ? level.bucket(r.x(k[i])) : kBuckets;
             if (b >= p.lo && b <= p.hi) mask |= 1u << i;
         }
         uint64_t all;
         const int mine = __popc(mask);
-        uint32_t at = placed + (uint32_t)block_upto((uint64_t)mine, sh.upart, all) - mine;
+        uint32_t at = placed + (uint32_t)block_upto((uint64_t)mine, part, all) - mine;
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (mask >> i & 1) put(at++, (uint32_t)(c + i), k[i]);
+            if (mask >> i & 1) put(at++, token_of(k[i], c + i));
         placed += (uint32_t)all;
-    }
+    });
     return placed;
 }
 
-// The tokens of the last buckets: in LDS, or, where they are too many, looked for in the row.
-template <typename T>
-struct Listed {
-    const T *row;
-    const Row &r;
-    const Plan &p;
-    Shared &sh;
-    int n;  // -1: not in LDS
-
-    // f(key, index) for every one of them, in any order; a thread's own ones in the same order each time
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {
-        if (n >= 0) {
-            for (int i = threadIdx.x; i < n; i += kThreads) f(sh.key[i], sh.index[i]);
-            return;
-        }
-        for (int64_t c = threadIdx.x * 8; c < r.vocab; c += kTile) {
-            uint32_t k[8];
-            keys8(row, c, r.vocab, k);
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (!k[i]) continue;
-                const int b = Row::bucket(r.x(logit_of_key(k[i])));
-                if (b >= p.lo && b <= p.hi) f(k[i], (uint32_t)(c + i));
-            }
-        }
-    }
-};
-
-// The index of the rank-th token with that key (from 1 on) in order of the indices.
-template <typename T>
-__device__ __forceinline__ int64_t nth_equal(const Listed<T> &l, uint32_t key, int64_t rank, Shared &sh) {
-    int64_t before = 0;
-    if (l.n >= 0) {
-        for (int c0 = 0; c0 < l.n; c0 += kThreads) {
-            const int i = c0 + threadIdx.x;
-            const bool equal = i < l.n && sh.key[i] == key;
-            int64_t all;
-            const int64_t upto = before + block_upto((int64_t)equal, sh.ipart, all);
-            if (equal && upto == rank) sh.found[0] = sh.index[i];
-            before += all;
-        }
-        __syncthreads();
-        return sh.found[0];
-    }
-    const T *row = l.row;
-    const int64_t vocab = l.r.vocab;
-    for (int64_t c0 = 0; c0 < vocab; c0 += kTile) {
-        const int64_t c = c0 + threadIdx.x * 8;
-        uint32_t k[8];
-        keys8(row, c, vocab, k);
-        int mine = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) mine += k[i] == key;
-        int64_t all;
-        int64_t at = before + block_upto((int64_t)mine, sh.ipart, all) - mine;
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (k[i] == key && ++at == rank) sh.found[0] = c + i;
-        before += all;
-        __syncthreads();
-        if (before >= rank) break;
-    }
-    return sh.found[0];
-}
-
-// Where an order ends: tokens with a larger key are in, those with this one up to the index.
-struct End {
-    uint32_t key = 0;
-    int64_t index = 0;
-    __device__ __forceinline__ bool holds(uint32_t k, int64_t i) const { return k > key || (k == key && i <= index); }
-};
-
-// The first of the listed tokens that are `in`, largest keys first, at which their number (MASS: the sum of their masses, in
-// units of the first bucket's) reaches `target`.
-template <bool MASS, typename T, typename F>
-__device__ __forceinline__ End select(const Listed<T> &l, uint64_t target, Shared &sh, F in) {
-    uint32_t prefix = 0;
-    int64_t equal = 0;
-    const double from = (double)l.p.lo / kPerNat, scale = ldexp(1.0, l.r.shift);
-    auto units = [&](uint32_t key) {
-        const double x = l.r.x(logit_of_key(key));
-        return x * kPerNat < (double)(kBuckets - 1) ? (uint64_t)rint(exp(from - x) * scale) : 0ull;
-    };
-    for (int level = 0; level < 3; level++) {
-        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, width = level == 2 ? 10 : 11;
-        __syncthreads();
-        for (int b = threadIdx.x; b < kBins; b += kThreads) sh.bins.counts[b] = 0, sh.bins.masses[b] = 0;
-        __syncthreads();
-        l.each([&](uint32_t key, uint32_t index) {
-            if (level > 0 && key >> (shift + width) != prefix) return;
-            if (!in(key, index)) return;
-            const uint32_t b = key >> shift & ((1u << width) - 1);
-            atomicAdd(&sh.bins.counts[b], 1u);
-            if (MASS) atomicAdd((unsigned long long *)&sh.bins.masses[b], (unsigned long long)units(key));
-        });
-        __syncthreads();
-        constexpr int kEach = kBins / kThreads;
-        uint64_t v[kEach], sum = 0;
-        uint64_t lowest = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; i++) {
-            const int b = kBins - 1 - (threadIdx.x * kEach + i);
-            v[i] = MASS ? sh.bins.masses[b] : (uint64_t)sh.bins.counts[b];
-            if (sh.bins.counts[b]) lowest = kBins - b;
-            sum += v[i];
-        }
-        uint64_t all;
-        uint64_t before = block_upto(sum, sh.upart, all) - sum;
-        lowest = block_max(lowest, sh.upart);  // the order's end, should the sum not reach the target
-        if (target > all) target = all;
-        if (threadIdx.x == 0) sh.found[0] = kBins - (int64_t)lowest, sh.found[1] = (int64_t)target, sh.found[2] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kEach; i++) {
-            const int b = kBins - 1 - (threadIdx.x * kEach + i);
-            if (before < target && before + v[i] >= target) sh.found[0] = b, sh.found[1] = (int64_t)before, sh.found[2] = 1;
-            before += v[i];
-        }
-        __syncthreads();
-        const uint32_t b = min((uint32_t)sh.found[0], (uint32_t)kBins - 1);
-        prefix = prefix << width | b;
-        if (sh.found[2]) target -= (uint64_t)sh.found[1];
-        equal = sh.bins.counts[b];
-    }
-    int64_t rank = (int64_t)target;
-    if (MASS) {
-        const uint64_t one = units(prefix);
-        rank = one ? (int64_t)((target + one - 1) / one) : equal;
-    }
-    rank = rank < 1 ? 1 : rank;
-    End end;
-    end.key = prefix;
-    end.index = rank >= equal ? l.r.vocab : nth_equal(l, prefix, rank, sh);
-    __syncthreads();
-    return end;
-}
-
-// What is kept of a row, and what is drawn of it.
+// What is kept of a row (the tokens up to `last` in their order, as far as min_p keeps them), and what is drawn of it.
 struct Kept {
-    End k, p;
+    uint64_t last;
     double most_x;
     int64_t count;
     double total, drawn;
-    __device__ __forceinline__ bool holds(uint32_t key, int64_t index, double x) const {
-        return k.holds(key, index) && p.holds(key, index) && x <= most_x;
-    }
+    __device__ __forceinline__ bool holds(uint64_t token, double x) const { return token >= last && x <= most_x; }
 };
-
-__device__ __forceinline__ Kept all_of(const Settings &s, const Row &r, const Plan &p) {
-    Kept k;
-    k.most_x = r.most_x, k.count = p.before, k.total = p.above, k.drawn = s.u * p.above;
-    return k;
-}
 
 __device__ __forceinline__ void answer(const SampleArgs &a, int64_t at, int64_t id, double prob, int64_t kept) {
     a.ids[at] = (int32_t)id;
@@ -533,72 +431,33 @@ __device__ __forceinline__ void answer(const SampleArgs &a, int64_t at, int64_t 
     a.kept[at] = (int32_t)kept;
 }
 
-// The token within [begin, end), whose kept tokens come after a mass of `before`: a thread takes a run of them.
-template <typename T>
-__device__ __forceinline__ void draw_in(const SampleArgs &a, int64_t at, const T *row, const Row &r, const Kept &kept,
-                                        int64_t begin, int64_t end, double before, Shared &sh) {
-    const int64_t each = (end - begin + kTile - 1) / kTile * 8;
-    const int64_t from = min(begin + threadIdx.x * each, end), to = min(from + each, end);
-    double sum = 0.0;
-    for (int64_t c = from; c < to; c += 8) {
-        uint32_t k[8];
-        keys8(row, c, to, k);
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            if (!k[i]) continue;
-            const double x = r.x(logit_of_key(k[i]));
-            if (kept.holds(k[i], c + i, x)) sum += mass(x);
-        }
-    }
-    double all;
-    const double upto = before + block_upto(sum, sh.part, all);
-    // the thread whose run passes the drawn share, or the last that has any mass
-    const uint64_t first = block_max(sum > 0.0 && upto > kept.drawn ? kThreads - threadIdx.x : 0, sh.upart);
-    const uint64_t any = block_max(sum > 0.0 ? threadIdx.x + 1 : 0, sh.upart);
-    if (!any) {
-        if (threadIdx.x == 0) answer(a, at, -1, 0.0, kept.count);
-        return;
-    }
-    if ((int64_t)threadIdx.x != (first ? kThreads - (int64_t)first : (int64_t)any - 1)) return;
-    double q = upto - sum, last = 0.0;
-    int64_t id = -1;
-    for (int64_t c = from; c < to; c++) {
-        const uint32_t k = key_of(load_f32(row + c));
-        if (!k) continue;
-        const double x = r.x(logit_of_key(k));
-        const double m = kept.holds(k, c, x) ? mass(x) : 0.0;
-        if (!(m > 0.0)) continue;
-        id = c, last = m;
-        q += m;
-        if (q > kept.drawn) break;
-    }
-    answer(a, at, id, last / kept.total, kept.count);
+// A row without a token to take, or whose first token is taken: true if that is all.
+__device__ __forceinline__ bool settled(const SampleArgs &a, int64_t at, const Row &r, uint64_t best, bool writes) {
+    const bool none = best == 0;
+    if (!none && !r.greedy) return false;
+    if (writes && threadIdx.x == 0) answer(a, at, none ? -1 : index_of(best), none ? 0.0 : 1.0, none ? 0 : 1);
+    return true;
 }
 
-// A list of up to a token for each thread: each finds its rank by counting the larger ones, and everything goes by ranks from
-// there.  Leaves in sh.sorted.upto the mass of the kept ones among the list's first so many.  Returns true if the token is drawn
-// and answered, which it is where no bucket is kept whole.
-__device__ __forceinline__ bool by_rank(const SampleArgs &a, int64_t at, const Settings &s, const Row &r, const Plan &p, int n,
-                                        Shared &sh, Kept &kept) {
+// ------------------------------------------------------------------------------------------------ the list
+// Up to a token for each thread: each finds its rank by counting those before it, and everything goes by ranks from there.
+// Returns true if the row is answered, which it is where nothing is kept whole before the list.
+__device__ __forceinline__ bool by_rank(const SampleArgs &a, int64_t at, const Row &r, const Plan &p, const uint64_t *tokens,
+                                        int n, Shared &sh, Kept &kept) {
     const int i = threadIdx.x;
     const bool mine = i < n;
-    const uint32_t key = mine ? sh.key[i] : 0;
+    const uint64_t token = mine ? tokens[i] : 0;
     int rank = 0;
-    if ((i & ~63) < n) {  // equal ones before a token are larger, and equal ones after it are not
-        const int w0 = i & ~63, w1 = min(w0 + 64, n);
+    if ((i & ~63) < n)
 #pragma unroll 8
-        for (int j = 0; j < w0; j++) rank += sh.key[j] >= key;
-        for (int j = w0; j < w1; j++) rank += sh.key[j] > key || (sh.key[j] == key && j < i);
-#pragma unroll 8
-        for (int j = w1; j < n; j++) rank += sh.key[j] > key;
-    }
+        for (int j = 0; j < n; j++) rank += tokens[j] > token;
     double m = 0.0;
     bool stays = false;
     if (mine) {
-        const double x = r.x(logit_of_key(key));
-        m = mass(x);
+        const double x = r.x((uint32_t)(token >> 32));
+        m = mass(x, sh.table);
         stays = x <= r.most_x;
-        sh.sorted.key[rank] = key, sh.sorted.index[rank] = sh.index[i], sh.sorted.mass[rank] = m;
+        sh.sorted.token[rank] = token, sh.sorted.mass[rank] = m;
     }
     int64_t left = block_sum((int64_t)stays, sh.ipart);  // what min_p leaves; its barriers make the sorted list visible too
     const int64_t left_k = p.cut_k ? p.k - p.before : n;
@@ -606,7 +465,7 @@ __device__ __forceinline__ bool by_rank(const SampleArgs &a, int64_t at, const S
     if (p.cut_p) {
         double all;
         const double v = mine && i < left_k ? sh.sorted.mass[i] : 0.0, upto = block_upto(v, sh.part, all);
-        const double share = s.masses && !p.cut_k ? p.all : p.above + all, target = s.top_p * share - p.above;
+        const double share = r.masses && !p.cut_k ? p.all : p.above + all, target = r.top_p * share - p.above;
         // the first that reaches the share, if any does
         const uint64_t reach = block_max(mine && upto >= target ? (uint64_t)(kThreads - i) : 0, sh.upart);
         if (reach) left = min(left, (int64_t)kThreads - (int64_t)reach + 1);
@@ -616,59 +475,204 @@ __device__ __forceinline__ bool by_rank(const SampleArgs &a, int64_t at, const S
     double listed;
     const double upto = block_upto(m, sh.part, listed);
     kept.total = p.above + listed;
-    kept.drawn = s.u * kept.total;
-    if (p.lo == 0) {
-        const uint64_t first = block_max(m > 0.0 && upto > kept.drawn ? (uint64_t)(kThreads - i) : 0, sh.upart);
-        const uint64_t any = first ? 1 : block_max(m > 0.0 ? (uint64_t)(i + 1) : 0, sh.upart);
-        if (i == (first ? kThreads - (int)first : (int)any - 1)) answer(a, at, sh.index[i], m / kept.total, kept.count);
-        return true;
-    }
-    if (i == 0) sh.sorted.upto[0] = 0.0;
-    sh.sorted.upto[i + 1] = upto;
-    // the kept tokens of the list are those up to the last one's place in the order
-    kept.k.key = sh.sorted.key[left > 0 ? left - 1 : 0];
-    kept.k.index = (int64_t)sh.sorted.index[left > 0 ? left - 1 : 0] - (left > 0 ? 0 : 1);
-    __syncthreads();
-    return false;
+    kept.drawn = r.u * kept.total;
+    kept.last = left > 0 ? sh.sorted.token[left - 1] : sh.sorted.token[0] + 1;
+    if (p.before > 0) return false;
+    if (i == elect(m > 0.0 && upto > kept.drawn, m > 0.0, sh)) answer(a, at, index_of(token), m / kept.total, kept.count);
+    return true;
 }
 
-// Longer lists.
-template <typename T>
-__device__ __forceinline__ void by_select(const Settings &s, const Row &r, const Plan &p, const Listed<T> &l, Shared &sh,
-                                          Kept &kept) {
-    if (p.cut_k) kept.k = select<false>(l, (uint64_t)(p.k - p.before), sh, [](uint32_t, uint32_t) { return true; });
+// A longer list in LDS: its tokens are counted again in buckets of a 1024th of its range, and those of the few buckets that
+// remain go by rank.  Returns 1 if the row is answered, 0 if not, and -1 if too many tokens remain (equal logits, mostly).
+__device__ __forceinline__ int by_zoom(const SampleArgs &a, int64_t at, const Row &r, const Plan &p, int n, int shift,
+                                       Shared &sh, Kept &kept) {
+    constexpr int kOwn = kList / kThreads;
+    const Level level = list_level(p.lo, p.hi);
+    clear(sh.hist);
+    int b[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; j++) {
+        const int i = threadIdx.x * kOwn + j;
+        b[j] = kBuckets;
+        if (i >= n) continue;
+        const double x = r.x((uint32_t)(sh.list[i] >> 32));
+        b[j] = level.bucket(x);
+        atomicAdd(&sh.hist.counts[b[j]], 1u);
+        atomicAdd((unsigned long long *)&sh.hist.masses[b[j]], (unsigned long long)whole_mass(x, level.from(b[j]), shift));
+    }
+    __syncthreads();
+    const Plan z = plan_of(r, level, true, &p, shift, sh);
+    uint64_t mine = 0, left;
+#pragma unroll
+    for (int j = 0; j < kOwn; j++) mine += b[j] >= z.lo && b[j] <= z.hi;
+    uint32_t place = (uint32_t)(block_upto(mine, sh.upart, left) - mine);
+    if (left > kRanked) return -1;
+    uint64_t in = 0, out = 0;  // of the last token before those buckets, the complement, and the first one after
+#pragma unroll
+    for (int j = 0; j < kOwn; j++) {
+        if (b[j] == kBuckets) continue;
+        const uint64_t token = sh.list[threadIdx.x * kOwn + j];
+        if (b[j] < z.lo)
+            in = max64(in, ~token);
+        else if (b[j] > z.hi)
+            out = max64(out, token);
+        else
+            sh.few[place++] = token;
+    }
+    if (left == 0) {
+        in = block_max(in, sh.upart), out = block_max(out, sh.upart);
+        kept.count = z.before, kept.total = z.above, kept.drawn = r.u * z.above;
+        kept.last = in ? ~in : out + 1;
+        return 0;
+    }
+    __syncthreads();
+    return by_rank(a, at, r, z, sh.few, (int)left, sh, kept) ? 1 : 0;
+}
+
+// f(token) for every token of the list, a thread's own ones in the same order each time.  n: -1 where it is not in LDS.
+template <typename T, typename F>
+__device__ __forceinline__ void each_listed(const T *row, int64_t vocab, const Row &r, const Plan &p, int n, const Shared &sh,
+                                            F f) {
+    if (n >= 0) {
+        for (int i = threadIdx.x; i < n; i += kThreads) f(sh.list[i]);
+        return;
+    }
+    const Level level = row_level();
+    each_tile(row, 0, vocab, [&](const uint32_t (&k)[8], int64_t c) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int b = k[i] ? level.bucket(r.x(k[i])) : kBuckets;
+            if (b >= p.lo && b <= p.hi) f(token_of(k[i], c + i));
+        }
+    });
+}
+
+// The first token of the list at which the number of those from `least` on (MASS: the sum of their masses, in units of the
+// list's first bucket) reaches `target`: by eight bits of the tokens after the other.
+template <bool MASS, typename E>
+__device__ __forceinline__ uint64_t select(const Row &r, const Plan &p, uint64_t target, uint64_t least, int shift, Shared &sh,
+                                           E each) {
+    uint64_t prefix = 0;
+    const double from = (double)p.lo / kPerNat;
+    for (int low = 56; low >= 0; low -= 8) {
+        __syncthreads();
+        if (threadIdx.x < kBins) sh.bins.counts[threadIdx.x] = 0, sh.bins.masses[threadIdx.x] = 0;
+        __syncthreads();
+        each([&](uint64_t token) {
+            if (token < least || (low < 56 && token >> (low + 8) != prefix)) return;
+            const int b = (int)(token >> low & (kBins - 1));
+            atomicAdd(&sh.bins.counts[b], 1u);
+            if (MASS) {
+                const double x = r.x((uint32_t)(token >> 32));
+                if (weighs(x))
+                    atomicAdd((unsigned long long *)&sh.bins.masses[b],
+                              (unsigned long long)rint(ldexp(exp(from - x), shift)));
+            }
+        });
+        __syncthreads();
+        const int b = kBins - 1 - (int)threadIdx.x;  // the largest first
+        const bool some = b >= 0 && sh.bins.counts[max(b, 0)] > 0;
+        const uint64_t v = !some ? 0 : MASS ? sh.bins.masses[b] : (uint64_t)sh.bins.counts[b];
+        uint64_t all;
+        const uint64_t upto = block_upto(v, sh.upart, all);
+        const int owner = max(elect(some && upto >= target, some, sh), 0);  // the last bin, should the sum not reach it
+        if ((int)threadIdx.x == owner) sh.found[0] = (int64_t)(upto - v);
+        __syncthreads();
+        prefix = prefix << 8 | (uint64_t)(kBins - 1 - min(owner, kBins - 1));
+        target -= min(target, (uint64_t)sh.found[0]);
+    }
+    __syncthreads();
+    return prefix;
+}
+
+// Any other list.
+template <typename E>
+__device__ __forceinline__ void by_select(const Row &r, const Plan &p, int shift, Shared &sh, Kept &kept, E each) {
+    if (p.cut_k) kept.last = select<false>(r, p, (uint64_t)(p.k - p.before), 0, shift, sh, each);
     if (p.cut_p) {
         double share = p.all;
-        if (!s.masses || p.cut_k) {
+        if (!r.masses || p.cut_k) {
             double sum = 0.0;
-            l.each([&](uint32_t k, uint32_t i) {
-                if (kept.k.holds(k, i)) sum += mass(r.x(logit_of_key(k)));
+            each([&](uint64_t token) {
+                if (token >= kept.last) sum += mass(r.x((uint32_t)(token >> 32)), sh.table);
             });
             share = p.above + block_sum(sum, sh.part);
         }
-        const double units = ceil((s.top_p * share - p.above) * exp((double)p.lo / kPerNat) * ldexp(1.0, r.shift));
-        kept.p = select<true>(l, units >= 1.0 ? (uint64_t)units : 1ull, sh,
-                              [&](uint32_t k, uint32_t i) { return kept.k.holds(k, i); });
+        const double units = ceil(ldexp((r.top_p * share - p.above) * exp((double)p.lo / kPerNat), shift));
+        kept.last = select<true>(r, p, units >= 1.0 ? (uint64_t)units : 1, kept.last, shift, sh, each);
     }
     double sum = 0.0;
     int64_t count = 0;
-    l.each([&](uint32_t k, uint32_t i) {
-        const double x = r.x(logit_of_key(k));
-        if (kept.holds(k, i, x)) sum += mass(x), count++;
+    each([&](uint64_t token) {
+        const double x = r.x((uint32_t)(token >> 32));
+        if (kept.holds(token, x)) sum += mass(x, sh.table), count++;
     });
     kept.total = p.above + block_sum(sum, sh.part);
     kept.count = p.before + block_sum(count, sh.ipart);
-    kept.drawn = s.u * kept.total;
+    kept.drawn = r.u * kept.total;
 }
 
-// A row without a token to take, or whose largest logit is taken: true if that is all.
-__device__ __forceinline__ bool settled(const SampleArgs &a, int64_t at, const Settings &s, uint64_t best, bool writes) {
-    const bool none = best == 0;
-    if (!none && !s.greedy) return false;
-    if (writes && threadIdx.x == 0) {
-        answer(a, at, none ? -1 : (int32_t)~(uint32_t)best, none ? 0.0 : 1.0, none ? 0 : 1);
+// What is kept of the row, from its list of n tokens (which lies in LDS where it fits).  True if the row is answered.
+template <typename T>
+__device__ __forceinline__ bool keep(const SampleArgs &a, int64_t at, const T *row, const Row &r, const Plan &p, int64_t n,
+                                     bool fits, int shift, Shared &sh, Kept &kept) {
+    kept = {0, r.most_x, p.before, p.above, r.u * p.above};
+    if (n == 0) return false;
+    if (fits && n <= kRanked) return by_rank(a, at, r, p, sh.list, (int)n, sh, kept);
+    const int done = fits ? by_zoom(a, at, r, p, (int)n, shift, sh, kept) : -1;
+    if (done < 0)
+        by_select(r, p, shift, sh, kept, [&](auto f) { each_listed(row, a.vocab, r, p, fits ? (int)n : -1, sh, f); });
+    return done > 0;
+}
+
+// The mass of the kept tokens of [begin, end) that are this thread's.
+template <typename T>
+__device__ __forceinline__ double kept_mass(const T *row, int64_t begin, int64_t end, const Row &r, const Kept &kept,
+                                            const Shared &sh) {
+    double sum = 0.0;
+    for (int64_t c = begin; c < end; c += 8) {
+        uint32_t k[8];
+        keys8(row, c, end, k);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (!k[i]) continue;
+            const double x = r.x(k[i]);
+            if (kept.holds(token_of(k[i], c + i), x)) sum += mass(x, sh.table);
+        }
     }
-    return true;
+    return sum;
+}
+
+// The token within [begin, end), whose kept tokens come after a mass of `before`: each thread takes a run of them, then all
+// of them the run in which it lies, until a run is one token.
+template <typename T>
+__device__ __forceinline__ void draw_in(const SampleArgs &a, int64_t at, const T *row, const Row &r, const Kept &kept,
+                                        int64_t begin, int64_t end, double before, Shared &sh) {
+    while (true) {
+        const int64_t each = end - begin <= kThreads ? 1 : (end - begin + kTile - 1) / kTile * 8;
+        const int64_t from = min(begin + threadIdx.x * each, end), to = min(from + each, end);
+        const double sum = kept_mass(row, from, to, r, kept, sh);
+        double all;
+        const double upto = before + block_upto(sum, sh.part, all);
+        const int owner = elect(sum > 0.0 && upto > kept.drawn, sum > 0.0, sh);
+        if (owner < 0) {
+            if (threadIdx.x == 0) answer(a, at, -1, 0.0, kept.count);
+            return;
+        }
+        if ((int)threadIdx.x == owner) {
+            if (each == 1) answer(a, at, from, sum / kept.total, kept.count);
+            sh.found[0] = from, sh.found[1] = to, sh.value[0] = upto - sum;
+        }
+        if (each == 1) return;
+        __syncthreads();
+        begin = sh.found[0], end = sh.found[1], before = sh.value[0];
+        __syncthreads();
+    }
+}
+
+__device__ __forceinline__ void fill_table(Shared &sh) {
+    for (int b = threadIdx.x; b < kBuckets; b += kThreads) sh.table[b] = exp(-(double)b / kPerNat);
+    __syncthreads();
 }
 
 // ------------------------------------------------------------------------------------------------ kernels
@@ -680,32 +684,26 @@ __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, in
     __shared__ Shared sh;
     const int64_t at = blockIdx.x;
     const T *row = (const T *)a.logits + at * a.ld;
-    const Settings s = settings_of(a, at);
+    Row r = row_of(a, at);
     const uint64_t best = best_of(row, 0, a.vocab, sh.upart);
-    if (settled(a, at, s, best, true)) return;
-    const Row r = row_of(a, s, logit_of_key((uint32_t)(best >> 32)), shift);
-    clear(sh.hist);
-    __syncthreads();
-    count_buckets(row, 0, a.vocab, r, s.masses, sh.hist);
-    __syncthreads();
-    const Plan p = plan_of(s, r, sh);
+    if (settled(a, at, r, best, true)) return;
+    r.top = logit_of_key((uint32_t)(best >> 32));
+    fill_table(sh);
+    count_buckets(row, 0, a.vocab, r, shift, sh.hist);
+    const Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
     uint32_t n = 0;
-    if (p.hi >= 0)
-        n = collect(row, 0, a.vocab, r, p, sh, [&](uint32_t place, uint32_t index, uint32_t key) {
-            if (place < kList) sh.key[place] = key, sh.index[place] = index;
+    if (p.hi >= p.lo)
+        n = collect(row, 0, a.vocab, r, p, sh.upart, [&](uint32_t place, uint64_t token) {
+            if (place < kList) sh.list[place] = token;
         });
     __syncthreads();
-    Kept kept = all_of(s, r, p);
-    if (n > 0 && n <= kSorted) {
-        if (by_rank(a, at, s, r, p, (int)n, sh, kept)) return;
-    } else if (n > 0) {
-        by_select(s, r, p, Listed<T>{row, r, p, sh, n <= kList ? (int)n : -1}, sh, kept);
-    }
+    Kept kept;
+    if (keep(a, at, row, r, p, n, n <= kList, shift, sh, kept)) return;
     draw_in(a, at, row, r, kept, 0, a.vocab, 0.0, sh);
 }
 
-// Longer ones in three: the largest logit of each chunk; the buckets; the list, and the row's end by whichever workgroup
-// of the row is through last.
+// Longer rows in four launches, the first three by chunks: the first token; the buckets, and the plan by whichever workgroup
+// of the row is through last; the list, and the mass of what is kept whole; the end.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_best_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk) {
     __shared__ uint64_t part[kWaves];
@@ -717,91 +715,99 @@ __global__ void __launch_bounds__(kThreads) sample_best_kernel(SampleArgs a, Sam
     if (threadIdx.x == 0) ws.best[blockIdx.x] = best;
 }
 
-__device__ __forceinline__ uint64_t row_best(const SampleSpace &ws, int64_t at, int64_t chunks, uint64_t *part) {
-    uint64_t best = 0;
-    for (int64_t c = threadIdx.x; c < chunks; c += kThreads) best = max64(best, ws.best[at * chunks + c]);
-    return block_max(best, part);
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_count_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk,
                                                                int shift) {
-    __shared__ Hist hist;
-    __shared__ uint64_t part[kWaves];
+    __shared__ Common sh;
     const int64_t at = blockIdx.x / chunks, c = blockIdx.x % chunks;
-    const Settings s = settings_of(a, at);
-    const uint64_t best = row_best(ws, at, chunks, part);
-    if (settled(a, at, s, best, c == 0)) return;
-    const Row r = row_of(a, s, logit_of_key((uint32_t)(best >> 32)), shift);
-    clear(hist);
-    __syncthreads();
-    count_buckets((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab), r, s.masses, hist);
-    __syncthreads();
-    for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
-        if (!hist.counts[b]) continue;
-        atomicAdd(&ws.counts[at * kBuckets + b], hist.counts[b]);
-        if (s.masses) atomicAdd((unsigned long long *)&ws.masses[at * kBuckets + b], (unsigned long long)hist.masses[b]);
+    Row r = row_of(a, at);
+    uint64_t best = 0;
+    for (int64_t w = threadIdx.x; w < chunks; w += kThreads) best = max64(best, ws.best[at * chunks + w]);
+    best = block_max(best, sh.upart);
+    if (settled(a, at, r, best, c == 0)) {
+        if (c == 0 && threadIdx.x == 0) ws.plan[at].settled = true;
+        return;
     }
-    if (s.masses)
-        for (int b = threadIdx.x; b < kBuckets; b += kThreads) ws.parts[blockIdx.x * (int64_t)kBuckets + b] = hist.masses[b];
+    r.top = logit_of_key((uint32_t)(best >> 32));
+    count_buckets((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab), r, shift, sh.hist);
+    uint32_t *const counts = ws.counts + at * kBuckets;
+    unsigned long long *const masses = (unsigned long long *)ws.masses + at * kBuckets;
+    for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
+        if (r.masses) ws.parts[blockIdx.x * (int64_t)kBuckets + b] = sh.hist.masses[b];
+        if (!sh.hist.counts[b]) continue;
+        atomicAdd(counts + b, sh.hist.counts[b]);
+        if (r.masses) atomicAdd(masses + b, (unsigned long long)sh.hist.masses[b]);
+    }
+    stores_arrived();
+    __syncthreads();
+    if (threadIdx.x == 0) sh.found[0] = atomicAdd(ws.done + at, 1u) == (uint32_t)chunks - 1;
+    __syncthreads();
+    if (!sh.found[0]) return;
+    for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
+        sh.hist.counts[b] = get_shared(counts + b);
+        if (r.masses) sh.hist.masses[b] = get_shared((const uint64_t *)masses + b);
+    }
+    __syncthreads();
+    const Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
+    if (threadIdx.x == 0) ws.plan[at] = p;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sample_list_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk,
+                                                              int shift) {
+    __shared__ uint64_t part[kWaves];
+    __shared__ double sums[kWaves];
+    const int64_t at = blockIdx.x / chunks, c = blockIdx.x % chunks;
+    const Plan p = ws.plan[at];
+    if (p.settled) return;
+    Row r = row_of(a, at);
+    r.top = p.top;
+    const uint32_t room = (uint32_t)(chunk / 8);
+    uint64_t *const list = ws.list + (at * chunks + c) * room;
+    uint32_t placed = 0;
+    if (p.hi >= p.lo)
+        placed = collect((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab), r, p, part,
+                         [&](uint32_t place, uint64_t token) {
+                             if (place < room) list[place] = token;
+                         });
+    double sum = 0.0;
+    if (r.masses) {
+        for (int b = threadIdx.x; b < min(p.lo, kBuckets); b += kThreads)
+            sum += ldexp((double)ws.parts[blockIdx.x * (int64_t)kBuckets + b] * exp(-(double)b / kPerNat), -shift);
+        sum = block_sum(sum, sums);
+    }
+    if (threadIdx.x == 0) ws.whole[blockIdx.x] = sum, ws.listed[blockIdx.x] = placed;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk,
                                                              int shift) {
     __shared__ Shared sh;
-    const int64_t at = blockIdx.x / chunks, c = blockIdx.x % chunks;
+    const int64_t at = blockIdx.x;
     const T *row = (const T *)a.logits + at * a.ld;
-    const Settings s = settings_of(a, at);
-    const uint64_t best = row_best(ws, at, chunks, sh.upart);
-    if (settled(a, at, s, best, false)) return;
-    const Row r = row_of(a, s, logit_of_key((uint32_t)(best >> 32)), shift);
-    for (int b = threadIdx.x; b < kBuckets; b += kThreads)
-        sh.hist.counts[b] = ws.counts[at * kBuckets + b], sh.hist.masses[b] = ws.masses[at * kBuckets + b];
-    __syncthreads();
-    const Plan p = plan_of(s, r, sh);
+    const Plan p = ws.plan[at];
+    if (p.settled) return;
+    Row r = row_of(a, at);
+    r.top = p.top;
     const uint32_t room = (uint32_t)(chunk / 8);
-    uint32_t *const list = ws.list + (at * chunks + c) * room;
-    uint32_t placed = 0;
-    if (p.hi >= 0)
-        placed = collect(row, c * chunk, min((c + 1) * chunk, a.vocab), r, p, sh,
-                         [&](uint32_t place, uint32_t index, uint32_t) {
-                             if (place < room) put_shared(list + place, index);
-                         });
-    if (p.lo > 0 && s.masses) {
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < kEach; i++) {
-            const int b = threadIdx.x * kEach + i;
-            if (b < p.lo) sum += (double)ws.parts[blockIdx.x * (int64_t)kBuckets + b] * p.unit[i];
-        }
-        sum = block_sum(sum, sh.part);
-        if (threadIdx.x == 0) put_shared(ws.whole + blockIdx.x, sum);
-    }
-    if (threadIdx.x == 0) put_shared(ws.listed + blockIdx.x, placed);
-    stores_arrived();
-    __syncthreads();
-    if (threadIdx.x == 0) sh.last = atomicAdd(&ws.done[at], 1u) == (uint32_t)chunks - 1;
-    __syncthreads();
-    if (!sh.last) return;
+    double *const whole = ws.whole + at * chunks;
     // the chunks' lists in LDS, where they fit
     int64_t n = 0;
-    bool fits = true;
+    bool fits = chunks <= kThreads;
     for (int64_t c0 = 0; c0 < chunks; c0 += kThreads) {
-        const uint32_t mine = c0 + threadIdx.x < chunks ? get_shared(ws.listed + at * chunks + c0 + threadIdx.x) : 0;
+        const uint32_t mine = c0 + threadIdx.x < chunks ? ws.listed[at * chunks + c0 + threadIdx.x] : 0;
         int64_t all;
         const int64_t upto = block_upto((int64_t)mine, sh.ipart, all);
         if (c0 == 0) sh.offset[threadIdx.x + 1] = (uint32_t)upto;
-        if (c0 == 0 && threadIdx.x == 0) sh.offset[0] = 0;
         fits = block_max(mine > room, sh.upart) == 0 && fits;
         n += all;
     }
-    __syncthreads();
-    fits = fits && n <= kList && chunks <= kThreads;
+    fits = fits && n <= kList;
+    if (threadIdx.x == 0) sh.offset[0] = 0;
+    fill_table(sh);
     if (fits && n > 0) {
-        // a thread finds the chunk of its place
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            int low = 0, high = (int)chunks;  // offset[low] <= i < offset[high]
+        for (int i = threadIdx.x; i < n; i += kThreads) {  // each finds the chunk of its place
+            int low = 0, high = (int)chunks;               // offset[low] <= i < offset[high]
             while (high - low > 1) {
                 const int mid = (low + high) / 2;
                 if (sh.offset[mid] <= (uint32_t)i)
@@ -809,77 +815,70 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
                 else
                     high = mid;
             }
-            const uint32_t index = get_shared(ws.list + (at * chunks + low) * room + (i - sh.offset[low]));
-            sh.index[i] = index;
-            sh.key[i] = key_of(load_f32(row + index));
+            sh.list[i] = ws.list[(at * chunks + low) * room + (i - sh.offset[low])];
         }
         __syncthreads();
     }
-    Kept kept = all_of(s, r, p);
-    const bool ranked = fits && n > 0 && n <= kSorted;
-    if (ranked) {
-        if (by_rank(a, at, s, r, p, (int)n, sh, kept)) return;
-    } else if (n > 0) {
-        const Listed<T> l{row, r, p, sh, fits ? (int)n : -1};
-        by_select(s, r, p, l, sh, kept);
-        // the list's part of each chunk's mass
-        if (fits) {
-            const int lane = threadIdx.x % 64;
-            for (int64_t w = threadIdx.x / 64; w < chunks; w += kWaves) {
-                double sum = 0.0;
-                for (uint32_t i = sh.offset[w] + lane; i < sh.offset[w + 1]; i += 64) {
-                    const double x = r.x(logit_of_key(sh.key[i]));
-                    if (kept.holds(sh.key[i], sh.index[i], x)) sum += mass(x);
-                }
-                sum = wave_sum(sum);
-                if (lane == 0) {
-                    double *const of = ws.whole + at * chunks + w;
-                    put_shared(of, (p.lo > 0 && s.masses ? get_shared(of) : 0.0) + sum);
-                }
-            }
-        } else {
-            for (int64_t w = 0; w < chunks; w++) {
-                double sum = 0.0;
-                const int64_t end = min((w + 1) * chunk, a.vocab);
-                for (int64_t t = w * chunk + threadIdx.x * 8; t < end; t += kTile) {
-                    uint32_t k[8];
-                    keys8(row, t, end, k);
+    Kept kept;
+    if (keep(a, at, row, r, p, n, fits, shift, sh, kept)) return;
+    if (n > 0 && fits) {
+        // the list's tokens give way to the mass of what is kept of them up to there
+        constexpr int kOwn = kList / kThreads;
+        double m[kOwn], sum = 0.0, all;
 #pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        if (!k[i]) continue;
-                        const double x = r.x(logit_of_key(k[i]));
-                        if (kept.holds(k[i], t + i, x)) sum += mass(x);
-                    }
-                }
-                sum = block_sum(sum, sh.part);
-                if (threadIdx.x == 0) put_shared(ws.whole + at * chunks + w, sum);
-            }
+        for (int j = 0; j < kOwn; j++) {
+            const int i = threadIdx.x * kOwn + j;
+            m[j] = 0.0;
+            if (i >= n) continue;
+            const double x = r.x((uint32_t)(sh.list[i] >> 32));
+            if (kept.holds(sh.list[i], x)) m[j] = mass(x, sh.table);
+            sum += m[j];
         }
-        stores_arrived();
+        double q = block_upto(sum, sh.part, all) - sum;  // its barriers come between reading and writing
+#pragma unroll
+        for (int j = 0; j < kOwn; j++) {
+            q += m[j];
+            sh.list[threadIdx.x * kOwn + j] = (uint64_t)__double_as_longlong(q);
+        }
+        __syncthreads();
+    } else if (n > 0) {
+        for (int64_t c = 0; c < chunks; c++) {
+            const int64_t end = min((c + 1) * chunk, a.vocab);
+            double sum = 0.0;
+            for (int64_t t = c * chunk + threadIdx.x * 8; t < end; t += kTile)
+                sum += kept_mass(row, t, min(t + 8, end), r, kept, sh);
+            sum = block_sum(sum, sh.part);
+            if (threadIdx.x == 0) whole[c] = sum;
+        }
         __syncthreads();
     }
     // the chunk whose tokens pass the drawn share, or the last that has any mass
     int64_t chosen = 0;
     double before = 0.0, start = 0.0;
     for (int64_t c0 = 0; c0 < chunks; c0 += kThreads) {
-        const int64_t w = c0 + threadIdx.x;
-        double m = w < chunks ? get_shared(ws.whole + at * chunks + w) : 0.0;
-        if (ranked && w < chunks) m += sh.sorted.upto[sh.offset[w + 1]] - sh.sorted.upto[sh.offset[w]];
+        const int64_t c = c0 + threadIdx.x;
+        double m = c < chunks ? whole[c] : 0.0;
+        if (n > 0 && fits && c < chunks) {
+            const uint32_t from = sh.offset[c], to = sh.offset[c + 1];
+            if (to > from)
+                m += __longlong_as_double((long long)sh.list[to - 1]) -
+                     (from ? __longlong_as_double((long long)sh.list[from - 1]) : 0.0);
+        }
         double all;
         const double upto = before + block_upto(m, sh.part, all);
-        const uint64_t hit = block_max(m > 0.0 && upto > kept.drawn ? kThreads - threadIdx.x : 0, sh.upart);
-        const uint64_t any = hit ? 1 : block_max(m > 0.0 ? threadIdx.x + 1 : 0, sh.upart);
-        if (any) {
-            const int64_t owner = hit ? kThreads - (int64_t)hit : (int64_t)any - 1;
-            if ((int64_t)threadIdx.x == owner) sh.value[0] = upto - m;
+        const bool hit = m > 0.0 && upto > kept.drawn;
+        const int owner = elect(hit, m > 0.0, sh);
+        if (owner >= 0) {
+            if ((int)threadIdx.x == owner) sh.value[0] = upto - m, sh.found[0] = hit;
             chosen = c0 + owner;
             __syncthreads();
             start = sh.value[0];
+            if (sh.found[0]) break;
             __syncthreads();
         }
-        if (hit) break;
         before += all;
     }
+    __syncthreads();
     draw_in(a, at, row, r, kept, chosen * chunk, min((chosen + 1) * chunk, a.vocab), start, sh);
 }
 
@@ -887,7 +886,7 @@ bool is_short(int64_t vocab) { return vocab <= kShort; }
 
 template <typename T>
 hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
-    int shift = 44;  // a bucket's mass, at most 2^shift for each token, fits 64 bits
+    int shift = 44;  // a bucket's mass, at most 2^shift for each token, fits 63 bits
     while (shift > 30 && a.vocab >> (63 - shift)) shift--;
     constexpr int64_t kStep = 1 << 22;  // workgroups of a launch, which holds fewer than 2^32 threads
     const int64_t chunk = chunk_of(a.rows, a.vocab), chunks = (a.vocab + chunk - 1) / chunk;
@@ -902,18 +901,22 @@ hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
         if (p.top_p) p.top_p += r0;
         if (p.min_p) p.min_p += r0;
         p.ids += r0, p.prob += r0, p.kept += r0;
-        const unsigned grid = (unsigned)(is_short(a.vocab) ? p.rows : p.rows * chunks);
         if (is_short(a.vocab)) {
-            sample_short_kernel<T><<<grid, kThreads, 0, s>>>(p, shift);
+            sample_short_kernel<T><<<(unsigned)p.rows, kThreads, 0, s>>>(p, shift);
         } else {
-            const SampleSpace ws = sample_space(a.ws, a.rows, a.vocab);
+            SampleSpace ws;
+            sample_sizes(a.rows, a.vocab, a.ws, &ws);
+            const unsigned grid = (unsigned)(p.rows * chunks);
             sample_best_kernel<T><<<grid, kThreads, 0, s>>>(p, ws, chunks, chunk);
             hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             sample_count_kernel<T><<<grid, kThreads, 0, s>>>(p, ws, chunks, chunk, shift);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
-            sample_end_kernel<T><<<grid, kThreads, 0, s>>>(p, ws, chunks, chunk, shift);
+            sample_list_kernel<T><<<grid, kThreads, 0, s>>>(p, ws, chunks, chunk, shift);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            sample_end_kernel<T><<<(unsigned)p.rows, kThreads, 0, s>>>(p, ws, chunks, chunk, shift);
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -924,7 +927,7 @@ hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
 }  // namespace
 
 size_t sample_workspace(int64_t rows, int64_t vocab) {
-    return rows == 0 || is_short(vocab) ? 0 : sample_sizes(rows, vocab).bytes;
+    return rows == 0 || is_short(vocab) ? 0 : sample_sizes(rows, vocab, nullptr, nullptr);
 }
 
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t stream) {
