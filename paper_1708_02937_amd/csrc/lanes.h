@@ -82,4 +82,33 @@ __device__ __forceinline__ V lanes_sum(V v) {
     return v;
 }
 
+
+// Sums and maxima of 64-bit values (0 where a lane has no neighbour) over the lanes up to each one: by moves between registers
+// within 16 lanes, then of each 16 lanes' and each 32 lanes' last value into the following ones.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t lower(uint64_t v) {
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false),
+              hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+    return (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;
+}
+template <typename F>
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v, F join) {
+    v = join(v, lower<0x111, 0xf>(v)), v = join(v, lower<0x112, 0xf>(v)), v = join(v, lower<0x114, 0xf>(v));
+    v = join(v, lower<0x118, 0xf>(v)), v = join(v, lower<0x142, 0xa>(v)), v = join(v, lower<0x143, 0xc>(v));
+    return v;
+}
+__device__ __forceinline__ uint64_t wave_upto(uint64_t v) {
+    return wave_scan(v, [](uint64_t a, uint64_t b) { return a + b; });
+}
+__device__ __forceinline__ int64_t wave_upto(int64_t v) { return (int64_t)wave_upto((uint64_t)v); }
+__device__ __forceinline__ double wave_upto(double v) {
+    return __longlong_as_double((long long)wave_scan((uint64_t)__double_as_longlong(v), [](uint64_t a, uint64_t b) {
+        return (uint64_t)__double_as_longlong(__longlong_as_double((long long)a) + __longlong_as_double((long long)b));
+    }));
+}
+// The largest, in the last lane.
+__device__ __forceinline__ uint64_t wave_max_last(uint64_t v) {
+    return wave_scan(v, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+}
+
 }  // namespace sdnn

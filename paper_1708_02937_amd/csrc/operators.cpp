@@ -334,7 +334,7 @@ sdnn_status sdnn_sample_workspace_size(int64_t rows, int64_t vocab, int64_t *byt
     sdnn::set_error(SDNN_OK, "");
     if (!bytes) return fail(SDNN_ERR_NULL_POINTER, "bytes is NULL");
     SDNN_CHECK(check_sample(rows, vocab));
-    *bytes = (int64_t)sdnn::sample_workspace(rows, vocab);
+    *bytes = (int64_t)sdnn::sample_workspace_upto(rows, vocab);
     return SDNN_OK;
 }
 

@@ -142,7 +142,9 @@ hipError_t launch_widen_groups(const GroupsArgs &a, bool bf16, hipStream_t strea
 hipError_t launch_product_groups(const GroupProductArgs &a, bool x_bf16, bool y_bf16, hipStream_t stream);
 hipError_t launch_layer(const LayerArgs &a, bool bf16, bool router_bf16, hipStream_t stream);
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t stream);
+// what a call needs, and what every call of up to so many rows does
 size_t sample_workspace(int64_t rows, int64_t vocab);
+size_t sample_workspace_upto(int64_t rows, int64_t vocab);
 size_t layer_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen);
 hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_quantize(const QuantizeArgs &a, bool bf16, hipStream_t stream);

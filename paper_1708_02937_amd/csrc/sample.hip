@@ -124,6 +124,7 @@ struct Plan {
     bool cut_k, cut_p;  // whether there is anything to cut within the list
     bool settled;       // the row has been answered
     float top;
+    uint32_t first_key, end_key;  // the list's keys are from this on and before that
 };
 
 struct SampleSpace {
@@ -206,9 +207,9 @@ struct Shared : Common {
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 __device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *part) {
-    for (int m = 1; m < 64; m <<= 1) v = max64(v, __shfl_xor((unsigned long long)v, m));
+    v = wave_max_last(v);
     __syncthreads();
-    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
+    if (threadIdx.x % 64 == 63) part[threadIdx.x / 64] = v;
     __syncthreads();
     v = part[0];
     for (int w = 1; w < kWaves; w++) v = max64(v, part[w]);
@@ -219,10 +220,7 @@ __device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *part) {
 template <typename V>
 __device__ __forceinline__ V block_upto(V v, V *part, V &all) {
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    for (int m = 1; m < 64; m <<= 1) {
-        const V o = __shfl_up(v, m);
-        if (lane >= m) v += o;
-    }
+    v = wave_upto(v);
     __syncthreads();
     if (lane == 63) part[wave] = v;
     __syncthreads();
@@ -244,9 +242,8 @@ __device__ __forceinline__ V block_sum(V v, V *part) {
 
 // The first thread with `hit`, or, where none has it, the last with `some`; -1 where none has either.
 __device__ __forceinline__ int elect(bool hit, bool some, Common &sh) {
-    const uint64_t first = block_max(hit ? kThreads - threadIdx.x : 0, sh.upart);
-    if (first) return kThreads - (int)first;
-    return (int)block_max(some ? threadIdx.x + 1 : 0, sh.upart) - 1;
+    const uint64_t best = block_max(hit ? (uint64_t)(kThreads - threadIdx.x) << 32 : some ? threadIdx.x + 1 : 0, sh.upart);
+    return best >> 32 ? kThreads - (int)(best >> 32) : (int)best - 1;
 }
 
 // f(keys, first index) for the tokens [begin, end), eight at a time, the next ones on their way meanwhile.
@@ -392,19 +389,47 @@ __device__ __forceinline__ Plan plan_of(const Row &r, const Level &level, bool m
     return p;
 }
 
+// The least key in bucket b or before it, by a wave: a lane tries a 64th of the range each time.
+__device__ __forceinline__ uint32_t least_key(const Row &r, int b) {
+    const int lane = threadIdx.x % 64;
+    const Level level = row_level();
+    uint64_t low = key_of(-3.402823466e38f), high = (uint64_t)key_of(r.top) + 1;  // the answer is from low on and before high
+    while (high - low > 1) {
+        const uint64_t step = (high - low + 63) / 64, at = low + lane * step;
+        // keys ascend and buckets descend: lanes from the first that is in bucket b or before
+        const bool in = at >= high - 1 || level.bucket(r.x((uint32_t)at)) <= b;
+        const int first = __ffsll((unsigned long long)__ballot(in)) - 1;  // -1: not even the last lane's
+        if (first == 0) return (uint32_t)low;
+        const uint64_t from = low + (uint64_t)(first < 0 ? 63 : first - 1) * step + 1;
+        high = first < 0 ? high : min(high, low + (uint64_t)first * step + 1);
+        low = from;
+    }
+    return (uint32_t)low;
+}
+
+__device__ __forceinline__ void find_keys(const Row &r, Plan &p, Common &sh) {
+    p.first_key = p.end_key = 0;
+    if (p.hi < p.lo) return;
+    const int wave = threadIdx.x / 64;
+    if (wave < 2) {
+        const uint32_t key = wave == 1 ? least_key(r, p.hi) : p.lo > 0 ? least_key(r, p.lo - 1) : key_of(r.top) + 1;
+        if (threadIdx.x % 64 == 0) sh.found[wave] = key;
+    }
+    __syncthreads();
+    p.end_key = (uint32_t)sh.found[0], p.first_key = (uint32_t)sh.found[1];
+    __syncthreads();
+}
+
 // put(place, token) for the tokens of the list's buckets in [begin, end), in order of the indices; returns how many there are.
 template <typename T, typename F>
-__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Row &r, const Plan &p,
-                                            uint64_t *part, F put) {
+__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Plan &p, uint64_t *part,
+                                            F put) {
     uint32_t placed = 0;
-    const Level level = row_level();
     each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t c) {
         uint32_t mask = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int b = k[i] ? level.bucket(r.x(k[i])) : kBuckets;
-            if (b >= p.lo && b <= p.hi) mask |= 1u << i;
-        }
+        for (int i = 0; i < 8; i++)
+            if (k[i] - p.first_key < p.end_key - p.first_key) mask |= 1u << i;
         uint64_t all;
         const int mine = __popc(mask);
         uint32_t at = placed + (uint32_t)block_upto((uint64_t)mine, part, all) - mine;
@@ -531,19 +556,15 @@ __device__ __forceinline__ int by_zoom(const SampleArgs &a, int64_t at, const Ro
 
 // f(token) for every token of the list, a thread's own ones in the same order each time.  n: -1 where it is not in LDS.
 template <typename T, typename F>
-__device__ __forceinline__ void each_listed(const T *row, int64_t vocab, const Row &r, const Plan &p, int n, const Shared &sh,
-                                            F f) {
+__device__ __forceinline__ void each_listed(const T *row, int64_t vocab, const Plan &p, int n, const Shared &sh, F f) {
     if (n >= 0) {
         for (int i = threadIdx.x; i < n; i += kThreads) f(sh.list[i]);
         return;
     }
-    const Level level = row_level();
     each_tile(row, 0, vocab, [&](const uint32_t (&k)[8], int64_t c) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int b = k[i] ? level.bucket(r.x(k[i])) : kBuckets;
-            if (b >= p.lo && b <= p.hi) f(token_of(k[i], c + i));
-        }
+        for (int i = 0; i < 8; i++)
+            if (k[i] - p.first_key < p.end_key - p.first_key) f(token_of(k[i], c + i));
     });
 }
 
@@ -621,49 +642,58 @@ __device__ __forceinline__ bool keep(const SampleArgs &a, int64_t at, const T *r
     if (fits && n <= kRanked) return by_rank(a, at, r, p, sh.list, (int)n, sh, kept);
     const int done = fits ? by_zoom(a, at, r, p, (int)n, shift, sh, kept) : -1;
     if (done < 0)
-        by_select(r, p, shift, sh, kept, [&](auto f) { each_listed(row, a.vocab, r, p, fits ? (int)n : -1, sh, f); });
+        by_select(r, p, shift, sh, kept, [&](auto f) { each_listed(row, a.vocab, p, fits ? (int)n : -1, sh, f); });
     return done > 0;
 }
 
-// The mass of the kept tokens of [begin, end) that are this thread's.
+// The masses of the kept ones of eight tokens, and their sum.
 template <typename T>
-__device__ __forceinline__ double kept_mass(const T *row, int64_t begin, int64_t end, const Row &r, const Kept &kept,
-                                            const Shared &sh) {
+__device__ __forceinline__ double kept_masses(const T *row, int64_t c, int64_t end, const Row &r, const Kept &kept,
+                                              const Shared &sh, double (&m)[8]) {
+    uint32_t k[8];
+    keys8(row, c, end, k);
     double sum = 0.0;
-    for (int64_t c = begin; c < end; c += 8) {
-        uint32_t k[8];
-        keys8(row, c, end, k);
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            if (!k[i]) continue;
-            const double x = r.x(k[i]);
-            if (kept.holds(token_of(k[i], c + i), x)) sum += mass(x, sh.table);
-        }
+    for (int i = 0; i < 8; i++) {
+        m[i] = 0.0;
+        if (!k[i]) continue;
+        const double x = r.x(k[i]);
+        if (kept.holds(token_of(k[i], c + i), x)) m[i] = mass(x, sh.table);
+        sum += m[i];
     }
     return sum;
 }
 
 // The token within [begin, end), whose kept tokens come after a mass of `before`: each thread takes a run of them, then all
-// of them the run in which it lies, until a run is one token.
+// of them the run in which it lies, until a run is eight tokens.
 template <typename T>
 __device__ __forceinline__ void draw_in(const SampleArgs &a, int64_t at, const T *row, const Row &r, const Kept &kept,
                                         int64_t begin, int64_t end, double before, Shared &sh) {
     while (true) {
-        const int64_t each = end - begin <= kThreads ? 1 : (end - begin + kTile - 1) / kTile * 8;
+        const int64_t each = (end - begin + kTile - 1) / kTile * 8;
         const int64_t from = min(begin + threadIdx.x * each, end), to = min(from + each, end);
-        const double sum = kept_mass(row, from, to, r, kept, sh);
-        double all;
+        double m[8], sum = 0.0, all;
+        for (int64_t c = from; c < to; c += 8) sum += kept_masses(row, c, to, r, kept, sh, m);
         const double upto = before + block_upto(sum, sh.part, all);
         const int owner = elect(sum > 0.0 && upto > kept.drawn, sum > 0.0, sh);
         if (owner < 0) {
             if (threadIdx.x == 0) answer(a, at, -1, 0.0, kept.count);
             return;
         }
-        if ((int)threadIdx.x == owner) {
-            if (each == 1) answer(a, at, from, sum / kept.total, kept.count);
-            sh.found[0] = from, sh.found[1] = to, sh.value[0] = upto - sum;
+        if (each == 8) {
+            if ((int)threadIdx.x != owner) return;
+            double q = upto - sum, taken = 0.0;
+            int id = 0;
+            bool open = true;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                q += m[i];
+                if (open && m[i] > 0.0) id = i, taken = m[i], open = !(q > kept.drawn);
+            }
+            answer(a, at, from + id, taken / kept.total, kept.count);
+            return;
         }
-        if (each == 1) return;
+        if ((int)threadIdx.x == owner) sh.found[0] = from, sh.found[1] = to, sh.value[0] = upto - sum;
         __syncthreads();
         begin = sh.found[0], end = sh.found[1], before = sh.value[0];
         __syncthreads();
@@ -677,8 +707,6 @@ __device__ __forceinline__ void fill_table(Shared &sh) {
 
 // ------------------------------------------------------------------------------------------------ kernels
 // A short row by one workgroup, in one launch.
-constexpr int64_t kShort = 8 * kTile;
-
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, int shift) {
     __shared__ Shared sh;
@@ -690,10 +718,11 @@ __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, in
     r.top = logit_of_key((uint32_t)(best >> 32));
     fill_table(sh);
     count_buckets(row, 0, a.vocab, r, shift, sh.hist);
-    const Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
+    Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
+    find_keys(r, p, sh);
     uint32_t n = 0;
     if (p.hi >= p.lo)
-        n = collect(row, 0, a.vocab, r, p, sh.upart, [&](uint32_t place, uint64_t token) {
+        n = collect(row, 0, a.vocab, p, sh.upart, [&](uint32_t place, uint64_t token) {
             if (place < kList) sh.list[place] = token;
         });
     __syncthreads();
@@ -748,7 +777,8 @@ __global__ void __launch_bounds__(kThreads) sample_count_kernel(SampleArgs a, Sa
         if (r.masses) sh.hist.masses[b] = get_shared((const uint64_t *)masses + b);
     }
     __syncthreads();
-    const Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
+    Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
+    find_keys(r, p, sh);
     if (threadIdx.x == 0) ws.plan[at] = p;
 }
 
@@ -760,18 +790,17 @@ __global__ void __launch_bounds__(kThreads) sample_list_kernel(SampleArgs a, Sam
     const int64_t at = blockIdx.x / chunks, c = blockIdx.x % chunks;
     const Plan p = ws.plan[at];
     if (p.settled) return;
-    Row r = row_of(a, at);
-    r.top = p.top;
+    const bool masses = row_of(a, at).masses;
     const uint32_t room = (uint32_t)(chunk / 8);
     uint64_t *const list = ws.list + (at * chunks + c) * room;
     uint32_t placed = 0;
     if (p.hi >= p.lo)
-        placed = collect((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab), r, p, part,
+        placed = collect((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab), p, part,
                          [&](uint32_t place, uint64_t token) {
                              if (place < room) list[place] = token;
                          });
     double sum = 0.0;
-    if (r.masses) {
+    if (masses) {
         for (int b = threadIdx.x; b < min(p.lo, kBuckets); b += kThreads)
             sum += ldexp((double)ws.parts[blockIdx.x * (int64_t)kBuckets + b] * exp(-(double)b / kPerNat), -shift);
         sum = block_sum(sum, sums);
@@ -806,17 +835,23 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
     if (threadIdx.x == 0) sh.offset[0] = 0;
     fill_table(sh);
     if (fits && n > 0) {
-        for (int i = threadIdx.x; i < n; i += kThreads) {  // each finds the chunk of its place
-            int low = 0, high = (int)chunks;               // offset[low] <= i < offset[high]
-            while (high - low > 1) {
+        constexpr int kOwn = kList / kThreads;
+        uint64_t token[kOwn];
+#pragma unroll
+        for (int j = 0; j < kOwn; j++) {
+            const int i = j * kThreads + threadIdx.x;
+            int low = 0, high = (int)chunks;  // the chunk of this place: offset[low] <= i < offset[high]
+            while (i < n && high - low > 1) {
                 const int mid = (low + high) / 2;
                 if (sh.offset[mid] <= (uint32_t)i)
                     low = mid;
                 else
                     high = mid;
             }
-            sh.list[i] = ws.list[(at * chunks + low) * room + (i - sh.offset[low])];
+            token[j] = i < n ? ws.list[(at * chunks + low) * room + (i - sh.offset[low])] : 0;
         }
+#pragma unroll
+        for (int j = 0; j < kOwn; j++) sh.list[j * kThreads + threadIdx.x] = token[j];
         __syncthreads();
     }
     Kept kept;
@@ -845,8 +880,9 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
         for (int64_t c = 0; c < chunks; c++) {
             const int64_t end = min((c + 1) * chunk, a.vocab);
             double sum = 0.0;
+            double m[8];
             for (int64_t t = c * chunk + threadIdx.x * 8; t < end; t += kTile)
-                sum += kept_mass(row, t, min(t + 8, end), r, kept, sh);
+                sum += kept_masses(row, t, end, r, kept, sh, m);
             sum = block_sum(sum, sh.part);
             if (threadIdx.x == 0) whole[c] = sum;
         }
@@ -882,7 +918,11 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
     draw_in(a, at, row, r, kept, chosen * chunk, min((chosen + 1) * chunk, a.vocab), start, sh);
 }
 
-bool is_short(int64_t vocab) { return vocab <= kShort; }
+// Rows that one workgroup each takes in one launch.  us (this | the four launches), float, temperature alone and all filters:
+//   1 row:     8000 tokens 16.8, 16.0 | 21.8, 23.1;  16000 24.9, 21.4 | 21.7, 23.1;  32000 40.8, 32.2 | 22.3, 23.5
+//   200 rows:  8000 tokens 18.0, 16.6 | 27.6, 27.6;  16000 27.9, 23.4 | 35.8, 34.1;  32000 45.9, 37.3 | 49.3, 42.0
+constexpr int64_t kShort = 4 * kTile, kShortOfMany = 8 * kTile, kMany = 128;
+bool is_short(int64_t rows, int64_t vocab) { return vocab <= (rows < kMany ? kShort : kShortOfMany); }
 
 template <typename T>
 hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
@@ -890,7 +930,7 @@ hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
     while (shift > 30 && a.vocab >> (63 - shift)) shift--;
     constexpr int64_t kStep = 1 << 22;  // workgroups of a launch, which holds fewer than 2^32 threads
     const int64_t chunk = chunk_of(a.rows, a.vocab), chunks = (a.vocab + chunk - 1) / chunk;
-    const int64_t step = is_short(a.vocab) ? kStep : kStep / chunks;
+    const int64_t step = is_short(a.rows, a.vocab) ? kStep : kStep / chunks;
     for (int64_t r0 = 0; r0 < a.rows; r0 += step) {
         SampleArgs p = a;
         p.rows = a.rows - r0 < step ? a.rows - r0 : step;
@@ -901,7 +941,7 @@ hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
         if (p.top_p) p.top_p += r0;
         if (p.min_p) p.min_p += r0;
         p.ids += r0, p.prob += r0, p.kept += r0;
-        if (is_short(a.vocab)) {
+        if (is_short(a.rows, a.vocab)) {
             sample_short_kernel<T><<<(unsigned)p.rows, kThreads, 0, s>>>(p, shift);
         } else {
             SampleSpace ws;
@@ -927,7 +967,12 @@ hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
 }  // namespace
 
 size_t sample_workspace(int64_t rows, int64_t vocab) {
-    return rows == 0 || is_short(vocab) ? 0 : sample_sizes(rows, vocab, nullptr, nullptr);
+    return rows == 0 || is_short(rows, vocab) ? 0 : sample_sizes(rows, vocab, nullptr, nullptr);
+}
+
+size_t sample_workspace_upto(int64_t rows, int64_t vocab) {
+    const int64_t most = is_short(rows, vocab) && rows >= kMany ? kMany - 1 : rows;
+    return sample_workspace(most, vocab);
 }
 
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t stream) {

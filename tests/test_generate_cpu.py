@@ -107,9 +107,9 @@ def test_sample_refusals(sd):  # noqa: F811
 
 def test_sample_workspace_sizes(sd):  # noqa: F811
     """One of the size for the most rows serves every smaller call."""
-    for vocab in (1, 100, 32768, 32769, 50021, 131072, 10**6, 5 * 10**6, 2**31 - 1):
+    for vocab in (1, 100, 16384, 16385, 32768, 32769, 50021, 131072, 10**6, 5 * 10**6, 2**31 - 1):
         sizes = [sd.sdnn_sample_workspace_size(r, vocab) for r in list(range(1100)) + [5000, 100000]]
-        assert sizes == sorted(sizes) and (sizes[1] == 0) == (vocab <= 32768)
+        assert sizes == sorted(sizes) and (sizes[1] == 0) == (vocab <= 16384)
     assert _status(sd, sd.sdnn_sample_workspace_size, -1, 8) == 2
     assert _status(sd, sd.sdnn_sample_workspace_size, 1, 0) == 2
     assert sd.lib.sdnn_sample_workspace_size(1, 8, None) == 1

@@ -50,7 +50,7 @@ def _settings(rng, T, mixed):
 
 
 @pytest.mark.parametrize("T,V", [(1, 1), (5, 2), (9, 3), (20, 7), (33, 100), (40, 1001), (8, 4096), (7, 4097), (5, 20000),
-                                 (4, 32768), (6, 32769), (13, 50021), (3, 131072), (1, 262144), (140, 33000)])
+                                 (4, 16384), (4, 16385), (3, 32768), (130, 32768), (6, 32769), (13, 50021), (3, 131072), (1, 262144), (140, 33000)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("mixed,banned", [(False, 0.0), (True, 0.0), (True, 0.5)])
 def test_sample(torch, sd, T, V, dtype, mixed, banned):  # noqa: F811
