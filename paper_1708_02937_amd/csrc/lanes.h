@@ -110,5 +110,13 @@ __device__ __forceinline__ double wave_upto(double v) {
 __device__ __forceinline__ uint64_t wave_max_last(uint64_t v) {
     return wave_scan(v, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
 }
+// A value of the last lane, in every lane.
+__device__ __forceinline__ uint64_t from_last(uint64_t v) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+}
+__device__ __forceinline__ double wave_total(double v) {
+    return __longlong_as_double((long long)from_last((uint64_t)__double_as_longlong(wave_upto(v))));
+}
 
 }  // namespace sdnn

@@ -11,32 +11,29 @@
 namespace sdnn {
 namespace {
 
-constexpr int kScoreThreads = 256, kScoreTokens = 4;
+constexpr int kScoreThreads = 512, kScoreTokens = 4;
 constexpr int kLayerWaves = 8;
 
 struct LayerSpace {
-    double *logits;  // tokens x experts
-    uint8_t *codes, *scales;  // q(z)
-    float *p;  // a row of code_pitch(inner) values for each slot
+    double *logits;            // tokens x experts
+    uint8_t *codes, *scales;   // q(z)
+    float *p;                  // a row of code_pitch(inner) values for each slot
 };
 
-struct LayerSizes {
-    size_t codes, scales, p, bytes;  // the logits lie at the start
-};
-
-LayerSizes layer_sizes(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen) {
-    LayerSizes s;
-    s.codes = align_up((size_t)tokens * experts * sizeof(double));
-    s.scales = s.codes + align_up((size_t)tokens * code_pitch(width));
-    s.p = s.scales + align_up((size_t)tokens * scale_pitch(width));
-    s.bytes = s.p + (size_t)tokens * chosen * code_pitch(inner) * sizeof(float);
-    return s;
-}
-
-LayerSpace layer_space(const LayerArgs &a) {
-    const LayerSizes s = layer_sizes(a.tokens, a.width, a.inner, a.experts, a.chosen);
-    char *ws = (char *)a.ws;
-    return {(double *)ws, (uint8_t *)ws + s.codes, (uint8_t *)ws + s.scales, (float *)(ws + s.p)};
+size_t layer_sizes(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen, void *at, LayerSpace *ws) {
+    char *p = (char *)at;
+    auto take = [&](size_t bytes) {
+        char *const q = p;
+        p += align_up(bytes);
+        return q;
+    };
+    LayerSpace s;
+    s.logits = (double *)take((size_t)tokens * experts * 8);
+    s.codes = (uint8_t *)take((size_t)tokens * code_pitch(width));
+    s.scales = (uint8_t *)take((size_t)tokens * scale_pitch(width));
+    s.p = (float *)take((size_t)tokens * chosen * code_pitch(inner) * 4);
+    if (ws) *ws = s;
+    return (size_t)(p - (char *)at);
 }
 
 // ------------------------------------------------------------------------------------------------ norm and logits
@@ -90,8 +87,9 @@ __global__ void __launch_bounds__(kScoreThreads) layer_scores_kernel(LayerArgs a
         }
 #pragma unroll
         for (int t = 0; t < kScoreTokens; t++) {
-            dot[t] = wave_sum(dot[t]), sq[t] = wave_sum(sq[t]);
-            if (lane == 0) part[wave][t] = dot[t], part[wave][kScoreTokens + t] = sq[t];
+            if (t0 + t >= a.tokens) break;
+            dot[t] = wave_upto(dot[t]), sq[t] = wave_upto(sq[t]);
+            if (lane == 63) part[wave][t] = dot[t], part[wave][kScoreTokens + t] = sq[t];
         }
         __syncthreads();
         const int64_t t = t0 + threadIdx.x;
@@ -110,8 +108,8 @@ __global__ void __launch_bounds__(kScoreThreads) layer_scores_kernel(LayerArgs a
 #pragma unroll
         for (int i = 0; i < 8; i++) sq = fma(s[i], s[i], sq);
     }
-    sq = wave_sum(sq);
-    if (lane == 0) part[wave][0] = sq;
+    sq = wave_upto(sq);
+    if (lane == 63) part[wave][0] = sq;
     __syncthreads();
     sq = 0.0;
     for (int w = 0; w < kScoreThreads / 64; w++) sq += part[w][0];
@@ -137,8 +135,9 @@ __global__ void __launch_bounds__(kScoreThreads) layer_scores_kernel(LayerArgs a
 }
 
 // ------------------------------------------------------------------------------------------------ the choice
-// The choice in LDS, by every workgroup for itself: a wave takes a token, a lane the experts that are lane modulo 64.
-
+// By every workgroup of the first product for itself, while its first loads could not start anyway: a wave takes a token, a
+// lane the experts that are the lane modulo 64.  A choice is held as a number in the order of its value, above 0 where it
+// can be taken.
 struct Chosen {
     int32_t ids[kLayerMaxTokens * kRouteMaxChosen];
     float weight[kLayerMaxTokens * kRouteMaxChosen];
@@ -147,102 +146,141 @@ struct Chosen {
     int count;
 };
 
+__device__ __forceinline__ uint64_t ordered(double v) {  // 0 for -inf and NaN
+    if (!(v > -INFINITY)) return 0;
+    const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);  // -0 is 0
+    return b ^ ((b >> 63) ? ~0ull : 1ull << 63);
+}
+
+__device__ __forceinline__ double value_of(uint64_t ordered) {
+    return __longlong_as_double((long long)(ordered ^ ((ordered >> 63) ? 1ull << 63 : ~0ull)));
+}
+
+// The largest of a wave's values, in every lane: by moves between registers, as wave_scan.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t max_lower(uint32_t v) {
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = max_lower<0x111, 0xf>(v), v = max_lower<0x112, 0xf>(v), v = max_lower<0x114, 0xf>(v);
+    v = max_lower<0x118, 0xf>(v), v = max_lower<0x142, 0xa>(v), v = max_lower<0x143, 0xc>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// The first index (at: the lane's own) of a wave's largest value, in every lane; -1 where all are 0.
+__device__ __forceinline__ int wave_first(uint64_t v, int at) {
+    const uint32_t high = wave_max((uint32_t)(v >> 32));
+    if (high == 0) return -1;  // ordered values above 0 are 2^32 or more
+    bool in = (uint32_t)(v >> 32) == high;
+    uint64_t equal = __ballot(in);
+    if (equal & (equal - 1)) {
+        const uint32_t low = wave_max(in ? (uint32_t)v : 0);
+        in = in && (uint32_t)v == low;
+        equal = __ballot(in);
+    }
+    int first = __builtin_amdgcn_readlane(at, __ffsll((unsigned long long)equal) - 1);
+    for (equal &= equal - 1; equal; equal &= equal - 1)
+        first = min(first, __builtin_amdgcn_readlane(at, __ffsll((unsigned long long)equal) - 1));
+    return first;
+}
+
 // One token by a wave; `choice` and `score` hold an expert's value each.
-__device__ __forceinline__ void choose(const LayerArgs &a, const double *logits, int t, double *choice, double *score,
+__device__ __forceinline__ void choose(const LayerArgs &a, const double *logits, int t, uint64_t *choice, double *score,
                                        Chosen &c) {
     const int lane = threadIdx.x % 64;
-    double top = -INFINITY;
-    for (int e = lane; e < a.experts; e += 64) {
-        const double l = logits[e];
-        top = l > top ? l : top;
-    }
-    double sum = 0.0;
+    double own = lane < a.experts ? logits[lane] : -INFINITY, sum = 1.0, s = 0.0;  // the lane's first logit, or all of them
     if (!a.sigmoid) {
-        for (int m = 1; m < 64; m <<= 1) top = fmax(top, __shfl_xor(top, m));
-        for (int e = lane; e < a.experts; e += 64) {
+        double top = own > -INFINITY ? own : -INFINITY;
+        for (int e = lane + 64; e < a.experts; e += 64) {
             const double l = logits[e];
-            const double s = !(l > -INFINITY) ? 0.0 : l == top ? 1.0 : exp(l - top);
+            top = l > top ? l : top;
+        }
+        const uint64_t most = from_last(wave_max_last(ordered(top)));
+        top = most ? value_of(most) : -INFINITY;
+        sum = 0.0;
+        for (int e = lane; e < a.experts; e += 64) {
+            const double l = e == lane ? own : logits[e];
+            s = !(l > -INFINITY) ? 0.0 : l == top ? 1.0 : exp(l - top);
             score[e] = s;
             sum += s;
         }
-        sum = wave_sum(sum);
+        sum = wave_total(sum);
     }
     for (int e = lane; e < a.experts; e += 64) {
-        const double l = logits[e];
-        double v = -INFINITY, s = 0.0;
+        const double l = e == lane ? own : logits[e];
+        double v = -INFINITY;
+        s = 0.0;
         if (l > -INFINITY) {
             s = a.sigmoid ? 1.0 / (1.0 + exp(-l)) : score[e] / sum;
             v = a.bias ? s + (double)a.bias[e] : s;
-            if (!(v > -INFINITY)) v = -INFINITY;
         }
         score[e] = s;
-        choice[e] = v;
+        choice[e] = ordered(v);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own LDS writes, read by its other lanes
     if (a.groups > 1) {
         const int size = a.experts / a.groups;
-        double worth = -INFINITY;
+        uint64_t worth = 0;
         if (lane < a.groups) {
-            double one = -INFINITY, two = -INFINITY;
+            uint64_t one = 0, two = 0;
             for (int i = 0; i < size; i++) {
-                const double v = choice[lane * size + i];
-                two = fmax(two, fmin(one, v));
-                one = fmax(one, v);
+                const uint64_t v = choice[lane * size + i];
+                two = two > min(one, v) ? two : min(one, v);
+                one = one > v ? one : v;
             }
-            worth = a.group_best == 2 && two > -INFINITY ? one + two : one;
+            worth = a.group_best == 2 && two ? ordered(value_of(one) + value_of(two)) : one;
         }
         uint64_t kept = 0;
         for (int g = 0; g < a.groups_kept; g++) {
-            double v = worth;
-            int i = lane;
-            wave_best(v, i);
+            const int i = wave_first(worth, lane);
+            if (i < 0) break;
             kept |= 1ull << i;
-            if (lane == i) worth = -INFINITY;
+            if (lane == i) worth = 0;
         }
         for (int e = lane; e < a.experts; e += 64)
-            if (!(kept >> (e / size) & 1)) choice[e] = -INFINITY;
+            if (!(kept >> (e / size) & 1)) choice[e] = 0;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    auto own_best = [&](double &v, int &i) {
-        v = -INFINITY, i = lane;
+    uint64_t mine = 0;
+    int at = lane, id = -1;
+    auto own_best = [&]() {
+        mine = 0;
+#pragma unroll 1
         for (int e = lane; e < a.experts; e += 64)
-            if (choice[e] > v) v = choice[e], i = e;
+            if (choice[e] > mine) mine = choice[e], at = e;
     };
-    double mine;
-    int at, id = -1;
-    own_best(mine, at);
+    own_best();
+#pragma unroll 1
     for (int j = 0; j < a.chosen; j++) {
-        double v = mine;
-        int i = at;
-        wave_best(v, i);
-        if (!(v > -INFINITY)) break;
+        const int i = wave_first(mine, at);
+        if (i < 0) break;
         if (lane == j) id = i;
         if (i % 64 == lane) {
-            choice[i] = -INFINITY;
-            own_best(mine, at);
+            mine = 0;
+            if (a.experts > 64) {
+                choice[i] = 0;
+                own_best();
+            }
         }
     }
-    double s = id >= 0 ? score[id] : 0.0;
+    s = id >= 0 ? score[id] : 0.0;
     if (a.normalize) {
-        const double all = wave_sum(s);
+        const double all = wave_total(s);
         s = all > 0.0 ? s / all : 0.0;
     }
     if (lane < a.chosen) {
         c.ids[t * a.chosen + lane] = id;
         c.weight[t * a.chosen + lane] = (float)(s * (double)a.factor);
-        if (id >= 0) atomicOr(&c.tokens[id], 1u << t);
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// `scratch`: 2 * experts doubles for each wave.
-__device__ __forceinline__ void choose_all(const LayerArgs &a, const LayerSpace &ws, double *scratch, Chosen &c) {
+// The experts' tokens and the busy experts from the ids.
+__device__ __forceinline__ void list_busy(const LayerArgs &a, Chosen &c) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     for (int e = threadIdx.x; e < a.experts; e += 64 * kLayerWaves) c.tokens[e] = 0;
     __syncthreads();
-    double *mine = scratch + (size_t)wave * 2 * a.experts;
-    for (int t = wave; t < a.tokens; t += kLayerWaves)
-        choose(a, ws.logits + (int64_t)t * a.experts, t, mine, mine + a.experts, c);
+    for (int i = threadIdx.x; i < a.tokens * a.chosen; i += 64 * kLayerWaves)
+        if (c.ids[i] >= 0) atomicOr(&c.tokens[c.ids[i]], 1u << (i / a.chosen));
     __syncthreads();
     if (wave == 0) {
         int count = 0;
@@ -264,127 +302,173 @@ __device__ __forceinline__ int place_of(const LayerArgs &a, const Chosen &c, int
     return j;
 }
 
-// ------------------------------------------------------------------------------------------------ the first product
-// p = silu(gate) * up in fp32: a workgroup takes 16 inner values of an expert for all tokens at a time, its waves share
-// the blocks of the width.
-__global__ void __launch_bounds__(64 * kLayerWaves) layer_in_kernel(LayerArgs a, LayerSpace ws) {
-    constexpr int kAhead = 4;
-    extern __shared__ double scratch[];
-    __shared__ Chosen c;
-    __shared__ v4f part[2][kLayerWaves][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
-    choose_all(a, ws, scratch, c);
-    if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < a.tokens * a.chosen; i += 64 * kLayerWaves)
-            a.ids[i] = c.ids[i], a.weight[i] = c.weight[i];
-    const int f_tiles = (int)((a.inner + 15) / 16), kb = (int)blocks_of(a.width);
-    const int64_t pitch = code_pitch(a.width), spitch = scale_pitch(a.width), fb = blocks_of(a.inner);
-    const int64_t row = min((int64_t)low, a.tokens - 1);
-    const uint8_t *x = ws.codes + row * pitch + high * 32, *xs = ws.scales + row * spitch;
-    for (int64_t task = blockIdx.x; task < (int64_t)c.count * f_tiles; task += gridDim.x) {
-        const int e = c.busy[task / f_tiles];
-        const int64_t f0 = task % f_tiles * 16, f = min(f0 + low, a.inner - 1);
-        const uint8_t *gate = a.w_in + ((int64_t)e * 2 * a.inner + f) * pitch + high * 32;
-        const uint8_t *gate_s = a.w_in_scale + ((int64_t)e * 2 * fb + f0 / kBlock) * spitch;
-        const uint8_t *w[2] = {gate, gate + a.inner * pitch}, *s[2] = {gate_s, gate_s + fb * spitch};
-        v4f acc[2] = {};
-        for (int b0 = wave; b0 < kb; b0 += kLayerWaves * kAhead) {
-            v8i wq[kAhead][2], xq[kAhead];
-            int wc[kAhead][2], xc[kAhead];
+// ------------------------------------------------------------------------------------------------ the experts
+// One launch for each product.  (Both in one, with tiles of outputs that load their weights and wait for p, were twice as slow:
+// a ticket for each tile is an atomic that all chiplets share, and a row of them takes 95 ns each.)
+
+// p = silu(gate) * up in fp32 of 16 inner values of an expert for all tokens; the waves share the blocks of the width.  A
+// wave's blocks are taken four at a time, and the next four, of the next tile where these are the last, are on their way while
+// these are multiplied.
+struct InTile {
+    v4f part[2][kLayerWaves][64];
+};
+
+constexpr int kAhead = 4;
+struct InWeights {
+    v8i q[kAhead][2];
+    int code[kAhead][2];
+};
+struct InRows {
+    v8i q[kAhead];
+    int code[kAhead];
+};
+
+__device__ __forceinline__ void load_weights(const LayerArgs &a, const Chosen &c, int64_t task, int turn, InWeights &w) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t f_tiles = (a.inner + 15) / 16, pitch = code_pitch(a.width), spitch = scale_pitch(a.width),
+                  fb = blocks_of(a.inner);
+    const int kb = (int)blocks_of(a.width), e = c.busy[task / f_tiles];
+    const int64_t f0 = task % f_tiles * 16, f = min(f0 + lane % 16, a.inner - 1);
+    const uint8_t *gate = a.w_in + ((int64_t)e * 2 * a.inner + f) * pitch + lane / 16 * 32;
+    const uint8_t *gate_s = a.w_in_scale + ((int64_t)e * 2 * fb + f0 / kBlock) * spitch;
 #pragma unroll
-            for (int u = 0; u < kAhead; u++) {
-                const int b = min(b0 + u * kLayerWaves, kb - 1);
+    for (int u = 0; u < kAhead; u++) {
+        const int b = min((turn * kAhead + u) * kLayerWaves + wave, kb - 1);
 #pragma unroll
-                for (int v = 0; v < 2; v++) wq[u][v] = load32(w[v] + (int64_t)b * kBlock), wc[u][v] = s[v][b];
-                xq[u] = load32(x + (int64_t)b * kBlock), xc[u] = xs[b];
-            }
-#pragma unroll
-            for (int u = 0; u < kAhead; u++)
-                if (b0 + u * kLayerWaves < kb)
-#pragma unroll
-                    for (int v = 0; v < 2; v++) acc[v] = block16(wq[u][v], xq[u], acc[v], wc[u][v], xc[u]);
+        for (int v = 0; v < 2; v++) {
+            w.q[u][v] = load32(gate + v * a.inner * pitch + (int64_t)b * kBlock);
+            w.code[u][v] = gate_s[v * fb * spitch + b];
         }
-        part[0][wave][lane] = acc[0], part[1][wave][lane] = acc[1];
-        __syncthreads();
-        if (wave == 0 && (c.tokens[e] >> low & 1)) {
-            v4f g = part[0][0][lane], u = part[1][0][lane];
-            for (int i = 1; i < kLayerWaves; i++) g += part[0][i][lane], u += part[1][i][lane];
-            float *to = ws.p + ((int64_t)low * a.chosen + place_of(a, c, low, e)) * code_pitch(a.inner);
-            for (int i = 0; i < 4; i++) {
-                const int64_t col = f0 + high * 4 + i;
-                if (col < a.inner) to[col] = silu_times<false>(g[i], u[i]);
-            }
-        }
-        __syncthreads();
     }
 }
 
-// ------------------------------------------------------------------------------------------------ the second product
-// A workgroup takes 16 outputs of all tokens, its waves share the busy experts' blocks, four at a time.
-template <typename T>
-__global__ void __launch_bounds__(64 * kLayerWaves) layer_out_kernel(LayerArgs a, LayerSpace ws) {
-    constexpr int kPass = 4;
-    extern __shared__ double scratch[];
-    __shared__ Chosen c;
-    __shared__ v4f part[kLayerWaves][64];
+__device__ __forceinline__ void load_rows(const LayerArgs &a, const LayerSpace &ws, int turn, InRows &x) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, kb = (int)blocks_of(a.width);
+    const int64_t row = min((int64_t)(lane % 16), a.tokens - 1);
+    const uint8_t *q = ws.codes + row * code_pitch(a.width) + lane / 16 * 32, *s = ws.scales + row * scale_pitch(a.width);
+#pragma unroll
+    for (int u = 0; u < kAhead; u++) {
+        const int b = min((turn * kAhead + u) * kLayerWaves + wave, kb - 1);
+        x.q[u] = load32(q + (int64_t)b * kBlock), x.code[u] = s[b];
+    }
+}
+
+// The end of a tile: the waves' sums, and p.
+__device__ __forceinline__ void put_p(const LayerArgs &a, const LayerSpace &ws, const Chosen &c, int64_t task, const v4f (&acc)[2],
+                                      InTile &tile) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
-    choose_all(a, ws, scratch, c);
-    const int kb = (int)blocks_of(a.inner), passes = (kb + kPass - 1) / kPass;
-    const int64_t pitch = code_pitch(a.inner), spitch = scale_pitch(a.inner);
-    const int64_t n0 = (int64_t)blockIdx.x * 16, n = min(n0 + low, a.width - 1);
-    // the wave's own: the scales of 16 rows' blocks, and the rows' codes
-    uint8_t *const codes = (uint8_t *)scratch + wave * (size_t)(kLayerMaxTokens * 16 + a.tokens * kPass * kBlock) +
-                           kLayerMaxTokens * 16;
-    int *const scale = (int *)(codes - kLayerMaxTokens * 16);
-    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int64_t f_tiles = (a.inner + 15) / 16, f0 = task % f_tiles * 16;
+    const int e = c.busy[task / f_tiles];
+    tile.part[0][wave][lane] = acc[0], tile.part[1][wave][lane] = acc[1];
     __syncthreads();
-    for (int64_t u = wave; u < (int64_t)c.count * passes; u += kLayerWaves) {
-        const int e = c.busy[u / passes], b0 = (int)(u % passes) * kPass;
-        const uint8_t *w = a.w_out + ((int64_t)e * a.width + n) * pitch + high * 32;
+    if (wave == 0 && (c.tokens[e] >> low & 1)) {
+        v4f g = tile.part[0][0][lane], u = tile.part[1][0][lane];
+        for (int i = 1; i < kLayerWaves; i++) g += tile.part[0][i][lane], u += tile.part[1][i][lane];
+        float *to = ws.p + ((int64_t)low * a.chosen + place_of(a, c, low, e)) * code_pitch(a.inner) + f0 + high * 4;
+        v4f p;  // rows are padded to 128 values, so four of them never leave their row
+        for (int i = 0; i < 4; i++) p[i] = silu_times<false>(g[i], u[i]);
+        *(v4f *)to = p;
+    }
+    __syncthreads();
+}
+
+// 16 outputs of all tokens; the waves share the busy experts' blocks, four at a time, and take the rows of up to four tokens
+// at a time through their own space.
+constexpr int kPass = 4;
+template <int ROWS>
+struct OutTile {
+    v4f part[kLayerWaves][64];
+    struct {
+        uint8_t codes[ROWS][kPass * kBlock];
+        int scale[ROWS][kPass];
+    } rows[kLayerWaves];
+};
+
+template <typename T, int ROWS>
+__device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &ws, const Chosen &c, int64_t n0,
+                                         OutTile<ROWS> &tile) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
+    const int kb = (int)blocks_of(a.inner), passes = (kb + kPass - 1) / kPass;
+    const int64_t pitch = code_pitch(a.inner), spitch = scale_pitch(a.inner), n = min(n0 + low, a.width - 1);
+    auto &own = tile.rows[wave];
+    const int units = c.count * passes;
+    struct Weights {
+        v8i q[kPass];
+        int code[kPass];
+    };
+    auto load = [&](int u, Weights &w) {
+        const int e = c.busy[u / passes], b0 = u % passes * kPass;
+        const uint8_t *p = a.w_out + ((int64_t)e * a.width + n) * pitch + high * 32;
         const uint8_t *s = a.w_out_scale + ((int64_t)e * blocks_of(a.width) + n0 / kBlock) * spitch;
-        v8i wq[kPass];
-        int wc[kPass];
 #pragma unroll
         for (int i = 0; i < kPass; i++) {
             const int b = min(b0 + i, kb - 1);
-            wq[i] = load32(w + (int64_t)b * kBlock), wc[i] = s[b];
+            w.q[i] = load32(p + (int64_t)b * kBlock), w.code[i] = s[b];
         }
-        // the routed rows of p in 8 bits, 16 lanes to a block; this lane's token is the place-th of them
+    };
+    Weights next;
+    if (wave < units) load(wave, next);
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int u = wave; u < units; u += kLayerWaves) {
+        const int e = c.busy[u / passes], b0 = u % passes * kPass;
+        const Weights w = next;
+        if (u + kLayerWaves < units) load(u + kLayerWaves, next);  // on their way while these are multiplied
         const uint32_t routed = c.tokens[e];
-        int place = 0;
-        for (uint32_t left = routed, r = 0; left; left &= left - 1, r++) {
-            const int t = __ffs(left) - 1;
-            if (t == low) place = r;
-            const float *row = ws.p + ((int64_t)t * a.chosen + place_of(a, c, t, e)) * pitch;
-            float v[8], amax = 0.0f;
-            load8<float, false>(row, (int64_t)b0 * kBlock + lane * 8, a.inner, v);
-#pragma unroll
-            for (int i = 0; i < 8; i++) amax = fmaxf(amax, finite_abs(v[i]));
-            const int code = scale_code(row16_max(amax));
-            const float inv = inverse_scale(code);
-            *(int2 *)(codes + r * (kPass * kBlock) + lane * 8) =
-                make_int2(pack_e4m3(v[0], v[1], v[2], v[3], inv), pack_e4m3(v[4], v[5], v[6], v[7], inv));
-            if (low == 0) scale[r * kPass + high] = code;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const bool mine = routed >> low & 1;
+        const int place = __popc(routed & ((1u << low) - 1));  // of this lane's token among the routed ones
         const float weight = mine ? c.weight[low * a.chosen + place_of(a, c, low, e)] : 0.0f;
+        const int64_t col = (int64_t)b0 * kBlock + lane * 8;
+        uint32_t left = routed;
+        for (int r0 = 0; left; r0 += ROWS) {
+            // the rows of p in 8 bits, 16 lanes to a block
+            float v[ROWS][8];
+            uint32_t rest = left;
 #pragma unroll
-        for (int i = 0; i < kPass; i++) {
-            if (b0 + i >= kb) break;
-            const v4f z = codes16(wq[i], load32(codes + place * (kPass * kBlock) + i * kBlock + high * 32));
-            const int shift = wc[i] + scale[place * kPass + i] - 2 * kOne;
-            if (mine)
+            for (int r = 0; r < ROWS; r++) {
+                if (!rest) break;
+                const int t = __ffs(rest) - 1;
+                rest &= rest - 1;
+                const float *row = ws.p + ((int64_t)t * a.chosen + place_of(a, c, t, e)) * pitch + min(col, pitch - 8);
+                const v4f lo = *(const v4f *)row, hi = *(const v4f *)(row + 4);
 #pragma unroll
-                for (int v = 0; v < 4; v++) acc[v] = fmaf(weight, ldexpf(z[v], shift), acc[v]);
+                for (int i = 0; i < 4; i++) v[r][i] = lo[i], v[r][4 + i] = hi[i];
+            }
+#pragma unroll
+            for (int r = 0; r < ROWS; r++) {
+                if (!left) break;
+                left &= left - 1;
+                float amax = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    if (col + i >= a.inner) v[r][i] = 0.0f;
+                    amax = fmaxf(amax, finite_abs(v[r][i]));
+                }
+                const int code = scale_code(row16_max(amax));
+                const float inv = inverse_scale(code);
+                *(int2 *)(own.codes[r] + lane * 8) = make_int2(pack_e4m3(v[r][0], v[r][1], v[r][2], v[r][3], inv),
+                                                               pack_e4m3(v[r][4], v[r][5], v[r][6], v[r][7], inv));
+                if (low == 0) own.scale[r][high] = code;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own LDS, read by its other lanes
+            const bool here = mine && place >= r0 && place < r0 + ROWS;
+            const int at = here ? place - r0 : 0;
+#pragma unroll
+            for (int i = 0; i < kPass; i++) {
+                if (b0 + i >= kb) break;
+                const v4f z = codes16(w.q[i], load32(own.codes[at] + i * kBlock + high * 32));
+                const int shift = w.code[i] + own.scale[at][i] - 2 * kOne;
+                if (here)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) acc[k] = fmaf(weight, ldexpf(z[k], shift), acc[k]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    part[wave][lane] = acc;
+    tile.part[wave][lane] = acc;
     __syncthreads();
     if (wave != 0 || low >= a.tokens) return;
-    v4f sum = part[0][lane];
-    for (int i = 1; i < kLayerWaves; i++) sum += part[i][lane];
+    v4f sum = tile.part[0][lane];
+    for (int i = 1; i < kLayerWaves; i++) sum += tile.part[i][lane];
     for (int i = 0; i < 4; i++) {
         const int64_t col = n0 + high * 4 + i;
         if (col >= a.width) break;
@@ -394,35 +478,90 @@ __global__ void __launch_bounds__(64 * kLayerWaves) layer_out_kernel(LayerArgs a
     }
 }
 
+constexpr int kMostIn = 256;  // workgroups of the first product: one to a CU, with two tiles' weights in its registers
+constexpr size_t choice_space(int64_t experts) { return (size_t)kLayerWaves * 2 * experts * sizeof(double); }
+
+__global__ void __launch_bounds__(64 * kLayerWaves) layer_in_kernel(LayerArgs a, LayerSpace ws) {
+    extern __shared__ double scratch[];  // the choices, then the tiles
+    __shared__ Chosen c;
+    const int wave = threadIdx.x / 64;
+    double *score = scratch + (size_t)wave * 2 * a.experts;
+    for (int t = wave; t < a.tokens; t += kLayerWaves)
+        choose(a, ws.logits + (int64_t)t * a.experts, t, (uint64_t *)(score + a.experts), score, c);
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < a.tokens * a.chosen; i += 64 * kLayerWaves)
+            a.ids[i] = c.ids[i], a.weight[i] = c.weight[i];
+    list_busy(a, c);
+    const int kb = (int)blocks_of(a.width), turns = (kb + kAhead * kLayerWaves - 1) / (kAhead * kLayerWaves);
+    const int64_t tasks = c.count * ((a.inner + 15) / 16);
+    int64_t task = blockIdx.x;
+    if (task >= tasks) return;
+    InWeights next;
+    InRows x;
+    load_rows(a, ws, 0, x);
+    load_weights(a, c, task, 0, next);
+    v4f acc[2] = {};
+    for (int turn = 0; task < tasks;) {
+        const InWeights w = next;
+        const bool last = turn + 1 == turns;
+        const int64_t then = last ? task + gridDim.x : task;
+        if (then < tasks) load_weights(a, c, then, last ? 0 : turn + 1, next);
+#pragma unroll
+        for (int u = 0; u < kAhead; u++)
+            if ((turn * kAhead + u) * kLayerWaves + wave < kb)
+#pragma unroll
+                for (int v = 0; v < 2; v++) acc[v] = block16(w.q[u][v], x.q[u], acc[v], w.code[u][v], x.code[u]);
+        if (turns > 1) load_rows(a, ws, last ? 0 : turn + 1, x);
+        if (last) {
+            put_p(a, ws, c, task, acc, *(InTile *)scratch);
+            acc[0] = acc[1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        task = then;
+        turn = last ? 0 : turn + 1;
+    }
+}
+
+template <typename T, int ROWS>
+__global__ void __launch_bounds__(64 * kLayerWaves) layer_out_kernel(LayerArgs a, LayerSpace ws) {
+    __shared__ Chosen c;
+    __shared__ OutTile<ROWS> tile;
+    for (int i = threadIdx.x; i < a.tokens * a.chosen; i += 64 * kLayerWaves)
+        c.ids[i] = a.ids[i], c.weight[i] = a.weight[i];
+    __syncthreads();
+    list_busy(a, c);
+    out_tile<T, ROWS>(a, ws, c, (int64_t)blockIdx.x * 16, tile);
+}
+
 template <typename T, typename R>
 hipError_t layer_go(const LayerArgs &a, hipStream_t s) {
-    const LayerSpace ws = layer_space(a);
+    LayerSpace ws;
+    layer_sizes(a.tokens, a.width, a.inner, a.experts, a.chosen, a.ws, &ws);
     const int parts = (int)((a.tokens + kScoreTokens - 1) / kScoreTokens);
     layer_scores_kernel<T, R><<<(unsigned)(a.experts * parts + a.tokens), kScoreThreads, 0, s>>>(a, ws, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    static std::atomic<unsigned long long> raised[2];
-    constexpr size_t kMostChoice = (size_t)kLayerWaves * 2 * kRouteMaxExperts * sizeof(double);
-    constexpr size_t kRow = 4 * kBlock;
-    const size_t choice = (size_t)kLayerWaves * 2 * a.experts * sizeof(double);
-    const size_t rows = (size_t)kLayerWaves * (kLayerMaxTokens * 16 + a.tokens * kRow);
-    const size_t out = choice > rows ? choice : rows;
-    e = raise_lds_limit((const void *)layer_in_kernel, kMostChoice, raised[0]);
-    if (e == hipSuccess) e = raise_lds_limit((const void *)layer_out_kernel<T>, kMostChoice, raised[1]);
+    static std::atomic<unsigned long long> raised;
+    e = raise_lds_limit((const void *)layer_in_kernel, choice_space(kRouteMaxExperts), raised);
     if (e != hipSuccess) return e;
+    const size_t choice = choice_space(a.experts), lds = choice > sizeof(InTile) ? choice : sizeof(InTile);
     const int64_t slots = a.tokens * a.chosen, most = slots < a.experts ? slots : a.experts;
-    const int64_t tasks = most * ((a.inner + 15) / 16), tiles = (a.width + 15) / 16;
-    layer_in_kernel<<<(unsigned)(tasks < 512 ? tasks : 512), 64 * kLayerWaves, choice, s>>>(a, ws);
+    const int64_t tasks = most * ((a.inner + 15) / 16);
+    layer_in_kernel<<<(unsigned)(tasks < kMostIn ? tasks : kMostIn), 64 * kLayerWaves, lds, s>>>(a, ws);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    layer_out_kernel<T><<<(unsigned)tiles, 64 * kLayerWaves, out, s>>>(a, ws);
+    const unsigned tiles = (unsigned)((a.width + 15) / 16);
+    if (a.tokens == 1)
+        layer_out_kernel<T, 1><<<tiles, 64 * kLayerWaves, 0, s>>>(a, ws);
+    else
+        layer_out_kernel<T, 4><<<tiles, 64 * kLayerWaves, 0, s>>>(a, ws);
     return hipGetLastError();
 }
 
 }  // namespace
 
 size_t layer_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen) {
-    return layer_sizes(tokens, width, inner, experts, chosen).bytes;
+    return layer_sizes(tokens, width, inner, experts, chosen, nullptr, nullptr);
 }
 
 hipError_t launch_layer(const LayerArgs &a, bool bf16, bool router_bf16, hipStream_t stream) {
