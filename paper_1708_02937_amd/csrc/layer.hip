@@ -11,13 +11,14 @@
 namespace sdnn {
 namespace {
 
-constexpr int kScoreThreads = 512, kScoreTokens = 4;
+constexpr int kScoreThreads = 512;
 constexpr int kLayerWaves = 8;
 
 struct LayerSpace {
     double *logits;            // tokens x experts
     uint8_t *codes, *scales;   // q(z)
     float *p;                  // a row of code_pitch(inner) values for each slot
+    uint32_t *busy;            // how many experts are busy, which, and each one's tokens
 };
 
 size_t layer_sizes(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen, void *at, LayerSpace *ws) {
@@ -32,6 +33,7 @@ size_t layer_sizes(int64_t tokens, int64_t width, int64_t inner, int32_t experts
     s.codes = (uint8_t *)take((size_t)tokens * code_pitch(width));
     s.scales = (uint8_t *)take((size_t)tokens * scale_pitch(width));
     s.p = (float *)take((size_t)tokens * chosen * code_pitch(inner) * 4);
+    s.busy = (uint32_t *)take((1 + 2 * (size_t)experts) * 4);
     if (ws) *ws = s;
     return (size_t)(p - (char *)at);
 }
@@ -59,25 +61,24 @@ __device__ __forceinline__ double rstd_of(const LayerArgs &a, double sq) {
     return 1.0 / sqrt(sq / (double)a.width + a.eps);
 }
 
-template <typename T, typename R>
+template <typename T, typename R, int TOKENS>
 __global__ void __launch_bounds__(kScoreThreads) layer_scores_kernel(LayerArgs a, LayerSpace ws, int parts) {
-    __shared__ double part[kScoreThreads / 64][2 * kScoreTokens];
+    __shared__ double part[kScoreThreads / 64][2 * TOKENS];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int scores = a.experts * parts;
     if ((int)blockIdx.x < scores) {
         const int e = blockIdx.x % a.experts;
-        const int64_t t0 = (int64_t)(blockIdx.x / a.experts) * kScoreTokens;
+        const int64_t t0 = (int64_t)(blockIdx.x / a.experts) * TOKENS;
         const R *router = (const R *)a.router + (int64_t)e * a.ldw;
-        double dot[kScoreTokens] = {}, sq[kScoreTokens] = {};
+        double dot[TOKENS] = {}, sq[TOKENS] = {};
         for (int64_t c = threadIdx.x * 8; c < a.width; c += kScoreThreads * 8) {
             float w[8], g[8];
             load8<R, false>(router, c, a.width, w);
             load8<float, false>(a.gamma, c, a.width, g);
 #pragma unroll
-            for (int t = 0; t < kScoreTokens; t++) {
-                if (t0 + t >= a.tokens) break;
+            for (int t = 0; t < TOKENS; t++) {
                 double s[8];
-                row8<T>(a, t0 + t, c, s);
+                row8<T>(a, min(t0 + t, a.tokens - 1), c, s);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     sq[t] = fma(s[i], s[i], sq[t]);
@@ -86,16 +87,15 @@ __global__ void __launch_bounds__(kScoreThreads) layer_scores_kernel(LayerArgs a
             }
         }
 #pragma unroll
-        for (int t = 0; t < kScoreTokens; t++) {
-            if (t0 + t >= a.tokens) break;
+        for (int t = 0; t < TOKENS; t++) {
             dot[t] = wave_upto(dot[t]), sq[t] = wave_upto(sq[t]);
-            if (lane == 63) part[wave][t] = dot[t], part[wave][kScoreTokens + t] = sq[t];
+            if (lane == 63) part[wave][t] = dot[t], part[wave][TOKENS + t] = sq[t];
         }
         __syncthreads();
         const int64_t t = t0 + threadIdx.x;
-        if (threadIdx.x >= kScoreTokens || t >= a.tokens) return;
+        if (threadIdx.x >= TOKENS || t >= a.tokens) return;
         double d = 0.0, q = 0.0;
-        for (int w = 0; w < kScoreThreads / 64; w++) d += part[w][threadIdx.x], q += part[w][kScoreTokens + threadIdx.x];
+        for (int w = 0; w < kScoreThreads / 64; w++) d += part[w][threadIdx.x], q += part[w][TOKENS + threadIdx.x];
         const bool live = !a.live || a.live[t];
         ws.logits[t * a.experts + e] = live ? d * rstd_of(a, q) : -INFINITY;
         return;
@@ -406,47 +406,62 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
             w.q[i] = load32(p + (int64_t)b * kBlock), w.code[i] = s[b];
         }
     };
+    // the next rows of p, as many as ROWS, of the tokens in `left`, which loses them
+    struct Rows {
+        v4f v[ROWS][2];
+    };
+    auto load_p = [&](int u, uint32_t &left, Rows &x) {
+        const int e = c.busy[u / passes];
+        const int64_t col = min((int64_t)(u % passes) * (kPass * kBlock) + lane * 8, pitch - 8);
+#pragma unroll
+        for (int r = 0; r < ROWS; r++) {
+            if (!left) break;
+            const int t = __ffs(left) - 1;
+            left &= left - 1;
+            const float *row = ws.p + ((int64_t)t * a.chosen + place_of(a, c, t, e)) * pitch + col;
+            x.v[r][0] = *(const v4f *)row, x.v[r][1] = *(const v4f *)(row + 4);
+        }
+    };
     Weights next;
-    if (wave < units) load(wave, next);
+    Rows next_p;
+    uint32_t next_left = 0;
+    if (wave < units) {
+        load(wave, next);
+        next_left = c.tokens[wave / passes];
+        load_p(wave, next_left, next_p);
+    }
     v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int u = wave; u < units; u += kLayerWaves) {
         const int e = c.busy[u / passes], b0 = u % passes * kPass;
+        const uint32_t routed = c.tokens[u / passes];
         const Weights w = next;
-        if (u + kLayerWaves < units) load(u + kLayerWaves, next);  // on their way while these are multiplied
-        const uint32_t routed = c.tokens[e];
+        Rows x = next_p;
+        uint32_t left = next_left;
+        if (u + kLayerWaves < units) {  // on their way while these are multiplied
+            load(u + kLayerWaves, next);
+            next_left = c.tokens[(u + kLayerWaves) / passes];
+            load_p(u + kLayerWaves, next_left, next_p);
+        }
         const bool mine = routed >> low & 1;
-        const int place = __popc(routed & ((1u << low) - 1));  // of this lane's token among the routed ones
+        const int place = __popc(routed & ((1u << low) - 1)), count = __popc(routed);  // of this lane's token among them
         const float weight = mine ? c.weight[low * a.chosen + place_of(a, c, low, e)] : 0.0f;
         const int64_t col = (int64_t)b0 * kBlock + lane * 8;
-        uint32_t left = routed;
-        for (int r0 = 0; left; r0 += ROWS) {
+        for (int r0 = 0; r0 < count; r0 += ROWS) {
+            if (r0 > 0) load_p(u, left, x);
             // the rows of p in 8 bits, 16 lanes to a block
-            float v[ROWS][8];
-            uint32_t rest = left;
 #pragma unroll
             for (int r = 0; r < ROWS; r++) {
-                if (!rest) break;
-                const int t = __ffs(rest) - 1;
-                rest &= rest - 1;
-                const float *row = ws.p + ((int64_t)t * a.chosen + place_of(a, c, t, e)) * pitch + min(col, pitch - 8);
-                const v4f lo = *(const v4f *)row, hi = *(const v4f *)(row + 4);
-#pragma unroll
-                for (int i = 0; i < 4; i++) v[r][i] = lo[i], v[r][4 + i] = hi[i];
-            }
-#pragma unroll
-            for (int r = 0; r < ROWS; r++) {
-                if (!left) break;
-                left &= left - 1;
-                float amax = 0.0f;
+                if (r0 + r >= count) break;
+                float v[8], amax = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    if (col + i >= a.inner) v[r][i] = 0.0f;
-                    amax = fmaxf(amax, finite_abs(v[r][i]));
+                    v[i] = col + i < a.inner ? x.v[r][i / 4][i % 4] : 0.0f;
+                    amax = fmaxf(amax, finite_abs(v[i]));
                 }
                 const int code = scale_code(row16_max(amax));
                 const float inv = inverse_scale(code);
-                *(int2 *)(own.codes[r] + lane * 8) = make_int2(pack_e4m3(v[r][0], v[r][1], v[r][2], v[r][3], inv),
-                                                               pack_e4m3(v[r][4], v[r][5], v[r][6], v[r][7], inv));
+                *(int2 *)(own.codes[r] + lane * 8) =
+                    make_int2(pack_e4m3(v[0], v[1], v[2], v[3], inv), pack_e4m3(v[4], v[5], v[6], v[7], inv));
                 if (low == 0) own.scale[r][high] = code;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own LDS, read by its other lanes
@@ -489,10 +504,14 @@ __global__ void __launch_bounds__(64 * kLayerWaves) layer_in_kernel(LayerArgs a,
     for (int t = wave; t < a.tokens; t += kLayerWaves)
         choose(a, ws.logits + (int64_t)t * a.experts, t, (uint64_t *)(score + a.experts), score, c);
     __syncthreads();
-    if (blockIdx.x == 0)
+    list_busy(a, c);
+    if (blockIdx.x == 0) {
         for (int i = threadIdx.x; i < a.tokens * a.chosen; i += 64 * kLayerWaves)
             a.ids[i] = c.ids[i], a.weight[i] = c.weight[i];
-    list_busy(a, c);
+        for (int i = threadIdx.x; i < c.count; i += 64 * kLayerWaves)
+            ws.busy[1 + 2 * i] = c.busy[i], ws.busy[2 + 2 * i] = c.tokens[c.busy[i]];
+        if (threadIdx.x == 0) ws.busy[0] = c.count;
+    }
     const int kb = (int)blocks_of(a.width), turns = (kb + kAhead * kLayerWaves - 1) / (kAhead * kLayerWaves);
     const int64_t tasks = c.count * ((a.inner + 15) / 16);
     int64_t task = blockIdx.x;
@@ -526,10 +545,13 @@ template <typename T, int ROWS>
 __global__ void __launch_bounds__(64 * kLayerWaves) layer_out_kernel(LayerArgs a, LayerSpace ws) {
     __shared__ Chosen c;
     __shared__ OutTile<ROWS> tile;
+    const int most = (int)min(a.tokens * a.chosen, (int64_t)a.experts);
+    if (threadIdx.x == 0) c.count = (int)ws.busy[0];
+    for (int i = threadIdx.x; i < most; i += 64 * kLayerWaves)  // past the count they are what the workspace held
+        c.busy[i] = (uint16_t)ws.busy[1 + 2 * i], c.tokens[i] = ws.busy[2 + 2 * i];  // by place among the busy ones
     for (int i = threadIdx.x; i < a.tokens * a.chosen; i += 64 * kLayerWaves)
         c.ids[i] = a.ids[i], c.weight[i] = a.weight[i];
     __syncthreads();
-    list_busy(a, c);
     out_tile<T, ROWS>(a, ws, c, (int64_t)blockIdx.x * 16, tile);
 }
 
@@ -537,8 +559,12 @@ template <typename T, typename R>
 hipError_t layer_go(const LayerArgs &a, hipStream_t s) {
     LayerSpace ws;
     layer_sizes(a.tokens, a.width, a.inner, a.experts, a.chosen, a.ws, &ws);
-    const int parts = (int)((a.tokens + kScoreTokens - 1) / kScoreTokens);
-    layer_scores_kernel<T, R><<<(unsigned)(a.experts * parts + a.tokens), kScoreThreads, 0, s>>>(a, ws, parts);
+    const int each = a.tokens == 1 ? 1 : 4, parts = (int)((a.tokens + each - 1) / each);
+    const unsigned scores = (unsigned)(a.experts * parts + a.tokens);
+    if (each == 1)
+        layer_scores_kernel<T, R, 1><<<scores, kScoreThreads, 0, s>>>(a, ws, parts);
+    else
+        layer_scores_kernel<T, R, 4><<<scores, kScoreThreads, 0, s>>>(a, ws, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     static std::atomic<unsigned long long> raised;
