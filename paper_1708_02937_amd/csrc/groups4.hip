@@ -135,6 +135,8 @@ struct Rows32<__bf16> {
     __device__ __forceinline__ void zero() {
         for (int i = 0; i < 4; i++) v[i] = v8bf{};
     }
+    // columns 8 i .. + 7 of 32 in LDS
+    __device__ __forceinline__ void read(int i, const uint8_t *p) { v[i] = *(const v8bf *)(p + 16 * i); }
     __device__ __forceinline__ void parts(int i, v8bf (&p)[1]) const { p[0] = v[i]; }
 };
 template <>
@@ -152,6 +154,9 @@ struct Rows32<float> {
     }
     __device__ __forceinline__ void zero() {
         for (int i = 0; i < 8; i++) v[i] = v4f{};
+    }
+    __device__ __forceinline__ void read(int i, const uint8_t *p) {
+        v[2 * i] = *(const v4f *)(p + 32 * i), v[2 * i + 1] = *(const v4f *)(p + 32 * i + 16);
     }
     // The upper half of a float's bits is the float cut off to bfloat16; a NaN whose bits are all below keeps one.
     __device__ __forceinline__ void parts(int i, v8bf (&p)[3]) const {
@@ -171,108 +176,227 @@ struct Rows32<float> {
     }
 };
 
-// 16 NW outputs of 16 MT rows.  Each wave takes a run of steps and loads AHEAD of them before it multiplies the first.
-template <typename TX, typename TY, int MT, int NW, int AHEAD>
+// ---- up to 16 rows: 16 NW outputs at a time, by workgroups that stay.  Each wave takes a run of the steps, STEPS at a turn, and
+// the weights of its next turn, of the next tile where this one is the tile's last, are on their way while this turn's are
+// multiplied.  Rows that fit one turn are kept in registers.
+template <int STEPS, int NW>
+struct Weights4 {
+    v4i q[STEPS][NW];
+    uint32_t code[STEPS][NW];  // of the step's four groups
+};
+
+template <typename TY>
+__device__ __forceinline__ void put_outputs(const GroupProductArgs &a, int64_t m, int64_t n0, v4f z) {
+    TY *y = (TY *)a.y + m * a.ldy;
+    for (int i = 0; i < 4; i++) {
+        if (n0 + i >= a.n) break;
+        if (a.bias) z[i] += a.bias[n0 + i];
+        if (a.activate) z[i] = relu_clamp(z[i], a.ymax);
+        y[n0 + i] = (TY)z[i];
+    }
+}
+
+// acc += the products of a step's columns 8 i .. + 7 of each lane's 32.
+template <int PARTS>
+__device__ __forceinline__ v4f multiply(const v8bf &wide, const v8bf (&p)[PARTS], v4f acc) {
+#pragma unroll
+    for (int c = PARTS - 1; c >= 0; c--) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, p[c], acc, 0, 0, 0);
+    return acc;
+}
+
+template <typename TX, typename TY, int NW, int STEPS>
 __global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProductArgs a) {
-    __shared__ v4f part[kWaves / 2][MT * NW][64];
+    __shared__ v4f part[2][kWaves][NW][64];  // of two tiles, so that each needs one barrier
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
-    const int64_t n0 = (int64_t)blockIdx.x * (16 * NW), m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int steps = (int)blocks_of(a.k), each = (steps + kWaves - 1) / kWaves;
+    const int64_t tiles = (a.n + 16 * NW - 1) / (16 * NW);
+    const int steps = (int)blocks_of(a.k), each = (steps + kWaves - 1) / kWaves, turns = (each + STEPS - 1) / STEPS;
     const int begin = min(wave * each, steps), end = min(begin + each, steps);
-    const uint8_t *w[NW], *ws[NW];
+    const int64_t pitch = group_pitch(a.k), spitch = group_scale_pitch(a.k);
+    const bool there = low < a.m;
+    const TX *const x = (const TX *)a.x + (there ? low : 0) * a.ldx;
+    auto load_weights = [&](int64_t tile, int turn, Weights4<STEPS, NW> &w) {
+        const int s0 = begin + turn * STEPS;
 #pragma unroll
-    for (int v = 0; v < NW; v++) {
-        const int64_t n = min(n0 + 16 * v + low, a.n - 1);
-        w[v] = a.w + n * group_pitch(a.k) + high * 16;
-        ws[v] = a.w_scale + n * group_scale_pitch(a.k) + high;
-    }
-    const TX *x[MT];
-    bool there[MT];
+        for (int v = 0; v < NW; v++) {
+            const int64_t n = min(tile * (16 * NW) + 16 * v + low, a.n - 1);
+            const uint8_t *q = a.w + n * pitch + (int64_t)s0 * (kBlock / 2) + high * 16;
+            const uint8_t *c = a.w_scale + n * spitch + (int64_t)s0 * (kBlock / kGroup);
 #pragma unroll
-    for (int t = 0; t < MT; t++) {
-        const int64_t m = m0 + 16 * t + low;
-        there[t] = m < a.m;
-        x[t] = (const TX *)a.x + (there[t] ? m : 0) * a.ldx;
-    }
-    v4f acc[MT][NW] = {};
-    for (int s0 = begin; s0 < end; s0 += AHEAD) {
-        v4i q[AHEAD][NW];
-        uint32_t code[AHEAD][NW];
-        Rows32<TX> r[AHEAD][MT];
+            for (int u = 0; u < STEPS; u++)
+                if (s0 + u < end) w.q[u][v] = *(const v4i *)(q + u * (kBlock / 2));
+            if (STEPS == 4 && s0 + 4 <= end) {
+                const v4i four = *(const v4i_any *)c;
 #pragma unroll
-        for (int u = 0; u < AHEAD; u++) {
-            const int64_t s = min(s0 + u, end - 1);
+                for (int u = 0; u < STEPS; u++) w.code[u][v] = (uint32_t)four[u];
+            } else {
 #pragma unroll
-            for (int v = 0; v < NW; v++) {
-                q[u][v] = *(const v4i *)(w[v] + s * (kBlock / 2));
-                code[u][v] = ws[v][s * (kBlock / kGroup)];
-            }
-#pragma unroll
-            for (int t = 0; t < MT; t++) {
-                r[u][t].zero();
-                if (there[t]) r[u][t].load(x[t], s * kBlock + high * 32, a.k);
+                for (int u = 0; u < STEPS; u++)
+                    if (s0 + u < end) w.code[u][v] = *(const uint32_t *)(c + u * (kBlock / kGroup));
             }
         }
+    };
+    Rows32<TX> r[STEPS];
+    auto load_rows = [&](int turn) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; u++) {
-            if (s0 + u >= end) break;
+        for (int u = 0; u < STEPS; u++) {
+            const int s = begin + turn * STEPS + u;
+            r[u].zero();
+            if (there && s < end) r[u].load(x, (int64_t)s * kBlock + high * 32, a.k);
+        }
+    };
+    int64_t tile = blockIdx.x;
+    Weights4<STEPS, NW> next;
+    load_weights(tile, 0, next);
+    load_rows(0);
+    v4f acc[NW] = {};
+    for (int turn = 0, odd = 0; tile < tiles;) {
+        const Weights4<STEPS, NW> w = next;
+        const bool last = turn + 1 == turns;
+        const int64_t then = last ? tile + gridDim.x : tile;
+        const int then_turn = last ? 0 : turn + 1;
+        if (then < tiles) load_weights(then, then_turn, next);
+#pragma unroll
+        for (int u = 0; u < STEPS; u++) {
+            if (begin + turn * STEPS + u >= end) break;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                v8bf p[kParts<TX>];
+                r[u].parts(i, p);
+#pragma unroll
+                for (int v = 0; v < NW; v++)
+                    acc[v] = multiply(widen4(w.q[u][v][i], group_scale(w.code[u][v] >> (8 * high) & 0xff)), p, acc[v]);
+            }
+        }
+        if (turns > 1) load_rows(then_turn);
+        if (last) {
+#pragma unroll
+            for (int v = 0; v < NW; v++) part[odd][wave][v][lane] = acc[v], acc[v] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            __syncthreads();
+            if (wave < NW && there) {  // 16 outputs each
+                v4f z = part[odd][0][wave][lane];
+                for (int i = 1; i < kWaves; i++) z += part[odd][i][wave][lane];
+                put_outputs<TY>(a, low, tile * (16 * NW) + 16 * wave + high * 4, z);
+            }
+            odd ^= 1;
+        }
+        tile = then;
+        turn = then_turn;
+    }
+}
+
+// ---- more rows: 64 outputs of 16 MT rows.  The rows come through LDS, a kilobyte of each at a time, since every wave needs them
+// all (from registers, waves that share the columns fetch each line for a quarter of it: 64 rows 45 us where this takes 14);
+// the weights still go straight to registers.  The waves share that kilobyte's steps and the outputs.
+constexpr int kRowBytes = 1024, kRowPitch = kRowBytes + 16;  // so that 16 rows' 16 bytes lie on different banks
+
+template <typename TX, typename TY, int MT>
+__global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupProductArgs a) {
+    constexpr int kCols = kRowBytes / sizeof(TX), kSteps = kCols / kBlock, kAcross = kWaves / kSteps, NW = 4 / kAcross;
+    constexpr int kLoads = 16 * MT * kRowBytes / 16 / (64 * kWaves);  // of 16 bytes, of a thread
+    constexpr int kEach = 16 / sizeof(TX);
+    extern __shared__ uint8_t stage[];  // two kilobytes of each row in turn; at the end the waves' sums
+    typedef TX row16 __attribute__((ext_vector_type(kEach)));
+    typedef row16 row16_any __attribute__((aligned(sizeof(TX))));
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
+    const int step = wave % kSteps, across = wave / kSteps;
+    const int64_t n0 = (int64_t)blockIdx.x * 64 + across * (16 * NW), m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int steps = (int)blocks_of(a.k), turns = (steps + kSteps - 1) / kSteps;
+    const int64_t pitch = group_pitch(a.k), spitch = group_scale_pitch(a.k);
+    auto load_weights = [&](int turn, Weights4<1, NW> &w) {
+        const int s = min(turn * kSteps + step, steps - 1);
+#pragma unroll
+        for (int v = 0; v < NW; v++) {
+            const int64_t n = min(n0 + 16 * v + low, a.n - 1);
+            w.q[0][v] = *(const v4i *)(a.w + n * pitch + (int64_t)s * (kBlock / 2) + high * 16);
+            w.code[0][v] = a.w_scale[n * spitch + (int64_t)s * (kBlock / kGroup) + high];
+        }
+    };
+    row16 held[kLoads];
+    auto load_rows = [&](int turn) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int at = i * (64 * kWaves) + threadIdx.x, row = at / 64;
+            const int64_t m = m0 + row, col = (int64_t)turn * kCols + at % 64 * kEach;
+            held[i] = row16{};
+            if (m >= a.m) continue;
+            const TX *const x = (const TX *)a.x + m * a.ldx + col;
+            if (col + kEach <= a.k)
+                held[i] = *(const row16_any *)x;
+            else
+                for (int j = 0; j < kEach; j++)
+                    if (col + j < a.k) held[i][j] = x[j];
+        }
+    };
+    auto put_rows = [&](int turn) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int at = i * (64 * kWaves) + threadIdx.x;
+            *(row16 *)(stage + ((turn & 1) * 16 * MT + at / 64) * kRowPitch + at % 64 * 16) = held[i];
+        }
+    };
+    Weights4<1, NW> next;
+    load_rows(0);
+    load_weights(0, next);
+    put_rows(0);
+    v4f acc[MT][NW] = {};
+    for (int turn = 0; turn < turns; turn++) {
+        const Weights4<1, NW> w = next;
+        if (turn + 1 < turns) load_rows(turn + 1), load_weights(turn + 1, next);
+        __syncthreads();  // this turn's rows are there, and the last one's have been read
+        if (turn * kSteps + step < steps) {
+            const uint8_t *const rows = stage + ((turn & 1) * 16 * MT + low) * kRowPitch + (step * kBlock + high * 32) * sizeof(TX);
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 v8bf wide[NW];
 #pragma unroll
-                for (int v = 0; v < NW; v++) wide[v] = widen4(q[u][v][i], group_scale(code[u][v]));
+                for (int v = 0; v < NW; v++) wide[v] = widen4(w.q[0][v][i], group_scale(w.code[0][v]));
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
+                    Rows32<TX> r;
+                    r.read(i, rows + t * 16 * kRowPitch);
                     v8bf p[kParts<TX>];
-                    r[u][t].parts(i, p);
+                    r.parts(i, p);
 #pragma unroll
-                    for (int v = 0; v < NW; v++)
-#pragma unroll
-                        for (int c = kParts<TX> - 1; c >= 0; c--)
-                            acc[t][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[v], p[c], acc[t][v], 0, 0, 0);
+                    for (int v = 0; v < NW; v++) acc[t][v] = multiply(wide[v], p, acc[t][v]);
                 }
             }
         }
+        if (turn + 1 < turns) put_rows(turn + 1);
     }
-    // the waves' sums, pair by pair
+    // the steps' sums: 16 x 16 outputs to a wave at a time
+    v4f(*const part)[MT][NW][64] = (v4f(*)[MT][NW][64])stage;
+    __syncthreads();
 #pragma unroll
-    for (int half = kWaves / 2; half >= 1; half /= 2) {
-        if (wave >= half && wave < 2 * half)
+    for (int t = 0; t < MT; t++)
 #pragma unroll
-            for (int t = 0; t < MT; t++)
-#pragma unroll
-                for (int v = 0; v < NW; v++) part[wave - half][t * NW + v][lane] = acc[t][v];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int t = 0; t < MT; t++)
-#pragma unroll
-                for (int v = 0; v < NW; v++) acc[t][v] += part[wave][t * NW + v][lane];
-        __syncthreads();
-    }
-    if (wave != 0) return;
-#pragma unroll
-    for (int t = 0; t < MT; t++) {
+        for (int v = 0; v < NW; v++) part[wave][t][v][lane] = acc[t][v];
+    __syncthreads();
+    for (int u = wave; u < MT * 4; u += kWaves) {
+        const int t = u / 4, of = u % 4 / NW, v = u % NW;  // the wave group that has it
         const int64_t m = m0 + 16 * t + low;
         if (m >= a.m) continue;
-        TY *y = (TY *)a.y + m * a.ldy;
-#pragma unroll
-        for (int v = 0; v < NW; v++)
-            for (int i = 0; i < 4; i++) {
-                const int64_t n = n0 + 16 * v + high * 4 + i;
-                if (n >= a.n) break;
-                float z = acc[t][v][i];
-                if (a.bias) z += a.bias[n];
-                if (a.activate) z = relu_clamp(z, a.ymax);
-                y[n] = (TY)z;
-            }
+        v4f z = part[of * kSteps][t][v][lane];
+        for (int i = 1; i < kSteps; i++) z += part[of * kSteps + i][t][v][lane];
+        put_outputs<TY>(a, m, (int64_t)blockIdx.x * 64 + of * (16 * NW) + 16 * v + high * 4, z);
     }
 }
 
-template <typename TX, typename TY, int MT, int NW, int AHEAD>
+template <typename TX, typename TY, int NW, int STEPS>
+hipError_t product_few_go(const GroupProductArgs &a, int64_t most, hipStream_t s) {
+    const int64_t tiles = (a.n + 16 * NW - 1) / (16 * NW);
+    product_groups_kernel<TX, TY, NW, STEPS><<<(unsigned)(tiles < most ? tiles : most), 64 * kWaves, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename TX, typename TY, int MT>
 hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
+    constexpr int kBytes = 2 * 16 * MT * kRowPitch;
+    static_assert(kWaves * MT * 2 * 64 * sizeof(v4f) <= kBytes, "the waves' sums, of two tiles each at the most");
+    static std::atomic<unsigned long long> raised;
+    hipError_t e = raise_lds_limit((const void *)product_groups_tile_kernel<TX, TY, MT>, kBytes, raised);
+    if (e != hipSuccess) return e;
     // a launch holds fewer than 2^32 threads along the outputs and 2^16 workgroups along the rows
-    constexpr int64_t kMostN = (int64_t)16 * NW << 22, kMostM = (int64_t)16 * MT << 15;
+    constexpr int64_t kMostN = (int64_t)64 << 22, kMostM = (int64_t)16 * MT << 15;
     for (int64_t n0 = 0; n0 < a.n; n0 += kMostN)
         for (int64_t m0 = 0; m0 < a.m; m0 += kMostM) {
             GroupProductArgs p = a;
@@ -283,9 +407,9 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
             p.w_scale = a.w_scale + n0 * group_scale_pitch(a.k);
             p.bias = a.bias ? a.bias + n0 : nullptr;
             p.y = (TY *)a.y + m0 * a.ldy + n0;
-            const dim3 grid((unsigned)((p.n + 16 * NW - 1) / (16 * NW)), (unsigned)((p.m + 16 * MT - 1) / (16 * MT)));
-            product_groups_kernel<TX, TY, MT, NW, AHEAD><<<grid, 64 * kWaves, 0, s>>>(p);
-            const hipError_t e = hipGetLastError();
+            const dim3 grid((unsigned)((p.n + 63) / 64), (unsigned)((p.m + 16 * MT - 1) / (16 * MT)));
+            product_groups_tile_kernel<TX, TY, MT><<<grid, 64 * kWaves, kBytes, s>>>(p);
+            e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
     return hipSuccess;
@@ -294,11 +418,10 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
 template <typename TX, typename TY>
 hipError_t product_go(const GroupProductArgs &a, hipStream_t s) {
     if (a.m <= 16) {
-        if (a.n <= 8192) return product_tile_go<TX, TY, 1, 1, 4>(a, s);
-        return product_tile_go<TX, TY, 1, 4, sizeof(TX) == 4 ? 2 : 4>(a, s);
+        if (a.n <= 8192) return product_few_go<TX, TY, 1, 4>(a, 512, s);
+        return product_few_go<TX, TY, 2, sizeof(TX) == 4 ? 2 : 4>(a, 256, s);
     }
-    if (a.m <= 32) return product_tile_go<TX, TY, 2, 2, sizeof(TX) == 4 ? 1 : 2>(a, s);
-    return product_tile_go<TX, TY, 4, 2, 1>(a, s);
+    return a.m <= 32 ? product_tile_go<TX, TY, 2>(a, s) : product_tile_go<TX, TY, 4>(a, s);
 }
 
 }  // namespace
