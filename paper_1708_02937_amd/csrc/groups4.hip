@@ -111,79 +111,106 @@ hipError_t each_slab(const GroupsArgs &a, F f) {
 //
 // A step is 128 columns: lane l holds the 32 columns from 32 (l / 16) on of weight row and activation row l % 16, one
 // group, in four instructions of eight columns a lane.  Any order of columns will do as long as both operands have it.
-constexpr int kWaves = 8;  // waves of a workgroup, which share the columns
+// The rows are split as they come into LDS, once for all waves and outputs, their parts one after the other.
+constexpr int kWaves = 8;  // waves of a workgroup
+constexpr int64_t kMostLds = 160 * 1024 - 512;
 
 template <typename TX>
 constexpr int kParts = sizeof(TX) == 4 ? 3 : 1;
 
-// The lane's 32 activations of a step: columns c .. c + 31 of a row of k, zeros past its end.
 template <typename TX>
-struct Rows32;
-template <>
-struct Rows32<__bf16> {
-    v8bf v[4];
-    __device__ __forceinline__ void load(const __bf16 *row, int64_t c, int64_t k) {
-        if (c + 32 <= k) {
-#pragma unroll
-            for (int i = 0; i < 4; i++) v[i] = *(const v8bf_any *)(row + c + 8 * i);
+struct Eight {  // values of a row, on their way to LDS
+    v8bf v;
+    __device__ __forceinline__ void load(const TX *p, int64_t c, int64_t k) {
+        if (c + 8 <= k) {
+            v = *(const v8bf_any *)(p + c);
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-                for (int j = 0; j < 8; j++) v[i][j] = c + 8 * i + j < k ? row[c + 8 * i + j] : (__bf16)0.0f;
+            for (int j = 0; j < 8; j++) v[j] = c + j < k ? p[c + j] : (TX)0.0f;
         }
     }
-    __device__ __forceinline__ void zero() {
-        for (int i = 0; i < 4; i++) v[i] = v8bf{};
-    }
-    // columns 8 i .. + 7 of 32 in LDS
-    __device__ __forceinline__ void read(int i, const uint8_t *p) { v[i] = *(const v8bf *)(p + 16 * i); }
-    __device__ __forceinline__ void parts(int i, v8bf (&p)[1]) const { p[0] = v[i]; }
+    __device__ __forceinline__ void zero() { v = v8bf{}; }
+    __device__ __forceinline__ void put(uint8_t *to, int64_t) const { *(v8bf *)to = v; }
 };
 template <>
-struct Rows32<float> {
-    v4f v[8];
-    __device__ __forceinline__ void load(const float *row, int64_t c, int64_t k) {
-        if (c + 32 <= k) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = *(const v4f_any *)(row + c + 4 * i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                for (int j = 0; j < 4; j++) v[i][j] = c + 4 * i + j < k ? row[c + 4 * i + j] : 0.0f;
-        }
-    }
+struct Eight<float> {
+    float v[8];
+    __device__ __forceinline__ void load(const float *p, int64_t c, int64_t k) { load8<float, false>(p, c, k, v); }
     __device__ __forceinline__ void zero() {
-        for (int i = 0; i < 8; i++) v[i] = v4f{};
+        for (int j = 0; j < 8; j++) v[j] = 0.0f;
     }
-    __device__ __forceinline__ void read(int i, const uint8_t *p) {
-        v[2 * i] = *(const v4f *)(p + 32 * i), v[2 * i + 1] = *(const v4f *)(p + 32 * i + 16);
-    }
-    // The upper half of a float's bits is the float cut off to bfloat16; a NaN whose bits are all below keeps one.
-    __device__ __forceinline__ void parts(int i, v8bf (&p)[3]) const {
+    // The upper half of a float's bits is the float cut off to bfloat16.  (Quieted first, a NaN's first bit is in there.)
+    __device__ __forceinline__ void put(uint8_t *to, int64_t part) const {
+        uint32_t w[3][4];
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float x = v[2 * i + j / 4][j % 4];
-            const uint32_t b = __float_as_uint(x);
-            const bool finite = (b & 0x7fffffffu) < 0x7f800000u;
-            const uint32_t nan = (b & 0x7fffffffu) > 0x7f800000u ? 0x400000u : 0u;
-            const float rest = finite ? x - __uint_as_float(b & 0xffff0000u) : 0.0f;
-            const uint32_t r = __float_as_uint(rest);
-            const uint32_t last = __float_as_uint(rest - __uint_as_float(r & 0xffff0000u));
-            p[0][j] = __builtin_bit_cast(__bf16, (uint16_t)((b | nan) >> 16));
-            p[1][j] = __builtin_bit_cast(__bf16, (uint16_t)(r >> 16));
-            p[2][j] = __builtin_bit_cast(__bf16, (uint16_t)(last >> 16));
+        for (int j = 0; j < 8; j += 2) {
+            uint32_t bits[2][3];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const float x = __builtin_canonicalizef(v[j + h]);
+                const uint32_t b = __float_as_uint(x);
+                const float rest = fabsf(x) < INFINITY ? x - __uint_as_float(b & 0xffff0000u) : 0.0f;
+                const uint32_t r = __float_as_uint(rest);
+                bits[h][0] = b, bits[h][1] = r, bits[h][2] = __float_as_uint(rest - __uint_as_float(r & 0xffff0000u));
+            }
+#pragma unroll
+            for (int c = 0; c < 3; c++) w[c][j / 2] = __builtin_amdgcn_perm(bits[1][c], bits[0][c], 0x07060302);
         }
+#pragma unroll
+        for (int c = 0; c < 3; c++) *(v4i *)(to + c * part) = v4i{(int)w[c][0], (int)w[c][1], (int)w[c][2], (int)w[c][3]};
     }
 };
 
-// ---- up to 16 rows: 16 NW outputs at a time, by workgroups that stay.  Each wave takes a run of the steps, STEPS at a turn, and
-// the weights of its next turn, of the next tile where this one is the tile's last, are on their way while this turn's are
-// multiplied.  Rows that fit one turn are kept in registers.
 template <int STEPS, int NW>
 struct Weights4 {
     v4i q[STEPS][NW];
     uint32_t code[STEPS][NW];  // of the step's four groups
 };
+
+// The steps s0 .. of 16 NW outputs from n0 on, those before `end`.
+template <int STEPS, int NW>
+__device__ __forceinline__ void load_weights(const GroupProductArgs &a, int64_t n0, int s0, int end, Weights4<STEPS, NW> &w) {
+    const int low = threadIdx.x % 16, high = threadIdx.x % 64 / 16;
+#pragma unroll
+    for (int v = 0; v < NW; v++) {
+        const int64_t n = min(n0 + 16 * v + low, a.n - 1);
+        const uint8_t *q = a.w + n * group_pitch(a.k) + (int64_t)s0 * (kBlock / 2) + high * 16;
+        const uint8_t *c = a.w_scale + n * group_scale_pitch(a.k) + (int64_t)s0 * (kBlock / kGroup);
+#pragma unroll
+        for (int u = 0; u < STEPS; u++)
+            if (s0 + u < end) w.q[u][v] = *(const v4i *)(q + u * (kBlock / 2));
+        if (STEPS == 4 && s0 + 4 <= end) {
+            const v4i four = *(const v4i_any *)c;
+#pragma unroll
+            for (int u = 0; u < STEPS; u++) w.code[u][v] = (uint32_t)four[u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < STEPS; u++)
+                if (s0 + u < end) w.code[u][v] = *(const uint32_t *)(c + u * (kBlock / kGroup));
+        }
+    }
+}
+
+// acc += a step's products, of 16 MT rows; rows: the lane's 32 columns of its first row in LDS.
+template <int PARTS, int MT, int NW>
+__device__ __forceinline__ void multiply(const v4i (&q)[NW], const uint32_t (&code)[NW], const uint8_t *rows, int64_t part,
+                                         int64_t rows16, v4f (&acc)[MT][NW]) {
+    const int high = threadIdx.x % 64 / 16;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        v8bf wide[NW];
+#pragma unroll
+        for (int v = 0; v < NW; v++) wide[v] = widen4(q[v][i], group_scale(code[v] >> (8 * high) & 0xff));
+#pragma unroll
+        for (int t = 0; t < MT; t++)
+#pragma unroll
+            for (int c = PARTS - 1; c >= 0; c--) {
+                const v8bf x = *(const v8bf *)(rows + t * rows16 + c * part + 16 * i);
+#pragma unroll
+                for (int v = 0; v < NW; v++)
+                    acc[t][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[v], x, acc[t][v], 0, 0, 0);
+            }
+    }
+}
 
 template <typename TY>
 __device__ __forceinline__ void put_outputs(const GroupProductArgs &a, int64_t m, int64_t n0, v4f z) {
@@ -196,172 +223,117 @@ __device__ __forceinline__ void put_outputs(const GroupProductArgs &a, int64_t m
     }
 }
 
-// acc += the products of a step's columns 8 i .. + 7 of each lane's 32.
-template <int PARTS>
-__device__ __forceinline__ v4f multiply(const v8bf &wide, const v8bf (&p)[PARTS], v4f acc) {
-#pragma unroll
-    for (int c = PARTS - 1; c >= 0; c--) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, p[c], acc, 0, 0, 0);
-    return acc;
-}
+// ---- up to 16 rows that fit LDS as a whole: 16 NW outputs at a time, by workgroups that stay.  Each wave takes a run of the
+// steps, STEPS at a turn, and the weights of its next turn, of the next tile where this one is the tile's last, are on their
+// way while this turn's are multiplied.
+constexpr int64_t row_pitch(int64_t k) { return blocks_of(k) * kBlock * 2 + 16; }  // 16 rows' 16 bytes lie on different banks
 
-template <typename TX, typename TY, int NW, int STEPS>
+template <typename TX, typename TY, int NW, int STEPS, int TURNS>
 __global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProductArgs a) {
-    __shared__ v4f part[2][kWaves][NW][64];  // of two tiles, so that each needs one barrier
+    extern __shared__ uint8_t rows[];
+    __shared__ v4f sums[TURNS][kWaves][NW][64];  // of two tiles in turn, so that each needs one barrier, or of one
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
-    const int64_t tiles = (a.n + 16 * NW - 1) / (16 * NW);
+    const int64_t tiles = (a.n + 16 * NW - 1) / (16 * NW), pitch = row_pitch(a.k), part = a.m * pitch;
     const int steps = (int)blocks_of(a.k), each = (steps + kWaves - 1) / kWaves, turns = (each + STEPS - 1) / STEPS;
     const int begin = min(wave * each, steps), end = min(begin + each, steps);
-    const int64_t pitch = group_pitch(a.k), spitch = group_scale_pitch(a.k);
-    const bool there = low < a.m;
-    const TX *const x = (const TX *)a.x + (there ? low : 0) * a.ldx;
-    auto load_weights = [&](int64_t tile, int turn, Weights4<STEPS, NW> &w) {
-        const int s0 = begin + turn * STEPS;
-#pragma unroll
-        for (int v = 0; v < NW; v++) {
-            const int64_t n = min(tile * (16 * NW) + 16 * v + low, a.n - 1);
-            const uint8_t *q = a.w + n * pitch + (int64_t)s0 * (kBlock / 2) + high * 16;
-            const uint8_t *c = a.w_scale + n * spitch + (int64_t)s0 * (kBlock / kGroup);
-#pragma unroll
-            for (int u = 0; u < STEPS; u++)
-                if (s0 + u < end) w.q[u][v] = *(const v4i *)(q + u * (kBlock / 2));
-            if (STEPS == 4 && s0 + 4 <= end) {
-                const v4i four = *(const v4i_any *)c;
-#pragma unroll
-                for (int u = 0; u < STEPS; u++) w.code[u][v] = (uint32_t)four[u];
-            } else {
-#pragma unroll
-                for (int u = 0; u < STEPS; u++)
-                    if (s0 + u < end) w.code[u][v] = *(const uint32_t *)(c + u * (kBlock / kGroup));
-            }
-        }
-    };
-    Rows32<TX> r[STEPS];
-    auto load_rows = [&](int turn) {
-#pragma unroll
-        for (int u = 0; u < STEPS; u++) {
-            const int s = begin + turn * STEPS + u;
-            r[u].zero();
-            if (there && s < end) r[u].load(x, (int64_t)s * kBlock + high * 32, a.k);
-        }
-    };
     int64_t tile = blockIdx.x;
     Weights4<STEPS, NW> next;
-    load_weights(tile, 0, next);
-    load_rows(0);
-    v4f acc[NW] = {};
+    load_weights(a, tile * (16 * NW), begin, end, next);
+    const int eights = steps * (kBlock / 8), all = (int)a.m * eights;
+    constexpr int kBatch = 4;
+    for (int i0 = threadIdx.x; i0 < all; i0 += 64 * kWaves * kBatch) {
+        Eight<TX> x[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            const int i = min(i0 + u * 64 * kWaves, all - 1);
+            x[u].load((const TX *)a.x + i / eights * a.ldx, (int64_t)(i % eights) * 8, a.k);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; u++) {
+            const int i = min(i0 + u * 64 * kWaves, all - 1);
+            x[u].put(rows + i / eights * pitch + i % eights * 16, part);
+        }
+    }
+    __syncthreads();
+    const uint8_t *const own = rows + (low < a.m ? low : 0) * pitch + high * 64;
+    v4f acc[1][NW] = {};
     for (int turn = 0, odd = 0; tile < tiles;) {
         const Weights4<STEPS, NW> w = next;
         const bool last = turn + 1 == turns;
         const int64_t then = last ? tile + gridDim.x : tile;
         const int then_turn = last ? 0 : turn + 1;
-        if (then < tiles) load_weights(then, then_turn, next);
+        if (then < tiles) load_weights(a, then * (16 * NW), begin + then_turn * STEPS, end, next);
 #pragma unroll
         for (int u = 0; u < STEPS; u++) {
-            if (begin + turn * STEPS + u >= end) break;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                v8bf p[kParts<TX>];
-                r[u].parts(i, p);
-#pragma unroll
-                for (int v = 0; v < NW; v++)
-                    acc[v] = multiply(widen4(w.q[u][v][i], group_scale(w.code[u][v] >> (8 * high) & 0xff)), p, acc[v]);
-            }
+            const int s = begin + turn * STEPS + u;
+            if (s >= end) break;
+            multiply<kParts<TX>>(w.q[u], w.code[u], own + (int64_t)s * (kBlock * 2), part, 0, acc);
         }
-        if (turns > 1) load_rows(then_turn);
         if (last) {
 #pragma unroll
-            for (int v = 0; v < NW; v++) part[odd][wave][v][lane] = acc[v], acc[v] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int v = 0; v < NW; v++) sums[odd][wave][v][lane] = acc[0][v], acc[0][v] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
             __syncthreads();
-            if (wave < NW && there) {  // 16 outputs each
-                v4f z = part[odd][0][wave][lane];
-                for (int i = 1; i < kWaves; i++) z += part[odd][i][wave][lane];
+            if (wave < NW && low < a.m) {  // 16 outputs each
+                v4f z = sums[odd][0][wave][lane];
+                for (int i = 1; i < kWaves; i++) z += sums[odd][i][wave][lane];
                 put_outputs<TY>(a, low, tile * (16 * NW) + 16 * wave + high * 4, z);
             }
-            odd ^= 1;
+            if (TURNS == 1)
+                __syncthreads();
+            else
+                odd ^= 1;
         }
         tile = then;
         turn = then_turn;
     }
 }
 
-// ---- more rows: 64 outputs of 16 MT rows.  The rows come through LDS, a kilobyte of each at a time, since every wave needs them
-// all (from registers, waves that share the columns fetch each line for a quarter of it: 64 rows 45 us where this takes 14);
-// the weights still go straight to registers.  The waves share that kilobyte's steps and the outputs.
-constexpr int kRowBytes = 1024, kRowPitch = kRowBytes + 16;  // so that 16 rows' 16 bytes lie on different banks
-
+// ---- any rows: 64 outputs of 16 MT rows.  The rows come through LDS a stage at a time, since every wave needs them all (straight
+// from registers, with waves that share the columns, each line is fetched for a quarter of it: 64 rows 45 us where this took
+// 20); the weights still go straight to registers.  The waves share a stage's steps and the outputs.  Rows and weights of the
+// next stage are on their way while one is multiplied.
 template <typename TX, typename TY, int MT>
 __global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupProductArgs a) {
-    constexpr int kCols = kRowBytes / sizeof(TX), kSteps = kCols / kBlock, kAcross = kWaves / kSteps, NW = 4 / kAcross;
-    constexpr int kLoads = 16 * MT * kRowBytes / 16 / (64 * kWaves);  // of 16 bytes, of a thread
-    constexpr int kEach = 16 / sizeof(TX);
-    extern __shared__ uint8_t stage[];  // two kilobytes of each row in turn; at the end the waves' sums
-    typedef TX row16 __attribute__((ext_vector_type(kEach)));
-    typedef row16 row16_any __attribute__((aligned(sizeof(TX))));
+    constexpr int kSteps = sizeof(TX) == 4 ? 2 : 4, kCols = kSteps * kBlock, kAcross = kWaves / kSteps, NW = 4 / kAcross;
+    constexpr int kPitch = kCols * 2 + 16, kPart = 16 * MT * kPitch, kStage = kParts<TX> * kPart;
+    constexpr int kStages = 2 * kStage <= kMostLds ? 2 : 1;
+    constexpr int kRowEights = kCols / 8, kLoads = 16 * MT * kRowEights / (64 * kWaves);
+    extern __shared__ uint8_t stage[];  // at the end the waves' sums
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
     const int step = wave % kSteps, across = wave / kSteps;
     const int64_t n0 = (int64_t)blockIdx.x * 64 + across * (16 * NW), m0 = (int64_t)blockIdx.y * (16 * MT);
     const int steps = (int)blocks_of(a.k), turns = (steps + kSteps - 1) / kSteps;
-    const int64_t pitch = group_pitch(a.k), spitch = group_scale_pitch(a.k);
-    auto load_weights = [&](int turn, Weights4<1, NW> &w) {
-        const int s = min(turn * kSteps + step, steps - 1);
-#pragma unroll
-        for (int v = 0; v < NW; v++) {
-            const int64_t n = min(n0 + 16 * v + low, a.n - 1);
-            w.q[0][v] = *(const v4i *)(a.w + n * pitch + (int64_t)s * (kBlock / 2) + high * 16);
-            w.code[0][v] = a.w_scale[n * spitch + (int64_t)s * (kBlock / kGroup) + high];
-        }
-    };
-    row16 held[kLoads];
-    auto load_rows = [&](int turn) {
-#pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const int at = i * (64 * kWaves) + threadIdx.x, row = at / 64;
-            const int64_t m = m0 + row, col = (int64_t)turn * kCols + at % 64 * kEach;
-            held[i] = row16{};
-            if (m >= a.m) continue;
-            const TX *const x = (const TX *)a.x + m * a.ldx + col;
-            if (col + kEach <= a.k)
-                held[i] = *(const row16_any *)x;
-            else
-                for (int j = 0; j < kEach; j++)
-                    if (col + j < a.k) held[i][j] = x[j];
-        }
-    };
-    auto put_rows = [&](int turn) {
+    auto load_rows = [&](int turn, Eight<TX> (&x)[kLoads]) {
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int at = i * (64 * kWaves) + threadIdx.x;
-            *(row16 *)(stage + ((turn & 1) * 16 * MT + at / 64) * kRowPitch + at % 64 * 16) = held[i];
+            const int64_t m = m0 + at / kRowEights;
+            x[i].zero();
+            if (m < a.m) x[i].load((const TX *)a.x + m * a.ldx, (int64_t)turn * kCols + at % kRowEights * 8, a.k);
         }
     };
-    Weights4<1, NW> next;
-    load_rows(0);
-    load_weights(0, next);
-    put_rows(0);
+    auto put_rows = [&](int turn, const Eight<TX> (&x)[kLoads]) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int at = i * (64 * kWaves) + threadIdx.x;
+            x[i].put(stage + turn % kStages * kStage + at / kRowEights * kPitch + at % kRowEights * 16, kPart);
+        }
+    };
     v4f acc[MT][NW] = {};
+    Eight<TX> x[kLoads];
+    Weights4<1, NW> next;
+    load_rows(0, x);
+    load_weights(a, n0, step, steps, next);
+    put_rows(0, x);
     for (int turn = 0; turn < turns; turn++) {
         const Weights4<1, NW> w = next;
-        if (turn + 1 < turns) load_rows(turn + 1), load_weights(turn + 1, next);
+        if (turn + 1 < turns) load_rows(turn + 1, x), load_weights(a, n0, (turn + 1) * kSteps + step, steps, next);
         __syncthreads();  // this turn's rows are there, and the last one's have been read
-        if (turn * kSteps + step < steps) {
-            const uint8_t *const rows = stage + ((turn & 1) * 16 * MT + low) * kRowPitch + (step * kBlock + high * 32) * sizeof(TX);
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                v8bf wide[NW];
-#pragma unroll
-                for (int v = 0; v < NW; v++) wide[v] = widen4(w.q[0][v][i], group_scale(w.code[0][v]));
-#pragma unroll
-                for (int t = 0; t < MT; t++) {
-                    Rows32<TX> r;
-                    r.read(i, rows + t * 16 * kRowPitch);
-                    v8bf p[kParts<TX>];
-                    r.parts(i, p);
-#pragma unroll
-                    for (int v = 0; v < NW; v++) acc[t][v] = multiply(wide[v], p, acc[t][v]);
-                }
-            }
-        }
-        if (turn + 1 < turns) put_rows(turn + 1);
+        if (turn * kSteps + step < steps)
+            multiply<kParts<TX>>(w.q[0], w.code[0], stage + turn % kStages * kStage + low * kPitch + step * (kBlock * 2) + high * 64,
+                                 kPart, 16 * kPitch, acc);
+        if (kStages == 1) __syncthreads();
+        if (turn + 1 < turns) put_rows(turn + 1, x);
     }
     // the steps' sums: 16 x 16 outputs to a wave at a time
     v4f(*const part)[MT][NW][64] = (v4f(*)[MT][NW][64])stage;
@@ -372,7 +344,7 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupP
         for (int v = 0; v < NW; v++) part[wave][t][v][lane] = acc[t][v];
     __syncthreads();
     for (int u = wave; u < MT * 4; u += kWaves) {
-        const int t = u / 4, of = u % 4 / NW, v = u % NW;  // the wave group that has it
+        const int t = u / 4, of = u % 4 / NW, v = u % NW;  // the waves that share these outputs
         const int64_t m = m0 + 16 * t + low;
         if (m >= a.m) continue;
         v4f z = part[of * kSteps][t][v][lane];
@@ -381,17 +353,28 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupP
     }
 }
 
-template <typename TX, typename TY, int NW, int STEPS>
+template <typename TX>
+constexpr int64_t rows_space(int64_t m, int64_t k) { return kParts<TX> * m * row_pitch(k); }
+constexpr int64_t sums_space(int nw, int turns) { return (int64_t)turns * kWaves * nw * 64 * sizeof(v4f); }
+
+template <typename TX, typename TY, int NW, int TURNS>
 hipError_t product_few_go(const GroupProductArgs &a, int64_t most, hipStream_t s) {
+    static std::atomic<unsigned long long> raised;
+    const void *const kernel = (const void *)product_groups_kernel<TX, TY, NW, 4, TURNS>;
+    const hipError_t e = raise_lds_limit(kernel, kMostLds - sums_space(NW, TURNS), raised);
+    if (e != hipSuccess) return e;
     const int64_t tiles = (a.n + 16 * NW - 1) / (16 * NW);
-    product_groups_kernel<TX, TY, NW, STEPS><<<(unsigned)(tiles < most ? tiles : most), 64 * kWaves, 0, s>>>(a);
+    product_groups_kernel<TX, TY, NW, 4, TURNS>
+        <<<(unsigned)(tiles < most ? tiles : most), 64 * kWaves, (size_t)rows_space<TX>(a.m, a.k), s>>>(a);
     return hipGetLastError();
 }
 
 template <typename TX, typename TY, int MT>
 hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
-    constexpr int kBytes = 2 * 16 * MT * kRowPitch;
-    static_assert(kWaves * MT * 2 * 64 * sizeof(v4f) <= kBytes, "the waves' sums, of two tiles each at the most");
+    constexpr int kStage = kParts<TX> * 16 * MT * ((sizeof(TX) == 4 ? 2 : 4) * kBlock * 2 + 16);
+    constexpr int kSums = kWaves * MT * (sizeof(TX) == 4 ? 1 : 2) * 64 * (int)sizeof(v4f);
+    constexpr int kRows = 2 * kStage <= kMostLds ? 2 * kStage : kStage, kBytes = kRows > kSums ? kRows : kSums;
+    static_assert(kBytes <= kMostLds, "");
     static std::atomic<unsigned long long> raised;
     hipError_t e = raise_lds_limit((const void *)product_groups_tile_kernel<TX, TY, MT>, kBytes, raised);
     if (e != hipSuccess) return e;
@@ -417,10 +400,13 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
 
 template <typename TX, typename TY>
 hipError_t product_go(const GroupProductArgs &a, hipStream_t s) {
-    if (a.m <= 16) {
-        if (a.n <= 8192) return product_few_go<TX, TY, 1, 4>(a, 512, s);
-        return product_few_go<TX, TY, 2, sizeof(TX) == 4 ? 2 : 4>(a, 256, s);
+    const int64_t rows = rows_space<TX>(a.m, a.k);
+    if (a.m <= 16 && rows <= kMostLds - sums_space(2, 1)) {
+        if (a.n <= 8192) return product_few_go<TX, TY, 1, 2>(a, 512, s);
+        if (rows <= kMostLds - sums_space(2, 2)) return product_few_go<TX, TY, 2, 2>(a, 256, s);
+        return product_few_go<TX, TY, 2, 1>(a, 256, s);
     }
+    if (a.m <= 16) return product_tile_go<TX, TY, 1>(a, s);
     return a.m <= 32 ? product_tile_go<TX, TY, 2>(a, s) : product_tile_go<TX, TY, 4>(a, s);
 }
 
