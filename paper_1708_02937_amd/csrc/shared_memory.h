@@ -1,7 +1,7 @@
 // Values that one workgroup writes and another reads in the same launch.
 //
-// Each chiplet has an L2 of its own, and a fence at device scope writes back and drops all of it: with 1024 workgroups of
-// eight waves that took 250 us of a launch of 290.  Here only the values themselves go past it: stores and loads at
+// Each chiplet has an L2 of its own, and a fence at device scope writes back and drops all of it: 128 rows of 131072 logits, 1024
+// workgroups of eight waves, took 371 us to sample with fences and 163 without.  Here only the values themselves go past it: stores and loads at
 // device scope, and before the flag that tells of them is raised, the wave waits until its stores have arrived.
 #pragma once
 
