@@ -230,7 +230,7 @@ constexpr int64_t row_pitch(int64_t k) { return blocks_of(k) * kBlock * 2 + 16; 
 
 template <typename TX, typename TY, int NW, int STEPS, int TURNS>
 __global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProductArgs a) {
-    extern __shared__ uint8_t rows[];
+    extern __shared__ __align__(16) uint8_t rows[];
     __shared__ v4f sums[TURNS][kWaves][NW][64];  // of two tiles in turn, so that each needs one barrier, or of one
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
     const int64_t tiles = (a.n + 16 * NW - 1) / (16 * NW), pitch = row_pitch(a.k), part = a.m * pitch;
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupP
     constexpr int kPitch = kCols * 2 + 16, kPart = 16 * MT * kPitch, kStage = kParts<TX> * kPart;
     constexpr int kStages = 2 * kStage <= kMostLds ? 2 : 1;
     constexpr int kRowEights = kCols / 8, kLoads = 16 * MT * kRowEights / (64 * kWaves);
-    extern __shared__ uint8_t stage[];  // at the end the waves' sums
+    extern __shared__ __align__(16) uint8_t stage[];  // at the end the waves' sums
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
     const int step = wave % kSteps, across = wave / kSteps;
     const int64_t n0 = (int64_t)blockIdx.x * 64 + across * (16 * NW), m0 = (int64_t)blockIdx.y * (16 * MT);

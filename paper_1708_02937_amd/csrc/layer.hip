@@ -379,7 +379,7 @@ template <int ROWS>
 struct OutTile {
     v4f part[kLayerWaves][64];
     struct {
-        uint8_t codes[ROWS][kPass * kBlock];
+        __bf16 codes[ROWS][kPass * kBlock];  // the values of the 8-bit codes, without their scales
         int scale[ROWS][kPass];
     } rows[kLayerWaves];
 };
@@ -399,11 +399,11 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
     auto load = [&](int u, Weights &w) {
         const int e = c.busy[u / passes], b0 = u % passes * kPass;
         const uint8_t *p = a.w_out + ((int64_t)e * a.width + n) * pitch + high * 32;
-        const uint8_t *s = a.w_out_scale + ((int64_t)e * blocks_of(a.width) + n0 / kBlock) * spitch;
+        const uint8_t *scales = a.w_out_scale + ((int64_t)e * blocks_of(a.width) + n0 / kBlock) * spitch;
 #pragma unroll
         for (int i = 0; i < kPass; i++) {
             const int b = min(b0 + i, kb - 1);
-            w.q[i] = load32(p + (int64_t)b * kBlock), w.code[i] = s[b];
+            w.q[i] = load32(p + (int64_t)b * kBlock), w.code[i] = scales[b];
         }
     };
     // the next rows of p, as many as ROWS, of the tokens in `left`, which loses them
@@ -422,6 +422,14 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
             x.v[r][0] = *(const v4f *)row, x.v[r][1] = *(const v4f *)(row + 4);
         }
     };
+    // the first wave's rows of s, for the end
+    float s[4] = {};
+    if (wave == 0 && low < a.tokens)
+        for (int i = 0; i < 4; i++) {
+            const int64_t col = min(n0 + high * 4 + i, a.width - 1);
+            s[i] = load_f32((const T *)a.x + low * a.ldx + col);
+            if (a.residual) s[i] += load_f32((const T *)a.residual + low * a.ldr + col);
+        }
     Weights next;
     Rows next_p;
     uint32_t next_left = 0;
@@ -460,8 +468,8 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
                 }
                 const int code = scale_code(row16_max(amax));
                 const float inv = inverse_scale(code);
-                *(int2 *)(own.codes[r] + lane * 8) =
-                    make_int2(pack_e4m3(v[0], v[1], v[2], v[3], inv), pack_e4m3(v[4], v[5], v[6], v[7], inv));
+                *(v8bf *)(own.codes[r] + lane * 8) =
+                    widen8(pack_e4m3(v[0], v[1], v[2], v[3], inv), pack_e4m3(v[4], v[5], v[6], v[7], inv), kOne);
                 if (low == 0) own.scale[r][high] = code;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own LDS, read by its other lanes
@@ -470,7 +478,12 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
 #pragma unroll
             for (int i = 0; i < kPass; i++) {
                 if (b0 + i >= kb) break;
-                const v4f z = codes16(w.q[i], load32(own.codes[at] + i * kBlock + high * 32));
+                const __bf16 *const row = own.codes[at] + i * kBlock + high * 32;
+                v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w.q[i][2 * j], w.q[i][2 * j + 1], kOne),
+                                                                *(const v8bf *)(row + 8 * j), z, 0, 0, 0);
                 const int shift = w.code[i] + own.scale[at][i] - 2 * kOne;
                 if (here)
 #pragma unroll
@@ -487,9 +500,7 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
     for (int i = 0; i < 4; i++) {
         const int64_t col = n0 + high * 4 + i;
         if (col >= a.width) break;
-        float s = load_f32((const T *)a.x + low * a.ldx + col);
-        if (a.residual) s += load_f32((const T *)a.residual + low * a.ldr + col);
-        ((T *)a.out)[low * a.ldo + col] = (T)(s + sum[i]);
+        ((T *)a.out)[low * a.ldo + col] = (T)(s[i] + sum[i]);
     }
 }
 
@@ -497,7 +508,7 @@ constexpr int kMostIn = 256;  // workgroups of the first product: one to a CU, w
 constexpr size_t choice_space(int64_t experts) { return (size_t)kLayerWaves * 2 * experts * sizeof(double); }
 
 __global__ void __launch_bounds__(64 * kLayerWaves) layer_in_kernel(LayerArgs a, LayerSpace ws) {
-    extern __shared__ double scratch[];  // the choices, then the tiles
+    extern __shared__ __align__(16) double scratch[];  // the choices, then the tiles
     __shared__ Chosen c;
     const int wave = threadIdx.x / 64;
     double *score = scratch + (size_t)wave * 2 * a.experts;

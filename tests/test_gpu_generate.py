@@ -95,3 +95,46 @@ def test_tensors_of_two_devices_are_refused(torch, sd):  # noqa: F811
         sd.sample(torch.zeros(2, 10, device="cuda"), torch.zeros(2, dtype=torch.float64))
     with pytest.raises(ValueError):
         sd.product_groups(x, model.head.cpu(), model.head_scale)
+
+
+def test_first_calls_inside_a_capture(torch, sd):  # noqa: F811
+    """In a process of its own, every call is made for the first time while a graph is captured: what a call sets up for its
+    kernels does not end the capture, and the replay's results are the eager ones."""
+    import os
+    import subprocess
+    import sys
+
+    program = """
+import torch, paper_1708_02937_amd as sd
+g = torch.Generator(device="cuda").manual_seed(1)
+x = torch.randn(5, 300, generator=g, device="cuda").bfloat16()
+many = torch.randn(40, 300, generator=g, device="cuda")
+w = torch.randn(70, 300, generator=g, device="cuda")
+router = torch.randn(9, 300, generator=g, device="cuda") / 17
+w_in, s_in = sd.quantize_blocks(torch.randn(9, 2, 130, 300, generator=g, device="cuda") / 17, 128)
+w_out, s_out = sd.quantize_blocks(torch.randn(9, 300, 130, generator=g, device="cuda") / 11, 128)
+gamma = torch.ones(300, device="cuda")
+logits = torch.randn(3, 40000, generator=g, device="cuda")
+u = torch.rand(3, generator=g, device="cuda", dtype=torch.float64)
+p = torch.full((3,), 0.9, device="cuda")
+
+def calls():
+    q, s = sd.quantize_groups(w)
+    return [sd.widen_groups(q, s, 300), sd.product_groups(x, q, s), sd.product_groups(many, q, s),
+            *sd.experts_layer(x, gamma, router, 3, w_in, s_in, w_out, s_out, 130), *sd.sample(logits, u, top_p=p),
+            *sd.sample(logits[:, :500], u, top_p=p)]
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = calls()
+for _ in range(3):
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, calls()))
+print("captured first")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    _say("first calls captured")
+    done = subprocess.run([sys.executable, "-c", program], cwd=root, capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0 and "captured first" in done.stdout, done.stderr[-2000:]
