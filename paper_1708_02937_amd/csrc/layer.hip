@@ -184,9 +184,10 @@ __device__ __forceinline__ int wave_first(uint64_t v, int at) {
     return first;
 }
 
-// One token by a wave; `choice` and `score` hold an expert's value each.
+// One token by a wave; `choice` and `score` hold an expert's value each.  weights: whether
+// they are wanted, as one workgroup's are.
 __device__ __forceinline__ void choose(const LayerArgs &a, const double *logits, int t, uint64_t *choice, double *score,
-                                       Chosen &c) {
+                                       bool weights, Chosen &c) {
     const int lane = threadIdx.x % 64;
     double own = lane < a.experts ? logits[lane] : -INFINITY, sum = 1.0, s = 0.0;  // the lane's first logit, or all of them
     if (!a.sigmoid) {
@@ -263,15 +264,19 @@ __device__ __forceinline__ void choose(const LayerArgs &a, const double *logits,
             }
         }
     }
+    if (lane < a.chosen) c.ids[t * a.chosen + lane] = id;
+    if (a.tokens == 1) {  // the busy experts are the chosen ones
+        const uint64_t there = __ballot(id >= 0);
+        if (id >= 0) c.busy[lane_rank(there)] = (uint16_t)id, c.tokens[id] = 1;
+        if (lane == 0) c.count = __popcll(there);
+    }
+    if (!weights) return;
     s = id >= 0 ? score[id] : 0.0;
     if (a.normalize) {
         const double all = wave_total(s);
         s = all > 0.0 ? s / all : 0.0;
     }
-    if (lane < a.chosen) {
-        c.ids[t * a.chosen + lane] = id;
-        c.weight[t * a.chosen + lane] = (float)(s * (double)a.factor);
-    }
+    if (lane < a.chosen) c.weight[t * a.chosen + lane] = (float)(s * (double)a.factor);
 }
 
 // The experts' tokens and the busy experts from the ids.
@@ -297,9 +302,10 @@ __device__ __forceinline__ void list_busy(const LayerArgs &a, Chosen &c) {
 
 // The place j of expert e among token t's, which has one.
 __device__ __forceinline__ int place_of(const LayerArgs &a, const Chosen &c, int t, int e) {
-    int j = 0;
-    while (j + 1 < a.chosen && c.ids[t * a.chosen + j] != e) j++;
-    return j;
+    int at = 0;
+#pragma unroll 4
+    for (int j = 0; j < a.chosen; j++) at = c.ids[t * a.chosen + j] == e ? j : at;
+    return at;
 }
 
 // ------------------------------------------------------------------------------------------------ the experts
@@ -513,9 +519,9 @@ __global__ void __launch_bounds__(64 * kLayerWaves) layer_in_kernel(LayerArgs a,
     const int wave = threadIdx.x / 64;
     double *score = scratch + (size_t)wave * 2 * a.experts;
     for (int t = wave; t < a.tokens; t += kLayerWaves)
-        choose(a, ws.logits + (int64_t)t * a.experts, t, (uint64_t *)(score + a.experts), score, c);
+        choose(a, ws.logits + (int64_t)t * a.experts, t, (uint64_t *)(score + a.experts), score, blockIdx.x == 0, c);
     __syncthreads();
-    list_busy(a, c);
+    if (a.tokens > 1) list_busy(a, c);
     if (blockIdx.x == 0) {
         for (int i = threadIdx.x; i < a.tokens * a.chosen; i += 64 * kLayerWaves)
             a.ids[i] = c.ids[i], a.weight[i] = c.weight[i];

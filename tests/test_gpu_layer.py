@@ -166,6 +166,24 @@ def test_zero_rows_and_ties(torch, sd):  # noqa: F811
         assert bool((got.weight[1] == 0.25).all())
 
 
+@pytest.mark.parametrize("T", [1, 3])
+@pytest.mark.parametrize("E", [7, 64, 100])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_equal_scores_of_unequal_logits(torch, sd, T, E, score):  # noqa: F811
+    """Scores of 1 or 0 whose logits differ are equal: the lower expert is chosen, and the weights are theirs."""
+    H, F, k = 64, 20, 5
+    args, values = _case(torch, sd, T, H, F, E, "float32", "float32", False, seed=7)
+    args["x"].fill_(1.0)
+    args["gamma"].fill_(1.0)
+    _say("layer equal scores", T, E, score)
+    for levels in ((40, 60, 50, 70, 45, 41, -3), (-800, 5, -900, -760, -850, -870, -820), (0, -1, -2, 2, 1, 3, -3)):
+        logits = [levels[(3 * e + e // 7) % 7] for e in range(E)]
+        args["router"].copy_((torch.tensor(logits, dtype=torch.float32) / H)[:, None].expand(E, H))
+        for normalize in (True, False):
+            got = _run(sd, args, k, use_bias=False, score=score, normalize=normalize)
+            _check(torch, got, _want(args, values, k, score=score, normalize=normalize), "float32")
+
+
 def test_in_place_strides_and_workspace(torch, sd):  # noqa: F811
     """The output over x and over the residual, rows with strides at odd addresses, a workspace full of NaN of the size for
     16 tokens that serves smaller calls, and nothing written beside the results."""
