@@ -51,13 +51,17 @@ struct Row {
     double most_x;             // x of min_p
     int64_t top_k;
     float top;  // largest logit
-    bool greedy, masses;
+    bool masses;
 
     __device__ __forceinline__ double x(uint32_t key) const {
         const float l = logit_of_key(key);
         return l == top ? 0.0 : ((double)top - (double)l) * inverse;
     }
 };
+
+__device__ __forceinline__ bool is_greedy(const SampleArgs &a, int64_t at) {
+    return a.temperature && !(a.temperature[at] > 0.0f);
+}
 
 __device__ __forceinline__ Row row_of(const SampleArgs &a, int64_t at) {
     Row r;
@@ -67,7 +71,6 @@ __device__ __forceinline__ Row row_of(const SampleArgs &a, int64_t at) {
     r.top_k = a.top_k ? a.top_k[at] : 0;
     r.top_p = a.top_p ? (double)a.top_p[at] : 1.0;
     if (r.top_p < 0.0) r.top_p = 0.0;
-    r.greedy = !(temperature > 0.0);
     if (temperature == (double)INFINITY) temperature = 1e300;  // every token alike
     r.inverse = 1.0 / temperature;
     r.most_x = min_p > 0.0 ? -log(fmin(min_p, 1.0)) : (double)INFINITY;
@@ -114,6 +117,10 @@ __device__ __forceinline__ uint64_t whole_mass(double x, double from, int shift)
     return (uint64_t)__double_as_longlong(exp_small(x - from) + magic) & ((1ull << 52) - 1);
 }
 
+struct Keys {
+    uint32_t first, end;  // keys from this on and before that
+};
+
 // What the buckets tell of a row.
 struct Plan {
     int64_t k;       // tokens that top_k leaves
@@ -123,8 +130,9 @@ struct Plan {
     int lo, hi;         // buckets of the list (hi < lo: none); those before are kept whole, those after not at all
     bool cut_k, cut_p;  // whether there is anything to cut within the list
     bool settled;       // the row has been answered
+    uint32_t bound;     // the list is of keys from this on, by the groups; 0: by the buckets
     float top;
-    uint32_t first_key, end_key;  // the list's keys are from this on and before that
+    Keys keys;          // the list's
 };
 
 struct SampleSpace {
@@ -246,7 +254,8 @@ __device__ __forceinline__ int elect(bool hit, bool some, Common &sh) {
     return best >> 32 ? kThreads - (int)(best >> 32) : (int)best - 1;
 }
 
-// f(keys, first index) for the tokens [begin, end), eight at a time, the next ones on their way meanwhile.
+// f(keys, first index) for the tokens [begin, end), eight at a time, the next ones on their way meanwhile.  next: this thread's
+// first ones, by first_keys.
 template <typename T>
 __device__ __forceinline__ void keys8(const T *row, int64_t c, int64_t end, uint32_t (&k)[8]) {
     float l[8];
@@ -254,11 +263,13 @@ __device__ __forceinline__ void keys8(const T *row, int64_t c, int64_t end, uint
 #pragma unroll
     for (int i = 0; i < 8; i++) k[i] = c + i < end ? key_of(l[i]) : 0;
 }
+template <typename T>
+__device__ __forceinline__ void first_keys(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8]) {
+    keys8(row, begin + threadIdx.x * 8, end, next);
+}
 template <typename T, typename F>
-__device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t end, F f) {
-    uint32_t next[8];
+__device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8], F f) {
     const int64_t own = threadIdx.x * 8;
-    keys8(row, begin + own, end, next);
     for (int64_t c0 = begin; c0 < end; c0 += kTile) {
         uint32_t k[8];
 #pragma unroll
@@ -267,17 +278,85 @@ __device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t e
         f(k, c0 + own);
     }
 }
+template <typename T, typename F>
+__device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t end, F f) {
+    uint32_t next[8];
+    first_keys(row, begin, end, next);
+    each_tile(row, begin, end, next, f);
+}
 
 // ------------------------------------------------------------------------------------------------ the parts of a row
 template <typename T>
-__device__ __forceinline__ uint64_t best_of(const T *row, int64_t begin, int64_t end, uint64_t *part) {
+__device__ __forceinline__ uint64_t own_best(const T *row, int64_t begin, int64_t end) {  // of a thread's tokens
     uint64_t best = 0;
     each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t c) {
 #pragma unroll
         for (int i = 0; i < 8; i++)
             if (k[i]) best = max64(best, token_of(k[i], c + i));
     });
-    return block_max(best, part);
+    return best;
+}
+
+// top_k without counting the row.  The tokens are in groups; k groups whose largest keys are at least b hold k tokens of at
+// least b, so no smaller one is among the k largest.  With twice as many groups as k, a group seldom has many of them: of
+// evenly spread tokens 2 k ln 2 = 1.4 k have such a key, which are the list.
+constexpr int kMostGroups = 8 * kThreads;
+__device__ __forceinline__ bool by_groups(int64_t k, int64_t groups) {
+    return k > 0 && k <= kCountOnly && 2 * k <= groups && groups <= kMostGroups;
+}
+
+// Such a b from the largest keys of groups (0: none), of which each thread has some, key(i) for i < own; 0 if fewer than k groups have one: by buckets of
+// their range, and again of the k-th's bucket while that has more than a quarter of k.
+template <typename F>
+__device__ __forceinline__ uint32_t bound_of(int own, F key, uint32_t top, int64_t k, Common &sh) {
+    uint32_t least = 0;  // its complement
+    for (int i = 0; i < own; i++) {
+        const uint32_t v = key(i);
+        least = max(least, v ? ~v : 0);
+    }
+    uint64_t low = (uint32_t)~(uint32_t)block_max(least, sh.upart), high = top;
+    int64_t wanted = k;
+    while (true) {
+        int shift = 0;
+        while ((high - low) >> shift >= kBuckets) shift++;
+        for (int b = threadIdx.x; b < kBuckets; b += kThreads) sh.hist.counts[b] = 0;
+        __syncthreads();
+        for (int i = 0; i < own; i++) {
+            const uint32_t v = key(i);
+            if (v && v >= low && v <= high) atomicAdd(&sh.hist.counts[(v - low) >> shift], 1u);
+        }
+        if (threadIdx.x == 0) sh.found[0] = -1;
+        __syncthreads();
+        int64_t n[kEach], sum = 0, all;
+        const int first = kBuckets - 1 - (int)threadIdx.x * kEach;
+#pragma unroll
+        for (int i = 0; i < kEach; i++) n[i] = sh.hist.counts[first - i], sum += n[i];
+        int64_t upto = block_upto(sum, sh.ipart, all) - sum;
+#pragma unroll
+        for (int i = 0; i < kEach; i++) {
+            if (upto < wanted && upto + n[i] >= wanted) sh.found[0] = first - i, sh.found[1] = upto << 16 | n[i];
+            upto += n[i];
+        }
+        __syncthreads();
+        const int64_t bucket = sh.found[0], before = sh.found[1] >> 16, in = sh.found[1] & 0xffff;
+        __syncthreads();
+        if (bucket < 0) return 0;
+        low += (uint64_t)bucket << shift;
+        if (shift == 0 || in <= 8 + k / 4) return (uint32_t)low;
+        high = min(high, low + (1ull << shift) - 1);
+        wanted -= before;
+    }
+}
+
+// The plan of such a row: its list begins with its first token and ends with the last of at least `bound`.
+__device__ __forceinline__ Plan plan_by_groups(const Row &r, uint32_t bound) {
+    Plan p;
+    p.k = r.top_k, p.before = 0, p.above = p.all = 0.0;
+    p.lo = 0, p.hi = row_level().bucket(r.x(bound));
+    p.cut_k = true, p.cut_p = r.top_p < 1.0, p.settled = false, p.bound = bound;
+    p.top = r.top;
+    p.keys = {bound, key_of(r.top) + 1};
+    return p;
 }
 
 __device__ __forceinline__ void clear(Hist &h) {
@@ -286,10 +365,11 @@ __device__ __forceinline__ void clear(Hist &h) {
 }
 
 template <typename T>
-__device__ __forceinline__ void count_buckets(const T *row, int64_t begin, int64_t end, const Row &r, int shift, Hist &h) {
+__device__ __forceinline__ void count_buckets(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8], const Row &r,
+                                              int shift, Hist &h) {
     clear(h);
     const Level level = row_level();
-    each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t) {
+    each_tile(row, begin, end, next, [&](const uint32_t (&k)[8], int64_t) {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             if (!k[i]) continue;
@@ -324,7 +404,7 @@ __device__ __forceinline__ Plan plan_of(const Row &r, const Level &level, bool m
     double listed = 0.0;
     const double m0 = masses ? under + block_upto(sum, sh.part, listed) - sum : 0.0;
     valid += base;
-    p.settled = false;
+    p.settled = false, p.bound = 0;
     p.top = r.top;
     p.all = outer && r.masses ? outer->all : under + listed;
     p.k = outer ? outer->k : r.top_k > 0 && r.top_k < valid ? r.top_k : valid;
@@ -408,7 +488,7 @@ __device__ __forceinline__ uint32_t least_key(const Row &r, int b) {
 }
 
 __device__ __forceinline__ void find_keys(const Row &r, Plan &p, Common &sh) {
-    p.first_key = p.end_key = 0;
+    p.keys = {0, 0};
     if (p.hi < p.lo) return;
     const int wave = threadIdx.x / 64;
     if (wave < 2) {
@@ -416,20 +496,20 @@ __device__ __forceinline__ void find_keys(const Row &r, Plan &p, Common &sh) {
         if (threadIdx.x % 64 == 0) sh.found[wave] = key;
     }
     __syncthreads();
-    p.end_key = (uint32_t)sh.found[0], p.first_key = (uint32_t)sh.found[1];
+    p.keys = {(uint32_t)sh.found[1], (uint32_t)sh.found[0]};
     __syncthreads();
 }
 
 // put(place, token) for the tokens of the list's buckets in [begin, end), in order of the indices; returns how many there are.
 template <typename T, typename F>
-__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Plan &p, uint64_t *part,
-                                            F put) {
+__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8], const Keys &keys,
+                                            uint64_t *part, F put) {
     uint32_t placed = 0;
-    each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t c) {
+    each_tile(row, begin, end, next, [&](const uint32_t (&k)[8], int64_t c) {
         uint32_t mask = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (k[i] - p.first_key < p.end_key - p.first_key) mask |= 1u << i;
+            if (k[i] - keys.first < keys.end - keys.first) mask |= 1u << i;
         uint64_t all;
         const int mine = __popc(mask);
         uint32_t at = placed + (uint32_t)block_upto((uint64_t)mine, part, all) - mine;
@@ -439,6 +519,12 @@ __device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t
         placed += (uint32_t)all;
     });
     return placed;
+}
+template <typename T, typename F>
+__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Plan &p, uint64_t *part, F put) {
+    uint32_t next[8];
+    first_keys(row, begin, end, next);
+    return collect(row, begin, end, next, p.keys, part, put);
 }
 
 // What is kept of a row (the tokens up to `last` in their order, as far as min_p keeps them), and what is drawn of it.
@@ -457,9 +543,9 @@ __device__ __forceinline__ void answer(const SampleArgs &a, int64_t at, int64_t 
 }
 
 // A row without a token to take, or whose first token is taken: true if that is all.
-__device__ __forceinline__ bool settled(const SampleArgs &a, int64_t at, const Row &r, uint64_t best, bool writes) {
+__device__ __forceinline__ bool settled(const SampleArgs &a, int64_t at, uint64_t best, bool writes) {
     const bool none = best == 0;
-    if (!none && !r.greedy) return false;
+    if (!none && !is_greedy(a, at)) return false;
     if (writes && threadIdx.x == 0) answer(a, at, none ? -1 : index_of(best), none ? 0.0 : 1.0, none ? 0 : 1);
     return true;
 }
@@ -564,7 +650,7 @@ __device__ __forceinline__ void each_listed(const T *row, int64_t vocab, const P
     each_tile(row, 0, vocab, [&](const uint32_t (&k)[8], int64_t c) {
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (k[i] - p.first_key < p.end_key - p.first_key) f(token_of(k[i], c + i));
+            if (k[i] - p.keys.first < p.keys.end - p.keys.first) f(token_of(k[i], c + i));
     });
 }
 
@@ -647,11 +733,8 @@ __device__ __forceinline__ bool keep(const SampleArgs &a, int64_t at, const T *r
 }
 
 // The masses of the kept ones of eight tokens, and their sum.
-template <typename T>
-__device__ __forceinline__ double kept_masses(const T *row, int64_t c, int64_t end, const Row &r, const Kept &kept,
+__device__ __forceinline__ double kept_masses(const uint32_t (&k)[8], int64_t c, const Row &r, const Kept &kept,
                                               const Shared &sh, double (&m)[8]) {
-    uint32_t k[8];
-    keys8(row, c, end, k);
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -673,7 +756,15 @@ __device__ __forceinline__ void draw_in(const SampleArgs &a, int64_t at, const T
         const int64_t each = (end - begin + kTile - 1) / kTile * 8;
         const int64_t from = min(begin + threadIdx.x * each, end), to = min(from + each, end);
         double m[8], sum = 0.0, all;
-        for (int64_t c = from; c < to; c += 8) sum += kept_masses(row, c, to, r, kept, sh, m);
+        uint32_t next[8];
+        keys8(row, from, to, next);
+        for (int64_t c = from; c < to; c += 8) {
+            uint32_t k[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) k[i] = next[i];
+            if (c + 8 < to) keys8(row, c + 8, to, next);
+            sum += kept_masses(k, c, r, kept, sh, m);
+        }
         const double upto = before + block_upto(sum, sh.part, all);
         const int owner = elect(sum > 0.0 && upto > kept.drawn, sum > 0.0, sh);
         if (owner < 0) {
@@ -713,13 +804,23 @@ __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, in
     const int64_t at = blockIdx.x;
     const T *row = (const T *)a.logits + at * a.ld;
     Row r = row_of(a, at);
-    const uint64_t best = best_of(row, 0, a.vocab, sh.upart);
-    if (settled(a, at, r, best, true)) return;
+    const uint64_t own = own_best(row, 0, a.vocab), best = block_max(own, sh.upart);
+    if (settled(a, at, best, true)) return;
     r.top = logit_of_key((uint32_t)(best >> 32));
     fill_table(sh);
-    count_buckets(row, 0, a.vocab, r, shift, sh.hist);
-    Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
-    find_keys(r, p, sh);
+    uint32_t bound = 0;
+    if (by_groups(r.top_k, kThreads))
+        bound = bound_of(1, [&](int) { return (uint32_t)(own >> 32); }, (uint32_t)(best >> 32), r.top_k, sh);
+    Plan p;
+    if (bound) {
+        p = plan_by_groups(r, bound);
+    } else {
+        uint32_t next[8];
+        first_keys(row, 0, a.vocab, next);
+        count_buckets(row, 0, a.vocab, next, r, shift, sh.hist);
+        p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
+        find_keys(r, p, sh);
+    }
     uint32_t n = 0;
     if (p.hi >= p.lo)
         n = collect(row, 0, a.vocab, p, sh.upart, [&](uint32_t place, uint64_t token) {
@@ -731,8 +832,29 @@ __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, in
     draw_in(a, at, row, r, kept, 0, a.vocab, 0.0, sh);
 }
 
-// Longer rows in four launches, the first three by chunks: the first token; the buckets, and the plan by whichever workgroup
-// of the row is through last; the list, and the mass of what is kept whole; the end.
+// The largest keys of a chunk's groups, in its part of ws.parts, which rows with few tokens to keep do not use otherwise.
+// lanes: of a group, 1, 8 or 64, so that a row has a few hundred to a few thousand of them.
+__device__ __forceinline__ int group_lanes(int64_t chunks) { return chunks < 8 ? 1 : chunks <= 64 ? 8 : 64; }
+__device__ __forceinline__ void put_groups(uint32_t key, int lanes, uint32_t *groups) {
+    if (lanes > 1) {
+        key = max(key, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)key, 0xb1, 0xf, 0xf, true));   // lanes 1 apart
+        key = max(key, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)key, 0x4e, 0xf, 0xf, true));   // 2 apart
+        key = max(key, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)key, 0x141, 0xf, 0xf, true));  // the other half of eight
+    }
+    if (lanes > 8) {
+        key = max(key, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)key, 0x140, 0xf, 0xf, true));  // of sixteen
+        Two t = across16(key);
+        t = across32(max(t.a, t.b));
+        key = max(t.a, t.b);
+    }
+    if (threadIdx.x % lanes == 0) groups[threadIdx.x / lanes] = key;
+}
+__device__ __forceinline__ uint32_t *groups_of(const SampleSpace &ws, int64_t chunk) {
+    return (uint32_t *)(ws.parts + chunk * kBuckets);
+}
+
+// Longer rows in four launches, the first three by chunks: the first token and the groups' largest keys; the buckets, and the plan by
+// whichever workgroup of the row is through last, or the list by the groups; any other list, and the mass of what is kept whole; the end.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_best_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk) {
     __shared__ uint64_t part[kWaves];
@@ -740,7 +862,11 @@ __global__ void __launch_bounds__(kThreads) sample_best_kernel(SampleArgs a, Sam
     for (int64_t b = c * kThreads + threadIdx.x; b < kBuckets; b += chunks * kThreads)
         ws.counts[at * kBuckets + b] = 0, ws.masses[at * kBuckets + b] = 0;
     if (c == 0 && threadIdx.x == 0) ws.done[at] = 0;
-    const uint64_t best = best_of((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab), part);
+    const uint64_t own = own_best((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab));
+    const int lanes = group_lanes(chunks);
+    if (by_groups(a.top_k ? a.top_k[at] : 0, chunks * (kThreads / lanes)))
+        put_groups((uint32_t)(own >> 32), lanes, groups_of(ws, blockIdx.x));
+    const uint64_t best = block_max(own, part);
     if (threadIdx.x == 0) ws.best[blockIdx.x] = best;
 }
 
@@ -748,17 +874,48 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_count_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk,
                                                                int shift) {
     __shared__ Common sh;
+    __shared__ uint32_t groups[kMostGroups];
     const int64_t at = blockIdx.x / chunks, c = blockIdx.x % chunks;
-    Row r = row_of(a, at);
+    const int64_t begin = c * chunk, end = min(begin + chunk, a.vocab);
+    const T *row = (const T *)a.logits + at * a.ld;
+    uint32_t next[8];
+    first_keys(row, begin, end, next);
     uint64_t best = 0;
     for (int64_t w = threadIdx.x; w < chunks; w += kThreads) best = max64(best, ws.best[at * chunks + w]);
     best = block_max(best, sh.upart);
-    if (settled(a, at, r, best, c == 0)) {
+    if (settled(a, at, best, c == 0)) {
         if (c == 0 && threadIdx.x == 0) ws.plan[at].settled = true;
         return;
     }
-    r.top = logit_of_key((uint32_t)(best >> 32));
-    count_buckets((const T *)a.logits + at * a.ld, c * chunk, min((c + 1) * chunk, a.vocab), r, shift, sh.hist);
+    const uint32_t top = (uint32_t)(best >> 32);
+    const int64_t top_k = a.top_k ? a.top_k[at] : 0;
+    const int each = kThreads / group_lanes(chunks);
+    if (by_groups(top_k, chunks * each)) {
+        const int own = (int)(chunks * each + kThreads - 1) / kThreads;
+#pragma unroll 4
+        for (int i = 0; i < own; i++) {
+            const int g = i * kThreads + threadIdx.x;
+            groups[g] = g < chunks * each ? groups_of(ws, at * chunks + g / each)[g % each] : 0;
+        }
+        const uint32_t bound =
+            bound_of(own, [&](int i) { return groups[i * kThreads + threadIdx.x]; }, top, top_k, sh);
+        if (bound) {  // or few groups have a token that can be taken, which every workgroup of the row finds alike
+            const uint32_t room = (uint32_t)(chunk / 8);
+            uint64_t *const list = ws.list + blockIdx.x * (int64_t)room;
+            const uint32_t placed = collect(row, begin, end, next, Keys{bound, top + 1}, sh.upart,
+                                            [&](uint32_t place, uint64_t token) {
+                                                if (place < room) list[place] = token;
+                                            });
+            if (threadIdx.x == 0) {
+                ws.whole[blockIdx.x] = 0.0, ws.listed[blockIdx.x] = placed;
+                if (c == 0) ws.plan[at].settled = false, ws.plan[at].bound = bound, ws.plan[at].top = logit_of_key(top);
+            }
+            return;
+        }
+    }
+    Row r = row_of(a, at);
+    r.top = logit_of_key(top);
+    count_buckets(row, begin, end, next, r, shift, sh.hist);
     uint32_t *const counts = ws.counts + at * kBuckets;
     unsigned long long *const masses = (unsigned long long *)ws.masses + at * kBuckets;
     for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
@@ -789,7 +946,7 @@ __global__ void __launch_bounds__(kThreads) sample_list_kernel(SampleArgs a, Sam
     __shared__ double sums[kWaves];
     const int64_t at = blockIdx.x / chunks, c = blockIdx.x % chunks;
     const Plan p = ws.plan[at];
-    if (p.settled) return;
+    if (p.settled || p.bound) return;
     const bool masses = row_of(a, at).masses;
     const uint32_t room = (uint32_t)(chunk / 8);
     uint64_t *const list = ws.list + (at * chunks + c) * room;
@@ -814,10 +971,11 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
     __shared__ Shared sh;
     const int64_t at = blockIdx.x;
     const T *row = (const T *)a.logits + at * a.ld;
-    const Plan p = ws.plan[at];
+    Plan p = ws.plan[at];
     if (p.settled) return;
     Row r = row_of(a, at);
     r.top = p.top;
+    if (p.bound) p = plan_by_groups(r, p.bound);
     const uint32_t room = (uint32_t)(chunk / 8);
     double *const whole = ws.whole + at * chunks;
     // the chunks' lists in LDS, where they fit
@@ -881,8 +1039,8 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
             const int64_t end = min((c + 1) * chunk, a.vocab);
             double sum = 0.0;
             double m[8];
-            for (int64_t t = c * chunk + threadIdx.x * 8; t < end; t += kTile)
-                sum += kept_masses(row, t, end, r, kept, sh, m);
+            each_tile(row, c * chunk, end,
+                      [&](const uint32_t (&k)[8], int64_t t) { sum += kept_masses(k, t, r, kept, sh, m); });
             sum = block_sum(sum, sh.part);
             if (threadIdx.x == 0) whole[c] = sum;
         }
