@@ -126,7 +126,7 @@ struct Plan {
     int64_t k;       // tokens that top_k leaves
     int64_t before;  // tokens of the buckets before lo, and their mass
     double above;
-    double all;         // the row's mass (0 where masses are not summed)
+    double all;         // the row's mass (0: not known, and without a cut by top_k the list goes to the row's end)
     int lo, hi;         // buckets of the list (hi < lo: none); those before are kept whole, those after not at all
     bool cut_k, cut_p;  // whether there is anything to cut within the list
     bool settled;       // the row has been answered
@@ -576,7 +576,7 @@ __device__ __forceinline__ bool by_rank(const SampleArgs &a, int64_t at, const R
     if (p.cut_p) {
         double all;
         const double v = mine && i < left_k ? sh.sorted.mass[i] : 0.0, upto = block_upto(v, sh.part, all);
-        const double share = r.masses && !p.cut_k ? p.all : p.above + all, target = r.top_p * share - p.above;
+        const double share = !p.cut_k && p.all > 0.0 ? p.all : p.above + all, target = r.top_p * share - p.above;
         // the first that reaches the share, if any does
         const uint64_t reach = block_max(mine && upto >= target ? (uint64_t)(kThreads - i) : 0, sh.upart);
         if (reach) left = min(left, (int64_t)kThreads - (int64_t)reach + 1);

@@ -124,6 +124,35 @@ def test_nearly_flat_rows(torch, sd, V):  # noqa: F811
         _check(torch, sd, logits[:, :V], rng.random(T), None, [40, 1024, 9000, 0, 0], [0.5, 0.3, 0.9, 0.99, 0.2], near=1e-13)
 
 
+@pytest.mark.parametrize("T,V", [(6, 5000), (6, 40000), (160, 40000), (2, 300000)])
+def test_few_tokens_kept_of_uneven_rows(torch, sd, T, V):  # noqa: F811
+    """top_k where the tokens that count lie together, in a few runs, or at even distances; where keys span all that floats
+    can; where many are equal; and around as many tokens as half the runs of 8 or 64 tokens that a row has."""
+    rng = np.random.default_rng(T + V)
+    _say("sample uneven", T, V)
+    at = np.arange(V)
+    base = 2 * rng.standard_normal((T, V))
+    rows = {
+        "banned but a run": np.where((at >= V // 3) & (at < V // 3 + 900), base, -np.inf),
+        "banned but a few": np.where(at % 97 == 5, base, -np.inf),
+        "banned but 70": np.where((at >= 64) & (at < 134), base, -np.inf),
+        "in order": np.broadcast_to(-at * (40.0 / V), (T, V)),
+        "against the order": np.broadcast_to(at * (40.0 / V), (T, V)),
+        "the best together": base + 30.0 * (at // 256 == 7),
+        "far apart": np.where(rng.random((T, V)) < 0.5, base, -3e38 * rng.random((T, V))),
+        "one far above": base + 1e30 * (at == V // 2),
+        "few values": np.round(base),
+        "subnormal": base * 1e-40,
+    }
+    k = np.resize([1, 2, 50, 64, 69, 70, 71, 128, 200, 256, 257, 312, 320, 400, 513, 900, 1024, 1025], T)
+    for name, l in rows.items():
+        logits = _cuda(torch, l, torch.float32)
+        for first in range(1 if T > 100 else 3):
+            near = None if name in ("in order", "against the order", "few values") else 1e-11
+            _check(torch, sd, logits, rng.random(T), top_k=np.roll(k, 5 * first)[:T], near=near)
+            _check(torch, sd, logits, rng.random(T), np.full(T, 0.7), np.roll(k, 6 * first + 1), np.full(T, 0.83), near=near)
+
+
 @pytest.mark.parametrize("V", [300, 40000])
 def test_rows_without_tokens_and_not_finite(torch, sd, V):  # noqa: F811
     rng = np.random.default_rng(1)
