@@ -16,6 +16,8 @@
 // A bucket's masses are in units of exp(-b / 16) 2^-shift: e^-d for 0 <= d < 1/16 is a polynomial of degree 8 (the next term is
 // 4e-17), and the sum of a bucket is as exact as its values.  The last bucket is x >= 63.9: its tokens count, but their mass,
 // below 2e-28 of the first token's each, is 0.
+#include <algorithm>
+
 #include "blocks8.h"
 #include "common.h"
 #include "lanes.h"
@@ -1076,11 +1078,14 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
     draw_in(a, at, row, r, kept, chosen * chunk, min((chosen + 1) * chunk, a.vocab), start, sh);
 }
 
-// Rows that one workgroup each takes in one launch.  us (this | the four launches), float, temperature alone and all filters:
-//   1 row:     8000 tokens 16.8, 16.0 | 21.8, 23.1;  16000 24.9, 21.4 | 21.7, 23.1;  32000 40.8, 32.2 | 22.3, 23.5
-//   200 rows:  8000 tokens 18.0, 16.6 | 27.6, 27.6;  16000 27.9, 23.4 | 35.8, 34.1;  32000 45.9, 37.3 | 49.3, 42.0
-constexpr int64_t kShort = 4 * kTile, kShortOfMany = 8 * kTile, kMany = 128;
-bool is_short(int64_t rows, int64_t vocab) { return vocab <= (rows < kMany ? kShort : kShortOfMany); }
+// Rows that one workgroup each takes in one launch.  us (this | the four launches), temperature alone, top-p, all filters, float:
+//   1 row:      8000 tokens 17, 25, 14 | 22, 34, 22;   16000 26, 38, 17 | 23, 35, 23;   32000 42, 61, 24 | 23, 39, 20
+//   128 rows:   32000 43, 61, 24 | 43, 59, 30;   64000 79, 107, 42 | 55, 80, 38;   131072 152, 202, 77 | 77, 105, 50
+//   256 rows:   32000 47, 66, 28 | 56, 78, 44;   64000 83, 113, 45 | 74, 103, 52
+//   512 rows:   64000 119, 154, 55 | 123, 164, 74;   131072 226, 287, 97 | 211, 279, 118
+//   1000 rows:  131072 463, 579, 206 | 513, 678, 249
+constexpr int64_t kShort = 4 * kTile, kOfARow = 256;
+bool is_short(int64_t rows, int64_t vocab) { return vocab <= kShort || vocab / kOfARow <= rows; }
 
 template <typename T>
 hipError_t sample_go(const SampleArgs &a, hipStream_t s) {
@@ -1129,8 +1134,7 @@ size_t sample_workspace(int64_t rows, int64_t vocab) {
 }
 
 size_t sample_workspace_upto(int64_t rows, int64_t vocab) {
-    const int64_t most = is_short(rows, vocab) && rows >= kMany ? kMany - 1 : rows;
-    return sample_workspace(most, vocab);
+    return sample_workspace(vocab <= kShort ? rows : std::min(rows, vocab / kOfARow - 1), vocab);  // the most that are not short
 }
 
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t stream) {

@@ -50,7 +50,8 @@ def _settings(rng, T, mixed):
 
 
 @pytest.mark.parametrize("T,V", [(1, 1), (5, 2), (9, 3), (20, 7), (33, 100), (40, 1001), (8, 4096), (7, 4097), (5, 20000),
-                                 (4, 16384), (4, 16385), (3, 32768), (130, 32768), (6, 32769), (13, 50021), (3, 131072), (1, 262144), (140, 33000)])
+                                 (4, 16384), (4, 16385), (3, 32768), (130, 32768), (6, 32769), (13, 50021), (3, 131072), (1, 262144), (140, 33000), (127, 33000),
+                                 (260, 66000)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("mixed,banned", [(False, 0.0), (True, 0.0), (True, 0.5)])
 def test_sample(torch, sd, T, V, dtype, mixed, banned):  # noqa: F811
@@ -124,7 +125,7 @@ def test_nearly_flat_rows(torch, sd, V):  # noqa: F811
         _check(torch, sd, logits[:, :V], rng.random(T), None, [40, 1024, 9000, 0, 0], [0.5, 0.3, 0.9, 0.99, 0.2], near=1e-13)
 
 
-@pytest.mark.parametrize("T,V", [(6, 5000), (6, 40000), (160, 40000), (2, 300000)])
+@pytest.mark.parametrize("T,V", [(6, 5000), (6, 40000), (150, 40000), (160, 40000), (2, 300000)])
 def test_few_tokens_kept_of_uneven_rows(torch, sd, T, V):  # noqa: F811
     """top_k where the tokens that count lie together, in a few runs, or at even distances; where keys span all that floats
     can; where many are equal; and around as many tokens as half the runs of 8 or 64 tokens that a row has."""
