@@ -288,20 +288,20 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProduc
     }
 }
 
-// ---- any rows: 64 outputs of 16 MT rows.  The rows come through LDS a stage at a time, since every wave needs them all (straight
-// from registers, with waves that share the columns, each line is fetched for a quarter of it: 64 rows 45 us where this took
-// 20); the weights still go straight to registers.  The waves share a stage's steps and the outputs.  Rows and weights of the
-// next stage are on their way while one is multiplied.
-template <typename TX, typename TY, int MT>
+// ---- any rows: OUTPUTS outputs of 16 MT rows.  The rows come through LDS a stage of kSteps steps at a time, since every wave needs
+// them all (straight from registers, with waves that share the columns, each line is fetched for a quarter of it: 64 rows 45 us
+// where this took 20); the weights still go straight to registers.  The waves share a stage's steps and the outputs.  Rows and weights of
+// the next stage are on their way while one is multiplied, in a buffer of its own where two fit LDS.
+template <typename TX, typename TY, int MT, int OUTPUTS, int kSteps>
 __global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupProductArgs a) {
-    constexpr int kSteps = sizeof(TX) == 4 ? 2 : 4, kCols = kSteps * kBlock, kAcross = kWaves / kSteps, NW = 4 / kAcross;
+    constexpr int kCols = kSteps * kBlock, kAcross = kWaves / kSteps, NW = OUTPUTS / 16 / kAcross;
     constexpr int kPitch = kCols * 2 + 16, kPart = 16 * MT * kPitch, kStage = kParts<TX> * kPart;
     constexpr int kStages = 2 * kStage <= kMostLds ? 2 : 1;
     constexpr int kRowEights = kCols / 8, kLoads = 16 * MT * kRowEights / (64 * kWaves);
     extern __shared__ __align__(16) uint8_t stage[];  // at the end the waves' sums
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, low = lane % 16, high = lane / 16;
     const int step = wave % kSteps, across = wave / kSteps;
-    const int64_t n0 = (int64_t)blockIdx.x * 64 + across * (16 * NW), m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int64_t n0 = (int64_t)blockIdx.x * OUTPUTS + across * (16 * NW), m0 = (int64_t)blockIdx.y * (16 * MT);
     const int steps = (int)blocks_of(a.k), turns = (steps + kSteps - 1) / kSteps;
     auto load_rows = [&](int turn, Eight<TX> (&x)[kLoads]) {
 #pragma unroll
@@ -343,13 +343,13 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupP
 #pragma unroll
         for (int v = 0; v < NW; v++) part[wave][t][v][lane] = acc[t][v];
     __syncthreads();
-    for (int u = wave; u < MT * 4; u += kWaves) {
-        const int t = u / 4, of = u % 4 / NW, v = u % NW;  // the waves that share these outputs
+    for (int u = wave; u < MT * (OUTPUTS / 16); u += kWaves) {
+        const int t = u / (OUTPUTS / 16), of = u % (OUTPUTS / 16) / NW, v = u % NW;  // the waves that share these outputs
         const int64_t m = m0 + 16 * t + low;
         if (m >= a.m) continue;
         v4f z = part[of * kSteps][t][v][lane];
         for (int i = 1; i < kSteps; i++) z += part[of * kSteps + i][t][v][lane];
-        put_outputs<TY>(a, m, (int64_t)blockIdx.x * 64 + of * (16 * NW) + 16 * v + high * 4, z);
+        put_outputs<TY>(a, m, (int64_t)blockIdx.x * OUTPUTS + of * (16 * NW) + 16 * v + high * 4, z);
     }
 }
 
@@ -369,17 +369,17 @@ hipError_t product_few_go(const GroupProductArgs &a, int64_t most, hipStream_t s
     return hipGetLastError();
 }
 
-template <typename TX, typename TY, int MT>
+template <typename TX, typename TY, int MT, int OUTPUTS, int STEPS>
 hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
-    constexpr int kStage = kParts<TX> * 16 * MT * ((sizeof(TX) == 4 ? 2 : 4) * kBlock * 2 + 16);
-    constexpr int kSums = kWaves * MT * (sizeof(TX) == 4 ? 1 : 2) * 64 * (int)sizeof(v4f);
+    constexpr int kStage = kParts<TX> * 16 * MT * (STEPS * kBlock * 2 + 16);
+    constexpr int kSums = kWaves * MT * (OUTPUTS / 16 * STEPS / kWaves) * 64 * (int)sizeof(v4f);
     constexpr int kRows = 2 * kStage <= kMostLds ? 2 * kStage : kStage, kBytes = kRows > kSums ? kRows : kSums;
     static_assert(kBytes <= kMostLds, "");
     static std::atomic<unsigned long long> raised;
-    hipError_t e = raise_lds_limit((const void *)product_groups_tile_kernel<TX, TY, MT>, kBytes, raised);
+    hipError_t e = raise_lds_limit((const void *)product_groups_tile_kernel<TX, TY, MT, OUTPUTS, STEPS>, kBytes, raised);
     if (e != hipSuccess) return e;
     // a launch holds fewer than 2^32 threads along the outputs and 2^16 workgroups along the rows
-    constexpr int64_t kMostN = (int64_t)64 << 22, kMostM = (int64_t)16 * MT << 15;
+    constexpr int64_t kMostN = (int64_t)16 << 22, kMostM = (int64_t)16 * MT << 15;
     for (int64_t n0 = 0; n0 < a.n; n0 += kMostN)
         for (int64_t m0 = 0; m0 < a.m; m0 += kMostM) {
             GroupProductArgs p = a;
@@ -390,24 +390,50 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
             p.w_scale = a.w_scale + n0 * group_scale_pitch(a.k);
             p.bias = a.bias ? a.bias + n0 : nullptr;
             p.y = (TY *)a.y + m0 * a.ldy + n0;
-            const dim3 grid((unsigned)((p.n + 63) / 64), (unsigned)((p.m + 16 * MT - 1) / (16 * MT)));
-            product_groups_tile_kernel<TX, TY, MT><<<grid, 64 * kWaves, kBytes, s>>>(p);
+            const dim3 grid((unsigned)((p.n + OUTPUTS - 1) / OUTPUTS), (unsigned)((p.m + 16 * MT - 1) / (16 * MT)));
+            product_groups_tile_kernel<TX, TY, MT, OUTPUTS, STEPS><<<grid, 64 * kWaves, kBytes, s>>>(p);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
     return hipSuccess;
 }
 
+// The widest tiles that still give every CU a workgroup, since a row through LDS serves the wider tile's outputs at once and a narrow
+// one's waves share the columns: of 16 x 16, 16 x 32, 16 x 64, 32 x 64 and 64 x 64 (rows x outputs), us,
+//   bfloat16, 4096 columns:  32 rows of 4096: 9.7, 9.0, 11.7, 13.5, 17.2;   48 of 8192: 22, 18, 20, 14.2, 19;   64 of 16384: 54, 40, 36, 24, 21
+//   float, 4096 columns:     16 rows of 4096: 11.5, 13.2, 17, 27, 46;   32 of 4096: 21, 14, 17.7, 29, 47;   64 of 16384: 145, 91, 48, 56, 51
+// Three parts of floats make LDS the bound of the tall ones, so floats have none.  64 x 64 runs by itself on a CU: a last round of
+// few workgroups costs as much as a full one (64 rows of 20000 outputs, 313 of them, 300 columns: 17.3 against 12.3).
+constexpr int64_t kCus = 256;
+template <typename TX, typename TY>
+hipError_t product_tiles_go(const GroupProductArgs &a, hipStream_t s) {
+    auto groups = [&](int64_t rows, int64_t outputs) { return (a.m + rows - 1) / rows * ((a.n + outputs - 1) / outputs); };
+    if (groups(16, 16) <= kCus) return product_tile_go<TX, TY, 1, 16, 8>(a, s);
+    if (groups(16, 32) <= kCus) return product_tile_go<TX, TY, 1, 32, 4>(a, s);
+    if constexpr (sizeof(TX) == 4) {
+        return product_tile_go<TX, TY, 1, 64, 2>(a, s);
+    } else {
+        if (a.m <= 16 || groups(16, 64) <= kCus) return product_tile_go<TX, TY, 1, 64, 4>(a, s);
+        if (a.m <= 32 || groups(32, 64) <= kCus || (groups(64, 64) - 1) % kCus < kCus * 4 / 5)
+            return product_tile_go<TX, TY, 2, 64, 4>(a, s);
+        return product_tile_go<TX, TY, 4, 64, 4>(a, s);
+    }
+}
+
+// Up to 16 rows that fit LDS stay there, but for few columns, where a workgroup's waves have little to share, and for more than 8 rows
+// in half precision of few outputs, which every workgroup would fetch.  us (resident | tiles), bfloat16, 1 and 16 rows:
+//   4096 columns: 4096 outputs 5.3, 7.8 | 5.7, 6.8;  8192: 7.9, 14.3 | 8.5, 9.3;  16384: 10.8, 13.2 | 11.5, 12.3;  32768: 17, 19.6 | 18.5, 20.4
+//   2048 columns: 4096 outputs 4.7, 5.8 | 4.6, 5.1;  65536: 26, 27 | 19, 22;   16384 columns, 4096 outputs: 10.9, - | 15, 18
+//   floats: 1 row of 4096 columns and 4096 outputs 7.3 | 10.2;  32768: 22 | 25;  of 2048 columns and 65536 outputs 30 | 24
 template <typename TX, typename TY>
 hipError_t product_go(const GroupProductArgs &a, hipStream_t s) {
     const int64_t rows = rows_space<TX>(a.m, a.k);
-    if (a.m <= 16 && rows <= kMostLds - sums_space(2, 1)) {
-        if (a.n <= 8192) return product_few_go<TX, TY, 1, 2>(a, 512, s);
-        if (rows <= kMostLds - sums_space(2, 2)) return product_few_go<TX, TY, 2, 2>(a, 256, s);
-        return product_few_go<TX, TY, 2, 1>(a, 256, s);
-    }
-    if (a.m <= 16) return product_tile_go<TX, TY, 1>(a, s);
-    return a.m <= 32 ? product_tile_go<TX, TY, 2>(a, s) : product_tile_go<TX, TY, 4>(a, s);
+    const bool resident = a.m <= 16 && rows <= kMostLds - sums_space(2, 1) && (a.n <= 8192 || a.k > 2048) &&
+                          !(sizeof(TX) == 2 && a.m > 8 && a.n <= 16384);
+    if (!resident) return product_tiles_go<TX, TY>(a, s);
+    if (a.n <= 8192) return product_few_go<TX, TY, 1, 2>(a, 512, s);
+    if (rows <= kMostLds - sums_space(2, 2)) return product_few_go<TX, TY, 2, 2>(a, 256, s);
+    return product_few_go<TX, TY, 2, 1>(a, 256, s);
 }
 
 }  // namespace
