@@ -398,25 +398,35 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
     return hipSuccess;
 }
 
-// The widest tiles that still give every CU a workgroup, since a row through LDS serves the wider tile's outputs at once and a narrow
-// one's waves share the columns: of 16 x 16, 16 x 32, 16 x 64, 32 x 64 and 64 x 64 (rows x outputs), us,
-//   bfloat16, 4096 columns:  32 rows of 4096: 9.7, 9.0, 11.7, 13.5, 17.2;   48 of 8192: 22, 18, 20, 14.2, 19;   64 of 16384: 54, 40, 36, 24, 21
-//   float, 4096 columns:     16 rows of 4096: 11.5, 13.2, 17, 27, 46;   32 of 4096: 21, 14, 17.7, 29, 47;   64 of 16384: 145, 91, 48, 56, 51
-// Three parts of floats make LDS the bound of the tall ones, so floats have none.  64 x 64 runs by itself on a CU: a last round of
-// few workgroups costs as much as a full one (64 rows of 20000 outputs, 313 of them, 300 columns: 17.3 against 12.3).
+// The largest tiles that still give every CU a workgroup: a small one's waves share the columns, a large one's rows and weights serve
+// more outputs.  us, 4096 columns, of 16 x 16, 16 x 32, 16 x 64 | 32 x 64, 64 x 64 | 32 x 128, 64 x 128 (rows x outputs), bfloat16:
+//   32 rows, 4096 outputs 9.7, 9.0, 11.7 | 13.5, 17.2 | 21, 24;    48 rows, 8192 22, 18, 20 | 14.2, 19 | 22, 29
+//   32 rows, 32768        -, 40, 36 | 24.2, 33 | 22.7, 26.5;       64 rows, 16384 54, 40, 36 | 24, 21.5 | 22.5, 30
+//   64 rows, 32768        105, 77, 70 | 44, 40 | 40, 31;           256 rows, 32768 -, -, 267 | 160, 151 | 146, 100
+// and of 16 x 16, 16 x 32, 16 x 64 | 16 x 128, 32 x 128 | 64 x 128, 64 x 256, float, of which a stage in LDS has three parts:
+//   16 rows, 4096 outputs 11.5, 13.2, 17 | -, - | -, -;            32 rows, 16384 73, 47, 29 | 25.5, 38 | 60, 91
+//   64 rows, 16384        145, 91, 52 | 45, 40 | 67, 98;           64 rows, 32768 288, 180, 94 | 82, 77 | 72, 98
+//   64 rows, 131072       -, -, 420 | 357, 314 | 277, 214;         256 rows, 32768 -, -, 363 | 300, 278 | 258, 199
 constexpr int64_t kCus = 256;
 template <typename TX, typename TY>
 hipError_t product_tiles_go(const GroupProductArgs &a, hipStream_t s) {
-    auto groups = [&](int64_t rows, int64_t outputs) { return (a.m + rows - 1) / rows * ((a.n + outputs - 1) / outputs); };
-    if (groups(16, 16) <= kCus) return product_tile_go<TX, TY, 1, 16, 8>(a, s);
-    if (groups(16, 32) <= kCus) return product_tile_go<TX, TY, 1, 32, 4>(a, s);
+    auto enough = [&](int64_t rows, int64_t outputs) {  // no more workgroups than CUs: a larger tile leaves some without
+        return (a.m + rows - 1) / rows * ((a.n + outputs - 1) / outputs) <= kCus;
+    };
+    if (enough(16, 16)) return product_tile_go<TX, TY, 1, 16, 8>(a, s);
+    if (enough(16, 32)) return product_tile_go<TX, TY, 1, 32, 4>(a, s);
     if constexpr (sizeof(TX) == 4) {
-        return product_tile_go<TX, TY, 1, 64, 2>(a, s);
+        if (enough(16, 64)) return product_tile_go<TX, TY, 1, 64, 2>(a, s);
+        if (a.m <= 16 || enough(16, 128)) return product_tile_go<TX, TY, 1, 128, 2>(a, s);
+        if (a.m <= 32 || enough(32, 128)) return product_tile_go<TX, TY, 2, 128, 2>(a, s);
+        if (enough(64, 128)) return product_tile_go<TX, TY, 4, 128, 2>(a, s);
+        return product_tile_go<TX, TY, 4, 256, 2>(a, s);
     } else {
-        if (a.m <= 16 || groups(16, 64) <= kCus) return product_tile_go<TX, TY, 1, 64, 4>(a, s);
-        if (a.m <= 32 || groups(32, 64) <= kCus || (groups(64, 64) - 1) % kCus < kCus * 4 / 5)
-            return product_tile_go<TX, TY, 2, 64, 4>(a, s);
-        return product_tile_go<TX, TY, 4, 64, 4>(a, s);
+        if (a.m <= 16 || enough(16, 64)) return product_tile_go<TX, TY, 1, 64, 4>(a, s);
+        if (enough(32, 64)) return product_tile_go<TX, TY, 2, 64, 4>(a, s);
+        if (a.m <= 32) return product_tile_go<TX, TY, 2, 128, 2>(a, s);
+        if (enough(64, 64)) return product_tile_go<TX, TY, 4, 64, 4>(a, s);
+        return product_tile_go<TX, TY, 4, 128, 2>(a, s);
     }
 }
 

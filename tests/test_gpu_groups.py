@@ -119,8 +119,8 @@ def _bound(x, w, kind):
 @pytest.mark.parametrize("m,n,k", [
     (1, 1, 1), (1, 17, 31), (2, 16, 33), (3, 100, 127), (1, 64, 128), (5, 65, 129), (16, 130, 500), (17, 33, 1000),
     (31, 200, 257), (32, 70, 1024), (33, 50, 1100), (64, 129, 640), (65, 40, 300), (130, 90, 200), (1, 300, 9000),
-    (7, 20, 16384), (1, 8200, 70), (4, 9001, 260), (20, 8300, 40), (16, 9000, 1100), (17, 2201, 1700), (33, 3001, 1300),
-    (48, 8190, 200), (64, 16380, 150), (64, 20001, 130), (9, 60, 5000), (40, 300, 4500), (16, 8192, 600), (3, 8300, 2100)])
+    (7, 20, 16384), (1, 8200, 70), (4, 9001, 260), (20, 8300, 40), (17, 2201, 1700), (33, 3001, 1300),
+    (9, 60, 5000), (40, 300, 4500), (16, 8192, 600)])
 @pytest.mark.parametrize("kinds", [("float32", "float32"), ("bfloat16", "bfloat16"), ("bfloat16", "float32"),
                                    ("float32", "bfloat16")])
 def test_product(torch, sd, m, n, k, kinds):  # noqa: F811
@@ -146,7 +146,8 @@ def test_product(torch, sd, m, n, k, kinds):  # noqa: F811
 def test_product_of_integers_is_exact(torch, sd):  # noqa: F811
     """Small integers sum exactly in any order, so every bit has to be right, at sizes that turn every loop."""
     rng = np.random.default_rng(8)
-    for m, n, k in ((1, 4096, 4096), (16, 500, 3000), (40, 300, 2048), (64, 8200, 512)):
+    for m, n, k in ((1, 4096, 4096), (16, 500, 3000), (40, 300, 2048), (64, 8200, 512), (48, 8190, 700), (64, 16380, 300),
+                    (17, 9000, 650), (20, 16500, 300), (48, 16000, 300), (64, 20001, 300), (64, 33000, 300), (130, 9000, 300), (16, 9000, 1100), (3, 8300, 2100)):
         wv = rng.choice([-4.0, -2.0, 0.0, 1.0, 2.0, 3.0, 6.0], (n, k))
         wv[:, ::32] = 6.0  # scale 1
         xv = rng.integers(-8, 9, (m, k)).astype(np.float64)
