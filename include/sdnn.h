@@ -497,8 +497,8 @@ sdnn_status sdnn_widen_groups(int64_t rows, int64_t k, const uint8_t *codes, con
  * Y = h(X W^T + bias) for dense X (m x k) and 4-bit W (n x k: row j holds output j's weights): Y (m x n).  X and Y have
  * types of their own.  bias: n fp32 values or NULL.  activate 0: h is the identity; 1: h(z) = min(max(z, 0), ymax),
  * ymax > 0 (+INFINITY for plain ReLU; NaN stays NaN).  Every product is exact (but for what a
- * float of X has below 2^-133), sums are fp32 and rounded once, and their order goes by m, n and k alone.  Made for few rows: the weights are read once for each 64 rows, and with up to that
- * many they are what a call costs.
+ * float of X has below 2^-133), sums are fp32 and rounded once, and their order goes by the types, m, n and k alone.  Made for
+ * few rows, up to a hundred or so.  Y overlaps nothing that is read.
  * Errors: NULL_POINTER, INVALID_VALUE, DEVICE.
  */
 sdnn_status sdnn_product_groups(int64_t m, int64_t n, int64_t k, int32_t x_type, const void *x, int64_t ldx,
@@ -554,8 +554,8 @@ sdnn_status sdnn_sample_workspace_size(int64_t rows, int64_t vocab, int64_t *byt
  * uniform: rows fp64 values in [0, 1), the caller's random numbers.  temperature, top_p, min_p (fp32) and top_k (int32): a
  * value for each row, or NULL for 1, 1, 0 and 0; a NaN temperature is 0, a NaN share none.
  * Outputs: ids (rows, int32), prob (rows, fp32: the token's share of what is kept) and kept (rows, int32: how many tokens
- * are).  All of it is decided by sums in 64 bits, in an order that goes by the row alone; tokens whose p is below 2e-28 are
- * counted but never drawn.
+ * are).  All of it is decided by sums in 64 bits, in an order that goes by the sizes and the values alone; tokens whose p is
+ * below 2e-28 are counted but never drawn.  The outputs overlap nothing that is read.
  * Errors: NULL_POINTER, INVALID_VALUE, WORKSPACE_TOO_SMALL, DEVICE.
  */
 sdnn_status sdnn_sample(int64_t rows, int64_t vocab, int32_t type, const void *logits, int64_t ldl,

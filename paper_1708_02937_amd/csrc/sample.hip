@@ -857,6 +857,9 @@ __device__ __forceinline__ uint32_t *groups_of(const SampleSpace &ws, int64_t ch
 
 // Longer rows in four launches, the first three by chunks: the first token and the groups' largest keys; the buckets, and the plan by
 // whichever workgroup of the row is through last, or the list by the groups; any other list, and the mass of what is kept whole; the end.
+// us, float, 131072 tokens, one row with all filters: 3.8, 8.4, 2.1, 7.9, chains of latencies; 128 rows with filters of their own: 15
+// (67 MB, 4.4 TB/s), 33, 11, 30.  The rows without top_k are what the last three wait for: an fp64 mass and two LDS atomics for each token,
+// then a workgroup a row.  Counting takes 17 us of VALU and as much of LDS if every row is counted.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_best_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk) {
     __shared__ uint64_t part[kWaves];
