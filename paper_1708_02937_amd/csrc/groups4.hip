@@ -403,7 +403,7 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
     return hipSuccess;
 }
 
-// The largest tiles that still give every CU a workgroup: a small one's waves share the columns, a large one's rows and weights serve
+// The largest tiles that still give every CU a workgroup, and no wider than the outputs: a small one's waves share the columns, a large one's rows and weights serve
 // more outputs.  us, 4096 columns, of 16 x 16, 16 x 32, 16 x 64 | 32 x 64, 64 x 64 | 32 x 128, 64 x 128 (rows x outputs), bfloat16:
 //   32 rows, 4096 outputs 9.7, 9.0, 11.7 | 13.5, 17.2 | 21, 24;    48 rows, 8192 22, 18, 20 | 14.2, 19 | 22, 29
 //   32 rows, 32768        -, 40, 36 | 24.2, 33 | 22.7, 26.5;       64 rows, 16384 54, 40, 36 | 24, 21.5 | 22.5, 30
@@ -421,16 +421,16 @@ hipError_t product_tiles_go(const GroupProductArgs &a, hipStream_t s) {
     if (enough(16, 16)) return product_tile_go<TX, TY, 1, 16, 8>(a, s);
     if (enough(16, 32)) return product_tile_go<TX, TY, 1, 32, 4>(a, s);
     if constexpr (sizeof(TX) == 4) {
-        if (enough(16, 64)) return product_tile_go<TX, TY, 1, 64, 2>(a, s);
+        if (a.n <= 64 || enough(16, 64)) return product_tile_go<TX, TY, 1, 64, 2>(a, s);
         if (a.m <= 16 || enough(16, 128)) return product_tile_go<TX, TY, 1, 128, 2>(a, s);
         if (a.m <= 32 || enough(32, 128)) return product_tile_go<TX, TY, 2, 128, 2>(a, s);
-        if (enough(64, 128)) return product_tile_go<TX, TY, 4, 128, 2>(a, s);
+        if (a.n <= 128 || enough(64, 128)) return product_tile_go<TX, TY, 4, 128, 2>(a, s);
         return product_tile_go<TX, TY, 4, 256, 2>(a, s);
     } else {
         if (a.m <= 16 || enough(16, 64)) return product_tile_go<TX, TY, 1, 64, 4>(a, s);
         if (enough(32, 64)) return product_tile_go<TX, TY, 2, 64, 4>(a, s);
         if (a.m <= 32) return product_tile_go<TX, TY, 2, 128, 2>(a, s);
-        if (enough(64, 64)) return product_tile_go<TX, TY, 4, 64, 4>(a, s);
+        if (a.n <= 64 || enough(64, 64)) return product_tile_go<TX, TY, 4, 64, 4>(a, s);
         return product_tile_go<TX, TY, 4, 128, 2>(a, s);
     }
 }

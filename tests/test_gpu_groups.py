@@ -147,7 +147,7 @@ def test_product_of_integers_is_exact(torch, sd):  # noqa: F811
     """Small integers sum exactly in any order, so every bit has to be right, at sizes that turn every loop."""
     rng = np.random.default_rng(8)
     for m, n, k in ((1, 4096, 4096), (16, 500, 3000), (40, 300, 2048), (64, 8200, 512), (48, 8190, 700), (64, 16380, 300),
-                    (17, 9000, 650), (20, 16500, 300), (48, 16000, 300), (64, 20001, 300), (64, 33000, 300), (130, 9000, 300), (16, 9000, 1100), (3, 8300, 2100)):
+                    (17, 9000, 650), (20, 16500, 300), (48, 16000, 300), (64, 20001, 300), (64, 33000, 300), (130, 9000, 300), (16, 9000, 1100), (3, 8300, 2100), (20000, 60, 200), (20000, 100, 200)):
         wv = rng.choice([-4.0, -2.0, 0.0, 1.0, 2.0, 3.0, 6.0], (n, k))
         wv[:, ::32] = 6.0  # scale 1
         xv = rng.integers(-8, 9, (m, k)).astype(np.float64)
