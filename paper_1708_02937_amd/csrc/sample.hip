@@ -102,6 +102,14 @@ __device__ __forceinline__ double exp_small(double d) {
     return fma(-d, e, 1.0);
 }
 
+// e^-(d / 16), 0 <= d <= 1, to 6e-15, a fifth of what rounding to 2^-44 takes from it.
+__device__ __forceinline__ double exp_sixteenth(double d) {
+    double e = -1.0 / (5040.0 * 268435456.0);
+    e = fma(d, e, 1.0 / (720.0 * 16777216.0)), e = fma(d, e, -1.0 / (120.0 * 1048576.0));
+    e = fma(d, e, 1.0 / (24.0 * 65536.0)), e = fma(d, e, -1.0 / (6.0 * 4096.0)), e = fma(d, e, 1.0 / 512.0);
+    return fma(d, fma(d, e, -1.0 / 16.0), 1.0);
+}
+
 // Past this tokens have no mass: the row's last bucket.
 __device__ __forceinline__ bool weighs(double x) { return x * kPerNat < (double)(kBuckets - 1); }
 
@@ -112,11 +120,13 @@ __device__ __forceinline__ double mass(double x, const double *table) {
     return table[b] * exp_small(x - (double)b / kPerNat);
 }
 
+// Its last place is 2^-shift.
+__device__ __forceinline__ double magic_of(int shift) { return __hiloint2double((1023 + 52 - shift) << 20, 0); }
+
 // The mass of x in the unit of its bucket, which starts at `from`: a whole number of 2^-shift.
 __device__ __forceinline__ uint64_t whole_mass(double x, double from, int shift) {
     if (!weighs(x)) return 0;
-    const double magic = __hiloint2double((1023 + 52 - shift) << 20, 0);  // its last place is 2^-shift
-    return (uint64_t)__double_as_longlong(exp_small(x - from) + magic) & ((1ull << 52) - 1);
+    return (uint64_t)__double_as_longlong(exp_small(x - from) + magic_of(shift)) & ((1ull << 52) - 1);
 }
 
 struct Keys {
@@ -256,34 +266,33 @@ __device__ __forceinline__ int elect(bool hit, bool some, Common &sh) {
     return best >> 32 ? kThreads - (int)(best >> 32) : (int)best - 1;
 }
 
-// f(keys, first index) for the tokens [begin, end), eight at a time, the next ones on their way meanwhile.  next: this thread's
-// first ones, by first_keys.
+// f(logits, first index) for the tokens [begin, end), eight at a time (NaN past the end), the next ones on their way meanwhile.
+// next: this thread's first ones, by first_logits.
 template <typename T>
-__device__ __forceinline__ void keys8(const T *row, int64_t c, int64_t end, uint32_t (&k)[8]) {
-    float l[8];
+__device__ __forceinline__ void logits8(const T *row, int64_t c, int64_t end, float (&l)[8]) {
     if (c < end) load8<T, false>(row, c, end, l);
 #pragma unroll
-    for (int i = 0; i < 8; i++) k[i] = c + i < end ? key_of(l[i]) : 0;
+    for (int i = 0; i < 8; i++) l[i] = c + i < end ? l[i] : NAN;
 }
 template <typename T>
-__device__ __forceinline__ void first_keys(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8]) {
-    keys8(row, begin + threadIdx.x * 8, end, next);
+__device__ __forceinline__ void first_logits(const T *row, int64_t begin, int64_t end, float (&next)[8]) {
+    logits8(row, begin + threadIdx.x * 8, end, next);
 }
 template <typename T, typename F>
-__device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8], F f) {
+__device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t end, float (&next)[8], F f) {
     const int64_t own = threadIdx.x * 8;
     for (int64_t c0 = begin; c0 < end; c0 += kTile) {
-        uint32_t k[8];
+        float l[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) k[i] = next[i];
-        if (c0 + kTile < end) keys8(row, c0 + kTile + own, end, next);
-        f(k, c0 + own);
+        for (int i = 0; i < 8; i++) l[i] = next[i];
+        if (c0 + kTile < end) logits8(row, c0 + kTile + own, end, next);
+        f(l, c0 + own);
     }
 }
 template <typename T, typename F>
 __device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t end, F f) {
-    uint32_t next[8];
-    first_keys(row, begin, end, next);
+    float next[8];
+    first_logits(row, begin, end, next);
     each_tile(row, begin, end, next, f);
 }
 
@@ -291,10 +300,12 @@ __device__ __forceinline__ void each_tile(const T *row, int64_t begin, int64_t e
 template <typename T>
 __device__ __forceinline__ uint64_t own_best(const T *row, int64_t begin, int64_t end) {  // of a thread's tokens
     uint64_t best = 0;
-    each_tile(row, begin, end, [&](const uint32_t (&k)[8], int64_t c) {
+    each_tile(row, begin, end, [&](const float (&l)[8], int64_t c) {
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (k[i]) best = max64(best, token_of(k[i], c + i));
+        for (int i = 0; i < 8; i++) {
+            const uint32_t k = key_of(l[i]);
+            if (k) best = max64(best, token_of(k, c + i));
+        }
     });
     return best;
 }
@@ -367,21 +378,25 @@ __device__ __forceinline__ void clear(Hist &h) {
 }
 
 template <typename T>
-__device__ __forceinline__ void count_buckets(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8], const Row &r,
+__device__ __forceinline__ void count_buckets(const T *row, int64_t begin, int64_t end, float (&next)[8], const Row &r,
                                               int shift, Hist &h) {
     clear(h);
-    const Level level = row_level();
-    each_tile(row, begin, end, next, [&](const uint32_t (&k)[8], int64_t) {
+    const double top = (double)r.top, scale = r.inverse * kPerNat;
+    const double magic = magic_of(shift);
+    each_tile(row, begin, end, next, [&](const float (&l)[8], int64_t) {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            if (!k[i]) continue;
-            const double x = r.x(k[i]);
-            const int b = level.bucket(x);
+            // as r.x and Level::bucket, which are exact in the factor of 16; infinity less itself is 0 here too
+            const double y = fmax((top - (double)l[i]) * scale, 0.0);
+            const int b = (int)fmin(y, (double)(kBuckets - 1));
+            const uint64_t m = (uint64_t)__double_as_longlong(exp_sixteenth(y - (double)b) + magic) & ((1ull << 52) - 1);
+            if (!(l[i] > -INFINITY)) continue;
             atomicAdd(&h.counts[b], 1u);
-            if (r.masses)
-                atomicAdd((unsigned long long *)&h.masses[b], (unsigned long long)whole_mass(x, level.from(b), shift));
+            if (r.masses) atomicAdd((unsigned long long *)&h.masses[b], (unsigned long long)m);
         }
     });
+    __syncthreads();
+    if (threadIdx.x == 0) h.masses[kBuckets - 1] = 0;
     __syncthreads();
 }
 
@@ -504,28 +519,28 @@ __device__ __forceinline__ void find_keys(const Row &r, Plan &p, Common &sh) {
 
 // put(place, token) for the tokens of the list's buckets in [begin, end), in order of the indices; returns how many there are.
 template <typename T, typename F>
-__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, uint32_t (&next)[8], const Keys &keys,
+__device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, float (&next)[8], const Keys &keys,
                                             uint64_t *part, F put) {
     uint32_t placed = 0;
-    each_tile(row, begin, end, next, [&](const uint32_t (&k)[8], int64_t c) {
+    each_tile(row, begin, end, next, [&](const float (&l)[8], int64_t c) {
         uint32_t mask = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (k[i] - keys.first < keys.end - keys.first) mask |= 1u << i;
+            if (key_of(l[i]) - keys.first < keys.end - keys.first) mask |= 1u << i;
         uint64_t all;
         const int mine = __popc(mask);
         uint32_t at = placed + (uint32_t)block_upto((uint64_t)mine, part, all) - mine;
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (mask >> i & 1) put(at++, token_of(k[i], c + i));
+            if (mask >> i & 1) put(at++, token_of(key_of(l[i]), c + i));
         placed += (uint32_t)all;
     });
     return placed;
 }
 template <typename T, typename F>
 __device__ __forceinline__ uint32_t collect(const T *row, int64_t begin, int64_t end, const Plan &p, uint64_t *part, F put) {
-    uint32_t next[8];
-    first_keys(row, begin, end, next);
+    float next[8];
+    first_logits(row, begin, end, next);
     return collect(row, begin, end, next, p.keys, part, put);
 }
 
@@ -649,10 +664,12 @@ __device__ __forceinline__ void each_listed(const T *row, int64_t vocab, const P
         for (int i = threadIdx.x; i < n; i += kThreads) f(sh.list[i]);
         return;
     }
-    each_tile(row, 0, vocab, [&](const uint32_t (&k)[8], int64_t c) {
+    each_tile(row, 0, vocab, [&](const float (&l)[8], int64_t c) {
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (k[i] - p.keys.first < p.keys.end - p.keys.first) f(token_of(k[i], c + i));
+        for (int i = 0; i < 8; i++) {
+            const uint32_t k = key_of(l[i]);
+            if (k - p.keys.first < p.keys.end - p.keys.first) f(token_of(k, c + i));
+        }
     });
 }
 
@@ -735,15 +752,16 @@ __device__ __forceinline__ bool keep(const SampleArgs &a, int64_t at, const T *r
 }
 
 // The masses of the kept ones of eight tokens, and their sum.
-__device__ __forceinline__ double kept_masses(const uint32_t (&k)[8], int64_t c, const Row &r, const Kept &kept,
+__device__ __forceinline__ double kept_masses(const float (&l)[8], int64_t c, const Row &r, const Kept &kept,
                                               const Shared &sh, double (&m)[8]) {
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         m[i] = 0.0;
-        if (!k[i]) continue;
-        const double x = r.x(k[i]);
-        if (kept.holds(token_of(k[i], c + i), x)) m[i] = mass(x, sh.table);
+        const uint32_t k = key_of(l[i]);
+        if (!k) continue;
+        const double x = r.x(k);
+        if (kept.holds(token_of(k, c + i), x)) m[i] = mass(x, sh.table);
         sum += m[i];
     }
     return sum;
@@ -758,14 +776,14 @@ __device__ __forceinline__ void draw_in(const SampleArgs &a, int64_t at, const T
         const int64_t each = (end - begin + kTile - 1) / kTile * 8;
         const int64_t from = min(begin + threadIdx.x * each, end), to = min(from + each, end);
         double m[8], sum = 0.0, all;
-        uint32_t next[8];
-        keys8(row, from, to, next);
+        float next[8];
+        logits8(row, from, to, next);
         for (int64_t c = from; c < to; c += 8) {
-            uint32_t k[8];
+            float l[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) k[i] = next[i];
-            if (c + 8 < to) keys8(row, c + 8, to, next);
-            sum += kept_masses(k, c, r, kept, sh, m);
+            for (int i = 0; i < 8; i++) l[i] = next[i];
+            if (c + 8 < to) logits8(row, c + 8, to, next);
+            sum += kept_masses(l, c, r, kept, sh, m);
         }
         const double upto = before + block_upto(sum, sh.part, all);
         const int owner = elect(sum > 0.0 && upto > kept.drawn, sum > 0.0, sh);
@@ -817,8 +835,8 @@ __global__ void __launch_bounds__(kThreads) sample_short_kernel(SampleArgs a, in
     if (bound) {
         p = plan_by_groups(r, bound);
     } else {
-        uint32_t next[8];
-        first_keys(row, 0, a.vocab, next);
+        float next[8];
+        first_logits(row, 0, a.vocab, next);
         count_buckets(row, 0, a.vocab, next, r, shift, sh.hist);
         p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
         find_keys(r, p, sh);
@@ -883,8 +901,8 @@ __global__ void __launch_bounds__(kThreads) sample_count_kernel(SampleArgs a, Sa
     const int64_t at = blockIdx.x / chunks, c = blockIdx.x % chunks;
     const int64_t begin = c * chunk, end = min(begin + chunk, a.vocab);
     const T *row = (const T *)a.logits + at * a.ld;
-    uint32_t next[8];
-    first_keys(row, begin, end, next);
+    float next[8];
+    first_logits(row, begin, end, next);
     uint64_t best = 0;
     for (int64_t w = threadIdx.x; w < chunks; w += kThreads) best = max64(best, ws.best[at * chunks + w]);
     best = block_max(best, sh.upart);
@@ -1045,7 +1063,7 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
             double sum = 0.0;
             double m[8];
             each_tile(row, c * chunk, end,
-                      [&](const uint32_t (&k)[8], int64_t t) { sum += kept_masses(k, t, r, kept, sh, m); });
+                      [&](const float (&l)[8], int64_t t) { sum += kept_masses(l, t, r, kept, sh, m); });
             sum = block_sum(sum, sh.part);
             if (threadIdx.x == 0) whole[c] = sum;
         }
