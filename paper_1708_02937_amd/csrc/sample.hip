@@ -876,8 +876,9 @@ __device__ __forceinline__ uint32_t *groups_of(const SampleSpace &ws, int64_t ch
 // Longer rows in four launches, the first three by chunks: the first token and the groups' largest keys; the buckets, and the plan by
 // whichever workgroup of the row is through last, or the list by the groups; any other list, and the mass of what is kept whole; the end.
 // us, float, 131072 tokens, one row with all filters: 3.8, 8.4, 2.1, 7.9, chains of latencies; 128 rows with filters of their own: 15
-// (67 MB, 4.4 TB/s), 33, 11, 30.  The rows without top_k are what the last three wait for: an fp64 mass and two LDS atomics for each token,
-// then a workgroup a row.  Counting takes 17 us of VALU and as much of LDS if every row is counted.
+// (67 MB, 4.4 TB/s), 29, 11, 30.  The rows without top_k are what the last three wait for: two LDS atomics for each token, then a
+// workgroup a row.  A CU that counts four chunks at once takes 1.4 us for 4096 tokens, as long as their atomics do; four copies of the buckets,
+// which spare equal addresses, change nothing, and chunks' counts summed by the planning workgroup in place of atomics in memory cost 4.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_best_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk) {
     __shared__ uint64_t part[kWaves];
@@ -1100,11 +1101,11 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
 }
 
 // Rows that one workgroup each takes in one launch.  us (this | the four launches), temperature alone, top-p, all filters, float:
-//   1 row:      8000 tokens 17, 25, 14 | 22, 34, 22;   16000 26, 38, 17 | 23, 35, 23;   32000 42, 61, 24 | 23, 39, 20
-//   128 rows:   32000 43, 61, 24 | 43, 59, 30;   64000 79, 107, 42 | 55, 80, 38;   131072 152, 202, 77 | 77, 105, 50
-//   256 rows:   32000 47, 66, 28 | 56, 78, 44;   64000 83, 113, 45 | 74, 103, 52
-//   512 rows:   64000 119, 154, 55 | 123, 164, 74;   131072 226, 287, 97 | 211, 279, 118
-//   1000 rows:  131072 463, 579, 206 | 513, 678, 249
+//   1 row:      8000 tokens 16, 24, 13 | 22, 33, 22;   16000 24, 35, 17 | 22, 34, 22;   32000 37, 56, 23 | 23, 37, 20
+//   128 rows:   32000 39, 57, 23 | 41, 60, 30;   64000 70, 99, 41 | 52, 75, 36;   131072 136, 185, 73 | 71, 100, 50
+//   256 rows:   32000 43, 62, 27 | 52, 75, 43;   64000 74, 103, 43 | 71, 100, 51
+//   512 rows:   64000 108, 143, 56 | 116, 157, 73;   131072 203, 266, 98 | 191, 261, 117
+//   1000 rows:  131072 416, 534, 204 | 502, 647, 249
 constexpr int64_t kShort = 4 * kTile, kOfARow = 256;
 bool is_short(int64_t rows, int64_t vocab) { return vocab <= kShort || vocab / kOfARow <= rows; }
 
