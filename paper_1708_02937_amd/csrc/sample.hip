@@ -876,9 +876,10 @@ __device__ __forceinline__ uint32_t *groups_of(const SampleSpace &ws, int64_t ch
 // Longer rows in four launches, the first three by chunks: the first token and the groups' largest keys; the buckets, and the plan by
 // whichever workgroup of the row is through last, or the list by the groups; any other list, and the mass of what is kept whole; the end.
 // us, float, 131072 tokens, one row with all filters: 3.8, 8.4, 2.1, 7.9, chains of latencies; 128 rows with filters of their own: 15
-// (67 MB, 4.4 TB/s), 29, 11, 30.  The rows without top_k are what the last three wait for: two LDS atomics for each token, then a
-// workgroup a row.  A CU that counts four chunks at once takes 1.4 us for 4096 tokens, as long as their atomics do; four copies of the buckets,
-// which spare equal addresses, change nothing, and chunks' counts summed by the planning workgroup in place of atomics in memory cost 4.
+// (67 MB, 4.4 TB/s), 29, 11, 30.  The rows without top_k are what the last three wait for: a mass and two LDS atomics for each token, then a
+// workgroup a row.  A CU that counts four chunks at once takes 1.4 us for 4096 tokens and fills nothing (VALU issue 37%, LDS 10% over the
+// call): half the instructions took a tenth off, four copies of the buckets, which spare equal addresses, nothing, and chunks' counts
+// summed by the planning workgroup in place of atomics in memory cost 4.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_best_kernel(SampleArgs a, SampleSpace ws, int64_t chunks, int64_t chunk) {
     __shared__ uint64_t part[kWaves];
