@@ -313,7 +313,8 @@ __device__ __forceinline__ int place_of(const LayerArgs &a, const Chosen &c, int
 // One launch for each product.  (Both in one, with tiles of outputs that load their weights and wait for p, were twice as slow:
 // a ticket for each tile is an atomic that all chiplets share, and a row of them takes 95 ns each.)  8 of 64 experts of 4096 x 1024
 // for one token: first product 18.9 us, of which the choice takes 4 and the weights 11 (67 MB, 5.9 TB/s), second 12.1 (34 MB);
-// 16 tokens, 57 experts: 96 us (5.0 TB/s) and 61 (3.9; its rows of p, rounded anew by every workgroup, keep VALU half busy).
+// 16 tokens, 57 experts: 96 us (5.0 TB/s) and 61 (3.9; its rows of p, rounded anew by every workgroup, keep VALU half busy; in a
+// launch of their own, the same bits, 151 for the call against 157, but 3 us more for smaller or fewer experts).
 
 // p = silu(gate) * up in fp32 of 16 inner values of an expert for all tokens; the waves share the blocks of the width.  A
 // wave's blocks are taken four at a time, and the next four, of the next tile where these are the last, are on their way while
