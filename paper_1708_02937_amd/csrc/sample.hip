@@ -13,8 +13,8 @@
 // A token is a number: its logit's place in the order of floats above the complement of its index, so that a larger one
 // comes first and no two are equal.
 //
-// A bucket's masses are in units of exp(-b / 16) 2^-shift: e^-d for 0 <= d < 1/16 is a polynomial of degree 8 (the next term is
-// 4e-17), and the sum of a bucket is as exact as its values.  The last bucket is x >= 63.9: its tokens count, but their mass,
+// A bucket's masses are in units of exp(-b / 16) 2^-shift: e^-d for 0 <= d < 1/16 is a polynomial, of degree 7 where it is rounded to
+// such a unit and 8 elsewhere (the next terms are 6e-15 and 4e-17), and the sum of a bucket is as exact as its values.  The last bucket is x >= 63.9: its tokens count, but their mass,
 // below 2e-28 of the first token's each, is 0.
 #include <algorithm>
 
