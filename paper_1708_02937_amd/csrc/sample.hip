@@ -209,6 +209,7 @@ struct Common {
             uint64_t token[kRanked];
             double mass[kRanked];
         } sorted;
+        uint16_t upto[kList];  // of the list's tokens up to there: how many are kept and have a mass
     };
     double part[kWaves];
     uint64_t upart[kWaves];
@@ -1040,9 +1041,10 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
     Kept kept;
     if (keep(a, at, row, r, p, n, fits, shift, sh, kept)) return;
     if (n > 0 && fits) {
-        // the list's tokens give way to the mass of what is kept of them up to there
+        // the list's tokens give way to the mass of what is kept of them up to there, and in `upto` to how many have one
         constexpr int kOwn = kList / kThreads;
         double m[kOwn], sum = 0.0, all;
+        int64_t weighty = 0, total;
 #pragma unroll
         for (int j = 0; j < kOwn; j++) {
             const int i = threadIdx.x * kOwn + j;
@@ -1050,13 +1052,15 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
             if (i >= n) continue;
             const double x = r.x((uint32_t)(sh.list[i] >> 32));
             if (kept.holds(sh.list[i], x)) m[j] = mass(x, sh.table);
-            sum += m[j];
+            sum += m[j], weighty += m[j] > 0.0;
         }
         double q = block_upto(sum, sh.part, all) - sum;  // its barriers come between reading and writing
+        int64_t n0 = block_upto(weighty, sh.ipart, total) - weighty;
 #pragma unroll
         for (int j = 0; j < kOwn; j++) {
-            q += m[j];
+            q += m[j], n0 += m[j] > 0.0;
             sh.list[threadIdx.x * kOwn + j] = (uint64_t)__double_as_longlong(q);
+            sh.upto[threadIdx.x * kOwn + j] = (uint16_t)n0;
         }
         __syncthreads();
     } else if (n > 0) {
@@ -1078,8 +1082,9 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
         const int64_t c = c0 + threadIdx.x;
         double m = c < chunks ? whole[c] : 0.0;
         if (n > 0 && fits && c < chunks) {
+            // a difference of sums that has a rounding of its own: it is not 0 where nothing is kept
             const uint32_t from = sh.offset[c], to = sh.offset[c + 1];
-            if (to > from)
+            if (to > from && sh.upto[to - 1] > (from ? sh.upto[from - 1] : 0))
                 m += __longlong_as_double((long long)sh.list[to - 1]) -
                      (from ? __longlong_as_double((long long)sh.list[from - 1]) : 0.0);
         }

@@ -215,6 +215,32 @@ def test_every_uniform_number(torch, sd, V):  # noqa: F811
     assert bool((got.ids[1:] >= got.ids[:-1]).all()) and len(set(got.ids.tolist())) > 10
 
 
+@pytest.mark.parametrize("T,V,k", [(64, 40000, 600), (64, 40000, 1000), (64, 131072, 1024), (64, 131072, 5000), (3, 131072, 1000),
+                                   (40, 40000, 5000)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_the_last_kept_token_before_dropped_ones(torch, sd, T, V, k, dtype):  # noqa: F811
+    """Numbers next to 1 take the last kept token, also where the row's last quarter holds many tokens just below the cut and
+    none that is kept: sums over those add nothing, whatever their rounding.  The least kept mass is above e^-12 of the row's
+    first and more than 1e-9 of all (5000 at the most); u leaves 2^-51 of all at the most, and sums are off by some 2^-50: the
+    last kept token is the first whose sum exceeds u."""
+    rng = np.random.default_rng(T + V + k)
+    l = 2 * rng.standard_normal((T, V))
+    at = 3 * V // 4
+    cut = np.sort(l[:, :at], axis=1)[:, -k]
+    l[:, at:] = -40.0
+    for t in range(T):
+        some = at + rng.choice(V - at, 400, replace=False)
+        l[t, some] = cut[t] - 0.02 * (1 + rng.random(400))
+    logits = _cuda(torch, l, getattr(torch, dtype))
+    l = logits.float().cpu().numpy().astype(np.float64)
+    _say("sample last kept", T, V, k, dtype)
+    for u in (1 - 2.0 ** -53, 1 - 2.0 ** -52, 1 - 2.0 ** -51):
+        got = _call(torch, sd, logits, [u] * T, top_k=[k] * T)
+        order = [np.lexsort((np.arange(V), -l[t]))[:k] for t in range(T)]
+        assert bool((got.kept == k).all()) and bool((got.prob > 0).all())
+        assert got.ids.tolist() == [int(o.max()) for o in order]
+
+
 def test_strides_workspace_streams_and_graphs(torch, sd):  # noqa: F811
     """Rows at odd addresses inside a wider tensor, a workspace of the size for 9 rows full of ones for fewer, a side stream,
     and captured calls of different sizes that share a workspace, replayed with eager work between."""
