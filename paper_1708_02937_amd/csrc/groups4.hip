@@ -213,14 +213,48 @@ __device__ __forceinline__ void multiply(const v4i (&q)[NW], const uint32_t (&co
     }
 }
 
-template <typename TY>
-__device__ __forceinline__ void put_outputs(const GroupProductArgs &a, int64_t m, int64_t n0, v4f z) {
-    TY *y = (TY *)a.y + m * a.ldy;
+// One output from its sum; true where it is a float row's and NaN.
+template <typename TX, typename TY>
+__device__ __forceinline__ bool put_output(const GroupProductArgs &a, int64_t m, int64_t n, float z) {
+    const bool none = kParts<TX> > 1 && z != z;
+    if (a.bias) z += a.bias[n];
+    if (a.activate) z = relu_clamp(z, a.ymax);
+    ((TY *)a.y)[m * a.ldy + n] = (TY)z;
+    return none;
+}
+template <typename TX, typename TY>
+__device__ __forceinline__ bool put_outputs(const GroupProductArgs &a, int64_t m, int64_t n0, v4f z) {
+    bool none = false;
     for (int i = 0; i < 4; i++) {
         if (n0 + i >= a.n) break;
-        if (a.bias) z[i] += a.bias[n0 + i];
-        if (a.activate) z[i] = relu_clamp(z[i], a.ymax);
-        y[n0 + i] = (TY)z[i];
+        none |= put_output<TX, TY>(a, m, n0 + i, z[i]);
+    }
+    return none;
+}
+
+// Again the outputs that are NaN and whose weights have scales that take codes (4 is the first) past the float range: a part of
+// 0 of a float times an infinite weight is NaN whatever the float is, so the products that are not finite decide, of whole
+// floats.  After the loops, which need every register: beside the outputs it cost a row of 131072 of them 5%, here nothing.
+constexpr int kPastRange = 253;
+template <typename TX, typename TY>
+__device__ __forceinline__ void put_infinite(const GroupProductArgs &a, int64_t m, int64_t n0) {
+    const TX *x = (const TX *)a.x + m * a.ldx;
+    const TY *y = (const TY *)a.y + m * a.ldy;
+#pragma unroll 1
+    for (int64_t n = n0; n < n0 + 4 && n < a.n; n++) {
+        if (!((float)y[n] != (float)y[n])) continue;
+        const uint8_t *codes = a.w + n * group_pitch(a.k), *scales = a.w_scale + n * group_scale_pitch(a.k);
+        int most = 0;
+        for (int64_t c = 0; c < a.k; c += kGroup) most = max(most, (int)scales[c / kGroup]);
+        if (most < kPastRange || most == 255) continue;
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int64_t c = 0; c < a.k; c++) {
+            const v8bf w8 = widen4(codes[c / 2] >> (c % 2 * 4) & 15, group_scale(scales[c / kGroup]));
+            const float w = (float)w8[0], v = (float)x[c];
+            if (!(fabsf(w) < INFINITY && fabsf(v) < INFINITY)) sum += w * v;
+        }
+        if (sum != 0.0f) put_output<TX, TY>(a, m, n, sum);
     }
 }
 
@@ -259,6 +293,7 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProduc
     __syncthreads();
     const uint8_t *const own = rows + (low < a.m ? low : 0) * pitch + high * 64;
     v4f acc[1][NW] = {};
+    bool none = false;
     for (int turn = 0, odd = 0; tile < tiles;) {
         const Weights4<STEPS, NW> w = next;
         const bool last = turn + 1 == turns;
@@ -278,7 +313,7 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProduc
             if (wave < NW && low < a.m) {  // 16 outputs each
                 v4f z = sums[odd][0][wave][lane];
                 for (int i = 1; i < kWaves; i++) z += sums[odd][i][wave][lane];
-                put_outputs<TY>(a, low, tile * (16 * NW) + 16 * wave + high * 4, z);
+                none |= put_outputs<TX, TY>(a, low, tile * (16 * NW) + 16 * wave + high * 4, z);
             }
             if (TURNS == 1)
                 __syncthreads();
@@ -288,6 +323,10 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_kernel(GroupProduc
         tile = then;
         turn = then_turn;
     }
+    if constexpr (kParts<TX> > 1)
+        if (none)
+            for (tile = blockIdx.x; tile < tiles; tile += gridDim.x)
+                put_infinite<TX, TY>(a, low, tile * (16 * NW) + 16 * wave + high * 4);
 }
 
 // ---- any rows: OUTPUTS outputs of 16 MT rows.  The rows come through LDS a stage of kSteps steps at a time, since every wave needs
@@ -348,14 +387,21 @@ __global__ void __launch_bounds__(64 * kWaves) product_groups_tile_kernel(GroupP
 #pragma unroll
         for (int v = 0; v < NW; v++) part[wave][t][v][lane] = acc[t][v];
     __syncthreads();
+    // output u's of this lane: its row and its first column
+    const auto row_of = [&](int u) { return m0 + 16 * (u / (OUTPUTS / 16)) + low; };
+    const auto col_of = [&](int u) { return (int64_t)blockIdx.x * OUTPUTS + u % (OUTPUTS / 16) * 16 + high * 4; };
+    bool none = false;
     for (int u = wave; u < MT * (OUTPUTS / 16); u += kWaves) {
         const int t = u / (OUTPUTS / 16), of = u % (OUTPUTS / 16) / NW, v = u % NW;  // the waves that share these outputs
-        const int64_t m = m0 + 16 * t + low;
-        if (m >= a.m) continue;
+        if (row_of(u) >= a.m) continue;
         v4f z = part[of * kSteps][t][v][lane];
         for (int i = 1; i < kSteps; i++) z += part[of * kSteps + i][t][v][lane];
-        put_outputs<TY>(a, m, (int64_t)blockIdx.x * OUTPUTS + of * (16 * NW) + 16 * v + high * 4, z);
+        none |= put_outputs<TX, TY>(a, row_of(u), col_of(u), z);
     }
+    if constexpr (kParts<TX> > 1)
+        if (none)
+            for (int u = wave; u < MT * (OUTPUTS / 16); u += kWaves)
+                if (row_of(u) < a.m) put_infinite<TX, TY>(a, row_of(u), col_of(u));
 }
 
 template <typename TX>

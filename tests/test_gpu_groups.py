@@ -208,6 +208,48 @@ def test_product_rows_and_weights_that_are_not_finite(torch, sd):  # noqa: F811
             assert torch.equal(got[:, keep], clean[:, keep])
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 70, 300), (3, 70, 300), (20, 70, 300), (50, 70, 300), (5, 60, 2300), (64, 9000, 260), (4, 70, 9000)])
+def test_product_of_infinite_weights(torch, sd, m, n, k):  # noqa: F811
+    """A weight past the float range is infinite: an output with one is that infinity with the sign of x, NaN where x is 0,
+    whatever bits x has and of whatever type it is; one with a finite weight of the same scale is its sum as ever."""
+    rng = np.random.default_rng(m + n + k)
+    wv = rng.choice([-1.0, 1.0, 2.0], (n, k))
+    wv[:, 32:64] = 0.0  # one weight in the second group, each output its own
+    code = np.resize([2, 3, 4, 6, -4, -6, 1.5, 1], n)  # the last two are finite
+    wv[np.arange(n), 32 + np.arange(n) % 32] = code
+    w, s = sd.quantize_groups(_cuda(torch, wv, torch.float32))
+    assert np.array_equal(sd.widen_groups(w, s, k, dtype=torch.float32).cpu().numpy(), wv)
+    # codes as for a scale of 1: 1 and 1.5 times 2^127 are floats, 2 times it is not
+    index = np.zeros((n, 32), np.uint8)
+    index[np.arange(n), np.arange(n) % 32] = gen.encode4(code)
+    w.view(torch.uint8)[:, 16:32] = _cuda(torch, gen.pack4(index))
+    s.view(torch.uint8)[:, 1] = 254
+    inf = np.abs(code) >= 2
+    x = rng.choice([1.0, 3.0, -0.5, 0.0, 2.0 ** -120, -1.0, 257.0], (m, k))
+    x[:, 32:64][np.abs(x[:, 32:64]) > 1] = 1.0  # finite weights times these stay below the largest float
+    x[0] = np.where(rng.random(k) < 0.5, 1.0, -1.0)
+    some = rng.uniform(-1, 1, (m, k))
+    for dt, rows in ((torch.float32, x), (torch.bfloat16, x), (torch.float32, some)):
+        xt = _cuda(torch, rows, dt)
+        xv = xt.double().cpu().numpy()
+        _say("product_groups infinite weights", m, n, k, dt)
+        got = sd.product_groups(xt, w, s, dtype=torch.float32).double().cpu().numpy()
+        own = xv[:, 32 + np.arange(n) % 32]
+        with np.errstate(invalid="ignore"):
+            want = own * np.where(inf, np.copysign(np.inf, code), 1.0)
+        assert np.array_equal(got[:, inf], want[:, inf], equal_nan=True)
+        # the rest of a row (at most a few thousand) is below a rounding of 2^127 times 2^-120 and more, or is all there is
+        values = wv.copy()
+        values[:, 32:64] = 0.0
+        values[np.arange(n), 32 + np.arange(n) % 32] = np.where(inf, 0.0, code * 2.0 ** 127)
+        exact, room = xv @ values.T, _bound(xv, values, "float32")
+        assert np.all(np.abs(got - exact)[:, ~inf] <= (room + 2.0 ** -24 * np.abs(exact))[:, ~inf])
+    # what the rounding itself makes of the largest floats
+    top = torch.full((2, 40), torch.finfo(torch.float32).max, device="cuda")
+    got = sd.product_groups(torch.ones(m, 40, device="cuda"), *sd.quantize_groups(top))
+    assert bool((got == math.inf).all())
+
+
 def test_product_strides_outputs_and_streams(torch, sd):  # noqa: F811
     """Rows at any element address, an output inside a wider tensor whose rest stays, a side stream, and a graph that is
     replayed between eager calls."""
