@@ -394,6 +394,12 @@ struct OutTile {
     } rows[kLayerWaves];
 };
 
+// A double rounded once; bfloat16 by way of a float that no second rounding misses.
+template <typename T>
+__device__ __forceinline__ T rounded(double v) {
+    return sizeof(T) == 4 ? (T)(float)v : (T)round_odd(v);
+}
+
 template <typename T, int ROWS>
 __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &ws, const Chosen &c, int64_t n0,
                                          OutTile<ROWS> &tile) {
@@ -432,13 +438,13 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
             x.v[r][0] = *(const v4f *)row, x.v[r][1] = *(const v4f *)(row + 4);
         }
     };
-    // the first wave's rows of s, for the end
-    float s[4] = {};
+    // the first wave's rows, for the end
+    T end_x[4] = {}, end_r[4] = {};
     if (wave == 0 && low < a.tokens)
         for (int i = 0; i < 4; i++) {
             const int64_t col = min(n0 + high * 4 + i, a.width - 1);
-            s[i] = load_f32((const T *)a.x + low * a.ldx + col);
-            if (a.residual) s[i] += load_f32((const T *)a.residual + low * a.ldr + col);
+            end_x[i] = ((const T *)a.x)[low * a.ldx + col];
+            if (a.residual) end_r[i] = ((const T *)a.residual)[low * a.ldr + col];
         }
     Weights next;
     Rows next_p;
@@ -510,7 +516,7 @@ __device__ __forceinline__ void out_tile(const LayerArgs &a, const LayerSpace &w
     for (int i = 0; i < 4; i++) {
         const int64_t col = n0 + high * 4 + i;
         if (col >= a.width) break;
-        ((T *)a.out)[low * a.ldo + col] = (T)(s[i] + sum[i]);
+        ((T *)a.out)[low * a.ldo + col] = rounded<T>((double)end_x[i] + (double)end_r[i] + (double)sum[i]);
     }
 }
 

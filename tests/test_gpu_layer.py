@@ -127,6 +127,38 @@ def test_layer_is_the_separate_calls(torch, sd, T, dtype):  # noqa: F811
     assert float((got.out.double() - want).norm() / want.norm()) <= (2e-5 if dtype == "float32" else 2.0 ** -8)
 
 
+def _rounded(v, bits):
+    """float64 values rounded to `bits` bits, ties to even (normal values)."""
+    m, e = np.frexp(v)
+    return np.ldexp(np.rint(np.ldexp(m, bits)), e - bits)
+
+
+@pytest.mark.parametrize("T,H,F,E,k", [(1, 1000, 100, 8, 2), (6, 700, 200, 8, 3), (16, 513, 130, 5, 1)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_the_result_is_rounded_once(torch, sd, T, H, F, E, k, dtype):  # noqa: F811
+    """Experts whose results are 2^-22 of the rows: what comes out is x + residual + theirs, in 64 bits, rounded once to its
+    type.  (Theirs has the error of float sums, which decides only next to a middle: the rounding of both ends is allowed.)"""
+    args, (v1, v2) = _case(torch, sd, T, H, F, E, dtype, "float32", True, seed=11)
+    codes = args["w_out_scale"].view(torch.uint8)
+    args["w_out_scale"] = torch.where(codes > 60, codes - 22, codes).view(torch.float8_e8m0fnu)  # but of empty blocks
+    values = v1, v2 * 2.0 ** -22
+    _say("layer rounded once", T, H, F, E, k, dtype)
+    got = _run(sd, args, k)
+    out, _, ids, weight = _want(args, values, k, bias=args["bias"].cpu().numpy())
+    assert np.array_equal(got.ids.cpu().numpy(), ids)
+    both = args["x"].double().cpu().numpy() + args["residual"].double().cpu().numpy()
+    _, z = ref.norm(args["x"].double().cpu().numpy(), args["gamma"].cpu().numpy(), EPS, args["residual"].double().cpu().numpy())
+    rows = ref.values(*ref.quantize(z), H)
+    _, tol = _experts_ref(rows, *values, ids, weight, True)
+    size, _ = _experts_ref(*(np.abs(v) for v in (rows, *values)), ids, np.abs(weight), False)
+    tol = tol + (-(-F // 128) * k + 20) * 2.0 ** -24 * np.abs(size) + 2.0 ** -50 * np.abs(both)
+    bits = 24 if dtype == "float32" else 8
+    low, high = _rounded(out - tol, bits), _rounded(out + tol, bits)
+    assert np.mean(low == high) > 0.5  # a code of p that may move takes a token's whole row of floats with it
+    res = got.out.double().cpu().numpy()
+    assert np.all((low <= res) & (res <= high)), int(np.sum((res < low) | (res > high)))
+
+
 def test_rows_that_are_not_finite(torch, sd):  # noqa: F811
     """A row with an infinity or NaN has NaN logits: no expert takes it, its result is its sum, and the others do not
     notice; a router row of NaN is an expert that nobody takes, one with an infinity the expert of half the tokens."""
