@@ -523,7 +523,7 @@ sdnn_status sdnn_experts_layer_workspace_size(int64_t tokens, int64_t width, int
  * x's type, which may be x or residual itself) is rounded once.  Sums have one order for given sizes and choices.  live
  * (a byte for each token, or NULL): a token whose byte is 0 takes part in no expert: ids -1, weights 0, out_t = s_t; so
  * does one whose logits are all -inf or NaN.  ids and weight (tokens x chosen) are written as sdnn_route writes them.
- * tokens <= 16, experts <= 1024, chosen <= 64, groups <= 64, width below 2^27.
+ * tokens <= 16, experts <= 1024, chosen <= 64, groups <= 64, width <= 2^27 - 16.
  * Errors: NULL_POINTER, INVALID_VALUE, UNSUPPORTED, WORKSPACE_TOO_SMALL, DEVICE.
  */
 sdnn_status sdnn_experts_layer(int64_t tokens, int64_t width, int64_t inner, int32_t experts, int32_t chosen,

@@ -275,7 +275,7 @@ static sdnn_status check_layer(int64_t tokens, int64_t width, int64_t inner, int
     if (tokens > sdnn::kLayerMaxTokens)
         return fail(SDNN_ERR_UNSUPPORTED, "more than 16 tokens: sdnn_norm_quantize, sdnn_route and sdnn_experts_forward "
                                           "take any number");
-    if (width >= sdnn::kLayerMaxWidth) return fail(SDNN_ERR_UNSUPPORTED, "rows of 2^27 columns or more");
+    if (width > sdnn::kLayerMaxWidth) return fail(SDNN_ERR_UNSUPPORTED, "rows of more than 2^27 - 16 columns");
     return SDNN_OK;
 }
 

@@ -15,7 +15,7 @@ constexpr int kRouteMaxChosen = 64;     // one chosen expert per lane
 constexpr int kRouteMaxGroups = 64;
 
 constexpr int kLayerMaxTokens = 16;     // one row of the matrix instructions' tiles each
-constexpr int64_t kLayerMaxWidth = (int64_t)1 << 27;  // a launch holds fewer than 2^32 threads, 512 to 16 columns
+constexpr int64_t kLayerMaxWidth = ((int64_t)1 << 27) - 16;  // a launch holds fewer than 2^32 threads, 512 to 16 columns
 constexpr int kGroup = 32;              // columns of a 4-bit matrix that share a scale
 
 constexpr int64_t blocks_of(int64_t k) { return (k + kBlock - 1) / kBlock; }

@@ -93,6 +93,15 @@ def test_layer_workspace_sizes(sd):  # noqa: F811
     assert sd.lib.sdnn_experts_layer_workspace_size(1, 8, 8, 4, 2, None) == 1
 
 
+def test_the_widest_layer(sd):  # noqa: F811
+    """A launch holds fewer than 2^32 threads: 512 for each 16 columns are one too many from 2^27 - 15 columns on."""
+    wide = (1 << 27) - 16
+    assert wide // 16 * 512 < 1 << 32 <= (wide + 1 + 15) // 16 * 512
+    assert sd.sdnn_experts_layer_workspace_size(1, wide, 8, 4, 2) > 0
+    for width in (wide + 1, wide + 15, wide + 16):
+        assert _status(sd, sd.sdnn_experts_layer_workspace_size, 1, width, 8, 4, 2) == 9
+
+
 def test_sample_refusals(sd):  # noqa: F811
     good = dict(rows=3, vocab=40000, type=1, logits=FAKE, ldl=40000, uniform=FAKE, temperature=FAKE, top_k=FAKE,
                 top_p=FAKE, min_p=FAKE, ids=FAKE, prob=FAKE, kept=FAKE, ws=FAKE, ws_bytes=1 << 30)
