@@ -957,7 +957,7 @@ __global__ void __launch_bounds__(kThreads) sample_count_kernel(SampleArgs a, Sa
     if (!sh.found[0]) return;
     for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
         sh.hist.counts[b] = get_shared(counts + b);
-        if (r.masses) sh.hist.masses[b] = get_shared((const uint64_t *)masses + b);
+        if (r.masses) sh.hist.masses[b] = get_shared(masses + b);
     }
     __syncthreads();
     Plan p = plan_of(r, row_level(), r.masses, nullptr, shift, sh);
