@@ -100,7 +100,7 @@ def main(argv=None):
     first = sd.sample(model.logits(rows[-1:]), torch.rand(1, generator=g, device="cuda", dtype=torch.float64),
                       temperature=torch.zeros(1, device="cuda"))
     places.tokens[:1] = first.ids
-    places.live[a.places // 2:] = False  # half of the places wait for a sequence
+    places.live[(a.places + 1) // 2:] = False  # half of the places wait for a sequence
     places.capture()
     taken = torch.stack([places.next()[0].clone() for _ in range(a.tokens)])
     t = seconds(places.next, 50)

@@ -84,6 +84,16 @@ def test_example(torch, sd, capsys):  # noqa: F811
     assert "tokens/s" in capsys.readouterr().out
 
 
+def test_example_with_one_place(torch, sd, capsys):  # noqa: F811
+    """The only place generates."""
+    import examples.generate as example
+
+    taken = example.main(["--width", "256", "--inner", "128", "--experts", "8", "--chosen", "2", "--vocab", "3001", "--places",
+                          "1", "--tokens", "6"])
+    assert taken.shape == (6, 1) and bool((taken >= 0).all())
+    assert " 0 tokens/s" not in capsys.readouterr().out
+
+
 def test_tensors_of_two_devices_are_refused(torch, sd):  # noqa: F811
     """Tensors of two devices in one call are refused (here: a host tensor among those of the GPU)."""
     model, g = _model(torch, 6)
