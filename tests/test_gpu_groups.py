@@ -76,6 +76,28 @@ def test_quantize_ties_and_extremes(torch, sd):  # noqa: F811
         assert np.array_equal(got, exact.astype(np.float32), equal_nan=True)
 
 
+def test_quantize_below_the_normal_floats(torch, sd):  # noqa: F811
+    """Groups at the least scale whose values are subnormal floats: codes to nearest even in steps of 2^-127, the middles and
+    the floats beside them too; and matrices of random subnormal values."""
+    middles = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]) * 2.0 ** -126
+    top = np.float32(6 * 2.0 ** -126)
+    middles = middles.astype(np.float32)
+    base = np.concatenate([(gen.MAGNITUDES * 2.0 ** -126).astype(np.float32), middles, np.nextafter(middles, top),
+                           np.nextafter(middles, np.float32(0))])
+    x = np.zeros((4, 64), np.float32)
+    x[0, :base.size], x[0, 32:32 + base.size] = base, -base
+    x[1, :base.size], x[1, 5] = base, np.nextafter(top, np.float32(1))  # the next scale
+    rng = np.random.default_rng(2)
+    x[2] = rng.standard_normal(64) * 2.0 ** -126
+    x[3] = rng.standard_normal(64) * 2.0 ** -130
+    _say("quantize_groups subnormal")
+    for dt in (torch.float32, torch.bfloat16):
+        t = _cuda(torch, x).to(dt)
+        codes, scales = sd.quantize_groups(t)
+        want, want_scales = gen.quantize4(t.double().cpu().numpy())
+        assert np.array_equal(_bytes(torch, scales), want_scales) and np.array_equal(_bytes(torch, codes), want)
+
+
 def test_widen_every_code_and_scale(torch, sd):  # noqa: F811
     """All 256 scales over all 16 codes: subnormal values, ones past the float range, and NaN."""
     scales = np.arange(256, dtype=np.uint8).reshape(64, 4)

@@ -127,6 +127,27 @@ def test_layer_is_the_separate_calls(torch, sd, T, dtype):  # noqa: F811
     assert float((got.out.double() - want).norm() / want.norm()) <= (2e-5 if dtype == "float32" else 2.0 ** -8)
 
 
+@pytest.mark.parametrize("T,H,F,E,k", [(5, 4200, 600, 16, 4), (16, 9000, 300, 20, 5), (1, 4097, 5000, 4, 2)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_wide_rows_of_many_experts(torch, sd, T, H, F, E, k, dtype):  # noqa: F811
+    """Several turns of the width for several tiles of a workgroup: the same as the separate calls, to the tolerances of
+    test_layer_is_the_separate_calls."""
+    g = torch.Generator(device="cuda").manual_seed(H)
+    rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda")  # noqa: E731
+    x = rand(T, H).to(getattr(torch, dtype))
+    gamma, router = 1 + 0.1 * rand(H), rand(E, H) / H ** 0.5
+    w_in, s_in = sd.quantize_blocks(rand(E, 2, F, H) / H ** 0.5, 128)
+    w_out, s_out = sd.quantize_blocks(rand(E, H, F) / F ** 0.5, 128)
+    _say("layer wide", T, H, F, E, k, dtype)
+    got = sd.experts_layer(x, gamma, router, k, w_in, s_in, w_out, s_out, F, eps=EPS)
+    q, s, _, _ = sd.norm_quantize(x, gamma, EPS)
+    z = x.double() / torch.sqrt((x.double() ** 2).mean(1, keepdim=True) + EPS) * gamma.double()
+    routes = sd.route((z @ router.double().t()).float(), k)
+    assert torch.equal(routes.ids, got.ids)
+    want = sd.experts_forward(q, s, routes, w_in, s_in, w_out, s_out, H, F, dtype=torch.float32).double() + x.double()
+    assert float((got.out.double() - want).norm() / want.norm()) <= (2e-5 if dtype == "float32" else 2.0 ** -8)
+
+
 def _rounded(v, bits):
     """float64 values rounded to `bits` bits, ties to even (normal values)."""
     m, e = np.frexp(v)
