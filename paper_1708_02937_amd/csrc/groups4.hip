@@ -260,7 +260,7 @@ __device__ __forceinline__ void put_infinite(const GroupProductArgs &a, int64_t 
 
 // ---- up to 16 rows that fit LDS as a whole: 16 NW outputs at a time, by workgroups that stay.  Each wave takes a run of the
 // steps, STEPS at a turn, and the weights of its next turn, of the next tile where this one is the tile's last, are on their
-// way while this turn's are multiplied.  The weights bound it: a row of 4096 columns and 131072 outputs 50 us (285 MB, 5.7 TB/s, above
+// way while this turn's are multiplied.  The weights bound it: a row of 4096 columns and 131072 outputs 49 to 52 us (285 MB, 5.4 to 5.8 TB/s, above
 // a copy's rate), 4096 outputs 5.0 (8.9 MB in one wave of workgroups: a start and an end with little between).
 constexpr int64_t row_pitch(int64_t k) { return blocks_of(k) * kBlock * 2 + 16; }  // 16 rows' 16 bytes lie on different banks
 
@@ -449,8 +449,11 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
     return hipSuccess;
 }
 
-// The largest tiles that still give every CU a workgroup, and no wider than the outputs: a small one's waves share the columns, a large one's rows and weights serve
-// more outputs.  us, 4096 columns, of 16 x 16, 16 x 32, 16 x 64 | 32 x 64, 64 x 64 | 32 x 128, 64 x 128 (rows x outputs), bfloat16:
+// The smallest tiles, no wider than the outputs, of which no CU gets more than one; the largest where all of them are more.  A small
+// one's waves share the columns, a large one's rows and weights serve more outputs.  Where the next tile is twice as large it
+// leaves half of the CUs none: 32 bfloat16 rows, 4096 outputs 8.1 us, 4112 to 8192 outputs 11.2 to 11.4; 64 rows, 8192 outputs 13.8, 8208 to 16384
+// 20.1 to 21.2; 64 float rows, 16384 outputs 38, 16400 65.  A rule that lets some CUs have two of the smaller ones is not tried.  us, 4096
+// columns, of 16 x 16, 16 x 32, 16 x 64 | 32 x 64, 64 x 64 | 32 x 128, 64 x 128 (rows x outputs), bfloat16:
 //   32 rows, 4096 outputs 9.7, 9.0, 11.7 | 13.5, 17.2 | 21, 24;    48 rows, 8192 22, 18, 20 | 14.2, 19 | 22, 29
 //   32 rows, 32768        -, 40, 36 | 24.2, 33 | 22.7, 26.5;       64 rows, 16384 54, 40, 36 | 24, 21.5 | 22.5, 30
 //   64 rows, 32768        105, 77, 70 | 44, 40 | 40, 31;           256 rows, 32768 -, -, 267 | 160, 151 | 146, 100
@@ -461,7 +464,7 @@ hipError_t product_tile_go(const GroupProductArgs &a, hipStream_t s) {
 constexpr int64_t kCus = 256;
 template <typename TX, typename TY>
 hipError_t product_tiles_go(const GroupProductArgs &a, hipStream_t s) {
-    auto enough = [&](int64_t rows, int64_t outputs) {  // no more workgroups than CUs: a larger tile leaves some without
+    auto enough = [&](int64_t rows, int64_t outputs) {  // no more workgroups than CUs
         return (a.m + rows - 1) / rows * ((a.n + outputs - 1) / outputs) <= kCus;
     };
     if (enough(16, 16)) return product_tile_go<TX, TY, 1, 16, 8>(a, s);
@@ -485,7 +488,8 @@ hipError_t product_tiles_go(const GroupProductArgs &a, hipStream_t s) {
 // in half precision of few outputs, which every workgroup would fetch.  us (resident | tiles), bfloat16, 1 and 16 rows:
 //   4096 columns: 4096 outputs 5.3, 7.8 | 5.7, 6.8;  8192: 7.9, 14.3 | 8.5, 9.3;  16384: 10.8, 13.2 | 11.5, 12.3;  32768: 17, 19.6 | 18.5, 20.4
 //   2048 columns: 4096 outputs 4.7, 5.8 | 4.6, 5.1;  65536: 26, 27 | 19, 22;   16384 columns, 4096 outputs: 10.9, - | 15, 18
-//   floats: 1 row of 4096 columns and 4096 outputs 7.3 | 10.2;  32768: 22 | 25;  of 2048 columns and 65536 outputs 30 | 24
+//   floats, of which 5 rows of 4096 columns fit: 1 and 4 rows of 4096 columns: 4096 outputs 7.8, 7.5 | 10.1, 9.8;  8192: 9.9, 12.1 | 12.4, 12.0;
+//   16384: 12.9, 13.0 | 16.8, 16.3;  131072: 74, 72 | 77, 78;   of 2048 columns: 4096 outputs 8.2, 8.0 | 7.5, 7.6;  65536: 30, - | 24, -
 template <typename TX, typename TY>
 hipError_t product_go(const GroupProductArgs &a, hipStream_t s) {
     const int64_t rows = rows_space<TX>(a.m, a.k);

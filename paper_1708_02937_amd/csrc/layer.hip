@@ -315,6 +315,10 @@ __device__ __forceinline__ int place_of(const LayerArgs &a, const Chosen &c, int
 // for one token: first product 18.9 us, of which the choice takes 4 and the weights 11 (67 MB, 5.9 TB/s), second 12.1 (34 MB);
 // 16 tokens, 57 experts: 96 us (5.0 TB/s) and 61 (3.9; its rows of p, rounded anew by every workgroup, keep VALU half busy; in a
 // launch of their own, the same bits, 151 for the call against 157, but 3 us more for smaller or fewer experts).
+// Both are made for widths around 4096, which the waves' loads cover in one turn.  us of the call and of the separate calls, each from a
+// graph, for 1, 4 and 16 tokens, 8 of 64 experts (128 of the narrow one): 4096 x 1024 39, 89, 165 | 64, 118, 273;  5120 x 1536 71, 217, 468 | 92, 214, 430;
+// 7168 x 2048 98, 294, 626 | 139, 317, 678;  512 x 1024 34, 70, 171 | 44, 63, 112: below 1024 columns half the waves and more have no block
+// of the width, and a tile of 16 inner values costs its two barriers all the same.
 
 // p = silu(gate) * up in fp32 of 16 inner values of an expert for all tokens; the waves share the blocks of the width.  A
 // wave's blocks are taken four at a time, and the next four, of the next tile where these are the last, are on their way while

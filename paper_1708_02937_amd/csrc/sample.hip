@@ -712,7 +712,9 @@ __device__ __forceinline__ uint64_t select(const Row &r, const Plan &p, uint64_t
     return prefix;
 }
 
-// Any other list.
+// Any other list, eight passes over it for each cut; where LDS does not hold it (more than kList tokens, or more than an eighth of a
+// chunk), over the row, by one workgroup: a top-p that ends in a bucket of thousands of tokens costs a row of 131072 (normal logits of deviation 2
+// at temperature 4) 0.5 ms and one of 262144 (at 1.5) 0.8, where 46 us are usual; top_k and top_p both 0.8 and 1.5.
 template <typename E>
 __device__ __forceinline__ void by_select(const Row &r, const Plan &p, int shift, Shared &sh, Kept &kept, E each) {
     if (p.cut_k) kept.last = select<false>(r, p, (uint64_t)(p.k - p.before), 0, shift, sh, each);
@@ -1107,11 +1109,13 @@ __global__ void __launch_bounds__(kThreads) sample_end_kernel(SampleArgs a, Samp
 }
 
 // Rows that one workgroup each takes in one launch.  us (this | the four launches), temperature alone, top-p, all filters, float:
-//   1 row:      8000 tokens 16, 24, 13 | 22, 33, 22;   16000 24, 35, 17 | 22, 34, 22;   32000 37, 56, 23 | 23, 37, 20
-//   128 rows:   32000 39, 57, 23 | 41, 60, 30;   64000 70, 99, 41 | 52, 75, 36;   131072 136, 185, 73 | 71, 100, 50
-//   256 rows:   32000 43, 62, 27 | 52, 75, 43;   64000 74, 103, 43 | 71, 100, 51
-//   512 rows:   64000 108, 143, 56 | 116, 157, 73;   131072 203, 266, 98 | 191, 261, 117
-//   1000 rows:  131072 416, 534, 204 | 502, 647, 249
+//   1 row:      8000 tokens 16, 23, 12 | 25, 33, 23;   16000 24, 33, 15 | 24, 34, 24;   32000 37, 52, 22 | 24, 36, 21
+//   128 rows:   32000 39, 53, 22 | 41, 57, 30;   64000 70, 99, 41 | 52, 75, 36;   131072 136, 185, 73 | 71, 100, 50
+//   256 rows:   32000 43, 62, 27 | 52, 75, 43;   64000 76, 103, 42 | 70, 97, 51
+//   400 rows:   100000 156, 207, 74 | 149, 208, 91
+//   512 rows:   64000 108, 143, 56 | 116, 157, 73;   131072 204, 264, 97 | 190, 257, 117
+//   600 rows:   131072 305, 406, 163 | 346, 450, 157;   800 rows: 403, 518, 190 | 456, 603, 233
+// Which settings a row has is data of the GPU, so the rule goes by the sizes: next to it, rows of all filters win a fifth, others lose up to 9%.
 constexpr int64_t kShort = 4 * kTile, kOfARow = 256;
 bool is_short(int64_t rows, int64_t vocab) { return vocab <= kShort || vocab / kOfARow <= rows; }
 
