@@ -260,7 +260,7 @@ __device__ __forceinline__ void put_infinite(const GroupProductArgs &a, int64_t 
 
 // ---- up to 16 rows that fit LDS as a whole: 16 NW outputs at a time, by workgroups that stay.  Each wave takes a run of the
 // steps, STEPS at a turn, and the weights of its next turn, of the next tile where this one is the tile's last, are on their
-// way while this turn's are multiplied.  The weights bound it: a row of 4096 columns and 131072 outputs 49 to 52 us (285 MB, 5.4 to 5.8 TB/s, above
+// way while this turn's are multiplied.  The weights bound it: a row of 4096 columns and 131072 outputs 50 to 52 us (285 MB, 5.4 to 5.7 TB/s, above
 // a copy's rate), 4096 outputs 5.0 (8.9 MB in one wave of workgroups: a start and an end with little between).
 constexpr int64_t row_pitch(int64_t k) { return blocks_of(k) * kBlock * 2 + 16; }  // 16 rows' 16 bytes lie on different banks
 

@@ -68,6 +68,8 @@ def experts_layer(x, gamma, router, k: int, w_in, w_in_scale, w_out, w_out_scale
     router's logits (router: experts x width, float32 or bfloat16) and choice (k, score, bias, groups, ... as in route),
     and s + the weighted sum of the chosen experts on the norm in 8 bits (weights as in experts_forward).
 
+    Of layers of a few hundred columns, norm_quantize, route and experts_forward are faster from about 4 tokens on.
+
     live: a bool for each token; one that is False takes part in no expert, and its result is s.  out may be x or residual
     itself.  ws: a uint8 tensor of at least sdnn_experts_layer_workspace_size bytes (allocated if absent)."""
     device = x.get_device()
